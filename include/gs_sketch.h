@@ -30,7 +30,8 @@
  *     the vectorised path (results are identical either way).
  *   - Sizes: 1 <= r <= GS_MAX_ROWS, 1 <= c <= GS_MAX_COLS, 1 <= d <= GS_MAX_DIM,
  *     1 <= k <= d, 1 <= P <= GS_MAX_WORKERS.  Vector values must be finite.
- *   - No call waits on the device for a flag; nothing spins.  Kernels launch with
+ *   - No call waits on the device for a flag; nothing spins (CTAs of a cluster meet at the
+ *     hardware's cluster barrier).  Kernels launch with
  *     programmatic stream serialization and wait in hardware for the grid before them.
  */
 #ifndef GS_SKETCH_H
@@ -414,6 +415,125 @@ gs_status gs_plan_query_times(gs_plan* plan, float* query_ms_out, float* select_
 
 /* Wait for the device to go idle if the plan was ever launched, then free it.  NULL is OK. */
 gs_status gs_plan_destroy(gs_plan* plan);
+
+/* ---- operators of a recurrent layer ------------------------------------------------ */
+/* What a residual recurrent layer computes besides its matrix products: a gated linear
+ * recurrence over time, dropout, and dropout with residual add and RMS norm, each with its
+ * backward pass.  Their parameter gradients are fp32, so they can be written into a slice of
+ * the gradient vector that gs_step or gs_train_step reads; the paper has no counterpart.
+ *
+ *   - Activations and their gradients share one type per call: GS_F32, GS_F16 or GS_BF16.
+ *     Parameters, states and parameter gradients are fp32.  All arithmetic is fp32; a stored
+ *     activation is rounded once.
+ *   - A matrix of rows x cols has adjacent columns; row k starts `stride` elements after row
+ *     k - 1.  A sequence tensor [B][T][D] has adjacent channels and two strides (gs_seq).
+ *     Strides are in elements, any non-negative value for an input (0 repeats a row); rows of
+ *     an output must not overlap.
+ *   - Data is aligned to its element; 16-byte alignment of every row (base and strides) selects
+ *     the vectorised path, with the same results.
+ *   - Sizes may be zero where a loop over them may be empty (rows, cols, B, T, D); such a call
+ *     does what is left of its work.  Limits: rows * cols and B * T * D up to 2^40, rows and T
+ *     below 2^31.
+ *   - Results do not depend on timing: sums are taken in an order fixed by the sizes. */
+#define GS_F32 0
+#define GS_F16 1
+#define GS_BF16 2
+
+/* Dropout whose mask is a function of (seed, offset, position) and is never stored.  Element
+ * e = row * cols + col takes 16 bits u of Philox4x32-10 (Salmon, Moraes, Dror and Shaw, SC 2011):
+ * key = seed, counter = (e / 8, offset), each 64 bits with the low word first; half (e mod 2,
+ * low first) of word (e mod 8) / 2.  With t = round(65536 p),
+ *   out[e] = (u < t ? 0 : x[e] * 65536 / (65536 - t)) (+ residual[e]),
+ * so p is taken to a multiple of 2^-16 and the scale fits that value exactly.  A dropped
+ * element counts as zero whatever it holds (infinities and NaN too).  Give every call that
+ * needs its own mask (layer, step, worker) another offset or seed.  0 <= p <= 1.  residual may
+ * be NULL.  out may be x or residual itself (same strides). */
+gs_status gs_dropout(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
+                     void* out, int64_t out_stride, int64_t rows, int64_t cols, int32_t dtype,
+                     float p, uint64_t seed, uint64_t offset, gs_stream stream);
+
+/* dx = the gradient of x from dout, the gradient of gs_dropout's out with the same p, seed and
+ * offset (the residual's gradient is dout itself).  dx may be dout. */
+gs_status gs_dropout_backward(const void* dout, int64_t dout_stride, void* dx, int64_t dx_stride,
+                              int64_t rows, int64_t cols, int32_t dtype, float p, uint64_t seed,
+                              uint64_t offset, gs_stream stream);
+
+/* The boundary of a residual layer in one pass:
+ *   y = residual + dropout(x),  rstd = 1 / sqrt(mean(y^2) + eps),  z = y * rstd * weight
+ * row by row, with the mask of gs_dropout.  y (the residual stream) and z are stored; z and
+ * rstd come from y before it is rounded.  weight: fp32[cols]; rstd: fp32[rows] for the backward
+ * pass.  1 <= cols <= GS_NORM_MAX_COLS, eps >= 0.  y may be x or residual itself. */
+#define GS_NORM_MAX_COLS 16384
+gs_status gs_dropout_add_norm(const void* x, int64_t x_stride, const void* residual,
+                              int64_t residual_stride, const float* weight, void* y, int64_t y_stride,
+                              void* z, int64_t z_stride, float* rstd, int64_t rows, int64_t cols,
+                              int32_t dtype, float p, uint64_t seed, uint64_t offset, float eps,
+                              gs_stream stream);
+
+/* Device workspace bytes gs_dropout_add_norm_backward needs. */
+gs_status gs_dropout_add_norm_workspace_size(int64_t rows, int64_t cols, size_t* bytes);
+
+/* From dz and dy (the gradients of z and of y; dy may be NULL for none), the stored y and rstd:
+ *   n = y * rstd,  u = dz * weight,  dresidual = rstd * (u - n * mean(u * n)) + dy,
+ *   dx = mask * dresidual * 65536 / (65536 - t),  dweight = sum over rows of dz * n.
+ * dx and dresidual may each be NULL; dweight (fp32[cols]) is overwritten.  workspace must hold
+ * gs_dropout_add_norm_workspace_size(rows, cols) bytes, 256-byte aligned. */
+gs_status gs_dropout_add_norm_backward(const void* dz, int64_t dz_stride, const void* dy, int64_t dy_stride,
+                                       const void* y, int64_t y_stride, const float* weight,
+                                       const float* rstd, void* dx, int64_t dx_stride, void* dresidual,
+                                       int64_t dresidual_stride, float* dweight, int64_t rows,
+                                       int64_t cols, int32_t dtype, float p, uint64_t seed,
+                                       uint64_t offset, void* workspace, size_t workspace_bytes,
+                                       gs_stream stream);
+
+/* A [B][T][D] tensor: element (b, t, d) at data + b * batch_stride + t * token_stride + d. */
+typedef struct {
+  void* data;
+  int64_t batch_stride, token_stride;
+} gs_seq;
+
+/* Gated linear recurrence.  With s() the logistic function, from the gates' values r and i
+ * before it and one decay parameter per channel (fp32[D]),
+ *   log a_t = -c * softplus(decay) * s(r_t),
+ *   h_t = a_t * h_{t-1} + sqrt(1 - a_t^2) * s(i_t) * x_t,   y_t = h_t,   h_{-1} = h0.
+ * h0 (fp32[B][D], NULL for zeros).  reset (uint8[B][T], nullable): where it is not zero a new
+ * document begins: a_t is 0, nothing before it (not even an infinity) is seen.  lengths
+ * (int32[B], nullable; taken to [0, T]): tokens from a row's length on are not read, their y is
+ * zero and the state stays.  h_last (fp32[B][D], nullable): the state after the last token, h0
+ * for a row of length zero; it may be h0.  states (nullable): gs_recurrence_states_size bytes,
+ * 256-byte aligned, filled for the backward pass (the fp32 state at fixed intervals).
+ * c > 0 and finite; decay must be finite.  The gs_seq are read during the call. */
+gs_status gs_recurrence_states_size(int64_t B, int64_t T, int64_t D, size_t* bytes);
+gs_status gs_recurrence_forward(const gs_seq* x, const gs_seq* r, const gs_seq* i, const float* decay,
+                                const float* h0, const uint8_t* reset, const int32_t* lengths,
+                                const gs_seq* y, float* h_last, void* states, int64_t B, int64_t T,
+                                int64_t D, int32_t dtype, float c, gs_stream stream);
+
+/* Gradients of gs_recurrence_forward from dy and dh_last (fp32[B][D], NULL for none), its inputs
+ * and the states it filled:
+ *   g_t = dy_t + a_{t+1} g_{t+1} (dh_last past the last token),
+ *   dlog a_t = g_t (a_t h_{t-1} - s(i_t) x_t a_t^2 / sqrt(1 - a_t^2))   (0 at a reset),
+ *   dx, di, dr by the chain rule, ddecay (fp32[D], overwritten) summed over all tokens,
+ *   dh0 (fp32[B][D], nullable) = a_0 g_0.
+ * Masked tokens get zeros; dy is not read there.  workspace must hold
+ * gs_recurrence_workspace_size bytes, 256-byte aligned. */
+gs_status gs_recurrence_workspace_size(int64_t B, int64_t T, int64_t D, size_t* bytes);
+gs_status gs_recurrence_backward(const gs_seq* dy, const float* dh_last, const gs_seq* x, const gs_seq* r,
+                                 const gs_seq* i, const float* decay, const uint8_t* reset,
+                                 const int32_t* lengths, const void* states, const gs_seq* dx,
+                                 const gs_seq* dr, const gs_seq* di, float* ddecay, float* dh0, int64_t B,
+                                 int64_t T, int64_t D, int32_t dtype, float c, void* workspace,
+                                 size_t workspace_bytes, gs_stream stream);
+
+/* One token of each of B streams: the recurrence's next state, in place, and y = that state.
+ * x, r, i, y are [B][D] matrices.  state: fp32, n_slots rows of state_stride elements; stream b
+ * lives in row slots[b] (int32[B], NULL for row b).  A slot outside [0, n_slots) is idle: its y
+ * is zero and nothing else is touched.  No two streams may share a slot. */
+gs_status gs_recurrence_step(const void* x, int64_t x_stride, const void* r, int64_t r_stride,
+                             const void* i, int64_t i_stride, const float* decay, float* state,
+                             int64_t state_stride, int64_t n_slots, const int32_t* slots, void* y,
+                             int64_t y_stride, int64_t B, int64_t D, int32_t dtype, float c,
+                             gs_stream stream);
 
 /* ---- measurement aid --------------------------------------------------------------- */
 /* The fused insert (gs_accumulate_insert over every group and row pass) is bound by the

@@ -26,12 +26,24 @@ GS_MAX_WORKERS = 64
 GS_MAX_DIM = (1 << 31) - 1
 GS_NOALLOC_MAX_DIM = 1 << 30
 GS_CEILING_WINDOW_FLOATS = 1 << 17
+GS_F32 = 0
+GS_F16 = 1
+GS_BF16 = 2
+GS_NORM_MAX_COLS = 16384
 
 _lib = None
 
 _vp = ctypes.c_void_p
 _i32, _i64, _u64, _f32, _sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_float, ctypes.c_size_t
 _PP = ctypes.POINTER(ctypes.c_void_p)
+
+
+class GsSeq(ctypes.Structure):
+    """A [B][T][D] tensor: its address, batch and token strides in elements."""
+    _fields_ = [("data", _vp), ("batch_stride", _i64), ("token_stride", _i64)]
+
+
+_SEQ = ctypes.POINTER(GsSeq)
 
 # name -> argument types (all return gs_status / int32 unless listed in _RESTYPES)
 SIGNATURES = {
@@ -77,6 +89,20 @@ SIGNATURES = {
     "gs_step_workspace_size": [_i64, _i64, ctypes.POINTER(_sz)],
     "gs_step": [_vp, _PP, _PP, _PP, _i64, _f32, _i64, _vp, _vp, _vp, _vp, _sz, _vp],
     "gs_step_host": [_vp, _PP, _PP, _PP, _PP, _i64, _f32, _i64, _vp, _vp, _vp, _sz, _vp],
+    "gs_dropout": [_vp, _i64, _vp, _i64, _vp, _i64, _i64, _i64, _i32, _f32, _u64, _u64, _vp],
+    "gs_dropout_backward": [_vp, _i64, _vp, _i64, _i64, _i64, _i32, _f32, _u64, _u64, _vp],
+    "gs_dropout_add_norm": [_vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _i32, _f32, _u64, _u64,
+                            _f32, _vp],
+    "gs_dropout_add_norm_workspace_size": [_i64, _i64, ctypes.POINTER(_sz)],
+    "gs_dropout_add_norm_backward": [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _i64,
+                                     _i32, _f32, _u64, _u64, _vp, _sz, _vp],
+    "gs_recurrence_states_size": [_i64, _i64, _i64, ctypes.POINTER(_sz)],
+    "gs_recurrence_workspace_size": [_i64, _i64, _i64, ctypes.POINTER(_sz)],
+    "gs_recurrence_forward": [_SEQ, _SEQ, _SEQ, _vp, _vp, _vp, _vp, _SEQ, _vp, _vp, _i64, _i64, _i64, _i32, _f32, _vp],
+    "gs_recurrence_backward": [_SEQ, _vp, _SEQ, _SEQ, _SEQ, _vp, _vp, _vp, _vp, _SEQ, _SEQ, _SEQ, _vp, _vp, _i64, _i64,
+                               _i64, _i32, _f32, _vp, _sz, _vp],
+    "gs_recurrence_step": [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64, _vp, _vp, _i64, _i64, _i64, _i32,
+                           _f32, _vp],
     "gs_insert_request_ceiling_window_size": [_vp, ctypes.POINTER(_sz)],
     "gs_insert_request_ceiling": [_vp, _i64, _vp, _sz, ctypes.POINTER(_f32), _vp],
     "gs_query_request_ceiling": [_vp, _i64, _vp, _sz, ctypes.POINTER(_f32), _vp],
@@ -409,6 +435,249 @@ def gs_plan_query_times(plan: int, n: int = 1024) -> tuple:
 
 def gs_plan_destroy(plan: int) -> None:
     _check(load_library().gs_plan_destroy(plan), "gs_plan_destroy")
+
+
+# ---- operators of a recurrent layer -------------------------------------------------------
+# Tensors are torch tensors on the GPU; shapes, strides and types are read from them, and what
+# the C ABI cannot see of them is checked here.
+
+_DTYPES = {}
+
+
+def _refuse(func: str, msg: str):
+    raise GsError(GS_ERR_INVALID_ARG, func, msg)
+
+
+def _dtype(func: str, t) -> int:
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: GS_F32, torch.float16: GS_F16, torch.bfloat16: GS_BF16})
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        _refuse(func, f"dtype {t.dtype} is none of float32, float16, bfloat16")
+    return code
+
+
+def _same(func: str, name: str, t, shape, dtype, device) -> None:
+    if t.shape != shape:
+        _refuse(func, f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.dtype != dtype:
+        _refuse(func, f"{name} has type {t.dtype}, expected {dtype}")
+    if t.device != device:
+        _refuse(func, f"{name} is on {t.device}, expected {device}")
+
+
+def _on_gpu(func: str, name: str, t) -> None:
+    if not t.is_cuda:
+        _refuse(func, f"{name} is on {t.device}, expected a CUDA device")
+
+
+def _dense(func: str, name: str, t, shape, dtype, device):
+    """Address of a contiguous tensor, or None for an absent one."""
+    if t is None:
+        return None
+    _same(func, name, t, shape, dtype, device)
+    if not t.is_contiguous():
+        _refuse(func, f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _f32_dtype():
+    import torch
+    return torch.float32
+
+
+def _matrix(func: str, name: str, t, shape, dtype, device):
+    """(address, row stride) of a tensor whose last dimension is adjacent and whose others can be
+    walked with one stride; (None, 0) for an absent one."""
+    if t is None:
+        return None, 0
+    _same(func, name, t, shape, dtype, device)
+    if t.is_contiguous():
+        return t.data_ptr(), shape[-1]
+    stride = t.stride()
+    if shape[-1] > 1 and stride[-1] != 1:
+        _refuse(func, f"{name}: the last dimension must be adjacent")
+    row, span = None, None   # of the innermost leading dimension with more than one entry, outwards
+    for size, st in zip(reversed(shape[:-1]), reversed(stride[:-1])):
+        if size == 1:
+            continue
+        if row is None:
+            row, span = st, st * size
+        elif st != span:
+            _refuse(func, f"{name}: the rows cannot be walked with one stride")
+        else:
+            span = st * size
+    return t.data_ptr(), shape[-1] if row is None else row
+
+
+def _rows_cols(func: str, t):
+    if t.dim() < 1:
+        _refuse(func, "a tensor of at least one dimension is expected")
+    _on_gpu(func, "the first tensor", t)
+    cols = t.shape[-1]
+    rows = 1
+    for n in t.shape[:-1]:
+        rows *= n
+    return rows, cols
+
+
+def gs_dropout(x, out, p: float, seed: int, offset: int, residual=None, stream=None) -> None:
+    """out = dropout(x) (+ residual); any shape, the mask indexed by the element's flat position."""
+    f = "gs_dropout"
+    code = _dtype(f, x)
+    rows, cols = _rows_cols(f, x)
+    xp, xs = _matrix(f, "x", x, x.shape, x.dtype, x.device)
+    rp, rs = _matrix(f, "residual", residual, x.shape, x.dtype, x.device)
+    op, os_ = _matrix(f, "out", out, x.shape, x.dtype, x.device)
+    _check(load_library().gs_dropout(xp, xs, rp, rs, op, os_, rows, cols, code, p, seed, offset, _stream(stream)), f)
+
+
+def gs_dropout_backward(dout, dx, p: float, seed: int, offset: int, stream=None) -> None:
+    f = "gs_dropout_backward"
+    code = _dtype(f, dout)
+    rows, cols = _rows_cols(f, dout)
+    gp, gstride = _matrix(f, "dout", dout, dout.shape, dout.dtype, dout.device)
+    op, os_ = _matrix(f, "dx", dx, dout.shape, dout.dtype, dout.device)
+    _check(load_library().gs_dropout_backward(gp, gstride, op, os_, rows, cols, code, p, seed, offset,
+                                              _stream(stream)), f)
+
+
+def gs_dropout_add_norm(x, residual, weight, y, z, rstd, p: float, seed: int, offset: int, eps: float = 1e-6,
+                        stream=None) -> None:
+    """y = residual + dropout(x), z = RMS norm of y times weight, over the last dimension."""
+    f = "gs_dropout_add_norm"
+    code = _dtype(f, x)
+    rows, cols = _rows_cols(f, x)
+    shape, dtype, dev, f32 = x.shape, x.dtype, x.device, _f32_dtype()
+    xp, xs = _matrix(f, "x", x, shape, dtype, dev)
+    rp, rs = _matrix(f, "residual", residual, shape, dtype, dev)
+    yp, ys = _matrix(f, "y", y, shape, dtype, dev)
+    zp, zs = _matrix(f, "z", z, shape, dtype, dev)
+    _check(load_library().gs_dropout_add_norm(
+        xp, xs, rp, rs, _dense(f, "weight", weight, (cols,), f32, dev), yp, ys, zp, zs,
+        _dense(f, "rstd", rstd, shape[:-1], f32, dev), rows, cols, code, p, seed, offset, eps, _stream(stream)), f)
+
+
+def gs_dropout_add_norm_workspace_size(rows: int, cols: int) -> int:
+    out = _sz()
+    _check(load_library().gs_dropout_add_norm_workspace_size(rows, cols, ctypes.byref(out)),
+           "gs_dropout_add_norm_workspace_size")
+    return out.value
+
+
+def gs_dropout_add_norm_backward(dz, dy, y, weight, rstd, dx, dresidual, dweight, p: float, seed: int, offset: int,
+                                 workspace, workspace_bytes=None, stream=None) -> None:
+    """Gradients of gs_dropout_add_norm; dy, dx and dresidual may be None."""
+    f = "gs_dropout_add_norm_backward"
+    code = _dtype(f, dz)
+    rows, cols = _rows_cols(f, dz)
+    shape, dtype, dev, f32 = dz.shape, dz.dtype, dz.device, _f32_dtype()
+    gp, gstride = _matrix(f, "dz", dz, shape, dtype, dev)
+    dp, ds = _matrix(f, "dy", dy, shape, dtype, dev)
+    yp, ys = _matrix(f, "y", y, shape, dtype, dev)
+    xp, xs = _matrix(f, "dx", dx, shape, dtype, dev)
+    rp, rs = _matrix(f, "dresidual", dresidual, shape, dtype, dev)
+    _check(load_library().gs_dropout_add_norm_backward(
+        gp, gstride, dp, ds, yp, ys, _dense(f, "weight", weight, (cols,), f32, dev),
+        _dense(f, "rstd", rstd, shape[:-1], f32, dev), xp, xs, rp, rs, _dense(f, "dweight", dweight, (cols,), f32, dev),
+        rows, cols, code, p, seed, offset, _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream)), f)
+
+
+def _seq(func: str, name: str, t, shape, dtype, device):
+    _same(func, name, t, shape, dtype, device)
+    b, s, d = t.stride()
+    if d != 1 and shape[2] > 1:
+        _refuse(func, f"{name}: the channels must be adjacent")
+    return ctypes.byref(GsSeq(t.data_ptr(), b, s))
+
+
+def _flags(func: str, name: str, t, shape, width: str, device):
+    if t is None:
+        return None
+    import torch
+    if width == "reset" and t.dtype == torch.bool:
+        t = t.view(torch.uint8)
+    return _dense(func, name, t, shape, torch.uint8 if width == "reset" else torch.int32, device)
+
+
+def _sequence(func: str, t):
+    if t.dim() != 3:
+        _refuse(func, f"tensors of [B][T][D] are expected, got {t.dim()} dimensions")
+    _on_gpu(func, "x", t)
+    return t.shape
+
+
+def gs_recurrence_states_size(B: int, T: int, D: int) -> int:
+    out = _sz()
+    _check(load_library().gs_recurrence_states_size(B, T, D, ctypes.byref(out)), "gs_recurrence_states_size")
+    return out.value
+
+
+def gs_recurrence_workspace_size(B: int, T: int, D: int) -> int:
+    out = _sz()
+    _check(load_library().gs_recurrence_workspace_size(B, T, D, ctypes.byref(out)), "gs_recurrence_workspace_size")
+    return out.value
+
+
+def _states_fit(func: str, states, B: int, T: int, D: int) -> None:
+    if states.numel() * states.element_size() < gs_recurrence_states_size(B, T, D) or not states.is_contiguous():
+        _refuse(func, "states must be contiguous and hold gs_recurrence_states_size(B, T, D) bytes")
+
+
+def gs_recurrence_forward(x, r, i, decay, y, h0=None, reset=None, lengths=None, h_last=None, states=None,
+                          c: float = 8.0, stream=None) -> None:
+    """y_t = h_t of the gated linear recurrence over [B][T][D]; states keeps what the backward
+    pass needs (None when there is none)."""
+    f = "gs_recurrence_forward"
+    code = _dtype(f, x)
+    shape = B, T, D = _sequence(f, x)
+    dtype, dev, f32 = x.dtype, x.device, _f32_dtype()
+    if states is not None:
+        _states_fit(f, states, B, T, D)
+    _check(load_library().gs_recurrence_forward(
+        _seq(f, "x", x, shape, dtype, dev), _seq(f, "r", r, shape, dtype, dev), _seq(f, "i", i, shape, dtype, dev),
+        _dense(f, "decay", decay, (D,), f32, dev), _dense(f, "h0", h0, (B, D), f32, dev),
+        _flags(f, "reset", reset, (B, T), "reset", dev), _flags(f, "lengths", lengths, (B,), "lengths", dev),
+        _seq(f, "y", y, shape, dtype, dev), _dense(f, "h_last", h_last, (B, D), f32, dev), _ptr(states), B, T, D, code,
+        c, _stream(stream)), f)
+
+
+def gs_recurrence_backward(dy, x, r, i, decay, states, dx, dr, di, ddecay, workspace, dh_last=None, reset=None,
+                           lengths=None, dh0=None, c: float = 8.0, workspace_bytes=None, stream=None) -> None:
+    """Gradients of gs_recurrence_forward from dy and dh_last, its inputs and the states it filled."""
+    f = "gs_recurrence_backward"
+    code = _dtype(f, x)
+    shape = B, T, D = _sequence(f, x)
+    dtype, dev, f32 = x.dtype, x.device, _f32_dtype()
+    _states_fit(f, states, B, T, D)
+    _check(load_library().gs_recurrence_backward(
+        _seq(f, "dy", dy, shape, dtype, dev), _dense(f, "dh_last", dh_last, (B, D), f32, dev),
+        _seq(f, "x", x, shape, dtype, dev), _seq(f, "r", r, shape, dtype, dev), _seq(f, "i", i, shape, dtype, dev),
+        _dense(f, "decay", decay, (D,), f32, dev), _flags(f, "reset", reset, (B, T), "reset", dev),
+        _flags(f, "lengths", lengths, (B,), "lengths", dev), _ptr(states), _seq(f, "dx", dx, shape, dtype, dev),
+        _seq(f, "dr", dr, shape, dtype, dev), _seq(f, "di", di, shape, dtype, dev),
+        _dense(f, "ddecay", ddecay, (D,), f32, dev), _dense(f, "dh0", dh0, (B, D), f32, dev), B, T, D, code, c,
+        _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream)), f)
+
+
+def gs_recurrence_step(x, r, i, decay, state, y, slots=None, c: float = 8.0, stream=None) -> None:
+    """One token of each of B streams: state rows (fp32, one per slot) in place, y = the new state."""
+    f = "gs_recurrence_step"
+    code = _dtype(f, x)
+    B, D = _rows_cols(f, x)
+    dtype, dev, f32 = x.dtype, x.device, _f32_dtype()
+    xp, xs = _matrix(f, "x", x, x.shape, dtype, dev)
+    rp, rs = _matrix(f, "r", r, x.shape, dtype, dev)
+    ip, istride = _matrix(f, "i", i, x.shape, dtype, dev)
+    yp, ys = _matrix(f, "y", y, x.shape, dtype, dev)
+    if state.dim() != 2:
+        _refuse(f, "state must have two dimensions")
+    n = state.shape[0]
+    sp, ss = _matrix(f, "state", state, (n, D), f32, dev)
+    _check(load_library().gs_recurrence_step(
+        xp, xs, rp, rs, ip, istride, _dense(f, "decay", decay, (D,), f32, dev), sp, ss, n,
+        _flags(f, "slots", slots, (B,), "slots", dev), yp, ys, B, D, code, c, _stream(stream)), f)
 
 
 def gs_insert_request_ceiling_window_size(sketch: int) -> int:

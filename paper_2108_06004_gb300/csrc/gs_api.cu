@@ -600,6 +600,16 @@ int blocks_per_sm(const void* kernel, int block) {
 
 }  // namespace gs
 
+namespace gs {
+
+gs_status record_failure(gs_status st, const char* msg) noexcept { return fail(st, msg); }
+gs_status record_cuda_failure(cudaError_t e, const char* what) noexcept {
+  cudaGetLastError();  // a refused launch is reported here, and not again by whoever asks next
+  return cuda_fail(e, what);
+}
+
+}  // namespace gs
+
 extern "C" {
 
 gs_status gs_sketch_create(int32_t r, int32_t c, uint64_t seed, int32_t workers, int32_t group_width,

@@ -1,0 +1,259 @@
+// Shared declarations of the recurrent layer's operators: element types, the counter-based
+// generator, parameter blocks and launchers called by the C ABI in gs_layer.cu.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "gs_common.cuh"
+
+namespace gs {
+
+// Status and thread-local message of a failing call (defined beside gs_last_error).
+gs_status record_failure(gs_status st, const char* msg) noexcept;
+gs_status record_cuda_failure(cudaError_t e, const char* what) noexcept;
+
+// ---- element types ------------------------------------------------------------------------
+// Two adjacent elements as one load or store, computed on in fp32.  The only rounding to fewer
+// bits is that of a stored result to the tensors' own type.
+template <typename E> struct Pack2;
+template <> struct Pack2<float> {
+  using type = float2;
+  static __device__ __forceinline__ float2 up(float2 v) { return v; }
+  static __device__ __forceinline__ float2 down(float2 v) { return v; }
+};
+template <> struct Pack2<__half> {
+  using type = __half2;
+  static __device__ __forceinline__ float2 up(__half2 v) { return __half22float2(v); }
+  static __device__ __forceinline__ __half2 down(float2 v) { return __floats2half2_rn(v.x, v.y); }
+};
+template <> struct Pack2<__nv_bfloat16> {
+  using type = __nv_bfloat162;
+  static __device__ __forceinline__ float2 up(__nv_bfloat162 v) { return __bfloat1622float2(v); }
+  static __device__ __forceinline__ __nv_bfloat162 down(float2 v) { return __floats2bfloat162_rn(v.x, v.y); }
+};
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename E> __device__ __forceinline__ E from_f32(float v);
+template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// Eight adjacent elements.  VEC: the address is a multiple of 16 bytes and all eight exist;
+// otherwise the first n of them one by one, zeros for the rest.
+template <typename E, bool VEC>
+__device__ __forceinline__ void load8(const E* p, int n, float (&v)[8]) {
+  if (VEC) {
+    constexpr int Q = sizeof(E) * 8 / 16;
+    uint4 raw[Q];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) raw[q] = reinterpret_cast<const uint4*>(p)[q];
+    const typename Pack2<E>::type* h = reinterpret_cast<const typename Pack2<E>::type*>(raw);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 f = Pack2<E>::up(h[j]);
+      v[2 * j] = f.x;
+      v[2 * j + 1] = f.y;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < n ? to_f32(p[j]) : 0.f;
+  }
+}
+
+template <typename E, bool VEC>
+__device__ __forceinline__ void store8(E* p, int n, const float (&v)[8]) {
+  if (VEC) {
+    constexpr int Q = sizeof(E) * 8 / 16;
+    uint4 raw[Q];
+    typename Pack2<E>::type* h = reinterpret_cast<typename Pack2<E>::type*>(raw);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) h[j] = Pack2<E>::down(make_float2(v[2 * j], v[2 * j + 1]));
+#pragma unroll
+    for (int q = 0; q < Q; ++q) reinterpret_cast<uint4*>(p)[q] = raw[q];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < n) p[j] = from_f32<E>(v[j]);
+  }
+}
+
+// ---- counter-based generator ----------------------------------------------------------------
+// Philox4x32-10 (Salmon, Moraes, Dror and Shaw, SC 2011): ten rounds of two 32 x 32 -> 64 bit
+// products over a 128-bit counter.  The key depends on the seed alone, so its ten pairs are
+// worked out on the host and read as kernel constants.
+struct DropParams {
+  uint32_t key[20];
+  uint64_t offset;     // upper half of the counter
+  uint32_t threshold;  // dropped when the element's 16 bits are below it; 0 ... 65536
+  float scale;         // 65536 / (65536 - threshold), 0 when everything is dropped
+};
+
+__device__ __forceinline__ uint4 philox(uint64_t block, const DropParams& d) {
+  uint32_t x0 = (uint32_t)block, x1 = (uint32_t)(block >> 32);
+  uint32_t x2 = (uint32_t)d.offset, x3 = (uint32_t)(d.offset >> 32);
+#pragma unroll
+  for (int k = 0; k < 10; ++k) {
+    const uint64_t m0 = (uint64_t)x0 * 0xD2511F53u, m1 = (uint64_t)x2 * 0xCD9E8D57u;
+    x0 = (uint32_t)(m1 >> 32) ^ x1 ^ d.key[2 * k];
+    x1 = (uint32_t)m1;
+    x2 = (uint32_t)(m0 >> 32) ^ x3 ^ d.key[2 * k + 1];
+    x3 = (uint32_t)m0;
+  }
+  return make_uint4(x0, x1, x2, x3);
+}
+
+// Bit j set: element 8 * block + j is kept.  Element 2w + h takes half h of word w.
+__device__ __forceinline__ uint32_t keep8_block(uint64_t block, const DropParams& d) {
+  const uint4 w = philox(block, d);
+  const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+  uint32_t bits = 0;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    bits |= ((word[q] & 0xFFFFu) >= d.threshold ? 1u : 0u) << (2 * q);
+    bits |= ((word[q] >> 16) >= d.threshold ? 1u : 0u) << (2 * q + 1);
+  }
+  return bits;
+}
+
+// The same for the eight elements from `first`, wherever it lies in its block.
+template <bool ALIGNED>
+__device__ __forceinline__ uint32_t keep8(uint64_t first, const DropParams& d) {
+  if (d.threshold == 0) return 0xFFu;
+  uint32_t bits = keep8_block(first >> 3, d);
+  if (!ALIGNED) {
+    const uint32_t skip = (uint32_t)first & 7u;
+    if (skip) bits = (bits | (keep8_block((first >> 3) + 1, d) << 8)) >> skip;
+  }
+  return bits;
+}
+
+// A dropped element is zero whatever its value was (infinities and NaN included).
+__device__ __forceinline__ float drop(float v, uint32_t bits, int j, float scale) {
+  return (bits >> j) & 1u ? v * scale : 0.f;
+}
+
+// ---- parameter blocks -----------------------------------------------------------------------
+struct DropoutParams {
+  const void* x;
+  const void* residual;  // nullable
+  void* out;
+  int64_t x_stride, residual_stride, out_stride;
+  int64_t rows, cols;
+  DropParams drop;
+};
+
+struct NormForwardParams {
+  const void* x;
+  const void* residual;
+  const float* weight;
+  void* y;
+  void* z;
+  float* rstd;
+  int64_t x_stride, residual_stride, y_stride, z_stride;
+  int64_t rows;
+  int32_t cols;
+  float eps;
+  DropParams drop;
+};
+
+struct NormBackwardParams {
+  const void* dz;
+  const void* dy;  // nullable
+  const void* y;
+  const float* weight;
+  const float* rstd;
+  void* dx;         // nullable
+  void* dresidual;  // nullable
+  float* partial;   // [CTAs][cols]
+  int64_t dz_stride, dy_stride, y_stride, dx_stride, dresidual_stride;
+  int64_t rows;
+  int32_t cols;
+  DropParams drop;
+};
+
+// One [B][T][D] tensor: element (b, t, d) at data + b*batch + t*token + d.
+template <typename P>
+struct Seq {
+  P data;
+  int64_t batch, token;
+};
+
+struct RecurrenceParams {
+  Seq<const void*> x, r, i, dy;
+  Seq<void*> y, dx, dr, di;
+  const float* decay;
+  const float* h0;          // nullable
+  const uint8_t* reset;     // nullable, [B][T]
+  const int32_t* lengths;   // nullable, [B]
+  float* h_last;            // nullable
+  float* states;            // [B][chunks][D]; written by the forward pass when not NULL
+  const float* dh_last;     // nullable
+  float* dh0;               // nullable
+  float* partial;           // [B * cluster][D] sums of the decay's gradient
+  int64_t B, T, D;
+  float c;
+  int32_t groups;           // channel groups of a row
+};
+
+struct RecurrenceStepParams {
+  const void* x;
+  const void* r;
+  const void* i;
+  void* y;
+  int64_t x_stride, r_stride, i_stride, y_stride, state_stride;
+  const float* decay;
+  float* state;
+  const int32_t* slots;  // nullable
+  int64_t B, D, n_slots;
+  float c;
+};
+
+// ---- launchers ------------------------------------------------------------------------------
+cudaError_t launch_dropout(const DropoutParams& p, int dtype, bool vec, cudaStream_t s);
+
+constexpr int kNormMaxCols = 16384;
+int norm_backward_ctas(int64_t rows, int cols);
+cudaError_t launch_norm_forward(const NormForwardParams& p, int dtype, bool vec, cudaStream_t s);
+cudaError_t launch_norm_backward(const NormBackwardParams& p, float* dweight, int dtype, bool vec, cudaStream_t s);
+
+int64_t recurrence_chunks(int64_t T);
+int recurrence_cluster(int64_t B, int64_t T, int64_t D);
+cudaError_t launch_recurrence_forward(RecurrenceParams p, int dtype, bool vec, cudaStream_t s);
+cudaError_t launch_recurrence_backward(RecurrenceParams p, float* ddecay, int dtype, bool vec, cudaStream_t s);
+cudaError_t launch_recurrence_step(const RecurrenceStepParams& p, int dtype, bool vec, cudaStream_t s);
+
+// launch() with dynamic shared memory and a cluster of `cluster` CTAs along x.
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, int cluster,
+                                  cudaStream_t s, Args&&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
+}
+
+// Calls f with a value of the element type that `dtype` names.
+template <typename F>
+inline cudaError_t with_type(int dtype, F&& f) {
+  switch (dtype) {
+    case GS_F32: return f(float());
+    case GS_F16: return f(__half());
+    default: return f(__nv_bfloat16());
+  }
+}
+
+}  // namespace gs
