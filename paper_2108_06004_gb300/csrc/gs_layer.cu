@@ -168,9 +168,19 @@ gs_status check_seq_output(const gs_seq* t, int64_t B, int64_t T, int64_t D, int
   return GS_OK;
 }
 
-// whether pairs of channels can be read and written as one
-bool pairs(const gs_seq* t, int32_t dtype) {
-  return aligned(t->data, 2 * item(dtype)) && t->batch_stride % 2 == 0 && t->token_stride % 2 == 0;
+// whether every row starts at a multiple of `bytes`
+bool rows_at(const gs_seq* t, int32_t dtype, int bytes) {
+  return aligned(t->data, (uintptr_t)bytes) && t->batch_stride * item(dtype) % bytes == 0 &&
+         t->token_stride * item(dtype) % bytes == 0;
+}
+
+int copy_unit(const gs_seq* const* t, int n, int32_t dtype) {
+  for (int unit : {16, 4}) {
+    bool all = true;
+    for (int k = 0; k < n; ++k) all = all && rows_at(t[k], dtype, unit);
+    if (all) return unit;
+  }
+  return 2;
 }
 
 gs::Seq<const void*> in(const gs_seq* t) { return {t->data, t->batch_stride, t->token_stride}; }
@@ -179,7 +189,7 @@ gs::Seq<void*> out(const gs_seq* t) { return {t->data, t->batch_stride, t->token
 size_t round256(size_t n) { return n ? (n + 255) & ~size_t(255) : 256; }
 
 size_t states_bytes(int64_t B, int64_t T, int64_t D) {
-  return round256((size_t)B * (size_t)gs::recurrence_chunks(T) * (size_t)D * sizeof(float));
+  return round256((size_t)B * (size_t)gs::recurrence_states(T) * (size_t)D * sizeof(float));
 }
 
 size_t recurrence_ws_bytes(int64_t B, int64_t T, int64_t D) {
@@ -358,8 +368,9 @@ gs_status gs_recurrence_forward(const gs_seq* x, const gs_seq* r, const gs_seq* 
   p.T = T;
   p.D = D;
   p.c = c;
-  const bool vec = D % 2 == 0 && pairs(x, dtype) && pairs(r, dtype) && pairs(i, dtype) && pairs(y, dtype);
-  const cudaError_t e = gs::launch_recurrence_forward(p, dtype, vec, as_stream(stream));
+  const gs_seq* inputs[] = {x, r, i};
+  const cudaError_t e = gs::launch_recurrence_forward(p, dtype, copy_unit(inputs, 3, dtype),
+                                                      rows_at(y, dtype, 2 * item(dtype)), as_stream(stream));
   return e == cudaSuccess ? GS_OK : gs::record_cuda_failure(e, "recurrence_forward launch");
   GS_GUARD_END
 }
@@ -409,9 +420,11 @@ gs_status gs_recurrence_backward(const gs_seq* dy, const float* dh_last, const g
   p.T = T;
   p.D = D;
   p.c = c;
-  const bool vec = D % 2 == 0 && pairs(x, dtype) && pairs(r, dtype) && pairs(i, dtype) && pairs(dy, dtype) &&
-                   pairs(dx, dtype) && pairs(dr, dtype) && pairs(di, dtype);
-  const cudaError_t e = gs::launch_recurrence_backward(p, ddecay, dtype, vec, as_stream(stream));
+  const gs_seq* inputs[] = {x, r, i, dy};
+  const bool pair = rows_at(dx, dtype, 2 * item(dtype)) && rows_at(dr, dtype, 2 * item(dtype)) &&
+                    rows_at(di, dtype, 2 * item(dtype));
+  const cudaError_t e = gs::launch_recurrence_backward(p, ddecay, dtype, copy_unit(inputs, 4, dtype), pair,
+                                                       as_stream(stream));
   return e == cudaSuccess ? GS_OK : gs::record_cuda_failure(e, "recurrence_backward launch");
   GS_GUARD_END
 }
@@ -454,9 +467,9 @@ gs_status gs_recurrence_step(const void* x, int64_t x_stride, const void* r, int
   p.n_slots = n_slots;
   p.c = c;
   const uintptr_t two = 2 * item(dtype);
-  const bool vec = D % 2 == 0 && (x_stride | r_stride | i_stride | y_stride) % 2 == 0 && aligned(x, two) &&
-                   aligned(r, two) && aligned(i, two) && aligned(y, two);
-  const cudaError_t e = gs::launch_recurrence_step(p, dtype, vec, as_stream(stream));
+  const bool pair = (x_stride | r_stride | i_stride | y_stride) % 2 == 0 && aligned(x, two) && aligned(r, two) &&
+                    aligned(i, two) && aligned(y, two);
+  const cudaError_t e = gs::launch_recurrence_step(p, dtype, pair, as_stream(stream));
   return e == cudaSuccess ? GS_OK : gs::record_cuda_failure(e, "recurrence_step launch");
   GS_GUARD_END
 }

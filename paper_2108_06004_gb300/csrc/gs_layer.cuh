@@ -189,7 +189,7 @@ struct RecurrenceParams {
   const uint8_t* reset;     // nullable, [B][T]
   const int32_t* lengths;   // nullable, [B]
   float* h_last;            // nullable
-  float* states;            // [B][chunks][D]; written by the forward pass when not NULL
+  float* states;            // [B][states of a row][D]; written by the forward pass when not NULL
   const float* dh_last;     // nullable
   float* dh0;               // nullable
   float* partial;           // [B * cluster][D] sums of the decay's gradient
@@ -219,11 +219,14 @@ int norm_backward_ctas(int64_t rows, int cols);
 cudaError_t launch_norm_forward(const NormForwardParams& p, int dtype, bool vec, cudaStream_t s);
 cudaError_t launch_norm_backward(const NormBackwardParams& p, float* dweight, int dtype, bool vec, cudaStream_t s);
 
-int64_t recurrence_chunks(int64_t T);
+int64_t recurrence_states(int64_t T);  // states kept of a row and channel
 int recurrence_cluster(int64_t B, int64_t T, int64_t D);
-cudaError_t launch_recurrence_forward(RecurrenceParams p, int dtype, bool vec, cudaStream_t s);
-cudaError_t launch_recurrence_backward(RecurrenceParams p, float* ddecay, int dtype, bool vec, cudaStream_t s);
-cudaError_t launch_recurrence_step(const RecurrenceStepParams& p, int dtype, bool vec, cudaStream_t s);
+// unit: the largest of 16, 4 and 2 bytes that every input row can be copied by; pair: two adjacent
+// channels of every output can be stored as one
+cudaError_t launch_recurrence_forward(RecurrenceParams p, int dtype, int unit, bool pair, cudaStream_t s);
+cudaError_t launch_recurrence_backward(RecurrenceParams p, float* ddecay, int dtype, int unit, bool pair,
+                                       cudaStream_t s);
+cudaError_t launch_recurrence_step(const RecurrenceStepParams& p, int dtype, bool pair, cudaStream_t s);
 
 // launch() with dynamic shared memory and a cluster of `cluster` CTAs along x.
 template <typename... KArgs, typename... Args>
