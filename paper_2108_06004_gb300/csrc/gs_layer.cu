@@ -144,8 +144,8 @@ gs_status check_sequence_shape(int64_t B, int64_t T, int64_t D) {
   if (B < 0 || T < 0 || D < 0) return bad("B, T and D must not be negative");
   if (B > kMaxElements || T > kMaxRows || D > kMaxElements || !product_fits(B, D) || !product_fits(B * D, T))
     return bad("T must be below 2^31 and B * T * D at most 2^40");
-  // one CTA a row and channel group at the least, up to eight
-  if (B > 0 && (D + 63) / 64 > ((int64_t(1) << 31) - 1) / 8 / B) return bad("B * ceil(D / 64) must be below 2^28");
+  // one CTA for each row and 64 channels
+  if (B > 0 && (D + 63) / 64 >= (int64_t(1) << 28) / B) return bad("B * ceil(D / 64) must be below 2^28");
   return GS_OK;
 }
 
@@ -193,7 +193,7 @@ size_t states_bytes(int64_t B, int64_t T, int64_t D) {
 }
 
 size_t recurrence_ws_bytes(int64_t B, int64_t T, int64_t D) {
-  return round256((size_t)B * (size_t)gs::recurrence_cluster(B, T, D) * (size_t)D * sizeof(float));
+  return round256((size_t)gs::recurrence_partials(B, T, D) * (size_t)D * sizeof(float));
 }
 
 gs_status check_c(float c) {

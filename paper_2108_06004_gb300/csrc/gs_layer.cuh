@@ -214,17 +214,25 @@ struct RecurrenceStepParams {
 // ---- launchers ------------------------------------------------------------------------------
 cudaError_t launch_dropout(const DropoutParams& p, int dtype, bool vec, cudaStream_t s);
 
+constexpr int kSMs = 152;  // the sizes of grids are rules on it, so that results do not depend on a query
 constexpr int kNormMaxCols = 16384;
 int norm_backward_ctas(int64_t rows, int cols);
 cudaError_t launch_norm_forward(const NormForwardParams& p, int dtype, bool vec, cudaStream_t s);
 cudaError_t launch_norm_backward(const NormBackwardParams& p, float* dweight, int dtype, bool vec, cudaStream_t s);
 
+struct RecurrenceShape {
+  int channels;      // of a CTA
+  int cluster;       // CTAs that share a row's time
+  int32_t groups;    // CTAs side by side over the channels
+  unsigned grid;
+};
+RecurrenceShape recurrence_shape(int64_t B, int64_t T, int64_t D, int run, bool narrow);
 int64_t recurrence_states(int64_t T);  // states kept of a row and channel
-int recurrence_cluster(int64_t B, int64_t T, int64_t D);
+int64_t recurrence_partials(int64_t B, int64_t T, int64_t D);
 // unit: the largest of 16, 4 and 2 bytes that every input row can be copied by; pair: two adjacent
 // channels of every output can be stored as one
-cudaError_t launch_recurrence_forward(RecurrenceParams p, int dtype, int unit, bool pair, cudaStream_t s);
-cudaError_t launch_recurrence_backward(RecurrenceParams p, float* ddecay, int dtype, int unit, bool pair,
+cudaError_t launch_recurrence_forward(const RecurrenceParams& p, int dtype, int unit, bool pair, cudaStream_t s);
+cudaError_t launch_recurrence_backward(const RecurrenceParams& p, float* ddecay, int dtype, int unit, bool pair,
                                        cudaStream_t s);
 cudaError_t launch_recurrence_step(const RecurrenceStepParams& p, int dtype, bool pair, cudaStream_t s);
 

@@ -22,74 +22,71 @@ namespace {
 using namespace rec;
 
 constexpr int kLen = 16;                 // tokens of a run
-constexpr int kChunk = kSlots * kLen;    // tokens of a CTA's step
 
-template <typename E>
+template <typename E, int CH>
 struct ForwardShared {
-  E tile[2][3][kChunk][kChannels];       // x, r, i; the next step's are under way
-  float4 run[kSlots][kPairs];            // the map of each warp's run
-  uint32_t cut[kSlots];
-  Totals totals;
+  static constexpr int kRuns = Tile<E, CH, kLen>::kRuns;
+  static constexpr int kStages = sizeof(E) == 2 ? 2 : 1;
+  Tile<E, CH, kLen> tile[kStages][3];    // x, r, i; those of steps to come are under way
+  float4 run[kRuns][CH / 2];             // the map of each run
+  uint32_t cut[kRuns];
 };
 
-template <typename E, int UNIT, bool PAIR, bool RESET>
-__global__ void __launch_bounds__(kThreads, sizeof(E) == 2 ? 2 : 1)
+template <typename E, int CH, int UNIT, bool PAIR, bool RESET>
+__global__ void __launch_bounds__(kThreads, 4)
 k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
+  using Shared = ForwardShared<E, CH>;
+  constexpr int kRuns = Shared::kRuns, kStages = Shared::kStages, kChunk = kRuns * kLen;
   extern __shared__ __align__(128) unsigned char raw[];
-  ForwardShared<E>& sh = *reinterpret_cast<ForwardShared<E>*>(raw);
+  Shared& sh = *reinterpret_cast<Shared*>(raw);
   grid_begin();
-  const Place w = place(p);
+  const Place w = place<CH>(p);
+  Total<CH>* totals = reinterpret_cast<Total<CH>*>(raw + sizeof(Shared));  // [2][cluster], with a cluster
   if (w.cluster > 1) cg::this_cluster().sync();  // every CTA of the cluster runs before its memory is written
   const int64_t chunks = (w.len + kChunk - 1) / kChunk;
-  const int64_t steps = (chunks + w.cluster - 1) / w.cluster;
+  const int steps = (int)((chunks + w.cluster - 1) / w.cluster);
   const int64_t kept = (p.T + kStateEvery - 1) / kStateEvery;
-  const int channels = clamp_int(p.D - w.d0, kChannels);
+  const int channels = clamp_int(p.D - w.d0, CH);
   const E* x = static_cast<const E*>(p.x.data) + w.b * p.x.batch + w.d0;
   const E* r = static_cast<const E*>(p.r.data) + w.b * p.r.batch + w.d0;
   const E* i = static_cast<const E*>(p.i.data) + w.b * p.i.batch + w.d0;
   E* y = static_cast<E*>(p.y.data) + w.b * p.y.batch + w.d;
-  auto load = [&](int64_t s) {
-    const int64_t t0 = (s * w.cluster + w.rank) * kChunk;
+  auto chunk_token = [&](int s) { return ((int64_t)s * w.cluster + w.rank) * kChunk; };
+  auto load = [&](int s) {
+    const int64_t t0 = chunk_token(s);
     const int live = clamp_int(w.len - t0, kChunk);
-    load_tile<E, UNIT, kChunk>(&sh.tile[s & 1][0][0][0], x, p.x.token, t0, live, channels);
-    load_tile<E, UNIT, kChunk>(&sh.tile[s & 1][1][0][0], r, p.r.token, t0, live, channels);
-    load_tile<E, UNIT, kChunk>(&sh.tile[s & 1][2][0][0], i, p.i.token, t0, live, channels);
+    load_tile<UNIT>(sh.tile[s % kStages][0], x, p.x.token, t0, live, channels);
+    load_tile<UNIT>(sh.tile[s % kStages][1], r, p.r.token, t0, live, channels);
+    load_tile<UNIT>(sh.tile[s % kStages][2], i, p.i.token, t0, live, channels);
   };
-  auto first_token = [&](int64_t s) { return (s * w.cluster + w.rank) * kChunk + w.slot * kLen; };
-  if (steps > 0) load(0);
-  copy_commit();
-  if (steps > 1) load(1);
-  copy_commit();
+#pragma unroll
+  for (int s = 0; s < kStages; ++s) {
+    if (s < steps) load(s);
+    copy_commit();
+  }
   const float2 rate = decay_rate(load_f32(p.decay + w.d, w.n), p.c);
   const bool series = __all_sync(0xFFFFFFFFu, rate.x <= kSeries && rate.y <= kSeries);
   float2 state = load_f32(p.h0 ? p.h0 + w.b * p.D + w.d : nullptr, w.n);
-  uint8_t flag = 0;
-  if (RESET && steps > 0) flag = reset_flag(p, w, first_token(0), clamp_int(w.len - first_token(0), kLen));
-  for (int64_t s = 0; s < steps; ++s) {
-    const int64_t t0 = first_token(s);
-    const int live = clamp_int(w.len - t0, kLen);
-    const uint32_t resets = RESET ? __ballot_sync(0xFFFFFFFFu, flag != 0) : 0;
-    if (RESET && s + 1 < steps)
-      flag = reset_flag(p, w, first_token(s + 1), clamp_int(w.len - first_token(s + 1), kLen));
-    copy_wait<1>();
+  uint8_t flag = RESET ? reset_flag<kLen>(p, w, chunk_token(0) + w.slot * kLen) : 0;
+  for (int s = 0; s < steps; ++s) {
+    const int64_t t0 = chunk_token(s) + w.slot * kLen;
+    const bool full = chunk_token(s) + kChunk <= w.len;  // the chunk has no masked token
+    const uint32_t resets = RESET ? reset_bits<CH, kLen>(flag) : 0;
+    if (RESET) flag = reset_flag<kLen>(p, w, chunk_token(s + 1) + w.slot * kLen);
+    copy_wait<kStages - 1>();
     __syncthreads();
     // the run's tokens as a_t and b_t, and their composition
     float2 a[kLen], b[kLen];
     Run run = identity();
     auto gates = [&](auto some, auto in_series) {
-      constexpr bool SOME = decltype(some)::value;
+      const auto& tile = sh.tile[s % kStages];
 #pragma unroll
       for (int k = 0; k < kLen; ++k) {
-        using Raw = typename Pack2<E>::type;
-        const int row = w.slot * kLen + k;
-        const float2 xv = Pack2<E>::up(reinterpret_cast<const Raw*>(sh.tile[s & 1][0][row])[w.pair]);
-        const float2 rv = Pack2<E>::up(reinterpret_cast<const Raw*>(sh.tile[s & 1][1][row])[w.pair]);
-        const float2 iv = Pack2<E>::up(reinterpret_cast<const Raw*>(sh.tile[s & 1][2][row])[w.pair]);
-        const Gate g = gate<decltype(in_series)::value>(rv, iv, rate);
         const bool cut = RESET && (resets >> k & 1u);
-        a[k] = choose(cut, two(0.f), g.a);
-        b[k] = mul(mul(choose(cut, two(1.f), g.gain), g.si), xv);
-        if (SOME && k >= live) {  // past the end of the row: the state stays
+        float2 K;
+        gate_forward<decltype(in_series)::value>(capped(tile[1].at(w, k)), capped(tile[2].at(w, k)), rate, cut, a[k], K);
+        b[k] = mul(K, widen(tile[0].at(w, k)));
+        if (decltype(some)::value && t0 + k >= w.len) {  // past the end of the row: the state stays
           a[k] = two(1.f);
           b[k] = two(0.f);
         }
@@ -97,24 +94,22 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
         run.b = RESET ? apply(Run{a[k], b[k]}, cut, run.b) : fma(a[k], run.b, b[k]);
       }
     };
-    if (live == kLen) {
-      if (series)
-        gates(std::false_type(), std::true_type());
-      else
-        gates(std::false_type(), std::false_type());
-    } else {
+    if (!full)
       gates(std::true_type(), std::false_type());
-    }
+    else if (series)
+      gates(std::false_type(), std::true_type());
+    else
+      gates(std::false_type(), std::false_type());
     sh.run[w.slot][w.pair] = as_float4(run);
     if (RESET && w.pair == 0) sh.cut[w.slot] = resets;
     __syncthreads();
-    if (s + 2 < steps) load(s + 2);  // this step's tile has been read
+    if (s + kStages < steps) load(s + kStages);  // this step's tile has been read
     copy_commit();
-    // the maps of the warps before this one, and of the whole chunk
+    // the maps of the runs before this one, and of the whole chunk
     Run before, total = identity();
     bool before_cut, cut = false;
 #pragma unroll
-    for (int k = 0; k < kSlots; ++k) {
+    for (int k = 0; k < kRuns; ++k) {
       if (k == w.slot) {
         before = total;
         before_cut = cut;
@@ -123,57 +118,65 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
     }
     float2 h = state;
     if (w.cluster > 1) {
-      exchange(sh.totals, (int)(s & 1), w, total, cut);
+      Total<CH>* table = totals + (s & 1) * w.cluster;
+      exchange<CH, kRuns>(table, w, total, cut);
       for (int k = 0; k < w.cluster; ++k) {
         if (k == w.rank) h = state;
-        state = apply(as_run(sh.totals.run[s & 1][k][w.pair]), RESET && sh.totals.cut[s & 1][k] != 0, state);
+        state = apply(as_run(table[k].run[w.pair]), RESET && table[k].cut != 0, state);
       }
     } else {
       state = apply(total, cut, state);
     }
     h = apply(before, before_cut, h);
-    if (p.states && w.slot % (kStateEvery / kLen) == 0 && t0 / kStateEvery < kept)
+    if (p.states && t0 % kStateEvery == 0 && t0 / kStateEvery < kept)
       store_f32(p.states + (w.b * kept + t0 / kStateEvery) * p.D + w.d, w.n, h);
     E* out = y + t0 * p.y.token;
+    if (full && PAIR && w.n == 2) {
 #pragma unroll
-    for (int k = 0; k < kLen; ++k) {
-      if (k < live) {
+      for (int k = 0; k < kLen; ++k) {
         h = RESET ? apply(Run{a[k], b[k]}, resets >> k & 1u, h) : fma(a[k], h, b[k]);
-        store2<E, PAIR>(out, w.n, h);
-      } else if (t0 + k < p.T) {
-        store2<E, PAIR>(out, w.n, two(0.f));
+        *reinterpret_cast<typename Pack2<E>::type*>(out) = Pack2<E>::down(h);
+        out += p.y.token;
       }
-      out += p.y.token;
+    } else {
+#pragma unroll
+      for (int k = 0; k < kLen; ++k) {
+        h = RESET ? apply(Run{a[k], b[k]}, resets >> k & 1u, h) : fma(a[k], h, b[k]);
+        if (t0 + k < p.T) store2<E, PAIR>(out, w.n, t0 + k < w.len ? h : two(0.f));
+        out += p.y.token;
+      }
     }
   }
   // past the last step every token is masked
-  for (int64_t chunk = steps * w.cluster + w.rank; chunk * kChunk < p.T; chunk += w.cluster)
+  for (int64_t t0 = chunk_token(steps); t0 < p.T; t0 += (int64_t)w.cluster * kChunk)
     for (int k = 0; k < kLen; ++k) {
-      const int64_t t = chunk * kChunk + w.slot * kLen + k;
+      const int64_t t = t0 + w.slot * kLen + k;
       if (t < p.T) store2<E, PAIR>(y + t * p.y.token, w.n, two(0.f));
     }
   if (p.h_last && w.rank == 0 && w.slot == 0) store_f32(p.h_last + w.b * p.D + w.d, w.n, state);
 }
 
-template <typename E, int UNIT, bool PAIR, bool RESET>
-cudaError_t run_forward(const RecurrenceParams& p, unsigned grid, int cluster, cudaStream_t s) {
+template <typename E, int CH, int UNIT, bool PAIR, bool RESET>
+cudaError_t run_forward(RecurrenceParams p, const RecurrenceShape& shape, cudaStream_t s) {
   static std::atomic<uint64_t> done{0};
-  const auto kernel = k_recurrence_forward<E, UNIT, PAIR, RESET>;
-  const cudaError_t e = prepare_kernel(kernel, sizeof(ForwardShared<E>), done);
+  const auto kernel = k_recurrence_forward<E, CH, UNIT, PAIR, RESET>;
+  constexpr size_t kBase = sizeof(ForwardShared<E, CH>), kTotal = 2 * sizeof(Total<CH>);
+  const cudaError_t e = prepare_kernel(kernel, kBase + kMaxCluster * kTotal, done);
   if (e != cudaSuccess) return e;
-  return launch_cluster(kernel, dim3(grid), dim3(kThreads), sizeof(ForwardShared<E>), cluster, s, p);
+  p.groups = shape.groups;
+  const size_t smem = kBase + (shape.cluster > 1 ? shape.cluster * kTotal : 0);
+  return launch_cluster(kernel, dim3(shape.grid), dim3(kThreads), smem, shape.cluster, s, p);
 }
 
-template <typename E, int UNIT, bool PAIR>
-cudaError_t run_forward(const RecurrenceParams& p, unsigned grid, int cluster, cudaStream_t s) {
-  return p.reset ? run_forward<E, UNIT, PAIR, true>(p, grid, cluster, s)
-                 : run_forward<E, UNIT, PAIR, false>(p, grid, cluster, s);
+template <typename E, int CH, int UNIT, bool PAIR>
+cudaError_t run_forward(const RecurrenceParams& p, const RecurrenceShape& shape, cudaStream_t s) {
+  return p.reset ? run_forward<E, CH, UNIT, PAIR, true>(p, shape, s) : run_forward<E, CH, UNIT, PAIR, false>(p, shape, s);
 }
 
 // Two adjacent channels of one token, zero where they do not exist.
 template <typename E, bool PAIR>
 __device__ __forceinline__ float2 load2(const E* p, int n) {
-  if (PAIR && n == 2) return Pack2<E>::up(*reinterpret_cast<const typename Pack2<E>::type*>(p));
+  if (PAIR && n == 2) return widen(*reinterpret_cast<const typename Pack2<E>::type*>(p));
   return make_float2(n > 0 ? to_f32(p[0]) : 0.f, n > 1 ? to_f32(p[1]) : 0.f);
 }
 
@@ -193,8 +196,9 @@ __global__ void __launch_bounds__(128) k_recurrence_step(const __grid_constant__
       const float2 iv = load2<E, PAIR>(static_cast<const E*>(p.i) + b * p.i_stride + d, n);
       float* state = p.state + slot * p.state_stride + d;
       h = load_f32(state, n);
-      const Gate g = gate<false>(rv, iv, decay_rate(lam, p.c));
-      h = fma(g.a, h, mul(mul(g.gain, g.si), xv));
+      float2 a, K;
+      gate_forward<false>(capped(rv), capped(iv), decay_rate(lam, p.c), false, a, K);
+      h = fma(a, h, mul(K, xv));
       store_f32(state, n, h);
     }
     store2<E, PAIR>(static_cast<E*>(p.y) + b * p.y_stride + d, n, h);
@@ -205,27 +209,37 @@ __global__ void __launch_bounds__(128) k_recurrence_step(const __grid_constant__
 
 int64_t recurrence_states(int64_t T) { return (T + kStateEvery - 1) / kStateEvery; }
 
-// CTAs that share a row's time: doubled while the device (152 SMs, two CTAs each) has room and
-// there are chunks to deal.
-int recurrence_cluster(int64_t B, int64_t T, int64_t D) {
-  const int64_t columns = B * ((D + kChannels - 1) / kChannels), chunks = (T + kChunk - 1) / kChunk;
-  int c = 1;
-  while (c < kMaxCluster && columns * c < 2 * 152 && 2 * c <= chunks) c *= 2;
-  return c;
+// How a pass of `run` tokens a thread is cut: the channels of a CTA, and the CTAs of a cluster that
+// share a row's time.  SMs hold about four CTAs; the cluster is doubled until there are three for
+// each SM or no chunks left to deal.  Where 64 channels a CTA do not get there, 32 do better: twice
+// the CTAs, with twice the tokens each.
+RecurrenceShape recurrence_shape(int64_t B, int64_t T, int64_t D, int run, bool narrow) {
+  RecurrenceShape best = {};
+  for (int channels : {64, 32}) {
+    RecurrenceShape c;
+    c.channels = channels;
+    c.groups = (int32_t)((D + channels - 1) / channels);
+    const int64_t columns = B * c.groups, chunk = kThreads / (channels / 2) * run;
+    c.cluster = 1;
+    while (c.cluster < kMaxCluster && columns * c.cluster < 3 * kSMs && 2 * c.cluster * chunk <= T) c.cluster *= 2;
+    c.grid = (unsigned)(columns * c.cluster);
+    if (channels == 64) best = c;
+    else if (narrow && best.grid < 2 * kSMs && c.grid > best.grid) best = c;
+  }
+  return best;
 }
 
-cudaError_t launch_recurrence_forward(RecurrenceParams p, int dtype, int unit, bool pair, cudaStream_t s) {
-  const int cluster = recurrence_cluster(p.B, p.T, p.D);
-  p.groups = (int32_t)((p.D + kChannels - 1) / kChannels);
-  const unsigned grid = (unsigned)(p.B * p.groups * cluster);
+cudaError_t launch_recurrence_forward(const RecurrenceParams& p, int dtype, int unit, bool pair, cudaStream_t s) {
+  const RecurrenceShape shape = recurrence_shape(p.B, p.T, p.D, kLen, unit == 16 && pair);
   return with_type(dtype, [&](auto e) {
     using E = decltype(e);
-    if (unit == 16 && pair) return run_forward<E, 16, true>(p, grid, cluster, s);
+    if (unit == 16 && pair)
+      return shape.channels == 64 ? run_forward<E, 64, 16, true>(p, shape, s) : run_forward<E, 32, 16, true>(p, shape, s);
     if constexpr (sizeof(E) == 2) {
-      if (unit >= 4 && pair) return run_forward<E, 4, true>(p, grid, cluster, s);
-      return run_forward<E, 2, false>(p, grid, cluster, s);
+      if (unit >= 4 && pair) return run_forward<E, 64, 4, true>(p, shape, s);
+      return run_forward<E, 64, 2, false>(p, shape, s);
     } else {
-      return run_forward<E, 4, false>(p, grid, cluster, s);
+      return run_forward<E, 64, 4, false>(p, shape, s);
     }
   });
 }

@@ -13,11 +13,8 @@ namespace rec {
 
 namespace cg = cooperative_groups;
 
-constexpr int kSlots = 8;                // warps of a CTA, one run of tokens each
-constexpr int kThreads = kSlots * 32;
-constexpr int kPairs = 32;               // lanes: two channels each
-constexpr int kChannels = 2 * kPairs;
-constexpr int kStateEvery = 64;          // tokens between the states kept for the backward pass
+constexpr int kThreads = 128;
+constexpr int kStateEvery = 32;          // tokens between the states kept for the backward pass
 constexpr int kMaxCluster = 16;
 
 __device__ __forceinline__ float ex2(float x) {
@@ -42,6 +39,25 @@ __device__ __forceinline__ float at_most(float x, float most) {
   return y;
 }
 
+// Two adjacent elements in fp32.  bf16 is the upper half of an fp32 value.
+__device__ __forceinline__ float2 widen(float2 v) { return v; }
+__device__ __forceinline__ float2 widen(__half2 v) { return __half22float2(v); }
+__device__ __forceinline__ float2 widen(__nv_bfloat162 v) {
+  const uint32_t u = *reinterpret_cast<const uint32_t*>(&v);
+  return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u));
+}
+constexpr float kMostGate = 27.f;   // sigmoid is 1 to fp32 from well below this
+
+// A gate's value, capped where its sigmoid is 1 in fp32, so that no square of an exponential below
+// overflows.  The cap is exact in every type and taken before widening, two elements at once.
+__device__ __forceinline__ float2 capped(float2 v) {
+  return make_float2(at_most(v.x, kMostGate), at_most(v.y, kMostGate));
+}
+__device__ __forceinline__ float2 capped(__half2 v) { return widen(__hmin2_nan(v, __float2half2_rn(kMostGate))); }
+__device__ __forceinline__ float2 capped(__nv_bfloat162 v) {
+  return widen(__hmin2_nan(v, __float2bfloat162_rn(kMostGate)));
+}
+
 // Two channels at a time: one instruction for both.
 __device__ __forceinline__ float2 two(float v) { return make_float2(v, v); }
 __device__ __forceinline__ float2 mul(float2 a, float2 b) { return __fmul2_rn(a, b); }
@@ -50,8 +66,7 @@ __device__ __forceinline__ float2 fma(float2 a, float2 b, float2 c) { return __f
 __device__ __forceinline__ float2 choose(bool c, float2 a, float2 b) { return make_float2(c ? a.x : b.x, c ? a.y : b.y); }
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kHuge = 1099511627776.f;  // 2^40
-constexpr float kSeries = 0.25f;          // the series serves -q up to here
+constexpr float kSeries = 0.5f;     // the series serves -q up to here
 
 // softplus without overflow; for very negative arguments it is exp(x) and goes to zero.
 __device__ __forceinline__ float softplus(float x) { return x > 20.f ? x : log1pf(expf(x)); }
@@ -62,55 +77,85 @@ __device__ __forceinline__ float2 decay_rate(float2 lam, float c) {
 }
 
 // What a token's gates give, with rate = c softplus(lambda) and q = log a = -rate sigmoid(r):
-//   z = sqrt(sigmoid(r)) = p / sqrt(1 + p^2), p = e^(r/2);   sigmoid(i) = p^2 / (1 + p^2), p = e^(i/2)
-//   a = 1 + q s,   s = (e^q - 1) / q,   1 - a^2 = (1 - a)(1 + a) = z^2 X,   X = rate s (1 + a)
-// Halving the exponents keeps both gates exact to a few roundings down to the smallest numbers,
-// and capping p at 2^40 (where they are 1) keeps them from overflowing.  1 - a is never taken as
-// a difference where it is small: s is a series for q > -1/4 (five terms past the first, a
-// relative error below 5e-8), and a = 1 + q s is then off by half a rounding, where the
-// exponential's own bias would add up over the thousands of tokens that a state lives.
-// sqrt(1 - a^2) = z X rsqrt(X), and its derivatives need z rsqrt(X) and no quotient that could
-// be 0/0: X is about 2 rate even where the gate is shut.
-struct Gate {
-  float2 z, sr, si;  // sqrt(sigmoid(r)), sigmoid(r), sigmoid(i)
-  float2 a;
-  float2 rx;         // rsqrt(X)
-  float2 gain;       // sqrt(1 - a^2)
-};
+//   sigmoid(r) = p^2 / (1 + p^2), p = e^(r/2), and i alike;  z = sqrt(sigmoid(r)) = p / sqrt(1 + p^2);
+//   a = 1 + q s,  s = (e^q - 1) / q,  1 - a^2 = (1 - a)(1 + a) = sigmoid(r) X,  X = rate s (1 + a);
+//   K = sqrt(1 - a^2) sigmoid(i).
+// Halving the exponents keeps both gates, and the root of the first, exact to a few roundings down
+// to the smallest numbers.  1 - a is never taken as a difference where it is small: for q >= -1/2
+// s is the polynomial of degree 4 through its values at the five Chebyshev points (relative error
+// below 9e-8), and a = 1 + q s is then off by half a rounding, where the exponential's own bias
+// would add up over the thousands of tokens that a state lives.  X is about 2 rate even where the
+// gate is shut, so nothing here is 0/0.
 
-// SERIES: rate is at most kSeries in both channels, so q always is in the series' range.
+// SERIES: rate is at most kSeries in both channels, so q always is in the polynomial's range.
 template <bool SERIES>
-__device__ __forceinline__ Gate gate(float2 r, float2 i, float2 rate) {
-  Gate g;
+__device__ __forceinline__ void decay_of(float2 sr, float2 rate, float2& a, float2& X) {
   const float2 one = two(1.f);
-  const float2 hr = mul(r, two(0.5f * kLog2e)), hi = mul(i, two(0.5f * kLog2e));
-  const float2 pr = make_float2(at_most(ex2(hr.x), kHuge), at_most(ex2(hr.y), kHuge));
-  const float2 pi = make_float2(at_most(ex2(hi.x), kHuge), at_most(ex2(hi.y), kHuge));
-  const float2 ur = fma(pr, pr, one);
-  g.z = mul(pr, make_float2(rsq(ur.x), rsq(ur.y)));
-  g.sr = mul(g.z, g.z);
-  const float2 sq = mul(pi, pi), ui = add(sq, one);
-  g.si = mul(sq, make_float2(rcp(ui.x), rcp(ui.y)));
-  const float2 q = mul(make_float2(-rate.x, -rate.y), g.sr);
-  float2 s = fma(q, two(1.f / 720.f), two(1.f / 120.f));
-  s = fma(q, s, two(1.f / 24.f));
-  s = fma(q, s, two(1.f / 6.f));
-  s = fma(q, s, two(0.5f));
-  s = fma(q, s, one);
-  g.a = fma(q, s, one);
+  const float2 q = mul(make_float2(-rate.x, -rate.y), sr);
+  float2 s = fma(q, two(0.006782862555491099f), two(0.041013210491015605f));
+  s = fma(q, s, two(0.16655192765429086f));
+  s = fma(q, s, two(0.4999928833780279f));
+  s = fma(q, s, two(0.999999928937559f));
+  a = fma(q, s, one);
   if (!SERIES) {
     if (q.x < -kSeries) {
-      g.a.x = ex2(kLog2e * q.x);
-      s.x = (1.f - g.a.x) * rcp(-q.x);
+      a.x = ex2(kLog2e * q.x);
+      s.x = (1.f - a.x) * rcp(-q.x);
     }
     if (q.y < -kSeries) {
-      g.a.y = ex2(kLog2e * q.y);
-      s.y = (1.f - g.a.y) * rcp(-q.y);
+      a.y = ex2(kLog2e * q.y);
+      s.y = (1.f - a.y) * rcp(-q.y);
     }
   }
-  const float2 X = mul(mul(rate, s), add(g.a, one));
-  g.rx = make_float2(rsq(X.x), rsq(X.y));
-  g.gain = mul(mul(g.z, X), g.rx);
+  X = mul(mul(rate, s), add(a, one));
+}
+
+__device__ __forceinline__ float2 half_exp(float2 v) {
+  const float2 h = mul(v, two(0.5f * kLog2e));
+  return make_float2(ex2(h.x), ex2(h.y));
+}
+__device__ __forceinline__ float2 rcp(float2 v) { return make_float2(rcp(v.x), rcp(v.y)); }
+__device__ __forceinline__ float2 rsq(float2 v) { return make_float2(rsq(v.x), rsq(v.y)); }
+
+// a and K, from capped gate values.  The three roots and quotients of K are one reciprocal root;
+// with the cap its argument stays
+// below 2^120 (X is large only where sigmoid(r) is small, and 1 + p^2 then is about 1).  `cut`: a reset, a = 0 and K = sigmoid(i).
+template <bool SERIES>
+__device__ __forceinline__ void gate_forward(float2 r, float2 i, float2 rate, bool cut, float2& a, float2& K) {
+  const float2 one = two(1.f);
+  const float2 pr = half_exp(r), pi = half_exp(i);
+  const float2 sqr = mul(pr, pr), sqi = mul(pi, pi);
+  const float2 ur = add(sqr, one), ui = add(sqi, one);
+  float2 X;
+  decay_of<SERIES>(mul(sqr, rcp(ur)), rate, a, X);
+  K = mul(mul(mul(pr, sqi), X), rsq(mul(mul(ur, ui), mul(ui, X))));
+  if (cut) {
+    a = two(0.f);
+    K = mul(sqi, rcp(ui));
+  }
+}
+
+// What the backward pass needs: sigmoid(r), a, K, 1 - sigmoid(i) and 1 / X.
+struct Gate {
+  float2 sr, a, K, off, inv_X;
+};
+template <bool SERIES>
+__device__ __forceinline__ Gate gate_backward(float2 r, float2 i, float2 rate, bool cut) {
+  Gate g;
+  const float2 one = two(1.f);
+  const float2 pr = half_exp(r), pi = half_exp(i);
+  const float2 z = mul(pr, rsq(fma(pr, pr, one))), sqi = mul(pi, pi);
+  g.off = rcp(add(sqi, one));
+  g.sr = mul(z, z);
+  float2 X;
+  decay_of<SERIES>(g.sr, rate, g.a, X);
+  const float2 si = mul(sqi, g.off), rx = rsq(X);
+  g.inv_X = mul(rx, rx);
+  g.K = mul(mul(mul(z, X), rx), si);
+  if (cut) {
+    g.a = two(0.f);
+    g.K = si;
+  }
   return g;
 }
 
@@ -153,6 +198,7 @@ __device__ __forceinline__ void store2(E* p, int n, float2 v) {
 }
 
 // Where a thread works: its row of the batch, its channels, its place in the CTA and cluster.
+// The CTA owns CH channels and kThreads / (CH / 2) runs of tokens.
 struct Place {
   int64_t b, d0, d;      // row, first channel of the CTA, first channel of the thread
   int n;                 // the thread's channels that exist, 0 ... 2
@@ -161,15 +207,16 @@ struct Place {
   int64_t len;           // tokens of the row
 };
 
+template <int CH>
 __device__ __forceinline__ Place place(const RecurrenceParams& p) {
   Place w;
   w.cluster = (int)cg::this_cluster().num_blocks();
   w.rank = (int)cg::this_cluster().block_rank();
   const unsigned column = blockIdx.x / (unsigned)w.cluster;
   w.b = column / (unsigned)p.groups;
-  w.pair = threadIdx.x & 31;
-  w.slot = threadIdx.x >> 5;
-  w.d0 = (int64_t)(column - (unsigned)w.b * (unsigned)p.groups) * kChannels;
+  w.pair = threadIdx.x % (CH / 2);
+  w.slot = threadIdx.x / (CH / 2);
+  w.d0 = (int64_t)(column - (unsigned)w.b * (unsigned)p.groups) * CH;
   w.d = w.d0 + 2 * w.pair;
   w.n = (int)(p.D - w.d < 0 ? 0 : p.D - w.d < 2 ? p.D - w.d : 2);
   w.len = p.T;
@@ -182,17 +229,37 @@ __device__ __forceinline__ Place place(const RecurrenceParams& p) {
 
 __device__ __forceinline__ int clamp_int(int64_t v, int most) { return v < 0 ? 0 : v < most ? (int)v : most; }
 
-// Resets among the `live` tokens of a warp from t0 on, one bit each: lane k reads the flag of
-// token k (ahead of time), the warp collects them.
-__device__ __forceinline__ uint8_t reset_flag(const RecurrenceParams& p, const Place& w, int64_t t0, int live) {
-  return w.pair < live ? p.reset[w.b * p.T + t0 + w.pair] : 0;
+// Resets among the LEN tokens of a run from t0 on, one bit each.  The first LEN lanes that work on
+// the run read one flag each, ahead of time; the warp collects them.
+template <int LEN>
+__device__ __forceinline__ uint8_t reset_flag(const RecurrenceParams& p, const Place& w, int64_t t0) {
+  return w.pair < LEN && t0 + w.pair < w.len ? p.reset[w.b * p.T + t0 + w.pair] : 0;
+}
+template <int CH, int LEN>
+__device__ __forceinline__ uint32_t reset_bits(uint8_t flag) {
+  const uint32_t all = __ballot_sync(0xFFFFFFFFu, flag != 0);
+  constexpr int kLanes = CH / 2 < 32 ? CH / 2 : 32;
+  return (all >> (threadIdx.x & 31) / kLanes * kLanes) & ((1u << LEN) - 1);
 }
 
 // ---- tile loads -----------------------------------------------------------------------------
-// A tile is [TOKENS][kChannels] elements in shared memory: tokens t0 ... t0 + live - 1 of the
-// CTA's channels, of which `channels` exist; what does not exist is zero.  UNIT is the size of one
-// copy: 16 or 4 bytes asynchronously, or single 2-byte elements through registers, where rows of a
-// 2-byte type start at odd elements.
+// A tile holds CH channels of kThreads / (CH / 2) runs of LEN tokens in shared memory: tokens
+// t0 ... t0 + live - 1 of the CTA's channels, of which `channels` exist; what does not exist is
+// zero.  Where a warp reads two runs at once, every other run is moved by half the banks.  UNIT is
+// the size of one copy: 16 or 4 bytes asynchronously, or single 2-byte elements through
+// registers, where rows of a 2-byte type start at odd elements.
+template <typename E, int CH, int LEN>
+struct Tile {
+  static constexpr int kRuns = kThreads / (CH / 2);
+  static constexpr int kTokens = kRuns * LEN;
+  static constexpr int kPad = CH == 32 && sizeof(E) == 2 ? CH : 0;
+  static constexpr int kRun = LEN * CH + kPad;  // elements from one run to the next
+  E v[kRuns * kRun];
+  __device__ __forceinline__ const typename Pack2<E>::type& at(const Place& w, int k) const {
+    return reinterpret_cast<const typename Pack2<E>::type*>(v + w.slot * kRun + k * CH)[w.pair];
+  }
+};
+
 template <int UNIT>
 __device__ __forceinline__ void copy_async(void* to, const void* from, int bytes) {
   const uint32_t dst = (uint32_t)__cvta_generic_to_shared(to);
@@ -207,53 +274,58 @@ __device__ __forceinline__ void copy_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
 }
 
-template <typename E, int UNIT, int TOKENS>
-__device__ __forceinline__ void load_tile(E* tile, const E* from, int64_t token_stride, int64_t t0, int live,
-                                          int channels) {
+template <int UNIT, typename E, int CH, int LEN>
+__device__ __forceinline__ void load_tile(Tile<E, CH, LEN>& tile, const E* from, int64_t token_stride, int64_t t0,
+                                          int live, int channels) {
+  using Shape = Tile<E, CH, LEN>;
   constexpr int PER = UNIT / (int)sizeof(E);      // elements of a copy
-  constexpr int U = kChannels / PER;              // copies of a token
+  constexpr int U = CH / PER;                     // copies of a token
   constexpr int R = kThreads / U;                 // tokens at a time
+  constexpr int N = Shape::kTokens / R;
   const int u = threadIdx.x % U, row = threadIdx.x / U;
-  const E* src = from + t0 * token_stride + (int64_t)row * token_stride + u * PER;
-  E* dst = tile + row * kChannels + u * PER;
+  const E* src = from + (t0 + row) * token_stride + u * PER;
   const int have = clamp_int(channels - u * PER, PER);
+  auto to = [&](int j) { return tile.v + (row + j * R) / LEN * Shape::kRun + (row + j * R) % LEN * CH + u * PER; };
   if constexpr (UNIT == 2) {
-    constexpr int BATCH = 8;
+    constexpr int BATCH = N < 8 ? N : 8;
 #pragma unroll
-    for (int j0 = 0; j0 < TOKENS / R; j0 += BATCH) {
+    for (int j0 = 0; j0 < N; j0 += BATCH) {
       E v[BATCH];
 #pragma unroll
       for (int j = 0; j < BATCH; ++j)
         v[j] = have > 0 && row + (j0 + j) * R < live ? src[(int64_t)(j0 + j) * R * token_stride] : from_f32<E>(0.f);
 #pragma unroll
-      for (int j = 0; j < BATCH; ++j) dst[(j0 + j) * R * kChannels] = v[j];
+      for (int j = 0; j < BATCH; ++j) *to(j0 + j) = v[j];
     }
   } else {
 #pragma unroll
-    for (int j = 0; j < TOKENS / R; ++j) {
+    for (int j = 0; j < N; ++j) {
       const bool some = have > 0 && row + j * R < live;
-      copy_async<UNIT>(dst + j * R * kChannels, some ? src : from, some ? have * (int)sizeof(E) : 0);
+      copy_async<UNIT>(to(j), some ? src : from, some ? have * (int)sizeof(E) : 0);
       src += R * token_stride;
     }
   }
 }
 
 // ---- exchange over the cluster ----------------------------------------------------------------
-// The chunks' maps.  `mine` of this CTA goes into every CTA's table at this rank; warp k writes to
-// the CTAs k, k + kSlots, ...  The two halves of the table alternate, so one barrier a step is
-// enough: a CTA writes step s + 2 only after all have passed the barrier of s + 1, and so have
-// read step s.
-struct Totals {
-  float4 run[2][kMaxCluster][kPairs];
-  uint32_t cut[2][kMaxCluster];
+// The chunks' maps.  `mine` of this CTA goes into every CTA's table at this rank; the threads of
+// run k write to the CTAs k, k + RUNS, ...  The two halves of the table alternate, so one barrier
+// a step is enough: a CTA writes step s + 2 only after all have passed the barrier of s + 1, and
+// so have read step s.  The table lies at the end of the CTA's shared memory, with as many rows as
+// the cluster has CTAs.
+template <int CH>
+struct Total {
+  float4 run[CH / 2];
+  uint32_t cut, unused[3];
 };
 
-__device__ __forceinline__ void exchange(Totals& t, int half, const Place& w, const Run& mine, bool cut) {
+template <int CH, int RUNS>
+__device__ __forceinline__ void exchange(Total<CH>* table, const Place& w, const Run& mine, bool cut) {
   cg::cluster_group cl = cg::this_cluster();
-  for (int k = w.slot; k < w.cluster; k += kSlots) {
-    Totals* to = cl.map_shared_rank(&t, k);
-    to->run[half][w.rank][w.pair] = as_float4(mine);
-    if (w.pair == 0) to->cut[half][w.rank] = cut;
+  for (int k = w.slot; k < w.cluster; k += RUNS) {
+    Total<CH>* to = cl.map_shared_rank(table, k) + w.rank;
+    to->run[w.pair] = as_float4(mine);
+    if (w.pair == 0) to->cut = cut;
   }
   cl.sync();
 }
