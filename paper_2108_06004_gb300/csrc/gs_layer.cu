@@ -1,6 +1,7 @@
 // C ABI of the recurrent layer's operators: argument checks and parameter blocks.
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 #include <new>
 #include <string>
 
@@ -174,13 +175,20 @@ bool rows_at(const gs_seq* t, int32_t dtype, int bytes) {
          t->token_stride * item(dtype) % bytes == 0;
 }
 
-int copy_unit(const gs_seq* const* t, int n, int32_t dtype) {
-  for (int unit : {16, 4}) {
-    bool all = true;
-    for (int k = 0; k < n; ++k) all = all && rows_at(t[k], dtype, unit);
-    if (all) return unit;
+// How the tensors of a call can be moved: 16 (tiles), 4 (with pairs of channels stored as one), or
+// the type's size.  Tiles want coordinates that fit 32 bits.
+int copy_unit(std::initializer_list<const gs_seq*> in, std::initializer_list<const gs_seq*> out, int64_t B, int64_t T,
+              int64_t D, int32_t dtype) {
+  bool tiles = D * item(dtype) % 16 == 0 && T < (1 << 30) && D < (1 << 30) && B < (1 << 30), words = true;
+  for (const gs_seq* t : in) {
+    tiles = tiles && rows_at(t, dtype, 16);
+    words = words && rows_at(t, dtype, 4);
   }
-  return 2;
+  for (const gs_seq* t : out) {
+    tiles = tiles && rows_at(t, dtype, 16);
+    words = words && rows_at(t, dtype, 2 * item(dtype));
+  }
+  return tiles ? 16 : words ? 4 : item(dtype);
 }
 
 gs::Seq<const void*> in(const gs_seq* t) { return {t->data, t->batch_stride, t->token_stride}; }
@@ -368,9 +376,8 @@ gs_status gs_recurrence_forward(const gs_seq* x, const gs_seq* r, const gs_seq* 
   p.T = T;
   p.D = D;
   p.c = c;
-  const gs_seq* inputs[] = {x, r, i};
-  const cudaError_t e = gs::launch_recurrence_forward(p, dtype, copy_unit(inputs, 3, dtype),
-                                                      rows_at(y, dtype, 2 * item(dtype)), as_stream(stream));
+  const int unit = copy_unit({x, r, i}, {y}, B, T, D, dtype);
+  const cudaError_t e = gs::launch_recurrence_forward(p, dtype, unit, as_stream(stream));
   return e == cudaSuccess ? GS_OK : gs::record_cuda_failure(e, "recurrence_forward launch");
   GS_GUARD_END
 }
@@ -420,11 +427,8 @@ gs_status gs_recurrence_backward(const gs_seq* dy, const float* dh_last, const g
   p.T = T;
   p.D = D;
   p.c = c;
-  const gs_seq* inputs[] = {x, r, i, dy};
-  const bool pair = rows_at(dx, dtype, 2 * item(dtype)) && rows_at(dr, dtype, 2 * item(dtype)) &&
-                    rows_at(di, dtype, 2 * item(dtype));
-  const cudaError_t e = gs::launch_recurrence_backward(p, ddecay, dtype, copy_unit(inputs, 4, dtype), pair,
-                                                       as_stream(stream));
+  const int unit = copy_unit({x, r, i, dy}, {dx, dr, di}, B, T, D, dtype);
+  const cudaError_t e = gs::launch_recurrence_backward(p, ddecay, dtype, unit, as_stream(stream));
   return e == cudaSuccess ? GS_OK : gs::record_cuda_failure(e, "recurrence_backward launch");
   GS_GUARD_END
 }

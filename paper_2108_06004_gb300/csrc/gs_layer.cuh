@@ -2,6 +2,7 @@
 // generator, parameter blocks and launchers called by the C ABI in gs_layer.cu.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -182,6 +183,7 @@ struct Seq {
 };
 
 struct RecurrenceParams {
+  CUtensorMap maps[7];      // x, r, i, dy and y or dx, dr, di as tiles, where those are used
   Seq<const void*> x, r, i, dy;
   Seq<void*> y, dx, dr, di;
   const float* decay;
@@ -197,6 +199,7 @@ struct RecurrenceParams {
   float c;
   int32_t groups;           // channel groups of a row
 };
+enum { kMapX, kMapR, kMapI, kMapDy, kMapY, kMapDx = kMapY, kMapDr, kMapDi };
 
 struct RecurrenceStepParams {
   const void* x;
@@ -226,14 +229,13 @@ struct RecurrenceShape {
   int32_t groups;    // CTAs side by side over the channels
   unsigned grid;
 };
-RecurrenceShape recurrence_shape(int64_t B, int64_t T, int64_t D, int run, bool narrow);
+RecurrenceShape recurrence_shape(int64_t B, int64_t T, int64_t D, int run);
 int64_t recurrence_states(int64_t T);  // states kept of a row and channel
 int64_t recurrence_partials(int64_t B, int64_t T, int64_t D);
-// unit: the largest of 16, 4 and 2 bytes that every input row can be copied by; pair: two adjacent
-// channels of every output can be stored as one
-cudaError_t launch_recurrence_forward(const RecurrenceParams& p, int dtype, int unit, bool pair, cudaStream_t s);
-cudaError_t launch_recurrence_backward(const RecurrenceParams& p, float* ddecay, int dtype, int unit, bool pair,
-                                       cudaStream_t s);
+// How the tensors can be moved: by tiles (16, every row starts at a multiple of 16 bytes), by copies of
+// 4 bytes with two adjacent channels stored as one, or by single elements (the type's size).
+cudaError_t launch_recurrence_forward(RecurrenceParams& p, int dtype, int unit, cudaStream_t s);
+cudaError_t launch_recurrence_backward(RecurrenceParams& p, float* ddecay, int dtype, int unit, cudaStream_t s);
 cudaError_t launch_recurrence_step(const RecurrenceStepParams& p, int dtype, bool pair, cudaStream_t s);
 
 // launch() with dynamic shared memory and a cluster of `cluster` CTAs along x.

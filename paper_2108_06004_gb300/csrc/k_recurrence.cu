@@ -23,26 +23,28 @@ using namespace rec;
 
 constexpr int kLen = 16;                 // tokens of a run
 
-template <typename E, int CH>
+template <typename E, int CH, int STAGES>
 struct ForwardShared {
   static constexpr int kRuns = Tile<E, CH, kLen>::kRuns;
-  static constexpr int kStages = sizeof(E) == 2 ? 2 : 1;
-  Tile<E, CH, kLen> tile[kStages][3];    // x, r, i; those of steps to come are under way
+  Tile<E, CH, kLen> in[STAGES][3];       // x, r, i
   float4 run[kRuns][CH / 2];             // the map of each run
   uint32_t cut[kRuns];
+  uint64_t full[STAGES];                 // a stage's tiles have come
 };
 
-template <typename E, int CH, int UNIT, bool PAIR, bool RESET>
+// UNIT: how the inputs are moved (16: tiles; 4; 2).  STAGES: steps whose inputs fit in shared memory.
+template <typename E, int CH, int UNIT, int STAGES, bool RESET>
 __global__ void __launch_bounds__(kThreads, 4)
 k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
-  using Shared = ForwardShared<E, CH>;
-  constexpr int kRuns = Shared::kRuns, kStages = Shared::kStages, kChunk = kRuns * kLen;
+  constexpr bool TILES = UNIT == 16, PAIR = UNIT > (int)sizeof(E);  // results as pairs
+  using Shared = ForwardShared<E, CH, STAGES>;
+  using Raw = typename Pack2<E>::type;
+  constexpr int kRuns = Shared::kRuns, kChunk = kRuns * kLen;
   extern __shared__ __align__(128) unsigned char raw[];
   Shared& sh = *reinterpret_cast<Shared*>(raw);
   grid_begin();
   const Place w = place<CH>(p);
-  Total<CH>* totals = reinterpret_cast<Total<CH>*>(raw + sizeof(Shared));  // [2][cluster], with a cluster
-  if (w.cluster > 1) cg::this_cluster().sync();  // every CTA of the cluster runs before its memory is written
+  Table<CH>& table = *reinterpret_cast<Table<CH>*>(raw + sizeof(Shared));  // there with a cluster only
   const int64_t chunks = (w.len + kChunk - 1) / kChunk;
   const int steps = (int)((chunks + w.cluster - 1) / w.cluster);
   const int64_t kept = (p.T + kStateEvery - 1) / kStateEvery;
@@ -53,17 +55,34 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
   E* y = static_cast<E*>(p.y.data) + w.b * p.y.batch + w.d;
   auto chunk_token = [&](int s) { return ((int64_t)s * w.cluster + w.rank) * kChunk; };
   auto load = [&](int s) {
+    if (s >= steps) return;
     const int64_t t0 = chunk_token(s);
-    const int live = clamp_int(w.len - t0, kChunk);
-    load_tile<UNIT>(sh.tile[s % kStages][0], x, p.x.token, t0, live, channels);
-    load_tile<UNIT>(sh.tile[s % kStages][1], r, p.r.token, t0, live, channels);
-    load_tile<UNIT>(sh.tile[s % kStages][2], i, p.i.token, t0, live, channels);
-  };
-#pragma unroll
-  for (int s = 0; s < kStages; ++s) {
-    if (s < steps) load(s);
+    auto& in = sh.in[s % STAGES];
+    if constexpr (TILES) {
+      if (threadIdx.x == 0) {
+        uint64_t* bar = &sh.full[s % STAGES];
+        barrier_expect(bar, 3 * sizeof(in[0]));
+        for (int k = 0; k < 3; ++k) tile_load(&in[k], &p.maps[kMapX + k], (int)w.d0, (int)t0, (int)w.b, bar);
+      }
+    } else {
+      const int live = clamp_int(w.len - t0, kChunk);
+      copy_tile<UNIT>(in[0], x, p.x.token, t0, live, channels);
+      copy_tile<UNIT>(in[1], r, p.r.token, t0, live, channels);
+      copy_tile<UNIT>(in[2], i, p.i.token, t0, live, channels);
+    }
     copy_commit();
+  };
+  if (TILES && threadIdx.x == 0) {
+    for (int k = 0; k < STAGES; ++k) barrier_init(&sh.full[k]);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    tile_fence();
   }
+  for (int s = 0; s < STAGES; ++s) load(s);
+  if (w.cluster > 1)
+    open_table(table);
+  else
+    __syncthreads();
+  bool connected = true;  // no wait has run out
   const float2 rate = decay_rate(load_f32(p.decay + w.d, w.n), p.c);
   const bool series = __all_sync(0xFFFFFFFFu, rate.x <= kSeries && rate.y <= kSeries);
   float2 state = load_f32(p.h0 ? p.h0 + w.b * p.D + w.d : nullptr, w.n);
@@ -73,13 +92,21 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
     const bool full = chunk_token(s) + kChunk <= w.len;  // the chunk has no masked token
     const uint32_t resets = RESET ? reset_bits<CH, kLen>(flag) : 0;
     if (RESET) flag = reset_flag<kLen>(p, w, chunk_token(s + 1) + w.slot * kLen);
-    copy_wait<kStages - 1>();
+    if constexpr (TILES) {
+      connected = connected && barrier_wait(&sh.full[s % STAGES], s / STAGES);
+    } else {
+      if (s + 1 < steps)
+        copy_wait<STAGES - 1>();
+      else
+        copy_wait<0>();
+    }
+    // the tiles are here; the tables of the step before have been read
     __syncthreads();
+    auto& tile = sh.in[s % STAGES];
     // the run's tokens as a_t and b_t, and their composition
     float2 a[kLen], b[kLen];
     Run run = identity();
     auto gates = [&](auto some, auto in_series) {
-      const auto& tile = sh.tile[s % kStages];
 #pragma unroll
       for (int k = 0; k < kLen; ++k) {
         const bool cut = RESET && (resets >> k & 1u);
@@ -103,45 +130,51 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
     sh.run[w.slot][w.pair] = as_float4(run);
     if (RESET && w.pair == 0) sh.cut[w.slot] = resets;
     __syncthreads();
-    if (s + kStages < steps) load(s + kStages);  // this step's tile has been read
-    copy_commit();
-    // the maps of the runs before this one, and of the whole chunk
-    Run before, total = identity();
-    bool before_cut, cut = false;
-#pragma unroll
-    for (int k = 0; k < kRuns; ++k) {
-      if (k == w.slot) {
-        before = total;
-        before_cut = cut;
-      }
-      extend(total, cut, as_run(sh.run[k][w.pair]), RESET && sh.cut[k] != 0);
-    }
+    load(s + STAGES);  // this step's tiles have been read
+    // the state at the start of the run, and at the end of the step
     float2 h = state;
     if (w.cluster > 1) {
-      Total<CH>* table = totals + (s & 1) * w.cluster;
-      exchange<CH, kRuns>(table, w, total, cut);
-      for (int k = 0; k < w.cluster; ++k) {
-        if (k == w.rank) h = state;
-        state = apply(as_run(table[k].run[w.pair]), RESET && table[k].cut != 0, state);
+      Run before, total = identity();
+      bool before_cut, cut = false;
+#pragma unroll
+      for (int k = 0; k < kRuns; ++k) {
+        if (k == w.slot) {
+          before = total;
+          before_cut = cut;
+        }
+        extend(total, cut, as_run(sh.run[k][w.pair]), RESET && sh.cut[k] != 0);
       }
+      send<CH, kRuns>(table, s & 1, w, total, RESET && cut);
+      connected = connected && barrier_wait(&table.arrived[s & 1], s >> 1);
+      if (!connected) state = two(nanf(""));
+#pragma unroll 4
+      for (int k = 0; k < w.rank; ++k) state = apply_total<RESET>(table, s & 1, k, w, state);
+      h = apply(before, RESET && before_cut, state);
+#pragma unroll 4
+      for (int k = w.rank; k < w.cluster; ++k) state = apply_total<RESET>(table, s & 1, k, w, state);
     } else {
-      state = apply(total, cut, state);
+      if (!connected) state = two(nanf(""));
+#pragma unroll
+      for (int k = 0; k < kRuns; ++k) {
+        if (k == w.slot) h = state;
+        state = apply(as_run(sh.run[k][w.pair]), RESET && sh.cut[k] != 0, state);
+      }
     }
-    h = apply(before, before_cut, h);
     if (p.states && t0 % kStateEvery == 0 && t0 / kStateEvery < kept)
       store_f32(p.states + (w.b * kept + t0 / kStateEvery) * p.D + w.d, w.n, h);
+    auto next = [&](int k) { h = RESET ? apply(Run{a[k], b[k]}, resets >> k & 1u, h) : fma(a[k], h, b[k]); };
     E* out = y + t0 * p.y.token;
     if (full && PAIR && w.n == 2) {
 #pragma unroll
       for (int k = 0; k < kLen; ++k) {
-        h = RESET ? apply(Run{a[k], b[k]}, resets >> k & 1u, h) : fma(a[k], h, b[k]);
-        *reinterpret_cast<typename Pack2<E>::type*>(out) = Pack2<E>::down(h);
+        next(k);
+        *reinterpret_cast<Raw*>(out) = Pack2<E>::down(h);
         out += p.y.token;
       }
     } else {
 #pragma unroll
       for (int k = 0; k < kLen; ++k) {
-        h = RESET ? apply(Run{a[k], b[k]}, resets >> k & 1u, h) : fma(a[k], h, b[k]);
+        next(k);
         if (t0 + k < p.T) store2<E, PAIR>(out, w.n, t0 + k < w.len ? h : two(0.f));
         out += p.y.token;
       }
@@ -154,23 +187,29 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
       if (t < p.T) store2<E, PAIR>(y + t * p.y.token, w.n, two(0.f));
     }
   if (p.h_last && w.rank == 0 && w.slot == 0) store_f32(p.h_last + w.b * p.D + w.d, w.n, state);
+  if (w.cluster > 1) cg::this_cluster().sync();  // no CTA leaves while another may still write to it
 }
 
-template <typename E, int CH, int UNIT, bool PAIR, bool RESET>
-cudaError_t run_forward(RecurrenceParams p, const RecurrenceShape& shape, cudaStream_t s) {
+template <typename E, int CH, int UNIT, int STAGES, bool RESET>
+cudaError_t run_forward(RecurrenceParams& p, const RecurrenceShape& shape, cudaStream_t s) {
   static std::atomic<uint64_t> done{0};
-  const auto kernel = k_recurrence_forward<E, CH, UNIT, PAIR, RESET>;
-  constexpr size_t kBase = sizeof(ForwardShared<E, CH>), kTotal = 2 * sizeof(Total<CH>);
-  const cudaError_t e = prepare_kernel(kernel, kBase + kMaxCluster * kTotal, done);
+  const auto kernel = k_recurrence_forward<E, CH, UNIT, STAGES, RESET>;
+  constexpr size_t kBase = sizeof(ForwardShared<E, CH, STAGES>), kTable = sizeof(Table<CH>);
+  const cudaError_t e = prepare_kernel(kernel, kBase + kTable, done);
   if (e != cudaSuccess) return e;
   p.groups = shape.groups;
-  const size_t smem = kBase + (shape.cluster > 1 ? shape.cluster * kTotal : 0);
+  const size_t smem = kBase + (shape.cluster > 1 ? kTable : 0);
   return launch_cluster(kernel, dim3(shape.grid), dim3(kThreads), smem, shape.cluster, s, p);
 }
 
-template <typename E, int CH, int UNIT, bool PAIR>
-cudaError_t run_forward(const RecurrenceParams& p, const RecurrenceShape& shape, cudaStream_t s) {
-  return p.reset ? run_forward<E, CH, UNIT, PAIR, true>(p, shape, s) : run_forward<E, CH, UNIT, PAIR, false>(p, shape, s);
+// Two stages where four CTAs an SM still have room for them: a 2-byte type, and no table of the
+// cluster's maps.
+template <typename E, int CH, int UNIT>
+cudaError_t run_forward(RecurrenceParams& p, const RecurrenceShape& shape, cudaStream_t s) {
+  if constexpr (sizeof(E) == 2 && UNIT == 16)
+    if (shape.cluster == 1)
+      return p.reset ? run_forward<E, CH, UNIT, 2, true>(p, shape, s) : run_forward<E, CH, UNIT, 2, false>(p, shape, s);
+  return p.reset ? run_forward<E, CH, UNIT, 1, true>(p, shape, s) : run_forward<E, CH, UNIT, 1, false>(p, shape, s);
 }
 
 // Two adjacent channels of one token, zero where they do not exist.
@@ -210,37 +249,43 @@ __global__ void __launch_bounds__(128) k_recurrence_step(const __grid_constant__
 int64_t recurrence_states(int64_t T) { return (T + kStateEvery - 1) / kStateEvery; }
 
 // How a pass of `run` tokens a thread is cut: the channels of a CTA, and the CTAs of a cluster that
-// share a row's time.  SMs hold about four CTAs; the cluster is doubled until there are three for
-// each SM or no chunks left to deal.  Where 64 channels a CTA do not get there, 32 do better: twice
-// the CTAs, with twice the tokens each.
-RecurrenceShape recurrence_shape(int64_t B, int64_t T, int64_t D, int run, bool narrow) {
-  RecurrenceShape best = {};
-  for (int channels : {64, 32}) {
-    RecurrenceShape c;
-    c.channels = channels;
-    c.groups = (int32_t)((D + channels - 1) / channels);
-    const int64_t columns = B * c.groups, chunk = kThreads / (channels / 2) * run;
-    c.cluster = 1;
-    while (c.cluster < kMaxCluster && columns * c.cluster < 3 * kSMs && 2 * c.cluster * chunk <= T) c.cluster *= 2;
-    c.grid = (unsigned)(columns * c.cluster);
-    if (channels == 64) best = c;
-    else if (narrow && best.grid < 2 * kSMs && c.grid > best.grid) best = c;
-  }
-  return best;
+// share a row's time.  An SM holds four CTAs.  64 channels a CTA where that makes three for each
+// SM; fewer columns are cut to 32 channels (twice the CTAs, with twice the tokens each: forward and
+// backward of 8x2048x2048 bf16 take 56 and 96 us against 56 and 109 us with 64, but 64x512x1024,
+// which has enough columns, 56 and 104 against 53 and 91 us), and then share time in clusters until
+// there are three CTAs for each SM or no chunks left to deal.  A cluster meets at every step, so it comes last:
+// 8x2048x2048 with 64 channels and clusters of two takes 58 and 134 us.  The cut goes by sizes alone,
+// so that results do not depend on alignment.
+RecurrenceShape recurrence_shape(int64_t B, int64_t T, int64_t D, int run) {
+  constexpr int64_t kEnough = 3 * kSMs;
+  RecurrenceShape c = {};
+  c.channels = B * ((D + 63) / 64) < kEnough ? 32 : 64;
+  c.groups = (int32_t)((D + c.channels - 1) / c.channels);
+  const int64_t columns = B * c.groups, chunk = kThreads / (c.channels / 2) * run;
+  c.cluster = 1;
+  while (c.cluster < kMaxCluster && columns * c.cluster < kEnough && 2 * c.cluster * chunk <= T) c.cluster *= 2;
+  c.grid = (unsigned)(columns * c.cluster);
+  return c;
 }
 
-cudaError_t launch_recurrence_forward(const RecurrenceParams& p, int dtype, int unit, bool pair, cudaStream_t s) {
-  const RecurrenceShape shape = recurrence_shape(p.B, p.T, p.D, kLen, unit == 16 && pair);
+cudaError_t launch_recurrence_forward(RecurrenceParams& p, int dtype, int unit, cudaStream_t s) {
+  const RecurrenceShape shape = recurrence_shape(p.B, p.T, p.D, kLen);
+  if (unit == 16) {
+    const int tokens = kThreads / (shape.channels / 2) * kLen;
+    if (!describe(p.maps[kMapX], p.x, p, dtype, shape.channels, tokens) ||
+        !describe(p.maps[kMapR], p.r, p, dtype, shape.channels, tokens) ||
+        !describe(p.maps[kMapI], p.i, p, dtype, shape.channels, tokens))
+      unit = 4;
+  }
   return with_type(dtype, [&](auto e) {
     using E = decltype(e);
-    if (unit == 16 && pair)
-      return shape.channels == 64 ? run_forward<E, 64, 16, true>(p, shape, s) : run_forward<E, 32, 16, true>(p, shape, s);
-    if constexpr (sizeof(E) == 2) {
-      if (unit >= 4 && pair) return run_forward<E, 64, 4, true>(p, shape, s);
-      return run_forward<E, 64, 2, false>(p, shape, s);
-    } else {
-      return run_forward<E, 64, 4, false>(p, shape, s);
-    }
+    return with_cut(shape, unit, [&](auto channels, auto copies) {
+      constexpr int CH = decltype(channels)::value, UNIT = decltype(copies)::value;
+      if constexpr (UNIT == 2 && sizeof(E) == 4)
+        return cudaErrorInvalidValue;
+      else
+        return run_forward<E, CH, UNIT>(p, shape, s);
+    });
   });
 }
 

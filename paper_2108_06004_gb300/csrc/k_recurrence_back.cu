@@ -20,28 +20,30 @@ using namespace rec;
 
 constexpr int kLen = 8;                  // tokens of a run
 
-template <typename E, int CH>
+template <typename E, int CH, bool OUT>
 struct BackwardShared {
   static constexpr int kRuns = Tile<E, CH, kLen>::kRuns;
-  Tile<E, CH, kLen> tile[2][4];          // x, r, i, dy; the next step's are under way
+  Tile<E, CH, kLen> in[2][4];            // x, r, i, dy; the next step's are under way
+  Tile<E, CH, OUT ? kLen : 0> out[3];    // dx, dr, di
   float4 run[kRuns][CH / 2];             // the map of h over each run
   float2 back[kRuns][CH / 2];            // the offset of the flow's map (its factor is the same)
   uint32_t cut[kRuns];
+  uint64_t full[2];                      // a stage's tiles have come
 };
 
-template <typename E, int CH, int UNIT, bool PAIR, bool RESET>
+// UNIT: how the inputs are moved (16: tiles; 4; 2).  OUT: results leave as tiles too.
+template <typename E, int CH, int UNIT, bool OUT, bool RESET>
 __global__ void __launch_bounds__(kThreads, 4)
 k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
-  using Shared = BackwardShared<E, CH>;
-  using Raw = typename Pack2<E>::type;
+  constexpr bool TILES = UNIT == 16, PAIR = UNIT > (int)sizeof(E);  // results as pairs
+  using Shared = BackwardShared<E, CH, OUT>;
   constexpr int kRuns = Shared::kRuns, kChunk = kRuns * kLen;
   static_assert(kChunk % kStateEvery == 0, "a step starts at a kept state");
   extern __shared__ __align__(128) unsigned char raw[];
   Shared& sh = *reinterpret_cast<Shared*>(raw);
   grid_begin();
   const Place w = place<CH>(p);
-  Total<CH>* totals = reinterpret_cast<Total<CH>*>(raw + sizeof(Shared));  // [2][cluster], with a cluster
-  if (w.cluster > 1) cg::this_cluster().sync();  // every CTA of the cluster runs before its memory is written
+  Table<CH>& table = *reinterpret_cast<Table<CH>*>(raw + sizeof(Shared));  // there with a cluster only
   const int steps = (int)(((w.len + kChunk - 1) / kChunk + w.cluster - 1) / w.cluster);
   const int64_t kept = (p.T + kStateEvery - 1) / kStateEvery;
   const int channels = clamp_int(p.D - w.d0, CH);
@@ -53,16 +55,36 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
   E* dr = static_cast<E*>(p.dr.data) + w.b * p.dr.batch + w.d;
   E* di = static_cast<E*>(p.di.data) + w.b * p.di.batch + w.d;
   auto chunk_token = [&](int s) { return ((int64_t)s * w.cluster + w.rank) * kChunk; };
-  auto load = [&](int s) {
-    const int64_t t0 = chunk_token(s);
-    const int live = clamp_int(w.len - t0, kChunk);
-    load_tile<UNIT>(sh.tile[s & 1][0], x, p.x.token, t0, live, channels);
-    load_tile<UNIT>(sh.tile[s & 1][1], r, p.r.token, t0, live, channels);
-    load_tile<UNIT>(sh.tile[s & 1][2], i, p.i.token, t0, live, channels);
-    load_tile<UNIT>(sh.tile[s & 1][3], dy, p.dy.token, t0, live, channels);
+  // step s is the turn-th from the end
+  auto load = [&](int turn) {
+    const int64_t t0 = chunk_token(steps - 1 - turn);
+    auto& in = sh.in[turn & 1];
+    if constexpr (TILES) {
+      if (threadIdx.x == 0) {
+        uint64_t* bar = &sh.full[turn & 1];
+        barrier_expect(bar, 4 * sizeof(in[0]));
+        for (int k = 0; k < 4; ++k) tile_load(&in[k], &p.maps[kMapX + k], (int)w.d0, (int)t0, (int)w.b, bar);
+      }
+    } else {
+      const int live = clamp_int(w.len - t0, kChunk);
+      copy_tile<UNIT>(in[0], x, p.x.token, t0, live, channels);
+      copy_tile<UNIT>(in[1], r, p.r.token, t0, live, channels);
+      copy_tile<UNIT>(in[2], i, p.i.token, t0, live, channels);
+      copy_tile<UNIT>(in[3], dy, p.dy.token, t0, live, channels);
+      copy_commit();
+    }
   };
-  if (steps > 0) load(steps - 1);
-  copy_commit();
+  if (TILES && threadIdx.x == 0) {
+    for (int k = 0; k < 2; ++k) barrier_init(&sh.full[k]);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    tile_fence();
+  }
+  if (steps > 0) load(0);
+  if (w.cluster > 1)
+    open_table(table);
+  else
+    __syncthreads();
+  bool connected = true;  // no wait has run out
   const float2 rate = decay_rate(load_f32(p.decay + w.d, w.n), p.c);
   const bool series = __all_sync(0xFFFFFFFFu, rate.x <= kSeries && rate.y <= kSeries);
   float2 flow = load_f32(p.dh_last ? p.dh_last + w.b * p.D + w.d : nullptr, w.n);
@@ -75,11 +97,15 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
     if (RESET && s > 0) flag = reset_flag<kLen>(p, w, chunk_token(s - 1) + w.slot * kLen);
     const int64_t kept_at = chunk_token(s) / kStateEvery;
     float2 h = kept_at < kept ? load_f32(p.states + (w.b * kept + kept_at) * p.D + w.d, w.n) : two(0.f);
-    copy_wait<0>();
-    __syncthreads();  // the tile is here, and the one before has been read
-    if (s > 0) load(s - 1);
-    copy_commit();
-    const auto& tile = sh.tile[s & 1];
+    const int turn = steps - 1 - s;
+    if constexpr (TILES) {
+      connected = connected && barrier_wait(&sh.full[turn & 1], turn >> 1);
+    } else {
+      copy_wait<0>();
+    }
+    __syncthreads();  // the tiles are here, and those of the step before have been read
+    if (s > 0) load(turn + 1);
+    auto& tile = sh.in[turn & 1];
     float2 a[kLen], sr[kLen], K[kLen], U[kLen], Q[kLen];
     Run run = identity();
     auto gates = [&](auto some, auto in_series) {
@@ -108,44 +134,62 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
     else
       gates(std::false_type(), std::false_type());
     float2 back = two(0.f);
+    auto flows = [&](auto some) {
 #pragma unroll
-    for (int k = kLen - 1; k >= 0; --k) {
-      const float2 f = mul(a[k], add(back, widen(tile[3].at(w, k))));  // past the end dy is zero in the tile
-      back = RESET ? choose(resets >> k & 1u, two(0.f), f) : f;
-    }
+      for (int k = kLen - 1; k >= 0; --k) {
+        float2 d = widen(tile[3].at(w, k));
+        if (decltype(some)::value && t0 + k >= w.len) d = two(0.f);
+        const float2 f = mul(a[k], add(back, d));
+        back = RESET ? choose(resets >> k & 1u, two(0.f), f) : f;
+      }
+    };
+    if (full)
+      flows(std::false_type());
+    else
+      flows(std::true_type());
     sh.run[w.slot][w.pair] = as_float4(run);
     sh.back[w.slot][w.pair] = back;
     if (RESET && w.pair == 0) sh.cut[w.slot] = resets;
+    if (OUT && threadIdx.x == 0) store_wait();  // the step before's results have left
     __syncthreads();
     // the maps of the flow over the runs after this one, and over the whole chunk; the state
     // before this run
-    Run after, total = identity();
-    bool after_cut, cut = false;
-#pragma unroll
-    for (int k = kRuns - 1; k >= 0; --k) {
-      if (k == w.slot) {
-        after = total;
-        after_cut = cut;
-      }
-      Run m = as_run(sh.run[k][w.pair]);
-      m.b = sh.back[k][w.pair];
-      extend(total, cut, m, RESET && sh.cut[k] != 0);
-    }
 #pragma unroll
     for (int k = 0; k < kRuns - 1; ++k)
       if (k < w.slot) h = apply(as_run(sh.run[k][w.pair]), RESET && sh.cut[k] != 0, h);
     float2 f = flow;
+    auto back_run = [&](int k) {
+      Run m = as_run(sh.run[k][w.pair]);
+      m.b = sh.back[k][w.pair];
+      return m;
+    };
     if (w.cluster > 1) {
-      Total<CH>* table = totals + (s & 1) * w.cluster;
-      exchange<CH, kRuns>(table, w, total, cut);
-      for (int k = w.cluster - 1; k >= 0; --k) {
-        if (k == w.rank) f = flow;
-        flow = apply(as_run(table[k].run[w.pair]), RESET && table[k].cut != 0, flow);
+      Run after, total = identity();
+      bool after_cut, cut = false;
+#pragma unroll
+      for (int k = kRuns - 1; k >= 0; --k) {
+        if (k == w.slot) {
+          after = total;
+          after_cut = cut;
+        }
+        extend(total, cut, back_run(k), RESET && sh.cut[k] != 0);
       }
+      send<CH, kRuns>(table, turn & 1, w, total, RESET && cut);
+      connected = connected && barrier_wait(&table.arrived[turn & 1], turn >> 1);
+      if (!connected) flow = two(nanf(""));
+#pragma unroll 4
+      for (int k = w.cluster - 1; k > w.rank; --k) flow = apply_total<RESET>(table, turn & 1, k, w, flow);
+      f = apply(after, RESET && after_cut, flow);
+#pragma unroll 4
+      for (int k = w.rank; k >= 0; --k) flow = apply_total<RESET>(table, turn & 1, k, w, flow);
     } else {
-      flow = apply(total, cut, flow);
+      if (!connected) flow = two(nanf(""));
+#pragma unroll
+      for (int k = kRuns - 1; k >= 0; --k) {
+        if (k == w.slot) f = flow;
+        flow = apply(back_run(k), RESET && sh.cut[k] != 0, flow);
+      }
     }
-    f = apply(after, after_cut, f);
 #pragma unroll
     for (int k = 0; k < kLen; ++k) {
       Q[k] = fma(h, sr[k], make_float2(-Q[k].x, -Q[k].y));
@@ -153,8 +197,6 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
       h = RESET ? apply(Run{a[k], b}, resets >> k & 1u, h) : fma(a[k], h, b);
     }
     float2 part = two(0.f);
-    E *out_x = dx + (t0 + kLen - 1) * p.dx.token, *out_r = dr + (t0 + kLen - 1) * p.dr.token,
-      *out_i = di + (t0 + kLen - 1) * p.di.token;
     auto token = [&](int k, float2& ox, float2& orr, float2& oi) {
       const bool cut = RESET && (resets >> k & 1u);
       const float2 g = add(f, widen(tile[3].at(w, k)));
@@ -165,32 +207,49 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
       oi = mul(g, U[k]);
       orr = mul(mul(rate, fma(sr[k], two(1.f), two(-1.f))), m);
     };
-    if (full && PAIR && w.n == 2) {
+    if constexpr (OUT) {
+      auto results = [&](auto some) {
 #pragma unroll
-      for (int k = kLen - 1; k >= 0; --k) {
-        float2 ox, orr, oi;
-        token(k, ox, orr, oi);
-        *reinterpret_cast<Raw*>(out_x) = Pack2<E>::down(ox);
-        *reinterpret_cast<Raw*>(out_r) = Pack2<E>::down(orr);
-        *reinterpret_cast<Raw*>(out_i) = Pack2<E>::down(oi);
-        out_x -= p.dx.token;
-        out_r -= p.dr.token;
-        out_i -= p.di.token;
+        for (int k = kLen - 1; k >= 0; --k) {
+          float2 ox = two(0.f), orr = two(0.f), oi = two(0.f);
+          if (!decltype(some)::value || t0 + k < w.len) token(k, ox, orr, oi);
+          sh.out[0].at(w, k) = Pack2<E>::down(ox);
+          sh.out[1].at(w, k) = Pack2<E>::down(orr);
+          sh.out[2].at(w, k) = Pack2<E>::down(oi);
+        }
+      };
+      if (full)
+        results(std::false_type());
+      else
+        results(std::true_type());
+      tile_fence();
+      __syncthreads();
+      if (threadIdx.x == 0 && chunk_token(s) < p.T) {
+        for (int k = 0; k < 3; ++k) tile_store(&sh.out[k], &p.maps[kMapDx + k], (int)w.d0, (int)chunk_token(s), (int)w.b);
+        store_commit();
       }
     } else {
+      E *out_x = dx + (t0 + kLen - 1) * p.dx.token, *out_r = dr + (t0 + kLen - 1) * p.dr.token,
+        *out_i = di + (t0 + kLen - 1) * p.di.token;
+      auto results = [&](auto some) {
 #pragma unroll
-      for (int k = kLen - 1; k >= 0; --k) {
-        float2 ox = two(0.f), orr = two(0.f), oi = two(0.f);
-        if (t0 + k < w.len) token(k, ox, orr, oi);
-        if (t0 + k < p.T) {
-          store2<E, PAIR>(out_x, w.n, ox);
-          store2<E, PAIR>(out_r, w.n, orr);
-          store2<E, PAIR>(out_i, w.n, oi);
+        for (int k = kLen - 1; k >= 0; --k) {
+          float2 ox = two(0.f), orr = two(0.f), oi = two(0.f);
+          if (!decltype(some)::value || t0 + k < w.len) token(k, ox, orr, oi);
+          if (!decltype(some)::value || t0 + k < p.T) {
+            store2<E, PAIR>(out_x, w.n, ox);
+            store2<E, PAIR>(out_r, w.n, orr);
+            store2<E, PAIR>(out_i, w.n, oi);
+          }
+          out_x -= p.dx.token;
+          out_r -= p.dr.token;
+          out_i -= p.di.token;
         }
-        out_x -= p.dx.token;
-        out_r -= p.dr.token;
-        out_i -= p.di.token;
-      }
+      };
+      if (full)
+        results(std::false_type());
+      else
+        results(std::true_type());
     }
     sum = add(sum, part);
   }
@@ -204,6 +263,8 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
         store2<E, PAIR>(di + t * p.di.token, w.n, two(0.f));
       }
     }
+  if (w.cluster > 1) cg::this_cluster().sync();  // no CTA leaves while another may still write to it
+  if (OUT && threadIdx.x == 0) store_wait();     // nor while its tiles are being read
   if (p.dh0 && w.rank == 0 && w.slot == 0) store_f32(p.dh0 + w.b * p.D + w.d, w.n, flow);
   // the CTA's share of the decay's gradient, its runs in order
   __syncthreads();
@@ -235,44 +296,52 @@ k_recurrence_decay(const float* partial, int64_t n, int64_t D, const float* deca
   }
 }
 
-template <typename E, int CH, int UNIT, bool PAIR, bool RESET>
-cudaError_t run_backward(RecurrenceParams p, const RecurrenceShape& shape, cudaStream_t s) {
+template <typename E, int CH, int UNIT, bool OUT, bool RESET>
+cudaError_t run_backward(RecurrenceParams& p, const RecurrenceShape& shape, cudaStream_t s) {
   static std::atomic<uint64_t> done{0};
-  const auto kernel = k_recurrence_backward<E, CH, UNIT, PAIR, RESET>;
-  constexpr size_t kBase = sizeof(BackwardShared<E, CH>), kTotal = 2 * sizeof(Total<CH>);
-  const cudaError_t e = prepare_kernel(kernel, kBase + kMaxCluster * kTotal, done);
+  const auto kernel = k_recurrence_backward<E, CH, UNIT, OUT, RESET>;
+  constexpr size_t kBase = sizeof(BackwardShared<E, CH, OUT>), kTable = sizeof(Table<CH>);
+  const cudaError_t e = prepare_kernel(kernel, kBase + kTable, done);
   if (e != cudaSuccess) return e;
   p.groups = shape.groups;
-  const size_t smem = kBase + (shape.cluster > 1 ? shape.cluster * kTotal : 0);
+  const size_t smem = kBase + (shape.cluster > 1 ? kTable : 0);
   return launch_cluster(kernel, dim3(shape.grid), dim3(kThreads), smem, shape.cluster, s, p);
 }
 
-template <typename E, int CH, int UNIT, bool PAIR>
-cudaError_t run_backward(const RecurrenceParams& p, const RecurrenceShape& shape, cudaStream_t s) {
-  return p.reset ? run_backward<E, CH, UNIT, PAIR, true>(p, shape, s) : run_backward<E, CH, UNIT, PAIR, false>(p, shape, s);
+// Results leave as tiles where shared memory has room for them beside two stages of inputs at four
+// CTAs an SM: with a 2-byte type.
+template <typename E, int CH, int UNIT>
+cudaError_t run_backward(RecurrenceParams& p, const RecurrenceShape& shape, cudaStream_t s) {
+  constexpr bool OUT = UNIT == 16 && sizeof(E) == 2;
+  return p.reset ? run_backward<E, CH, UNIT, OUT, true>(p, shape, s) : run_backward<E, CH, UNIT, OUT, false>(p, shape, s);
 }
 
 }  // namespace
 
-// Rows of the workspace: one for each row of the batch and CTA of a cluster, at the most.
-int64_t recurrence_partials(int64_t B, int64_t T, int64_t D) {
-  const int wide = recurrence_shape(B, T, D, kLen, false).cluster, narrow = recurrence_shape(B, T, D, kLen, true).cluster;
-  return B * (wide > narrow ? wide : narrow);
-}
+// Rows of the workspace: one for each row of the batch and CTA of a cluster.
+int64_t recurrence_partials(int64_t B, int64_t T, int64_t D) { return B * recurrence_shape(B, T, D, kLen).cluster; }
 
-cudaError_t launch_recurrence_backward(const RecurrenceParams& p, float* ddecay, int dtype, int unit, bool pair,
-                                       cudaStream_t s) {
-  const RecurrenceShape shape = recurrence_shape(p.B, p.T, p.D, kLen, unit == 16 && pair);
+cudaError_t launch_recurrence_backward(RecurrenceParams& p, float* ddecay, int dtype, int unit, cudaStream_t s) {
+  const RecurrenceShape shape = recurrence_shape(p.B, p.T, p.D, kLen);
+  if (unit == 16 && shape.grid > 0) {
+    const int tokens = kThreads / (shape.channels / 2) * kLen;
+    const Seq<const void*>* in[4] = {&p.x, &p.r, &p.i, &p.dy};
+    const Seq<void*>* out[3] = {&p.dx, &p.dr, &p.di};
+    bool all = true;
+    for (int k = 0; k < 4; ++k) all = all && describe(p.maps[kMapX + k], *in[k], p, dtype, shape.channels, tokens);
+    if (dtype != GS_F32)  // whose results are stored from registers
+      for (int k = 0; k < 3; ++k) all = all && describe(p.maps[kMapDx + k], *out[k], p, dtype, shape.channels, tokens);
+    if (!all) unit = 4;
+  }
   cudaError_t err = shape.grid == 0 ? cudaSuccess : with_type(dtype, [&](auto e) {
     using E = decltype(e);
-    if (unit == 16 && pair)
-      return shape.channels == 64 ? run_backward<E, 64, 16, true>(p, shape, s) : run_backward<E, 32, 16, true>(p, shape, s);
-    if constexpr (sizeof(E) == 2) {
-      if (unit >= 4 && pair) return run_backward<E, 64, 4, true>(p, shape, s);
-      return run_backward<E, 64, 2, false>(p, shape, s);
-    } else {
-      return run_backward<E, 64, 4, false>(p, shape, s);
-    }
+    return with_cut(shape, unit, [&](auto channels, auto copies) {
+      constexpr int CH = decltype(channels)::value, UNIT = decltype(copies)::value;
+      if constexpr (UNIT == 2 && sizeof(E) == 4)
+        return cudaErrorInvalidValue;
+      else
+        return run_backward<E, CH, UNIT>(p, shape, s);
+    });
   });
   if (err != cudaSuccess) return err;
   return launch(k_recurrence_decay, dim3((unsigned)((p.D + 31) / 32)), dim3(256), s, (const float*)p.partial,

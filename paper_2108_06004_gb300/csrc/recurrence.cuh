@@ -4,6 +4,8 @@
 
 #include <cooperative_groups.h>
 
+#include <cudaTypedefs.h>
+
 #include <atomic>
 
 #include "gs_layer.cuh"
@@ -62,6 +64,9 @@ __device__ __forceinline__ float2 capped(__nv_bfloat162 v) {
 __device__ __forceinline__ float2 two(float v) { return make_float2(v, v); }
 __device__ __forceinline__ float2 mul(float2 a, float2 b) { return __fmul2_rn(a, b); }
 __device__ __forceinline__ float2 add(float2 a, float2 b) { return __fadd2_rn(a, b); }
+__device__ __forceinline__ float2 fmac(float2 a, float2 b, float c) { return __ffma2_rn(a, b, two(c)); }
+__device__ __forceinline__ float2 mulc(float2 a, float c) { return __fmul2_rn(a, two(c)); }
+__device__ __forceinline__ float2 addc(float2 a, float c) { return __fadd2_rn(a, two(c)); }
 __device__ __forceinline__ float2 fma(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
 __device__ __forceinline__ float2 choose(bool c, float2 a, float2 b) { return make_float2(c ? a.x : b.x, c ? a.y : b.y); }
 
@@ -90,13 +95,12 @@ __device__ __forceinline__ float2 decay_rate(float2 lam, float c) {
 // SERIES: rate is at most kSeries in both channels, so q always is in the polynomial's range.
 template <bool SERIES>
 __device__ __forceinline__ void decay_of(float2 sr, float2 rate, float2& a, float2& X) {
-  const float2 one = two(1.f);
   const float2 q = mul(make_float2(-rate.x, -rate.y), sr);
-  float2 s = fma(q, two(0.006782862555491099f), two(0.041013210491015605f));
-  s = fma(q, s, two(0.16655192765429086f));
-  s = fma(q, s, two(0.4999928833780279f));
-  s = fma(q, s, two(0.999999928937559f));
-  a = fma(q, s, one);
+  float2 s = addc(mulc(q, 0.006782862555491099f), 0.041013210491015605f);
+  s = fmac(q, s, 0.16655192765429086f);
+  s = fmac(q, s, 0.4999928833780279f);
+  s = fmac(q, s, 0.999999928937559f);
+  a = fmac(q, s, 1.f);
   if (!SERIES) {
     if (q.x < -kSeries) {
       a.x = ex2(kLog2e * q.x);
@@ -107,11 +111,11 @@ __device__ __forceinline__ void decay_of(float2 sr, float2 rate, float2& a, floa
       s.y = (1.f - a.y) * rcp(-q.y);
     }
   }
-  X = mul(mul(rate, s), add(a, one));
+  X = mul(mul(rate, s), addc(a, 1.f));
 }
 
 __device__ __forceinline__ float2 half_exp(float2 v) {
-  const float2 h = mul(v, two(0.5f * kLog2e));
+  const float2 h = mulc(v, 0.5f * kLog2e);
   return make_float2(ex2(h.x), ex2(h.y));
 }
 __device__ __forceinline__ float2 rcp(float2 v) { return make_float2(rcp(v.x), rcp(v.y)); }
@@ -122,10 +126,9 @@ __device__ __forceinline__ float2 rsq(float2 v) { return make_float2(rsq(v.x), r
 // below 2^120 (X is large only where sigmoid(r) is small, and 1 + p^2 then is about 1).  `cut`: a reset, a = 0 and K = sigmoid(i).
 template <bool SERIES>
 __device__ __forceinline__ void gate_forward(float2 r, float2 i, float2 rate, bool cut, float2& a, float2& K) {
-  const float2 one = two(1.f);
   const float2 pr = half_exp(r), pi = half_exp(i);
   const float2 sqr = mul(pr, pr), sqi = mul(pi, pi);
-  const float2 ur = add(sqr, one), ui = add(sqi, one);
+  const float2 ur = addc(sqr, 1.f), ui = addc(sqi, 1.f);
   float2 X;
   decay_of<SERIES>(mul(sqr, rcp(ur)), rate, a, X);
   K = mul(mul(mul(pr, sqi), X), rsq(mul(mul(ur, ui), mul(ui, X))));
@@ -243,30 +246,68 @@ __device__ __forceinline__ uint32_t reset_bits(uint8_t flag) {
 }
 
 // ---- tile loads -----------------------------------------------------------------------------
-// A tile holds CH channels of kThreads / (CH / 2) runs of LEN tokens in shared memory: tokens
-// t0 ... t0 + live - 1 of the CTA's channels, of which `channels` exist; what does not exist is
-// zero.  Where a warp reads two runs at once, every other run is moved by half the banks.  UNIT is
-// the size of one copy: 16 or 4 bytes asynchronously, or single 2-byte elements through
-// registers, where rows of a 2-byte type start at odd elements.
+// A tile holds CH channels of kThreads / (CH / 2) runs of LEN tokens in shared memory.  The tiles of
+// tensors whose rows start at multiples of 16 bytes (UNIT 16) are moved by the tensor memory
+// accelerator, one instruction a tile and no address arithmetic in the threads (with 16-byte copies
+// by each thread instead, the forward pass issues an eighth more instructions, and it is bound by
+// those); tokens and channels past a tensor's end read as zero and are not written.  Others are
+// copied 4 bytes at a time asynchronously, or by single 2-byte elements through registers where
+// rows of a 2-byte type start at odd elements, and their results stored from registers.
 template <typename E, int CH, int LEN>
 struct Tile {
   static constexpr int kRuns = kThreads / (CH / 2);
   static constexpr int kTokens = kRuns * LEN;
-  static constexpr int kPad = CH == 32 && sizeof(E) == 2 ? CH : 0;
-  static constexpr int kRun = LEN * CH + kPad;  // elements from one run to the next
-  E v[kRuns * kRun];
-  __device__ __forceinline__ const typename Pack2<E>::type& at(const Place& w, int k) const {
-    return reinterpret_cast<const typename Pack2<E>::type*>(v + w.slot * kRun + k * CH)[w.pair];
+  using Raw = typename Pack2<E>::type;
+  E v[LEN ? kTokens * CH : 8];
+  __device__ __forceinline__ Raw& at(const Place& w, int k) {
+    return reinterpret_cast<Raw*>(v + (w.slot * LEN + k) * CH)[w.pair];
   }
 };
 
-template <int UNIT>
+__device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void barrier_init(uint64_t* bar) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(bar)) : "memory");
+}
+__device__ __forceinline__ void barrier_expect(uint64_t* bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(shared_address(bar)), "r"(bytes) : "memory");
+}
+// Whether the barrier's `phase`-th phase has come to its end.  Every wait is bounded: one that runs
+// out, which nothing that these kernels do can cause, makes the caller give up all further waits
+// and turn its state into NaN.
+__device__ __forceinline__ bool barrier_wait(uint64_t* bar, int phase) {
+  for (int tries = 0; tries < (1 << 20); ++tries) {
+    uint32_t done;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(done)
+        : "r"(shared_address(bar)), "r"(phase & 1)
+        : "memory");
+    if (done) return true;
+  }
+  return false;
+}
+
+__device__ __forceinline__ void tile_load(void* to, const CUtensorMap* map, int d, int t, int b, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+          shared_address(to)),
+      "l"(map), "r"(d), "r"(t), "r"(b), "r"(shared_address(bar))
+      : "memory");
+}
+__device__ __forceinline__ void tile_store(const void* from, const CUtensorMap* map, int d, int t, int b) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(d), "r"(t),
+               "r"(b), "r"(shared_address(from))
+               : "memory");
+}
+__device__ __forceinline__ void store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+// All stores of this thread have read their tiles.
+__device__ __forceinline__ void store_wait() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+// What this thread has written to shared memory is seen by tile stores that are issued after.
+__device__ __forceinline__ void tile_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
 __device__ __forceinline__ void copy_async(void* to, const void* from, int bytes) {
-  const uint32_t dst = (uint32_t)__cvta_generic_to_shared(to);
-  if (UNIT == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(from), "r"(bytes) : "memory");
-  else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(from), "r"(bytes) : "memory");
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(shared_address(to)), "l"(from), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT>
@@ -274,8 +315,9 @@ __device__ __forceinline__ void copy_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
 }
 
+// Tokens t0 ... t0 + live - 1 of the CTA's channels, of which `channels` exist; zeros for the rest.
 template <int UNIT, typename E, int CH, int LEN>
-__device__ __forceinline__ void load_tile(Tile<E, CH, LEN>& tile, const E* from, int64_t token_stride, int64_t t0,
+__device__ __forceinline__ void copy_tile(Tile<E, CH, LEN>& tile, const E* from, int64_t token_stride, int64_t t0,
                                           int live, int channels) {
   using Shape = Tile<E, CH, LEN>;
   constexpr int PER = UNIT / (int)sizeof(E);      // elements of a copy
@@ -285,7 +327,7 @@ __device__ __forceinline__ void load_tile(Tile<E, CH, LEN>& tile, const E* from,
   const int u = threadIdx.x % U, row = threadIdx.x / U;
   const E* src = from + (t0 + row) * token_stride + u * PER;
   const int have = clamp_int(channels - u * PER, PER);
-  auto to = [&](int j) { return tile.v + (row + j * R) / LEN * Shape::kRun + (row + j * R) % LEN * CH + u * PER; };
+  auto to = [&](int j) { return tile.v + (row + j * R) * CH + u * PER; };
   if constexpr (UNIT == 2) {
     constexpr int BATCH = N < 8 ? N : 8;
 #pragma unroll
@@ -301,33 +343,105 @@ __device__ __forceinline__ void load_tile(Tile<E, CH, LEN>& tile, const E* from,
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       const bool some = have > 0 && row + j * R < live;
-      copy_async<UNIT>(to(j), some ? src : from, some ? have * (int)sizeof(E) : 0);
+      copy_async(to(j), some ? src : from, some ? have * (int)sizeof(E) : 0);
       src += R * token_stride;
     }
   }
 }
 
 // ---- exchange over the cluster ----------------------------------------------------------------
-// The chunks' maps.  `mine` of this CTA goes into every CTA's table at this rank; the threads of
-// run k write to the CTAs k, k + RUNS, ...  The two halves of the table alternate, so one barrier
-// a step is enough: a CTA writes step s + 2 only after all have passed the barrier of s + 1, and
-// so have read step s.  The table lies at the end of the CTA's shared memory, with as many rows as
-// the cluster has CTAs.
+// The chunks' maps.  Each CTA sends its own into every CTA's table, at its rank; the threads of run
+// k send to the CTAs k, k + RUNS, ...  A message is an asynchronous store that reports its bytes to
+// the receiver's mbarrier, so neither side has to wait for the stores of results that are still
+// under way, as the release of a cluster barrier does (64x512x1024, which needs no exchange,
+// against 1x65536x1024, bf16 forward, per element: 1.5 and 2.0 ps, with the cluster barrier 3.3).  The table and its
+// mbarrier alternate between two halves: a CTA sends step s + 2 only when it has all of step s + 1,
+// which every CTA sends only after it has read step s.  A map that holds a reset is sent with the
+// factor -1, which no product of decays is.
 template <int CH>
-struct Total {
-  float4 run[CH / 2];
-  uint32_t cut, unused[3];
+struct Table {
+  float4 run[2][kMaxCluster][CH / 2];
+  uint64_t arrived[2];
 };
 
-template <int CH, int RUNS>
-__device__ __forceinline__ void exchange(Total<CH>* table, const Place& w, const Run& mine, bool cut) {
-  cg::cluster_group cl = cg::this_cluster();
-  for (int k = w.slot; k < w.cluster; k += RUNS) {
-    Total<CH>* to = cl.map_shared_rank(table, k) + w.rank;
-    to->run[w.pair] = as_float4(mine);
-    if (w.pair == 0) to->cut = cut;
+__device__ __forceinline__ uint32_t in_cta(uint32_t address, int rank) {
+  uint32_t there;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(address), "r"(rank));
+  return there;
+}
+
+// Called by all threads of the cluster before anything else touches the table.
+template <int CH>
+__device__ __forceinline__ void open_table(Table<CH>& t) {
+  if (threadIdx.x == 0) {
+    barrier_init(&t.arrived[0]);
+    barrier_init(&t.arrived[1]);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  cl.sync();
+  cg::this_cluster().sync();
+}
+
+template <int CH, int RUNS>
+__device__ __forceinline__ void send(Table<CH>& t, int half, const Place& w, Run mine, bool cut) {
+  if (threadIdx.x == 0) barrier_expect(&t.arrived[half], (uint32_t)w.cluster * sizeof(t.run[0][0]));
+  if (cut) mine.a = two(-1.f);
+  const uint32_t slot = shared_address(&t.run[half][w.rank][w.pair]), bar = shared_address(&t.arrived[half]);
+  for (int k = w.slot; k < w.cluster; k += RUNS)
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(in_cta(slot, k)),
+                 "f"(mine.a.x), "f"(mine.a.y), "f"(mine.b.x), "f"(mine.b.y), "r"(in_cta(bar, k))
+                 : "memory");
+}
+
+// The table's map of the chunk of CTA k, applied to h.
+template <bool RESET, int CH>
+__device__ __forceinline__ float2 apply_total(const Table<CH>& t, int half, int k, const Place& w, float2 h) {
+  const Run m = as_run(t.run[half][k][w.pair]);
+  return apply(m, RESET && m.a.x < 0.f, h);
+}
+
+// ---- host side --------------------------------------------------------------------------------
+// The encoder of tile descriptors is a function of the driver.
+inline PFN_cuTensorMapEncodeTiled_v12000 tile_encoder() {
+  static const PFN_cuTensorMapEncodeTiled_v12000 found = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult how;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &how) != cudaSuccess ||
+        how != cudaDriverEntryPointSuccess)
+      f = nullptr;
+    return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
+  }();
+  return found;
+}
+
+// Describes a tensor as tiles of `channels` x `tokens`; false where that is not possible.
+template <typename P>
+inline bool describe(CUtensorMap& map, const Seq<P>& t, const RecurrenceParams& p, int dtype, int channels, int tokens) {
+  const uint64_t item = dtype == GS_F32 ? 4 : 2;
+  const cuuint64_t row = (cuuint64_t)((p.D * item + 15) / 16 * 16);
+  const cuuint64_t size[3] = {(cuuint64_t)p.D, (cuuint64_t)p.T, (cuuint64_t)p.B};
+  // a dimension of one entry may come with any stride
+  const cuuint64_t stride[2] = {p.T > 1 ? t.token * item : row, p.B > 1 ? t.batch * item : row};
+  const cuuint32_t box[3] = {(cuuint32_t)channels, (cuuint32_t)tokens, 1}, step[3] = {1, 1, 1};
+  const CUtensorMapDataType type = dtype == GS_F32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : dtype == GS_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                                     : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  const auto encode = tile_encoder();
+  return encode && stride[0] && stride[1] &&
+         encode(&map, type, 3, const_cast<void*>(static_cast<const void*>(t.data)), size, stride, box, step,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Calls f with the channels of a CTA and the size of a copy as constants.
+template <typename F>
+inline cudaError_t with_cut(const RecurrenceShape& shape, int unit, F&& f) {
+  using std::integral_constant;
+  auto with_unit = [&](auto channels) {
+    return unit == 16  ? f(channels, integral_constant<int, 16>())
+           : unit == 4 ? f(channels, integral_constant<int, 4>())
+                       : f(channels, integral_constant<int, 2>());
+  };
+  return shape.channels == 64 ? with_unit(integral_constant<int, 64>()) : with_unit(integral_constant<int, 32>());
 }
 
 // Shared memory beyond the default and clusters beyond the portable size are asked for once per
