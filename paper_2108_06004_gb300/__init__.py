@@ -157,8 +157,26 @@ def _ptr_array(xs):
 def _stream(stream):
     if stream is not None:
         return _ptr(getattr(stream, "cuda_stream", stream))
-    import torch
-    return torch.cuda.current_stream().cuda_stream
+    return _current_stream(_torch().cuda.current_device())
+
+
+_torch_module = None
+
+
+def _torch():
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
+
+
+def _current_stream(device: int) -> int:
+    """Handle of PyTorch's current stream.  The stream object that the public call makes costs
+    more than a kernel launch, so the handle is taken from where that call takes it."""
+    torch = _torch()
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device) if raw is not None else torch.cuda.current_stream(device).cuda_stream
 
 
 # ---- C ABI, same names ------------------------------------------------------------------
@@ -441,7 +459,7 @@ def gs_plan_destroy(plan: int) -> None:
 # Tensors are torch tensors on the GPU; shapes, strides and types are read from them, and what
 # the C ABI cannot see of them is checked here.
 
-_DTYPES = {}
+_CODES = {}
 
 
 def _refuse(func: str, msg: str):
@@ -449,42 +467,43 @@ def _refuse(func: str, msg: str):
 
 
 def _dtype(func: str, t) -> int:
-    if not _DTYPES:
-        import torch
-        _DTYPES.update({torch.float32: GS_F32, torch.float16: GS_F16, torch.bfloat16: GS_BF16})
-    code = _DTYPES.get(t.dtype)
+    if not _CODES:
+        torch = _torch()
+        _CODES.update({torch.float32: GS_F32, torch.float16: GS_F16, torch.bfloat16: GS_BF16})
+    code = _CODES.get(t.dtype)
     if code is None:
         _refuse(func, f"dtype {t.dtype} is none of float32, float16, bfloat16")
     return code
 
 
-def _same(func: str, name: str, t, shape, dtype, device) -> None:
+def _expect(func: str, name: str, t, shape, dtype, device) -> None:
+    if t.shape == shape and t.dtype == dtype and t.device == device:
+        return
     if t.shape != shape:
         _refuse(func, f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if t.dtype != dtype:
         _refuse(func, f"{name} has type {t.dtype}, expected {dtype}")
-    if t.device != device:
-        _refuse(func, f"{name} is on {t.device}, expected {device}")
+    _refuse(func, f"{name} is on {t.device}, expected {device}")
 
 
-def _on_gpu(func: str, name: str, t) -> None:
+def _launch_stream(func: str, t, stream):
+    """The stream to launch on; the tensors have to be on the current device."""
     if not t.is_cuda:
-        _refuse(func, f"{name} is on {t.device}, expected a CUDA device")
+        _refuse(func, f"the tensors are on {t.device}, expected a CUDA device")
+    device = _torch().cuda.current_device()
+    if t.get_device() != device:
+        _refuse(func, f"the tensors are on {t.device}, the current device is {device}")
+    return _current_stream(device) if stream is None else _stream(stream)
 
 
 def _dense(func: str, name: str, t, shape, dtype, device):
     """Address of a contiguous tensor, or None for an absent one."""
     if t is None:
         return None
-    _same(func, name, t, shape, dtype, device)
+    _expect(func, name, t, shape, dtype, device)
     if not t.is_contiguous():
         _refuse(func, f"{name} must be contiguous")
     return t.data_ptr()
-
-
-def _f32_dtype():
-    import torch
-    return torch.float32
 
 
 def _matrix(func: str, name: str, t, shape, dtype, device):
@@ -492,7 +511,7 @@ def _matrix(func: str, name: str, t, shape, dtype, device):
     walked with one stride; (None, 0) for an absent one."""
     if t is None:
         return None, 0
-    _same(func, name, t, shape, dtype, device)
+    _expect(func, name, t, shape, dtype, device)
     if t.is_contiguous():
         return t.data_ptr(), shape[-1]
     stride = t.stride()
@@ -514,8 +533,9 @@ def _matrix(func: str, name: str, t, shape, dtype, device):
 def _rows_cols(func: str, t):
     if t.dim() < 1:
         _refuse(func, "a tensor of at least one dimension is expected")
-    _on_gpu(func, "the first tensor", t)
     cols = t.shape[-1]
+    if cols:
+        return t.numel() // cols, cols
     rows = 1
     for n in t.shape[:-1]:
         rows *= n
@@ -526,21 +546,25 @@ def gs_dropout(x, out, p: float, seed: int, offset: int, residual=None, stream=N
     """out = dropout(x) (+ residual); any shape, the mask indexed by the element's flat position."""
     f = "gs_dropout"
     code = _dtype(f, x)
+    stream = _launch_stream(f, x, stream)
     rows, cols = _rows_cols(f, x)
-    xp, xs = _matrix(f, "x", x, x.shape, x.dtype, x.device)
-    rp, rs = _matrix(f, "residual", residual, x.shape, x.dtype, x.device)
-    op, os_ = _matrix(f, "out", out, x.shape, x.dtype, x.device)
-    _check(load_library().gs_dropout(xp, xs, rp, rs, op, os_, rows, cols, code, p, seed, offset, _stream(stream)), f)
+    shape, dtype, dev = x.shape, x.dtype, x.device
+    xp, xs = _matrix(f, "x", x, shape, dtype, dev)
+    rp, rs = _matrix(f, "residual", residual, shape, dtype, dev)
+    op, os_ = _matrix(f, "out", out, shape, dtype, dev)
+    _check(load_library().gs_dropout(xp, xs, rp, rs, op, os_, rows, cols, code, p, seed, offset, stream), f)
 
 
 def gs_dropout_backward(dout, dx, p: float, seed: int, offset: int, stream=None) -> None:
+    """dx = the gradient of gs_dropout's x from that of its out."""
     f = "gs_dropout_backward"
     code = _dtype(f, dout)
+    stream = _launch_stream(f, dout, stream)
     rows, cols = _rows_cols(f, dout)
-    gp, gstride = _matrix(f, "dout", dout, dout.shape, dout.dtype, dout.device)
-    op, os_ = _matrix(f, "dx", dx, dout.shape, dout.dtype, dout.device)
-    _check(load_library().gs_dropout_backward(gp, gstride, op, os_, rows, cols, code, p, seed, offset,
-                                              _stream(stream)), f)
+    shape, dtype, dev = dout.shape, dout.dtype, dout.device
+    gp, gstride = _matrix(f, "dout", dout, shape, dtype, dev)
+    op, os_ = _matrix(f, "dx", dx, shape, dtype, dev)
+    _check(load_library().gs_dropout_backward(gp, gstride, op, os_, rows, cols, code, p, seed, offset, stream), f)
 
 
 def gs_dropout_add_norm(x, residual, weight, y, z, rstd, p: float, seed: int, offset: int, eps: float = 1e-6,
@@ -548,15 +572,16 @@ def gs_dropout_add_norm(x, residual, weight, y, z, rstd, p: float, seed: int, of
     """y = residual + dropout(x), z = RMS norm of y times weight, over the last dimension."""
     f = "gs_dropout_add_norm"
     code = _dtype(f, x)
+    stream = _launch_stream(f, x, stream)
     rows, cols = _rows_cols(f, x)
-    shape, dtype, dev, f32 = x.shape, x.dtype, x.device, _f32_dtype()
+    shape, dtype, dev, f32 = x.shape, x.dtype, x.device, _torch().float32
     xp, xs = _matrix(f, "x", x, shape, dtype, dev)
     rp, rs = _matrix(f, "residual", residual, shape, dtype, dev)
     yp, ys = _matrix(f, "y", y, shape, dtype, dev)
     zp, zs = _matrix(f, "z", z, shape, dtype, dev)
     _check(load_library().gs_dropout_add_norm(
         xp, xs, rp, rs, _dense(f, "weight", weight, (cols,), f32, dev), yp, ys, zp, zs,
-        _dense(f, "rstd", rstd, shape[:-1], f32, dev), rows, cols, code, p, seed, offset, eps, _stream(stream)), f)
+        _dense(f, "rstd", rstd, shape[:-1], f32, dev), rows, cols, code, p, seed, offset, eps, stream), f)
 
 
 def gs_dropout_add_norm_workspace_size(rows: int, cols: int) -> int:
@@ -571,8 +596,9 @@ def gs_dropout_add_norm_backward(dz, dy, y, weight, rstd, dx, dresidual, dweight
     """Gradients of gs_dropout_add_norm; dy, dx and dresidual may be None."""
     f = "gs_dropout_add_norm_backward"
     code = _dtype(f, dz)
+    stream = _launch_stream(f, dz, stream)
     rows, cols = _rows_cols(f, dz)
-    shape, dtype, dev, f32 = dz.shape, dz.dtype, dz.device, _f32_dtype()
+    shape, dtype, dev, f32 = dz.shape, dz.dtype, dz.device, _torch().float32
     gp, gstride = _matrix(f, "dz", dz, shape, dtype, dev)
     dp, ds = _matrix(f, "dy", dy, shape, dtype, dev)
     yp, ys = _matrix(f, "y", y, shape, dtype, dev)
@@ -581,30 +607,31 @@ def gs_dropout_add_norm_backward(dz, dy, y, weight, rstd, dx, dresidual, dweight
     _check(load_library().gs_dropout_add_norm_backward(
         gp, gstride, dp, ds, yp, ys, _dense(f, "weight", weight, (cols,), f32, dev),
         _dense(f, "rstd", rstd, shape[:-1], f32, dev), xp, xs, rp, rs, _dense(f, "dweight", dweight, (cols,), f32, dev),
-        rows, cols, code, p, seed, offset, _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream)), f)
+        rows, cols, code, p, seed, offset, _ptr(workspace), _nbytes(workspace, workspace_bytes), stream), f)
 
 
 def _seq(func: str, name: str, t, shape, dtype, device):
-    _same(func, name, t, shape, dtype, device)
+    _expect(func, name, t, shape, dtype, device)
     b, s, d = t.stride()
     if d != 1 and shape[2] > 1:
         _refuse(func, f"{name}: the channels must be adjacent")
-    return ctypes.byref(GsSeq(t.data_ptr(), b, s))
+    return GsSeq(t.data_ptr(), b, s)
 
 
-def _flags(func: str, name: str, t, shape, width: str, device):
+def _resets(func: str, t, shape, device):
     if t is None:
         return None
-    import torch
-    if width == "reset" and t.dtype == torch.bool:
-        t = t.view(torch.uint8)
-    return _dense(func, name, t, shape, torch.uint8 if width == "reset" else torch.int32, device)
+    torch = _torch()
+    return _dense(func, "reset", t.view(torch.uint8) if t.dtype == torch.bool else t, shape, torch.uint8, device)
+
+
+def _whole(func: str, name: str, t, shape, device):
+    return None if t is None else _dense(func, name, t, shape, _torch().int32, device)
 
 
 def _sequence(func: str, t):
     if t.dim() != 3:
         _refuse(func, f"tensors of [B][T][D] are expected, got {t.dim()} dimensions")
-    _on_gpu(func, "x", t)
     return t.shape
 
 
@@ -632,15 +659,16 @@ def gs_recurrence_forward(x, r, i, decay, y, h0=None, reset=None, lengths=None, 
     f = "gs_recurrence_forward"
     code = _dtype(f, x)
     shape = B, T, D = _sequence(f, x)
-    dtype, dev, f32 = x.dtype, x.device, _f32_dtype()
+    stream = _launch_stream(f, x, stream)
+    dtype, dev, f32 = x.dtype, x.device, _torch().float32
     if states is not None:
         _states_fit(f, states, B, T, D)
     _check(load_library().gs_recurrence_forward(
         _seq(f, "x", x, shape, dtype, dev), _seq(f, "r", r, shape, dtype, dev), _seq(f, "i", i, shape, dtype, dev),
         _dense(f, "decay", decay, (D,), f32, dev), _dense(f, "h0", h0, (B, D), f32, dev),
-        _flags(f, "reset", reset, (B, T), "reset", dev), _flags(f, "lengths", lengths, (B,), "lengths", dev),
+        _resets(f, reset, (B, T), dev), _whole(f, "lengths", lengths, (B,), dev),
         _seq(f, "y", y, shape, dtype, dev), _dense(f, "h_last", h_last, (B, D), f32, dev), _ptr(states), B, T, D, code,
-        c, _stream(stream)), f)
+        c, stream), f)
 
 
 def gs_recurrence_backward(dy, x, r, i, decay, states, dx, dr, di, ddecay, workspace, dh_last=None, reset=None,
@@ -649,35 +677,37 @@ def gs_recurrence_backward(dy, x, r, i, decay, states, dx, dr, di, ddecay, works
     f = "gs_recurrence_backward"
     code = _dtype(f, x)
     shape = B, T, D = _sequence(f, x)
-    dtype, dev, f32 = x.dtype, x.device, _f32_dtype()
+    stream = _launch_stream(f, x, stream)
+    dtype, dev, f32 = x.dtype, x.device, _torch().float32
     _states_fit(f, states, B, T, D)
     _check(load_library().gs_recurrence_backward(
         _seq(f, "dy", dy, shape, dtype, dev), _dense(f, "dh_last", dh_last, (B, D), f32, dev),
         _seq(f, "x", x, shape, dtype, dev), _seq(f, "r", r, shape, dtype, dev), _seq(f, "i", i, shape, dtype, dev),
-        _dense(f, "decay", decay, (D,), f32, dev), _flags(f, "reset", reset, (B, T), "reset", dev),
-        _flags(f, "lengths", lengths, (B,), "lengths", dev), _ptr(states), _seq(f, "dx", dx, shape, dtype, dev),
+        _dense(f, "decay", decay, (D,), f32, dev), _resets(f, reset, (B, T), dev),
+        _whole(f, "lengths", lengths, (B,), dev), _ptr(states), _seq(f, "dx", dx, shape, dtype, dev),
         _seq(f, "dr", dr, shape, dtype, dev), _seq(f, "di", di, shape, dtype, dev),
         _dense(f, "ddecay", ddecay, (D,), f32, dev), _dense(f, "dh0", dh0, (B, D), f32, dev), B, T, D, code, c,
-        _ptr(workspace), _nbytes(workspace, workspace_bytes), _stream(stream)), f)
+        _ptr(workspace), _nbytes(workspace, workspace_bytes), stream), f)
 
 
 def gs_recurrence_step(x, r, i, decay, state, y, slots=None, c: float = 8.0, stream=None) -> None:
     """One token of each of B streams: state rows (fp32, one per slot) in place, y = the new state."""
     f = "gs_recurrence_step"
     code = _dtype(f, x)
+    stream = _launch_stream(f, x, stream)
     B, D = _rows_cols(f, x)
-    dtype, dev, f32 = x.dtype, x.device, _f32_dtype()
-    xp, xs = _matrix(f, "x", x, x.shape, dtype, dev)
-    rp, rs = _matrix(f, "r", r, x.shape, dtype, dev)
-    ip, istride = _matrix(f, "i", i, x.shape, dtype, dev)
-    yp, ys = _matrix(f, "y", y, x.shape, dtype, dev)
+    shape, dtype, dev, f32 = x.shape, x.dtype, x.device, _torch().float32
+    xp, xs = _matrix(f, "x", x, shape, dtype, dev)
+    rp, rs = _matrix(f, "r", r, shape, dtype, dev)
+    ip, istride = _matrix(f, "i", i, shape, dtype, dev)
+    yp, ys = _matrix(f, "y", y, shape, dtype, dev)
     if state.dim() != 2:
         _refuse(f, "state must have two dimensions")
     n = state.shape[0]
     sp, ss = _matrix(f, "state", state, (n, D), f32, dev)
     _check(load_library().gs_recurrence_step(
         xp, xs, rp, rs, ip, istride, _dense(f, "decay", decay, (D,), f32, dev), sp, ss, n,
-        _flags(f, "slots", slots, (B,), "slots", dev), yp, ys, B, D, code, c, _stream(stream)), f)
+        _whole(f, "slots", slots, (B,), dev), yp, ys, B, D, code, c, stream), f)
 
 
 def gs_insert_request_ceiling_window_size(sketch: int) -> int:

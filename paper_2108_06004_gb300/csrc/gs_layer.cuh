@@ -30,7 +30,11 @@ template <> struct Pack2<__half> {
 };
 template <> struct Pack2<__nv_bfloat16> {
   using type = __nv_bfloat162;
-  static __device__ __forceinline__ float2 up(__nv_bfloat162 v) { return __bfloat1622float2(v); }
+  // bf16 is the upper half of an fp32 value
+  static __device__ __forceinline__ float2 up(__nv_bfloat162 v) {
+    const uint32_t u = *reinterpret_cast<const uint32_t*>(&v);
+    return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u));
+  }
   static __device__ __forceinline__ __nv_bfloat162 down(float2 v) { return __floats2bfloat162_rn(v.x, v.y); }
 };
 
@@ -42,26 +46,42 @@ template <> __device__ __forceinline__ float from_f32<float>(float v) { return v
 template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// Eight adjacent elements.  VEC: the address is a multiple of 16 bytes and all eight exist;
-// otherwise the first n of them one by one, zeros for the rest.
+// Eight adjacent elements as they are in memory, so that loads can be issued well before their
+// values are needed.  VEC: the address is a multiple of 16 bytes and all eight exist; otherwise the
+// first n of them one by one, zeros for the rest.
+template <typename E>
+struct Raw8 {
+  uint4 q[sizeof(E) / 2];
+};
+
+template <typename E, bool VEC>
+__device__ __forceinline__ Raw8<E> fetch8(const E* p, int n) {
+  Raw8<E> r;
+  if (VEC) {
+#pragma unroll
+    for (int k = 0; k < (int)(sizeof(E) / 2); ++k) r.q[k] = reinterpret_cast<const uint4*>(p)[k];
+  } else {
+    E* e = reinterpret_cast<E*>(&r);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = j < n ? p[j] : from_f32<E>(0.f);
+  }
+  return r;
+}
+
+template <typename E>
+__device__ __forceinline__ void unpack8(const Raw8<E>& r, float (&v)[8]) {
+  const typename Pack2<E>::type* h = reinterpret_cast<const typename Pack2<E>::type*>(&r);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 f = Pack2<E>::up(h[j]);
+    v[2 * j] = f.x;
+    v[2 * j + 1] = f.y;
+  }
+}
+
 template <typename E, bool VEC>
 __device__ __forceinline__ void load8(const E* p, int n, float (&v)[8]) {
-  if (VEC) {
-    constexpr int Q = sizeof(E) * 8 / 16;
-    uint4 raw[Q];
-#pragma unroll
-    for (int q = 0; q < Q; ++q) raw[q] = reinterpret_cast<const uint4*>(p)[q];
-    const typename Pack2<E>::type* h = reinterpret_cast<const typename Pack2<E>::type*>(raw);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float2 f = Pack2<E>::up(h[j]);
-      v[2 * j] = f.x;
-      v[2 * j + 1] = f.y;
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = j < n ? to_f32(p[j]) : 0.f;
-  }
+  unpack8(fetch8<E, VEC>(p, n), v);
 }
 
 template <typename E, bool VEC>
@@ -106,34 +126,46 @@ __device__ __forceinline__ uint4 philox(uint64_t block, const DropParams& d) {
   return make_uint4(x0, x1, x2, x3);
 }
 
-// Bit j set: element 8 * block + j is kept.  Element 2w + h takes half h of word w.
+// Bit j set: element 8 * block + j is kept.  Element 2w + h takes half h of word w.  A half is
+// compared in the upper 16 bits of a word, where what lies below it does not matter.
 __device__ __forceinline__ uint32_t keep8_block(uint64_t block, const DropParams& d) {
   const uint4 w = philox(block, d);
-  const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+  const uint32_t word[4] = {w.x, w.y, w.z, w.w}, least = d.threshold << 16;
   uint32_t bits = 0;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    bits |= ((word[q] & 0xFFFFu) >= d.threshold ? 1u : 0u) << (2 * q);
-    bits |= ((word[q] >> 16) >= d.threshold ? 1u : 0u) << (2 * q + 1);
+    bits |= (word[q] << 16 >= least ? 1u : 0u) << (2 * q);
+    bits |= (word[q] >= least ? 1u : 0u) << (2 * q + 1);
   }
   return bits;
 }
 
-// The same for the eight elements from `first`, wherever it lies in its block.
+// Dropout of the eight elements from `first` on, which lie in one block (ALIGNED) or in two.  A
+// dropped element is zero whatever its value was (infinities and NaN included).
 template <bool ALIGNED>
-__device__ __forceinline__ uint32_t keep8(uint64_t first, const DropParams& d) {
-  if (d.threshold == 0) return 0xFFu;
-  uint32_t bits = keep8_block(first >> 3, d);
-  if (!ALIGNED) {
-    const uint32_t skip = (uint32_t)first & 7u;
-    if (skip) bits = (bits | (keep8_block((first >> 3) + 1, d) << 8)) >> skip;
+__device__ __forceinline__ void drop8(float (&v)[8], uint64_t first, const DropParams& d) {
+  if (d.threshold == 0) return;
+  if (d.threshold > 0xFFFF) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+    return;
   }
-  return bits;
-}
-
-// A dropped element is zero whatever its value was (infinities and NaN included).
-__device__ __forceinline__ float drop(float v, uint32_t bits, int j, float scale) {
-  return (bits >> j) & 1u ? v * scale : 0.f;
+  if (ALIGNED) {
+    const uint4 w = philox(first >> 3, d);
+    const uint32_t word[4] = {w.x, w.y, w.z, w.w}, least = d.threshold << 16;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float2 s = __fmul2_rn(make_float2(v[2 * q], v[2 * q + 1]), make_float2(d.scale, d.scale));
+      v[2 * q] = word[q] << 16 >= least ? s.x : 0.f;
+      v[2 * q + 1] = word[q] >= least ? s.y : 0.f;
+    }
+  } else {
+    const uint32_t skip = (uint32_t)first & 7u;
+    uint32_t bits = keep8_block(first >> 3, d);
+    if (skip) bits = (bits | (keep8_block((first >> 3) + 1, d) << 8)) >> skip;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (bits >> j) & 1u ? v[j] * d.scale : 0.f;
+  }
 }
 
 // ---- parameter blocks -----------------------------------------------------------------------

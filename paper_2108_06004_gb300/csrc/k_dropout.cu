@@ -11,39 +11,53 @@ namespace gs {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kAhead = 2;  // groups of eight whose loads a thread has under way
 
 // FLAT: one row of 8 * groups elements or fewer (the tensors are contiguous).  Otherwise rows
 // with strides, `groups` of them a row.  VEC: groups are whole and 16-byte aligned, but for a
 // last one of a FLAT row.
-template <typename E, bool FLAT, bool VEC>
+template <typename E, bool FLAT, bool VEC, bool RESIDUAL>
 __global__ void __launch_bounds__(kThreads) k_dropout(const __grid_constant__ DropoutParams p, int64_t groups) {
   grid_begin();
-  const E* x = static_cast<const E*>(p.x);
-  const E* res = static_cast<const E*>(p.residual);
-  E* out = static_cast<E*>(p.out);
-  const int64_t total = groups * p.rows;
-  for (int64_t g = (int64_t)blockIdx.x * kThreads + threadIdx.x; g < total; g += (int64_t)gridDim.x * kThreads) {
-    const int64_t row = FLAT ? 0 : (total <= 0xFFFFFFFFll ? (int64_t)((uint32_t)g / (uint32_t)groups) : g / groups);
-    const int64_t col = (g - row * groups) * 8;
-    const int n = (int)(p.cols - col < 8 ? p.cols - col : 8);
-    const uint32_t bits = keep8<(FLAT || VEC)>((uint64_t)(row * p.cols + col), p.drop);
-    const E* px = x + row * p.x_stride + col;
-    const E* pr = res + row * p.residual_stride + col;
-    E* po = out + row * p.out_stride + col;
-    float v[8], w[8];
-    if (VEC && n == 8) {
-      load8<E, true>(px, 8, v);
-      if (res) load8<E, true>(pr, 8, w);
-    } else {
-      load8<E, false>(px, n, v);
-      if (res) load8<E, false>(pr, n, w);
+  const int64_t total = groups * p.rows, step = (int64_t)gridDim.x * kThreads;
+  for (int64_t g0 = (int64_t)blockIdx.x * kThreads + threadIdx.x; g0 < total; g0 += kAhead * step) {
+    Raw8<E> x[kAhead], res[kAhead];
+    int64_t row[kAhead], col[kAhead];
+    int n[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int64_t g = g0 + u * step;
+      row[u] = FLAT ? 0 : total <= 0xFFFFFFFFll ? (int64_t)((uint32_t)g / (uint32_t)groups) : g / groups;
+      col[u] = (g - row[u] * groups) * 8;
+      n[u] = g < total ? (int)(p.cols - col[u] < 8 ? p.cols - col[u] : 8) : 0;
+      const E* px = static_cast<const E*>(p.x) + row[u] * p.x_stride + col[u];
+      const E* pr = static_cast<const E*>(p.residual) + row[u] * p.residual_stride + col[u];
+      if (VEC && n[u] == 8) {
+        x[u] = fetch8<E, true>(px, 8);
+        if (RESIDUAL) res[u] = fetch8<E, true>(pr, 8);
+      } else {
+        x[u] = fetch8<E, false>(px, n[u]);
+        if (RESIDUAL) res[u] = fetch8<E, false>(pr, n[u]);
+      }
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = drop(v[j], bits, j, p.drop.scale) + (res ? w[j] : 0.f);
-    if (VEC && n == 8)
-      store8<E, true>(po, 8, v);
-    else
-      store8<E, false>(po, n, v);
+    for (int u = 0; u < kAhead; ++u) {
+      if (n[u] == 0) continue;
+      float v[8];
+      unpack8(x[u], v);
+      drop8<(FLAT || VEC)>(v, (uint64_t)(row[u] * p.cols + col[u]), p.drop);
+      if (RESIDUAL) {
+        float w[8];
+        unpack8(res[u], w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += w[j];
+      }
+      E* po = static_cast<E*>(p.out) + row[u] * p.out_stride + col[u];
+      if (VEC && n[u] == 8)
+        store8<E, true>(po, 8, v);
+      else
+        store8<E, false>(po, n[u], v);
+    }
   }
 }
 
@@ -51,8 +65,10 @@ template <typename E, bool FLAT, bool VEC>
 cudaError_t run(const DropoutParams& p, cudaStream_t s) {
   const int64_t groups = (p.cols + 7) / 8;
   const int64_t ctas = (groups * p.rows + kThreads - 1) / kThreads;
-  const int64_t most = (int64_t)device_info().sms * 64;
-  return launch(k_dropout<E, FLAT, VEC>, dim3((unsigned)(ctas < most ? ctas : most)), dim3(kThreads), s, p, groups);
+  const int64_t most = (int64_t)kSMs * 64;
+  const dim3 grid((unsigned)(ctas < most ? ctas : most));
+  return p.residual ? launch(k_dropout<E, FLAT, VEC, true>, grid, dim3(kThreads), s, p, groups)
+                    : launch(k_dropout<E, FLAT, VEC, false>, grid, dim3(kThreads), s, p, groups);
 }
 
 }  // namespace

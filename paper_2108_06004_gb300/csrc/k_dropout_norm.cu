@@ -13,14 +13,14 @@
 namespace gs {
 namespace {
 
-// Sum over the TPR threads of a row; every thread of the CTA takes part.
+// Sum over the TPR threads of a row; every thread of the CTA takes part.  Two sums in turn use two
+// scratch arrays, so one barrier each is enough.
 template <int TPR>
 __device__ __forceinline__ float row_sum(float v, float* scratch) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
   if (TPR > 32) {
     const int warp = threadIdx.x >> 5;
-    __syncthreads();  // the scratch of the sum before has been read
     if ((threadIdx.x & 31) == 0) scratch[warp] = v;
     __syncthreads();
     constexpr int W = TPR / 32;
@@ -53,10 +53,10 @@ k_norm_forward(const __grid_constant__ NormForwardParams p) {
     float res[8];
     load8<E, VEC>(static_cast<const E*>(p.x) + row * p.x_stride + col, n, t[v]);
     load8<E, VEC>(static_cast<const E*>(p.residual) + row * p.residual_stride + col, n, res);
-    const uint32_t bits = keep8<VEC>((uint64_t)row * (uint64_t)p.cols + col, p.drop);
+    drop8<VEC>(t[v], (uint64_t)row * (uint64_t)p.cols + col, p.drop);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      t[v][j] = res[j] + drop(t[v][j], bits, j, p.drop.scale);
+      t[v][j] += res[j];
       if (VEC || j < n) sum += t[v][j] * t[v][j];
     }
     store8<E, VEC>(static_cast<E*>(p.y) + row * p.y_stride + col, n, t[v]);
@@ -79,62 +79,102 @@ k_norm_forward(const __grid_constant__ NormForwardParams p) {
 }
 
 template <typename E, int TPR, int V, bool VEC>
-__global__ void __launch_bounds__(kCtaThreads<TPR>)
+__global__ void __launch_bounds__(kCtaThreads<TPR>, kCtaThreads<TPR> == 256 ? 2 : 1)
 k_norm_backward(const __grid_constant__ NormBackwardParams p) {
   grid_begin();
-  __shared__ float scratch[32];
+  __shared__ float scratch[2][32];
   constexpr int RPC = kCtaThreads<TPR> / TPR;
   extern __shared__ float fold[];  // RPC > 1: [RPC][cols]
   const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  const int64_t step = (int64_t)gridDim.x * RPC;
   float dw[V][8];
 #pragma unroll
   for (int v = 0; v < V; ++v)
 #pragma unroll
     for (int j = 0; j < 8; ++j) dw[v][j] = 0.f;
-  for (int64_t first = (int64_t)blockIdx.x * RPC; first < p.rows; first += (int64_t)gridDim.x * RPC) {
-    const int64_t row = first + sub;
+  // A row's inputs stay as they are in memory and are unpacked once for the sums and again for the
+  // results: half the registers that fp32 values take.  The next row's are loaded meanwhile, but in the
+  // widest rows, whose 1024 threads have registers for one row only.
+  constexpr bool AHEAD = TPR < 1024;
+  Raw8<E> dz[V], y[V], dy[V];
+  float rstd = 0.f;
+  auto fetch = [&](int64_t row, Raw8<E>(&dz)[V], Raw8<E>(&y)[V], Raw8<E>(&dy)[V], float& rstd) {
+    if (row >= p.rows) return;
+    rstd = p.rstd[row];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int col = (v * TPR + lane) * 8;
+      if (col >= p.cols) continue;
+      const int m = p.cols - col;
+      dz[v] = fetch8<E, VEC>(static_cast<const E*>(p.dz) + row * p.dz_stride + col, m);
+      y[v] = fetch8<E, VEC>(static_cast<const E*>(p.y) + row * p.y_stride + col, m);
+      if (p.dy) dy[v] = fetch8<E, VEC>(static_cast<const E*>(p.dy) + row * p.dy_stride + col, m);
+    }
+  };
+  const int64_t first = (int64_t)blockIdx.x * RPC;
+  if (AHEAD) fetch(first + sub, dz, y, dy, rstd);
+  int turn = 0;
+  for (int64_t row0 = first; row0 < p.rows; row0 += step, turn ^= 1) {
+    const int64_t row = row0 + sub;
     const bool live = row < p.rows;
-    const float rstd = live ? p.rstd[row] : 0.f;
-    float u[V][8], n[V][8];
+    Raw8<E> next_dz[V], next_y[V], next_dy[V];
+    float next_rstd = 0.f;
+    if (AHEAD)
+      fetch(row + step, next_dz, next_y, next_dy, next_rstd);
+    else
+      fetch(row, dz, y, dy, rstd);
     float sum = 0.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int col = (v * TPR + lane) * 8;
       if (!live || col >= p.cols) continue;
       const int m = p.cols - col;
-      float w[8];
-      load8<E, VEC>(static_cast<const E*>(p.dz) + row * p.dz_stride + col, m, u[v]);
-      load8<E, VEC>(static_cast<const E*>(p.y) + row * p.y_stride + col, m, n[v]);
+      float u[8], n[8], w[8];
+      unpack8(dz[v], u);
+      unpack8(y[v], n);
       load8<float, VEC>(p.weight + col, m, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        n[v][j] *= rstd;
-        if (VEC || j < m) dw[v][j] += u[v][j] * n[v][j];
-        u[v][j] *= w[j];
-        if (VEC || j < m) sum += u[v][j] * n[v][j];
+        const float t = u[j] * (n[j] * rstd);
+        if (VEC || j < m) {
+          dw[v][j] += t;
+          sum += t * w[j];
+        }
       }
     }
-    sum = row_sum<TPR>(sum, scratch) / (float)p.cols;
-    if (!live) continue;
+    sum = row_sum<TPR>(sum, scratch[turn]) / (float)p.cols;
+    if (live) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int col = (v * TPR + lane) * 8;
-      if (col >= p.cols) continue;
-      const int m = p.cols - col;
-      float d[8];
-      if (p.dy)
-        load8<E, VEC>(static_cast<const E*>(p.dy) + row * p.dy_stride + col, m, d);
-      else
+      for (int v = 0; v < V; ++v) {
+        const int col = (v * TPR + lane) * 8;
+        if (col >= p.cols) continue;
+        const int m = p.cols - col;
+        float u[8], n[8], d[8], w[8];
+        unpack8(dz[v], u);
+        unpack8(y[v], n);
+        load8<float, VEC>(p.weight + col, m, w);
+        if (p.dy) {
+          unpack8(dy[v], d);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) d[j] = 0.f;
+          for (int j = 0; j < 8; ++j) d[j] = 0.f;
+        }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) d[j] += rstd * (u[v][j] - n[v][j] * sum);
-      if (p.dresidual) store8<E, VEC>(static_cast<E*>(p.dresidual) + row * p.dresidual_stride + col, m, d);
-      if (p.dx) {
-        const uint32_t bits = keep8<VEC>((uint64_t)row * (uint64_t)p.cols + col, p.drop);
+        for (int j = 0; j < 8; ++j) d[j] += rstd * (u[j] * w[j] - n[j] * rstd * sum);
+        if (p.dresidual) store8<E, VEC>(static_cast<E*>(p.dresidual) + row * p.dresidual_stride + col, m, d);
+        if (p.dx) {
+          drop8<VEC>(d, (uint64_t)row * (uint64_t)p.cols + col, p.drop);
+          store8<E, VEC>(static_cast<E*>(p.dx) + row * p.dx_stride + col, m, d);
+        }
+      }
+    }
+    if (AHEAD) {
+      rstd = next_rstd;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) d[j] = drop(d[j], bits, j, p.drop.scale);
-        store8<E, VEC>(static_cast<E*>(p.dx) + row * p.dx_stride + col, m, d);
+      for (int v = 0; v < V; ++v) {
+        dz[v] = next_dz[v];
+        y[v] = next_y[v];
+        dy[v] = next_dy[v];
       }
     }
   }
@@ -201,7 +241,7 @@ int rows_per_cta(int cols) {
 int norm_backward_ctas(int64_t rows, int cols) {
   const int64_t rpc = rows_per_cta(cols);
   const int64_t need = (rows + rpc - 1) / rpc;
-  const int64_t most = cols <= 4096 ? 152 * 3 : 152;
+  const int64_t most = cols <= 4096 ? 2 * kSMs : kSMs;
   return (int)(need < most ? need : most);
 }
 

@@ -41,13 +41,11 @@ __device__ __forceinline__ float at_most(float x, float most) {
   return y;
 }
 
-// Two adjacent elements in fp32.  bf16 is the upper half of an fp32 value.
+// Two adjacent elements in fp32.
 __device__ __forceinline__ float2 widen(float2 v) { return v; }
-__device__ __forceinline__ float2 widen(__half2 v) { return __half22float2(v); }
-__device__ __forceinline__ float2 widen(__nv_bfloat162 v) {
-  const uint32_t u = *reinterpret_cast<const uint32_t*>(&v);
-  return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u));
-}
+__device__ __forceinline__ float2 widen(__half2 v) { return Pack2<__half>::up(v); }
+__device__ __forceinline__ float2 widen(__nv_bfloat162 v) { return Pack2<__nv_bfloat16>::up(v); }
+
 constexpr float kMostGate = 27.f;   // sigmoid is 1 to fp32 from well below this
 
 // A gate's value, capped where its sigmoid is 1 in fp32, so that no square of an exponential below

@@ -129,5 +129,5 @@ def test_binding_refusals(gs):
     assert gs._matrix("f", "t", t.expand(5, 4, 8)[:, :1], (5, 1, 8), t.dtype, t.device)[1] == 0
     check(gs._dense, "t", t.t(), (8, 4), t.dtype, t.device)
     check(gs._seq, "t", torch.empty(2, 8, 4, device=m).transpose(1, 2), (2, 4, 8), torch.float32, m)
-    check(gs._flags, "lengths", torch.empty(2, dtype=torch.int64, device=m), (2,), "lengths", m)
+    check(gs._whole, "lengths", torch.empty(2, dtype=torch.int64, device=m), (2,), m)
     check(gs._states_fit, torch.empty(8, dtype=torch.uint8), 2, 1000, 64)
