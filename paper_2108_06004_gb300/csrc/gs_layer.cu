@@ -75,6 +75,31 @@ gs_status check_shape(int64_t rows, int64_t cols) {
   return GS_OK;
 }
 
+// How the rows of these tensors lie to one another; `lead`: see gs::Layout.  Absent tensors agree
+// with everything.
+struct Matrix {
+  const void* data;
+  int64_t stride;
+};
+gs::Layout layout_of(std::initializer_list<Matrix> all, int64_t rows, int64_t cols, int32_t dtype, int* lead) {
+  const Matrix* first = nullptr;
+  *lead = 0;
+  for (const Matrix& m : all) {
+    if (!m.data) continue;
+    const int at = (int)(reinterpret_cast<uintptr_t>(m.data) / item(dtype) % 8);
+    if (!first) {
+      first = &m;
+      *lead = at;
+    }
+    if (at != *lead || (rows > 1 && (m.stride - first->stride) % 8 != 0)) {
+      *lead = 0;
+      return gs::kApart;
+    }
+  }
+  const bool even = *lead == 0 && cols % 8 == 0 && (rows == 1 || !first || first->stride % 8 == 0);
+  return even ? gs::kEven : gs::kTogether;
+}
+
 gs_status make_drop(float p, uint64_t seed, uint64_t offset, gs::DropParams& d) {
   if (!(p >= 0.f && p <= 1.f)) return bad("p must lie in [0, 1]");
   d.threshold = (uint32_t)std::floor((double)p * 65536.0 + 0.5);
@@ -116,10 +141,9 @@ gs_status dropout_impl(const void* x, int64_t x_stride, const void* residual, in
     q.rows = 1;
     q.cols = rows * cols;
   }
-  bool vec = aligned(x, 16) && aligned(out, 16) && (!residual || aligned(residual, 16));
-  if (q.rows > 1)
-    vec = vec && cols % 8 == 0 && x_stride % 8 == 0 && out_stride % 8 == 0 && (!residual || residual_stride % 8 == 0);
-  const cudaError_t e = gs::launch_dropout(q, dtype, vec, as_stream(stream));
+  const gs::Layout layout =
+      layout_of({{x, x_stride}, {residual, residual_stride}, {out, out_stride}}, q.rows, q.cols, dtype, &q.lead);
+  const cudaError_t e = gs::launch_dropout(q, dtype, layout, as_stream(stream));
   return e == cudaSuccess ? GS_OK : gs::record_cuda_failure(e, "dropout launch");
 }
 
@@ -131,7 +155,10 @@ gs_status check_norm(int64_t rows, int64_t cols) {
 }
 
 size_t norm_ws_bytes(int64_t rows, int64_t cols) {
-  const size_t n = (size_t)gs::norm_backward_ctas(rows, (int)cols) * (size_t)cols * sizeof(float);
+  // with and without the elements that an odd start of a row adds to its width
+  const int wide = (int)(cols + 7 <= GS_NORM_MAX_COLS ? cols + 7 : cols);
+  const int a = gs::norm_backward_ctas(rows, (int)cols), b = gs::norm_backward_ctas(rows, wide);
+  const size_t n = (size_t)(a > b ? a : b) * (size_t)cols * sizeof(float);
   return n ? (n + 255) & ~size_t(255) : 256;
 }
 
@@ -146,7 +173,7 @@ gs_status check_sequence_shape(int64_t B, int64_t T, int64_t D) {
   if (B > kMaxElements || T > kMaxRows || D > kMaxElements || !product_fits(B, D) || !product_fits(B * D, T))
     return bad("T must be below 2^31 and B * T * D at most 2^40");
   // one CTA for each row and 64 channels
-  if (B > 0 && (D + 63) / 64 >= (int64_t(1) << 28) / B) return bad("B * ceil(D / 64) must be below 2^28");
+  if ((D + 63) / 64 >= (int64_t(1) << 28) / (B > 0 ? B : 1)) return bad("B * ceil(D / 64) must be below 2^28");
   return GS_OK;
 }
 
@@ -262,9 +289,10 @@ gs_status gs_dropout_add_norm(const void* x, int64_t x_stride, const void* resid
   q.rows = rows;
   q.cols = (int32_t)cols;
   q.eps = eps;
-  const bool vec = aligned(x, 16) && aligned(residual, 16) && aligned(weight, 16) && aligned(y, 16) && aligned(z, 16) &&
-                   cols % 8 == 0 && (x_stride | residual_stride | y_stride | z_stride) % 8 == 0;
-  const cudaError_t e = gs::launch_norm_forward(q, dtype, vec, as_stream(stream));
+  gs::Layout layout = layout_of({{x, x_stride}, {residual, residual_stride}, {y, y_stride}, {z, z_stride}}, rows, cols,
+                                dtype, &q.lead);
+  if (!aligned(weight, 16)) layout = gs::kApart;
+  const cudaError_t e = gs::launch_norm_forward(q, dtype, layout, as_stream(stream));
   return e == cudaSuccess ? GS_OK : gs::record_cuda_failure(e, "dropout_add_norm launch");
   GS_GUARD_END
 }
@@ -315,10 +343,10 @@ gs_status gs_dropout_add_norm_backward(const void* dz, int64_t dz_stride, const 
   q.dresidual_stride = dresidual ? dresidual_stride : 0;
   q.rows = rows;
   q.cols = (int32_t)cols;
-  const bool vec = aligned(dz, 16) && aligned(dy, 16) && aligned(y, 16) && aligned(weight, 16) && aligned(dx, 16) &&
-                   aligned(dresidual, 16) && cols % 8 == 0 &&
-                   (q.dz_stride | q.dy_stride | q.y_stride | q.dx_stride | q.dresidual_stride) % 8 == 0;
-  const cudaError_t e = gs::launch_norm_backward(q, dweight, dtype, vec, as_stream(stream));
+  gs::Layout layout = layout_of({{dz, dz_stride}, {dy, dy_stride}, {y, y_stride}, {dx, dx_stride},
+                                 {dresidual, dresidual_stride}}, rows, cols, dtype, &q.lead);
+  if (!aligned(weight, 16)) layout = gs::kApart;
+  const cudaError_t e = gs::launch_norm_backward(q, dweight, dtype, layout, as_stream(stream));
   return e == cudaSuccess ? GS_OK : gs::record_cuda_failure(e, "dropout_add_norm_backward launch");
   GS_GUARD_END
 }
@@ -440,6 +468,7 @@ gs_status gs_recurrence_step(const void* x, int64_t x_stride, const void* r, int
   GS_GUARD_BEGIN
   GS_TRY(check_type(dtype));
   GS_TRY(check_shape(B, D));
+  if (D > kMaxRows) return bad("D must be below 2^31");
   GS_TRY(check_c(c));
   if (n_slots < 0) return bad("n_slots must not be negative");
   const bool some = B > 0 && D > 0;

@@ -46,24 +46,51 @@ template <> __device__ __forceinline__ float from_f32<float>(float v) { return v
 template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// Eight adjacent elements as they are in memory, so that loads can be issued well before their
-// values are needed.  VEC: the address is a multiple of 16 bytes and all eight exist; otherwise the
-// first n of them one by one, zeros for the rest.
+// Rows are worked on in groups of eight adjacent elements, in one of three ways.
+//   kEven: every row starts at a 16-byte boundary (by the element's size: at eight elements) and
+//     has whole groups only.
+//   kTogether: all tensors of a call have their rows at the same distance, `lead` elements, past
+//     a boundary.  The groups start at the boundaries: group k of a row holds columns 8k - lead ...
+//     8k - lead + 7, so that all groups but a row's first and last move as 16-byte words whatever
+//     the width and the alignment are.  Contiguous tensors of an odd width are of this kind.
+//   kApart: anything else; elements move one by one.
+enum Layout { kApart, kEven, kTogether };
+
+struct Span {
+  int col;     // of the group's first element; negative where the row starts inside the group
+  int lo, hi;  // the elements of the group that exist
+  __device__ __forceinline__ bool some() const { return hi > lo; }
+  __device__ __forceinline__ bool whole() const { return hi - lo == 8; }
+};
+template <int L>
+__device__ __forceinline__ Span span(int64_t group, int lead, int64_t cols) {
+  const int64_t col = group * 8 - (L == kTogether ? lead : 0);
+  if (L == kEven) return Span{(int)col, 0, col < cols ? 8 : 0};
+  return Span{(int)col, col < 0 ? (int)-col : 0, cols - col < 8 ? (int)(cols - col) : 8};
+}
+// lead of a row of `stride` elements from the row before, where row 0 has `first`.
+template <int L>
+__device__ __forceinline__ int lead_of(int64_t row, int64_t stride, int first) {
+  return L == kTogether ? (int)(((uint32_t)row * (uint32_t)stride + (uint32_t)first) & 7u) : 0;
+}
+
+// A group as it is in memory, so that loads can be issued well before their values are needed.
+// What does not exist is zero.
 template <typename E>
 struct Raw8 {
   uint4 q[sizeof(E) / 2];
 };
 
-template <typename E, bool VEC>
-__device__ __forceinline__ Raw8<E> fetch8(const E* p, int n) {
+template <typename E, int L>
+__device__ __forceinline__ Raw8<E> fetch8(const E* p, const Span& g) {
   Raw8<E> r;
-  if (VEC) {
+  if (L == kEven || (L == kTogether && g.whole())) {
 #pragma unroll
     for (int k = 0; k < (int)(sizeof(E) / 2); ++k) r.q[k] = reinterpret_cast<const uint4*>(p)[k];
   } else {
     E* e = reinterpret_cast<E*>(&r);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = j < n ? p[j] : from_f32<E>(0.f);
+    for (int j = 0; j < 8; ++j) e[j] = j >= g.lo && j < g.hi ? p[j] : from_f32<E>(0.f);
   }
   return r;
 }
@@ -79,15 +106,10 @@ __device__ __forceinline__ void unpack8(const Raw8<E>& r, float (&v)[8]) {
   }
 }
 
-template <typename E, bool VEC>
-__device__ __forceinline__ void load8(const E* p, int n, float (&v)[8]) {
-  unpack8(fetch8<E, VEC>(p, n), v);
-}
-
-template <typename E, bool VEC>
-__device__ __forceinline__ void store8(E* p, int n, const float (&v)[8]) {
-  if (VEC) {
-    constexpr int Q = sizeof(E) * 8 / 16;
+template <typename E, int L>
+__device__ __forceinline__ void store8(E* p, const Span& g, const float (&v)[8]) {
+  if (L == kEven || (L == kTogether && g.whole())) {
+    constexpr int Q = sizeof(E) / 2;
     uint4 raw[Q];
     typename Pack2<E>::type* h = reinterpret_cast<typename Pack2<E>::type*>(raw);
 #pragma unroll
@@ -97,7 +119,7 @@ __device__ __forceinline__ void store8(E* p, int n, const float (&v)[8]) {
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      if (j < n) p[j] = from_f32<E>(v[j]);
+      if (j >= g.lo && j < g.hi) p[j] = from_f32<E>(v[j]);
   }
 }
 
@@ -126,9 +148,22 @@ __device__ __forceinline__ uint4 philox(uint64_t block, const DropParams& d) {
   return make_uint4(x0, x1, x2, x3);
 }
 
-// Bit j set: element 8 * block + j is kept.  Element 2w + h takes half h of word w.  A half is
-// compared in the upper 16 bits of a word, where what lies below it does not matter.
-__device__ __forceinline__ uint32_t keep8_block(uint64_t block, const DropParams& d) {
+// Dropout of the eight elements of a block.  Element 2w + h takes half h of word w.  A half is
+// compared in the upper 16 bits of a word, where what lies below it does not matter.  A dropped
+// element is zero whatever its value was (infinities and NaN included).
+__device__ __forceinline__ void drop_block(float (&v)[8], uint64_t block, const DropParams& d) {
+  const uint4 w = philox(block, d);
+  const uint32_t word[4] = {w.x, w.y, w.z, w.w}, least = d.threshold << 16;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const float2 s = __fmul2_rn(make_float2(v[2 * q], v[2 * q + 1]), make_float2(d.scale, d.scale));
+    v[2 * q] = word[q] << 16 >= least ? s.x : 0.f;
+    v[2 * q + 1] = word[q] >= least ? s.y : 0.f;
+  }
+}
+
+// Bit j set: element 8 * block + j is kept.
+__device__ __forceinline__ uint32_t keep_block(uint64_t block, const DropParams& d) {
   const uint4 w = philox(block, d);
   const uint32_t word[4] = {w.x, w.y, w.z, w.w}, least = d.threshold << 16;
   uint32_t bits = 0;
@@ -140,29 +175,23 @@ __device__ __forceinline__ uint32_t keep8_block(uint64_t block, const DropParams
   return bits;
 }
 
-// Dropout of the eight elements from `first` on, which lie in one block (ALIGNED) or in two.  A
-// dropped element is zero whatever its value was (infinities and NaN included).
+// Dropout of the eight elements from `first` on, which lie in one block or in two.  `first` is
+// negative where a row's first group starts before the first element of all; what does not exist
+// may get any mask.
 template <bool ALIGNED>
-__device__ __forceinline__ void drop8(float (&v)[8], uint64_t first, const DropParams& d) {
+__device__ __forceinline__ void drop8(float (&v)[8], int64_t first, const DropParams& d) {
   if (d.threshold == 0) return;
   if (d.threshold > 0xFFFF) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = 0.f;
     return;
   }
-  if (ALIGNED) {
-    const uint4 w = philox(first >> 3, d);
-    const uint32_t word[4] = {w.x, w.y, w.z, w.w}, least = d.threshold << 16;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float2 s = __fmul2_rn(make_float2(v[2 * q], v[2 * q + 1]), make_float2(d.scale, d.scale));
-      v[2 * q] = word[q] << 16 >= least ? s.x : 0.f;
-      v[2 * q + 1] = word[q] >= least ? s.y : 0.f;
-    }
+  const int64_t block = first >> 3;
+  const uint32_t skip = (uint32_t)first & 7u;
+  if (ALIGNED || skip == 0) {
+    drop_block(v, (uint64_t)block, d);
   } else {
-    const uint32_t skip = (uint32_t)first & 7u;
-    uint32_t bits = keep8_block(first >> 3, d);
-    if (skip) bits = (bits | (keep8_block((first >> 3) + 1, d) << 8)) >> skip;
+    const uint32_t bits = (keep_block((uint64_t)block, d) | keep_block((uint64_t)(block + 1), d) << 8) >> skip;
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = (bits >> j) & 1u ? v[j] * d.scale : 0.f;
   }
@@ -175,6 +204,7 @@ struct DropoutParams {
   void* out;
   int64_t x_stride, residual_stride, out_stride;
   int64_t rows, cols;
+  int lead;  // of row 0
   DropParams drop;
 };
 
@@ -188,6 +218,7 @@ struct NormForwardParams {
   int64_t x_stride, residual_stride, y_stride, z_stride;
   int64_t rows;
   int32_t cols;
+  int lead;
   float eps;
   DropParams drop;
 };
@@ -204,6 +235,7 @@ struct NormBackwardParams {
   int64_t dz_stride, dy_stride, y_stride, dx_stride, dresidual_stride;
   int64_t rows;
   int32_t cols;
+  int lead;
   DropParams drop;
 };
 
@@ -247,13 +279,17 @@ struct RecurrenceStepParams {
 };
 
 // ---- launchers ------------------------------------------------------------------------------
-cudaError_t launch_dropout(const DropoutParams& p, int dtype, bool vec, cudaStream_t s);
+cudaError_t launch_dropout(const DropoutParams& p, int dtype, Layout layout, cudaStream_t s);
 
 constexpr int kSMs = 152;  // the sizes of grids are rules on it, so that results do not depend on a query
 constexpr int kNormMaxCols = 16384;
 int norm_backward_ctas(int64_t rows, int cols);
-cudaError_t launch_norm_forward(const NormForwardParams& p, int dtype, bool vec, cudaStream_t s);
-cudaError_t launch_norm_backward(const NormBackwardParams& p, float* dweight, int dtype, bool vec, cudaStream_t s);
+cudaError_t launch_norm_forward(const NormForwardParams& p, int dtype, Layout layout, cudaStream_t s);
+cudaError_t launch_norm_backward(const NormBackwardParams& p, float* dweight, int dtype, Layout layout, cudaStream_t s);
+
+// out[c] = sum over n rows of partial[row][c]; times -scale sigmoid(decay[c]) where decay is given
+cudaError_t launch_column_sums(const float* partial, int64_t n, int64_t cols, const float* decay, float scale,
+                               float* out, cudaStream_t s);
 
 struct RecurrenceShape {
   int channels;      // of a CTA
@@ -289,6 +325,16 @@ inline cudaError_t launch_cluster(void (*kernel)(KArgs...), dim3 grid, dim3 bloc
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
+}
+
+// Calls f with the layout as a constant.
+template <typename F>
+inline cudaError_t with_layout(Layout layout, F&& f) {
+  switch (layout) {
+    case kEven: return f(std::integral_constant<int, kEven>());
+    case kTogether: return f(std::integral_constant<int, kTogether>());
+    default: return f(std::integral_constant<int, kApart>());
+  }
 }
 
 // Calls f with a value of the element type that `dtype` names.

@@ -13,71 +13,84 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kAhead = 2;  // groups of eight whose loads a thread has under way
 
-// FLAT: one row of 8 * groups elements or fewer (the tensors are contiguous).  Otherwise rows
-// with strides, `groups` of them a row.  VEC: groups are whole and 16-byte aligned, but for a
-// last one of a FLAT row.
-template <typename E, bool FLAT, bool VEC, bool RESIDUAL>
-__global__ void __launch_bounds__(kThreads) k_dropout(const __grid_constant__ DropoutParams p, int64_t groups) {
+// n / d for n below 2^31: with 2^(k-1) < d <= 2^k and m = floor(2^(31+k) / d) + 1, m n / 2^(31+k) exceeds
+// n / d by less than n / 2^(31+k) < 1 / d, which does not reach the next whole number.
+struct Divisor {
+  uint32_t d, m, k;
+};
+Divisor divisor(uint32_t d) {
+  uint32_t k = 0;
+  while ((uint64_t(1) << k) < d) ++k;
+  return Divisor{d, (uint32_t)(((uint64_t(1) << 31) << k) / d + 1), k};
+}
+__device__ __forceinline__ uint32_t divide(uint32_t n, const Divisor& v) {
+  return (uint32_t)((uint64_t)n * v.m >> 31 >> v.k);
+}
+
+// ROWS 0: one row (the tensors are contiguous); 1: rows of `groups` groups, fewer than 2^31 in all;
+// 2: any number.
+template <typename E, int ROWS, int L, bool RESIDUAL>
+__global__ void __launch_bounds__(kThreads)
+k_dropout(const __grid_constant__ DropoutParams p, int64_t groups, Divisor by_groups) {
   grid_begin();
   const int64_t total = groups * p.rows, step = (int64_t)gridDim.x * kThreads;
   for (int64_t g0 = (int64_t)blockIdx.x * kThreads + threadIdx.x; g0 < total; g0 += kAhead * step) {
     Raw8<E> x[kAhead], res[kAhead];
     int64_t row[kAhead], col[kAhead];
-    int n[kAhead];
+    Span part[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const int64_t g = g0 + u * step;
-      row[u] = FLAT ? 0 : total <= 0xFFFFFFFFll ? (int64_t)((uint32_t)g / (uint32_t)groups) : g / groups;
-      col[u] = (g - row[u] * groups) * 8;
-      n[u] = g < total ? (int)(p.cols - col[u] < 8 ? p.cols - col[u] : 8) : 0;
-      const E* px = static_cast<const E*>(p.x) + row[u] * p.x_stride + col[u];
-      const E* pr = static_cast<const E*>(p.residual) + row[u] * p.residual_stride + col[u];
-      if (VEC && n[u] == 8) {
-        x[u] = fetch8<E, true>(px, 8);
-        if (RESIDUAL) res[u] = fetch8<E, true>(pr, 8);
-      } else {
-        x[u] = fetch8<E, false>(px, n[u]);
-        if (RESIDUAL) res[u] = fetch8<E, false>(pr, n[u]);
-      }
+      row[u] = ROWS == 0 ? 0 : ROWS == 1 ? (int64_t)divide((uint32_t)g, by_groups) : g / groups;
+      const int lead = lead_of<L>(row[u], p.x_stride, p.lead);
+      col[u] = (g - row[u] * groups) * 8 - lead;
+      part[u] = span<L>(g - row[u] * groups, lead, p.cols);
+      if (g >= total) part[u].hi = part[u].lo = 0;
+      if (!part[u].some()) continue;
+      x[u] = fetch8<E, L>(static_cast<const E*>(p.x) + row[u] * p.x_stride + col[u], part[u]);
+      if (RESIDUAL)
+        res[u] = fetch8<E, L>(static_cast<const E*>(p.residual) + row[u] * p.residual_stride + col[u], part[u]);
     }
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      if (n[u] == 0) continue;
+      if (!part[u].some()) continue;
       float v[8];
       unpack8(x[u], v);
-      drop8<(FLAT || VEC)>(v, (uint64_t)(row[u] * p.cols + col[u]), p.drop);
+      drop8<L == kEven>(v, row[u] * p.cols + col[u], p.drop);
       if (RESIDUAL) {
         float w[8];
         unpack8(res[u], w);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] += w[j];
       }
-      E* po = static_cast<E*>(p.out) + row[u] * p.out_stride + col[u];
-      if (VEC && n[u] == 8)
-        store8<E, true>(po, 8, v);
-      else
-        store8<E, false>(po, n[u], v);
+      store8<E, L>(static_cast<E*>(p.out) + row[u] * p.out_stride + col[u], part[u], v);
     }
   }
 }
 
-template <typename E, bool FLAT, bool VEC>
-cudaError_t run(const DropoutParams& p, cudaStream_t s) {
-  const int64_t groups = (p.cols + 7) / 8;
+template <typename E, int ROWS, int L>
+cudaError_t run(const DropoutParams& p, int64_t groups, cudaStream_t s) {
   const int64_t ctas = (groups * p.rows + kThreads - 1) / kThreads;
   const int64_t most = (int64_t)kSMs * 64;
   const dim3 grid((unsigned)(ctas < most ? ctas : most));
-  return p.residual ? launch(k_dropout<E, FLAT, VEC, true>, grid, dim3(kThreads), s, p, groups)
-                    : launch(k_dropout<E, FLAT, VEC, false>, grid, dim3(kThreads), s, p, groups);
+  const Divisor by = ROWS == 1 ? divisor((uint32_t)groups) : Divisor{};
+  return p.residual ? launch(k_dropout<E, ROWS, L, true>, grid, dim3(kThreads), s, p, groups, by)
+                    : launch(k_dropout<E, ROWS, L, false>, grid, dim3(kThreads), s, p, groups, by);
 }
 
 }  // namespace
 
-cudaError_t launch_dropout(const DropoutParams& p, int dtype, bool vec, cudaStream_t s) {
+cudaError_t launch_dropout(const DropoutParams& p, int dtype, Layout layout, cudaStream_t s) {
+  // a row's last group may start up to seven columns earlier than its number says
+  const int64_t groups = (p.cols + 7) / 8 + (layout == kTogether ? 1 : 0);
+  // groups past the end of the last one are asked for too, before they are found not to exist
+  const bool few = groups * p.rows < (int64_t(1) << 31) - kAhead * int64_t(kSMs) * 64 * kThreads;
   return with_type(dtype, [&](auto e) {
     using E = decltype(e);
-    if (p.rows == 1) return vec ? run<E, true, true>(p, s) : run<E, true, false>(p, s);
-    return vec ? run<E, false, true>(p, s) : run<E, false, false>(p, s);
+    return with_layout(layout, [&](auto how) {
+      constexpr int L = decltype(how)::value;
+      return p.rows == 1 ? run<E, 0, L>(p, groups, s) : few ? run<E, 1, L>(p, groups, s) : run<E, 2, L>(p, groups, s);
+    });
   });
 }
 

@@ -5,9 +5,9 @@
 //     n = y rstd,  u = dz w,  dt = rstd (u - n mean(u n)) + dy
 //     dresidual = dt,  dx = mask dt scale,  dw = sum over rows of dz n
 //
-// A row is held in the registers of TPR threads, 8 * V adjacent-by-8 elements each, so every
-// tensor is read and written once.  dw is summed by each thread over the rows of its CTA, then
-// over the CTAs by a second kernel, in a fixed order.
+// A row is held in the registers of TPR threads, V groups of eight elements each, so every tensor
+// is read and written once.  dw is summed by each thread over the rows of its CTA, then over the
+// CTAs by a second kernel, in a fixed order.
 #include "gs_layer.cuh"
 
 namespace gs {
@@ -32,9 +32,30 @@ __device__ __forceinline__ float row_sum(float v, float* scratch) {
   return v;
 }
 
+// The weights of a group, which start at a 16-byte boundary where the row does not have a lead.
+// Otherwise they are taken out of the three words of four that hold them.
+template <int L>
+__device__ __forceinline__ void weight8(const float* weight, const Span& g, int lead, int cols, float (&w)[8]) {
+  if (L == kEven || (L == kTogether && lead == 0 && g.whole())) {
+    unpack8(fetch8<float, kEven>(weight + g.col, g), w);
+  } else if (L == kTogether && g.whole() && (g.col & ~3) + 12 <= cols) {
+    float t[12];
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      *reinterpret_cast<float4*>(t + 4 * k) = *reinterpret_cast<const float4*>(weight + (g.col & ~3) + 4 * k);
+    const bool one = g.col & 1, two = g.col & 2;
+#pragma unroll
+    for (int k = 0; k < 11; ++k) t[k] = one ? t[k + 1] : t[k];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = two ? t[k + 2] : t[k];
+  } else {
+    unpack8(fetch8<float, kApart>(weight + g.col, g), w);
+  }
+}
+
 template <int TPR> constexpr int kCtaThreads = TPR > 256 ? TPR : 256;
 
-template <typename E, int TPR, int V, bool VEC>
+template <typename E, int TPR, int V, int L>
 __global__ void __launch_bounds__(kCtaThreads<TPR>)
 k_norm_forward(const __grid_constant__ NormForwardParams p) {
   grid_begin();
@@ -43,23 +64,23 @@ k_norm_forward(const __grid_constant__ NormForwardParams p) {
   const int lane = threadIdx.x % TPR;
   const int64_t row = (int64_t)blockIdx.x * RPC + threadIdx.x / TPR;
   const bool live = row < p.rows;
+  const int lead = lead_of<L>(row, p.x_stride, p.lead);
   float t[V][8];
   float sum = 0.f;
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    const int col = (v * TPR + lane) * 8;
-    if (!live || col >= p.cols) continue;
-    const int n = p.cols - col;
+    const Span g = span<L>(v * TPR + lane, lead, p.cols);
+    if (!live || !g.some()) continue;
     float res[8];
-    load8<E, VEC>(static_cast<const E*>(p.x) + row * p.x_stride + col, n, t[v]);
-    load8<E, VEC>(static_cast<const E*>(p.residual) + row * p.residual_stride + col, n, res);
-    drop8<VEC>(t[v], (uint64_t)row * (uint64_t)p.cols + col, p.drop);
+    unpack8(fetch8<E, L>(static_cast<const E*>(p.x) + row * p.x_stride + g.col, g), t[v]);
+    unpack8(fetch8<E, L>(static_cast<const E*>(p.residual) + row * p.residual_stride + g.col, g), res);
+    drop8<L == kEven>(t[v], row * p.cols + g.col, p.drop);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      t[v][j] += res[j];
-      if (VEC || j < n) sum += t[v][j] * t[v][j];
+      t[v][j] += res[j];  // zero where there is no element
+      sum += t[v][j] * t[v][j];
     }
-    store8<E, VEC>(static_cast<E*>(p.y) + row * p.y_stride + col, n, t[v]);
+    store8<E, L>(static_cast<E*>(p.y) + row * p.y_stride + g.col, g, t[v]);
   }
   sum = row_sum<TPR>(sum, scratch);
   const float rstd = rsqrtf(sum / (float)p.cols + p.eps);
@@ -67,18 +88,17 @@ k_norm_forward(const __grid_constant__ NormForwardParams p) {
   if (lane == 0) p.rstd[row] = rstd;
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    const int col = (v * TPR + lane) * 8;
-    if (col >= p.cols) continue;
-    const int n = p.cols - col;
+    const Span g = span<L>(v * TPR + lane, lead, p.cols);
+    if (!g.some()) continue;
     float w[8];
-    load8<float, VEC>(p.weight + col, n, w);
+    weight8<L>(p.weight, g, lead, p.cols, w);
 #pragma unroll
     for (int j = 0; j < 8; ++j) w[j] *= t[v][j] * rstd;
-    store8<E, VEC>(static_cast<E*>(p.z) + row * p.z_stride + col, n, w);
+    store8<E, L>(static_cast<E*>(p.z) + row * p.z_stride + g.col, g, w);
   }
 }
 
-template <typename E, int TPR, int V, bool VEC>
+template <typename E, int TPR, int V, int L>
 __global__ void __launch_bounds__(kCtaThreads<TPR>, kCtaThreads<TPR> == 256 ? 2 : 1)
 k_norm_backward(const __grid_constant__ NormBackwardParams p) {
   grid_begin();
@@ -86,7 +106,10 @@ k_norm_backward(const __grid_constant__ NormBackwardParams p) {
   constexpr int RPC = kCtaThreads<TPR> / TPR;
   extern __shared__ float fold[];  // RPC > 1: [RPC][cols]
   const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
-  const int64_t step = (int64_t)gridDim.x * RPC;
+  // a thread's rows, `step` apart, all have the same lead: step is a multiple of eight where a thread
+  // has more than one
+  const int64_t step = (int64_t)gridDim.x * RPC, first = (int64_t)blockIdx.x * RPC;
+  const int lead = lead_of<L>(first + sub, p.dz_stride, p.lead);
   float dw[V][8];
 #pragma unroll
   for (int v = 0; v < V; ++v)
@@ -103,16 +126,22 @@ k_norm_backward(const __grid_constant__ NormBackwardParams p) {
     rstd = p.rstd[row];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int col = (v * TPR + lane) * 8;
-      if (col >= p.cols) continue;
-      const int m = p.cols - col;
-      dz[v] = fetch8<E, VEC>(static_cast<const E*>(p.dz) + row * p.dz_stride + col, m);
-      y[v] = fetch8<E, VEC>(static_cast<const E*>(p.y) + row * p.y_stride + col, m);
-      if (p.dy) dy[v] = fetch8<E, VEC>(static_cast<const E*>(p.dy) + row * p.dy_stride + col, m);
+      const Span g = span<L>(v * TPR + lane, lead, p.cols);
+      if (!g.some()) continue;
+      dz[v] = fetch8<E, L>(static_cast<const E*>(p.dz) + row * p.dz_stride + g.col, g);
+      y[v] = fetch8<E, L>(static_cast<const E*>(p.y) + row * p.y_stride + g.col, g);
+      if (p.dy) dy[v] = fetch8<E, L>(static_cast<const E*>(p.dy) + row * p.dy_stride + g.col, g);
     }
   };
-  const int64_t first = (int64_t)blockIdx.x * RPC;
-  if (AHEAD) fetch(first + sub, dz, y, dy, rstd);
+  float weight[AHEAD ? V : 1][8];  // a thread's columns are the same in all its rows
+  if (AHEAD) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const Span g = span<L>(v * TPR + lane, lead, p.cols);
+      if (g.some()) weight8<L>(p.weight, g, lead, p.cols, weight[AHEAD ? v : 0]);
+    }
+    fetch(first + sub, dz, y, dy, rstd);
+  }
   int turn = 0;
   for (int64_t row0 = first; row0 < p.rows; row0 += step, turn ^= 1) {
     const int64_t row = row0 + sub;
@@ -126,33 +155,31 @@ k_norm_backward(const __grid_constant__ NormBackwardParams p) {
     float sum = 0.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int col = (v * TPR + lane) * 8;
-      if (!live || col >= p.cols) continue;
-      const int m = p.cols - col;
-      float u[8], n[8], w[8];
+      const Span g = span<L>(v * TPR + lane, lead, p.cols);
+      if (!live || !g.some()) continue;
+      float u[8], n[8];
+      float(&w)[8] = weight[AHEAD ? v : 0];
       unpack8(dz[v], u);
       unpack8(y[v], n);
-      load8<float, VEC>(p.weight + col, m, w);
+      if (!AHEAD) weight8<L>(p.weight, g, lead, p.cols, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float t = u[j] * (n[j] * rstd);
-        if (VEC || j < m) {
-          dw[v][j] += t;
-          sum += t * w[j];
-        }
+        const float t = u[j] * (n[j] * rstd);  // zero where there is no element
+        dw[v][j] += t;
+        sum += t * w[j];
       }
     }
     sum = row_sum<TPR>(sum, scratch[turn]) / (float)p.cols;
     if (live) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const int col = (v * TPR + lane) * 8;
-        if (col >= p.cols) continue;
-        const int m = p.cols - col;
-        float u[8], n[8], d[8], w[8];
+        const Span g = span<L>(v * TPR + lane, lead, p.cols);
+        if (!g.some()) continue;
+        float u[8], n[8], d[8];
+        float(&w)[8] = weight[AHEAD ? v : 0];
         unpack8(dz[v], u);
         unpack8(y[v], n);
-        load8<float, VEC>(p.weight + col, m, w);
+        if (!AHEAD) weight8<L>(p.weight, g, lead, p.cols, w);
         if (p.dy) {
           unpack8(dy[v], d);
         } else {
@@ -161,10 +188,10 @@ k_norm_backward(const __grid_constant__ NormBackwardParams p) {
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) d[j] += rstd * (u[j] * w[j] - n[j] * rstd * sum);
-        if (p.dresidual) store8<E, VEC>(static_cast<E*>(p.dresidual) + row * p.dresidual_stride + col, m, d);
+        if (p.dresidual) store8<E, L>(static_cast<E*>(p.dresidual) + row * p.dresidual_stride + g.col, g, d);
         if (p.dx) {
-          drop8<VEC>(d, (uint64_t)row * (uint64_t)p.cols + col, p.drop);
-          store8<E, VEC>(static_cast<E*>(p.dx) + row * p.dx_stride + col, m, d);
+          drop8<L == kEven>(d, row * p.cols + g.col, p.drop);
+          store8<E, L>(static_cast<E*>(p.dx) + row * p.dx_stride + g.col, g, d);
         }
       }
     }
@@ -181,12 +208,12 @@ k_norm_backward(const __grid_constant__ NormBackwardParams p) {
   float* part = p.partial + (int64_t)blockIdx.x * p.cols;
   float* to = RPC > 1 ? fold + sub * p.cols : part;
 #pragma unroll
-  for (int v = 0; v < V; ++v)
+  for (int v = 0; v < V; ++v) {
+    const Span g = span<L>(v * TPR + lane, lead, p.cols);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int col = (v * TPR + lane) * 8 + j;
-      if (col < p.cols) to[col] = dw[v][j];
-    }
+    for (int j = 0; j < 8; ++j)
+      if (j >= g.lo && j < g.hi) to[g.col + j] = dw[v][j];
+  }
   if constexpr (RPC > 1) {
     __syncthreads();
     for (int col = threadIdx.x; col < p.cols; col += blockDim.x) {
@@ -198,27 +225,10 @@ k_norm_backward(const __grid_constant__ NormBackwardParams p) {
   }
 }
 
-// dweight[col] = sum over the CTAs' partial rows, 32 columns a CTA, the rows dealt to 8 warps.
-__global__ void __launch_bounds__(256) k_norm_weight(const float* partial, int n, int cols, float* dweight) {
-  grid_begin();
-  __shared__ float part[8][32];
-  const int col = blockIdx.x * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
-  float sum = 0.f;
-  if (col < cols)
-    for (int k = w; k < n; k += 8) sum += partial[(int64_t)k * cols + col];
-  part[w][threadIdx.x & 31] = sum;
-  __syncthreads();
-  if (w == 0 && col < cols) {
-#pragma unroll
-    for (int k = 1; k < 8; ++k) sum += part[k][threadIdx.x];
-    dweight[col] = sum;
-  }
-}
-
 // Threads a row and groups of eight a thread: a row of up to 512 elements is one warp's, wider
 // ones have two groups a thread.
 template <typename F>
-cudaError_t with_shape(int cols, F&& f) {
+cudaError_t with_shape(int cols, F&& f) {  // cols: with the elements that leads may add
   using std::integral_constant;
   if (cols <= 256) return f(integral_constant<int, 32>(), integral_constant<int, 1>());
   if (cols <= 512) return f(integral_constant<int, 32>(), integral_constant<int, 2>());
@@ -235,45 +245,54 @@ int rows_per_cta(int cols) {
   return tpr >= 256 ? 1 : 256 / tpr;
 }
 
+// Elements that a row takes: its first group may start up to seven before it.
+int width(int cols, Layout layout) { return layout == kTogether ? cols + 7 : cols; }
+
 }  // namespace
 
-// CTAs of the backward pass: as many as stay resident, each with its rows dealt round robin.
+// CTAs of the backward pass: as many as stay resident, each with its rows dealt round robin.  (Both
+// numbers are multiples of eight, and so are the rows from one of a thread's to its next.)
 int norm_backward_ctas(int64_t rows, int cols) {
+  static_assert(kSMs % 8 == 0, "rows of a thread must share their lead");
   const int64_t rpc = rows_per_cta(cols);
   const int64_t need = (rows + rpc - 1) / rpc;
   const int64_t most = cols <= 4096 ? 2 * kSMs : kSMs;
   return (int)(need < most ? need : most);
 }
 
-cudaError_t launch_norm_forward(const NormForwardParams& p, int dtype, bool vec, cudaStream_t s) {
+cudaError_t launch_norm_forward(const NormForwardParams& p, int dtype, Layout layout, cudaStream_t s) {
+  if (width(p.cols, layout) > kNormMaxCols) layout = kApart;  // the row with its lead does not fit
   return with_type(dtype, [&](auto e) {
     using E = decltype(e);
-    return with_shape(p.cols, [&](auto tpr, auto v) {
+    return with_shape(width(p.cols, layout), [&](auto tpr, auto v) {
       constexpr int TPR = decltype(tpr)::value, V = decltype(v)::value;
       constexpr int N = kCtaThreads<TPR>;
       const int64_t ctas = (p.rows + N / TPR - 1) / (N / TPR);
-      return vec ? launch(k_norm_forward<E, TPR, V, true>, dim3((unsigned)ctas), dim3(N), s, p)
-                 : launch(k_norm_forward<E, TPR, V, false>, dim3((unsigned)ctas), dim3(N), s, p);
+      return with_layout(layout, [&](auto how) {
+        return launch(k_norm_forward<E, TPR, V, decltype(how)::value>, dim3((unsigned)ctas), dim3(N), s, p);
+      });
     });
   });
 }
 
-cudaError_t launch_norm_backward(const NormBackwardParams& p, float* dweight, int dtype, bool vec, cudaStream_t s) {
-  const int ctas = norm_backward_ctas(p.rows, p.cols);
+cudaError_t launch_norm_backward(const NormBackwardParams& p, float* dweight, int dtype, Layout layout, cudaStream_t s) {
+  if (width(p.cols, layout) > kNormMaxCols) layout = kApart;
+  const int wide = width(p.cols, layout), ctas = norm_backward_ctas(p.rows, wide);
   if (ctas > 0) {
     cudaError_t err = with_type(dtype, [&](auto e) {
       using E = decltype(e);
-      return with_shape(p.cols, [&](auto tpr, auto v) {
+      return with_shape(wide, [&](auto tpr, auto v) {
         constexpr int TPR = decltype(tpr)::value, V = decltype(v)::value;
         constexpr int N = kCtaThreads<TPR>;
         const size_t smem = N > TPR ? (size_t)(N / TPR) * p.cols * sizeof(float) : 0;
-        return vec ? launch_cluster(k_norm_backward<E, TPR, V, true>, dim3(ctas), dim3(N), smem, 1, s, p)
-                   : launch_cluster(k_norm_backward<E, TPR, V, false>, dim3(ctas), dim3(N), smem, 1, s, p);
+        return with_layout(layout, [&](auto how) {
+          return launch_cluster(k_norm_backward<E, TPR, V, decltype(how)::value>, dim3(ctas), dim3(N), smem, 1, s, p);
+        });
       });
     });
     if (err != cudaSuccess) return err;
   }
-  return launch(k_norm_weight, dim3((p.cols + 31) / 32), dim3(256), s, (const float*)p.partial, ctas, p.cols, dweight);
+  return launch_column_sums(p.partial, ctas, p.cols, nullptr, 0.f, dweight, s);
 }
 
 }  // namespace gs

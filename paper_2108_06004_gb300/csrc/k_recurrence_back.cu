@@ -277,25 +277,6 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
   }
 }
 
-// ddecay[d] = -c sigmoid(lambda) * the sum of the CTAs' shares, in a fixed order.
-__global__ void __launch_bounds__(256)
-k_recurrence_decay(const float* partial, int64_t n, int64_t D, const float* decay, float c, float* ddecay) {
-  grid_begin();
-  __shared__ float part[8][32];
-  const int64_t d = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
-  const int w = threadIdx.x >> 5;
-  float sum = 0.f;
-  if (d < D)
-    for (int64_t k = w; k < n; k += 8) sum += partial[k * D + d];
-  part[w][threadIdx.x & 31] = sum;
-  __syncthreads();
-  if (w == 0 && d < D) {
-#pragma unroll
-    for (int k = 1; k < 8; ++k) sum += part[k][threadIdx.x];
-    ddecay[d] = -c * sum / (1.f + expf(-decay[d]));
-  }
-}
-
 template <typename E, int CH, int UNIT, bool OUT, bool RESET>
 cudaError_t run_backward(RecurrenceParams& p, const RecurrenceShape& shape, cudaStream_t s) {
   static std::atomic<uint64_t> done{0};
@@ -344,8 +325,7 @@ cudaError_t launch_recurrence_backward(RecurrenceParams& p, float* ddecay, int d
     });
   });
   if (err != cudaSuccess) return err;
-  return launch(k_recurrence_decay, dim3((unsigned)((p.D + 31) / 32)), dim3(256), s, (const float*)p.partial,
-                p.B * shape.cluster, p.D, p.decay, p.c, ddecay);
+  return launch_column_sums(p.partial, p.B * shape.cluster, p.D, p.decay, p.c, ddecay, s);
 }
 
 }  // namespace gs
