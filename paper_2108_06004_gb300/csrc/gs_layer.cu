@@ -100,6 +100,12 @@ gs::Layout layout_of(std::initializer_list<Matrix> all, int64_t rows, int64_t co
   return even ? gs::kEven : gs::kTogether;
 }
 
+bool spaced(std::initializer_list<Matrix> all) {
+  for (const Matrix& m : all)
+    if (m.data && m.stride < 8) return false;
+  return true;
+}
+
 gs_status make_drop(float p, uint64_t seed, uint64_t offset, gs::DropParams& d) {
   if (!(p >= 0.f && p <= 1.f)) return bad("p must lie in [0, 1]");
   d.threshold = (uint32_t)std::floor((double)p * 65536.0 + 0.5);
@@ -141,8 +147,9 @@ gs_status dropout_impl(const void* x, int64_t x_stride, const void* residual, in
     q.rows = 1;
     q.cols = rows * cols;
   }
-  const gs::Layout layout =
-      layout_of({{x, x_stride}, {residual, residual_stride}, {out, out_stride}}, q.rows, q.cols, dtype, &q.lead);
+  const std::initializer_list<Matrix> all = {{x, x_stride}, {residual, residual_stride}, {out, out_stride}};
+  const gs::Layout layout = layout_of(all, q.rows, q.cols, dtype, &q.lead);
+  q.spaced = spaced(all);
   const cudaError_t e = gs::launch_dropout(q, dtype, layout, as_stream(stream));
   return e == cudaSuccess ? GS_OK : gs::record_cuda_failure(e, "dropout launch");
 }
@@ -155,10 +162,7 @@ gs_status check_norm(int64_t rows, int64_t cols) {
 }
 
 size_t norm_ws_bytes(int64_t rows, int64_t cols) {
-  // with and without the elements that an odd start of a row adds to its width
-  const int wide = (int)(cols + 7 <= GS_NORM_MAX_COLS ? cols + 7 : cols);
-  const int a = gs::norm_backward_ctas(rows, (int)cols), b = gs::norm_backward_ctas(rows, wide);
-  const size_t n = (size_t)(a > b ? a : b) * (size_t)cols * sizeof(float);
+  const size_t n = (size_t)gs::norm_backward_most_ctas(rows, (int)cols) * (size_t)cols * sizeof(float);
   return n ? (n + 255) & ~size_t(255) : 256;
 }
 
@@ -289,8 +293,9 @@ gs_status gs_dropout_add_norm(const void* x, int64_t x_stride, const void* resid
   q.rows = rows;
   q.cols = (int32_t)cols;
   q.eps = eps;
-  gs::Layout layout = layout_of({{x, x_stride}, {residual, residual_stride}, {y, y_stride}, {z, z_stride}}, rows, cols,
-                                dtype, &q.lead);
+  const std::initializer_list<Matrix> all = {{x, x_stride}, {residual, residual_stride}, {y, y_stride}, {z, z_stride}};
+  gs::Layout layout = layout_of(all, rows, cols, dtype, &q.lead);
+  q.spaced = spaced(all);
   if (!aligned(weight, 16)) layout = gs::kApart;
   const cudaError_t e = gs::launch_norm_forward(q, dtype, layout, as_stream(stream));
   return e == cudaSuccess ? GS_OK : gs::record_cuda_failure(e, "dropout_add_norm launch");
@@ -343,8 +348,10 @@ gs_status gs_dropout_add_norm_backward(const void* dz, int64_t dz_stride, const 
   q.dresidual_stride = dresidual ? dresidual_stride : 0;
   q.rows = rows;
   q.cols = (int32_t)cols;
-  gs::Layout layout = layout_of({{dz, dz_stride}, {dy, dy_stride}, {y, y_stride}, {dx, dx_stride},
-                                 {dresidual, dresidual_stride}}, rows, cols, dtype, &q.lead);
+  const std::initializer_list<Matrix> all = {
+      {dz, dz_stride}, {dy, dy_stride}, {y, y_stride}, {dx, dx_stride}, {dresidual, dresidual_stride}};
+  gs::Layout layout = layout_of(all, rows, cols, dtype, &q.lead);
+  q.spaced = spaced(all);
   if (!aligned(weight, 16)) layout = gs::kApart;
   const cudaError_t e = gs::launch_norm_backward(q, dweight, dtype, layout, as_stream(stream));
   return e == cudaSuccess ? GS_OK : gs::record_cuda_failure(e, "dropout_add_norm_backward launch");

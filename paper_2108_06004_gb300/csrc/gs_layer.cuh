@@ -53,6 +53,8 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(flo
 //     a boundary.  The groups start at the boundaries: group k of a row holds columns 8k - lead ...
 //     8k - lead + 7, so that all groups but a row's first and last move as 16-byte words whatever
 //     the width and the alignment are.  Contiguous tensors of an odd width are of this kind.
+//     The first and last groups are read as whole words too (`inner`) where the rows before and
+//     after, or the space between rows, are what lies beside them.
 //   kApart: anything else; elements move one by one.
 enum Layout { kApart, kEven, kTogether };
 
@@ -75,16 +77,15 @@ __device__ __forceinline__ int lead_of(int64_t row, int64_t stride, int first) {
 }
 
 // A group as it is in memory, so that loads can be issued well before their values are needed.
-// What does not exist is zero.
 template <typename E>
 struct Raw8 {
   uint4 q[sizeof(E) / 2];
 };
 
 template <typename E, int L>
-__device__ __forceinline__ Raw8<E> fetch8(const E* p, const Span& g) {
+__device__ __forceinline__ Raw8<E> fetch8(const E* p, const Span& g, bool inner = false) {
   Raw8<E> r;
-  if (L == kEven || (L == kTogether && g.whole())) {
+  if (L == kEven || (L == kTogether && (g.whole() || inner))) {
 #pragma unroll
     for (int k = 0; k < (int)(sizeof(E) / 2); ++k) r.q[k] = reinterpret_cast<const uint4*>(p)[k];
   } else {
@@ -95,14 +96,19 @@ __device__ __forceinline__ Raw8<E> fetch8(const E* p, const Span& g) {
   return r;
 }
 
-template <typename E>
-__device__ __forceinline__ void unpack8(const Raw8<E>& r, float (&v)[8]) {
+// Its values, zero where there is no element.
+template <typename E, int L>
+__device__ __forceinline__ void unpack8(const Raw8<E>& r, const Span& g, float (&v)[8]) {
   const typename Pack2<E>::type* h = reinterpret_cast<const typename Pack2<E>::type*>(&r);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const float2 f = Pack2<E>::up(h[j]);
     v[2 * j] = f.x;
     v[2 * j + 1] = f.y;
+  }
+  if (L == kTogether && !g.whole()) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j >= g.lo && j < g.hi ? v[j] : 0.f;
   }
 }
 
@@ -204,7 +210,8 @@ struct DropoutParams {
   void* out;
   int64_t x_stride, residual_stride, out_stride;
   int64_t rows, cols;
-  int lead;  // of row 0
+  int lead;     // of row 0
+  bool spaced;  // every tensor's rows are at least eight elements apart
   DropParams drop;
 };
 
@@ -219,6 +226,7 @@ struct NormForwardParams {
   int64_t rows;
   int32_t cols;
   int lead;
+  bool spaced;
   float eps;
   DropParams drop;
 };
@@ -236,6 +244,7 @@ struct NormBackwardParams {
   int64_t rows;
   int32_t cols;
   int lead;
+  bool spaced;
   DropParams drop;
 };
 
@@ -283,7 +292,7 @@ cudaError_t launch_dropout(const DropoutParams& p, int dtype, Layout layout, cud
 
 constexpr int kSMs = 152;  // the sizes of grids are rules on it, so that results do not depend on a query
 constexpr int kNormMaxCols = 16384;
-int norm_backward_ctas(int64_t rows, int cols);
+int norm_backward_most_ctas(int64_t rows, int cols);
 cudaError_t launch_norm_forward(const NormForwardParams& p, int dtype, Layout layout, cudaStream_t s);
 cudaError_t launch_norm_backward(const NormBackwardParams& p, float* dweight, int dtype, Layout layout, cudaStream_t s);
 

@@ -47,19 +47,20 @@ k_dropout(const __grid_constant__ DropoutParams p, int64_t groups, Divisor by_gr
       part[u] = span<L>(g - row[u] * groups, lead, p.cols);
       if (g >= total) part[u].hi = part[u].lo = 0;
       if (!part[u].some()) continue;
-      x[u] = fetch8<E, L>(static_cast<const E*>(p.x) + row[u] * p.x_stride + col[u], part[u]);
+      const bool inner = ROWS > 0 && p.spaced && row[u] > 0 && row[u] + 1 < p.rows;
+      x[u] = fetch8<E, L>(static_cast<const E*>(p.x) + row[u] * p.x_stride + col[u], part[u], inner);
       if (RESIDUAL)
-        res[u] = fetch8<E, L>(static_cast<const E*>(p.residual) + row[u] * p.residual_stride + col[u], part[u]);
+        res[u] = fetch8<E, L>(static_cast<const E*>(p.residual) + row[u] * p.residual_stride + col[u], part[u], inner);
     }
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       if (!part[u].some()) continue;
       float v[8];
-      unpack8(x[u], v);
+      unpack8<E, L>(x[u], part[u], v);
       drop8<L == kEven>(v, row[u] * p.cols + col[u], p.drop);
       if (RESIDUAL) {
         float w[8];
-        unpack8(res[u], w);
+        unpack8<E, L>(res[u], part[u], w);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] += w[j];
       }
