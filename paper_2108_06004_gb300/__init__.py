@@ -10,6 +10,7 @@ is no fallback.  A non-OK status raises ``GsError`` with the library's message.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libgs_sketch.so")
@@ -647,8 +648,11 @@ def gs_recurrence_workspace_size(B: int, T: int, D: int) -> int:
     return out.value
 
 
+_states_size = functools.lru_cache(maxsize=256)(gs_recurrence_states_size)   # a function of the sizes alone
+
+
 def _states_fit(func: str, states, B: int, T: int, D: int) -> None:
-    if states.numel() * states.element_size() < gs_recurrence_states_size(B, T, D) or not states.is_contiguous():
+    if states.numel() * states.element_size() < _states_size(B, T, D) or not states.is_contiguous():
         _refuse(func, "states must be contiguous and hold gs_recurrence_states_size(B, T, D) bytes")
 
 

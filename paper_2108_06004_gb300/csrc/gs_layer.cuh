@@ -306,7 +306,7 @@ struct RecurrenceShape {
   int32_t groups;    // CTAs side by side over the channels
   unsigned grid;
 };
-RecurrenceShape recurrence_shape(int64_t B, int64_t T, int64_t D, int run);
+RecurrenceShape recurrence_shape(int64_t B, int64_t T, int64_t D, int run, bool fp32);
 int64_t recurrence_states(int64_t T);  // states kept of a row and channel
 int64_t recurrence_partials(int64_t B, int64_t T, int64_t D);
 // How the tensors can be moved: by tiles (16, every row starts at a multiple of 16 bytes), by copies of

@@ -106,22 +106,26 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
     // the run's tokens as a_t and b_t, and their composition
     float2 a[kLen], b[kLen];
     Run run = identity();
+    // SOME: there may be masked tokens and resets.  Runs of whole chunks without a reset, nearly all
+    // of them, do without the selections.
     auto gates = [&](auto some, auto in_series) {
+      constexpr bool SOME = decltype(some)::value;
 #pragma unroll
       for (int k = 0; k < kLen; ++k) {
-        const bool cut = RESET && (resets >> k & 1u);
+        const bool cut = RESET && SOME && (resets >> k & 1u);
         float2 K;
         gate_forward<decltype(in_series)::value>(capped(tile[1].at(w, k)), capped(tile[2].at(w, k)), rate, cut, a[k], K);
         b[k] = mul(K, widen(tile[0].at(w, k)));
-        if (decltype(some)::value && t0 + k >= w.len) {  // past the end of the row: the state stays
+        if (SOME && t0 + k >= w.len) {  // past the end of the row: the state stays
           a[k] = two(1.f);
           b[k] = two(0.f);
         }
         run.a = mul(run.a, a[k]);
-        run.b = RESET ? apply(Run{a[k], b[k]}, cut, run.b) : fma(a[k], run.b, b[k]);
+        run.b = RESET && SOME ? apply(Run{a[k], b[k]}, cut, run.b) : fma(a[k], run.b, b[k]);
       }
     };
-    if (!full)
+    const bool plain = full && !(RESET && __any_sync(0xFFFFFFFFu, resets != 0));
+    if (!plain)
       gates(std::true_type(), std::false_type());
     else if (series)
       gates(std::false_type(), std::true_type());
@@ -162,19 +166,18 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
     }
     if (p.states && t0 % kStateEvery == 0 && t0 / kStateEvery < kept)
       store_f32(p.states + (w.b * kept + t0 / kStateEvery) * p.D + w.d, w.n, h);
-    auto next = [&](int k) { h = RESET ? apply(Run{a[k], b[k]}, resets >> k & 1u, h) : fma(a[k], h, b[k]); };
     E* out = y + t0 * p.y.token;
-    if (full && PAIR && w.n == 2) {
+    if (plain && PAIR && w.n == 2) {
 #pragma unroll
       for (int k = 0; k < kLen; ++k) {
-        next(k);
+        h = fma(a[k], h, b[k]);
         *reinterpret_cast<Raw*>(out) = Pack2<E>::down(h);
         out += p.y.token;
       }
     } else {
 #pragma unroll
       for (int k = 0; k < kLen; ++k) {
-        next(k);
+        h = RESET ? apply(Run{a[k], b[k]}, resets >> k & 1u, h) : fma(a[k], h, b[k]);
         if (t0 + k < p.T) store2<E, PAIR>(out, w.n, t0 + k < w.len ? h : two(0.f));
         out += p.y.token;
       }
@@ -249,27 +252,31 @@ __global__ void __launch_bounds__(128) k_recurrence_step(const __grid_constant__
 int64_t recurrence_states(int64_t T) { return (T + kStateEvery - 1) / kStateEvery; }
 
 // How a pass of `run` tokens a thread is cut: the channels of a CTA, and the CTAs of a cluster that
-// share a row's time.  An SM holds four CTAs.  64 channels a CTA where that makes three for each
+// share a row's time.  An SM holds four CTAs, three with fp32.  64 channels a CTA where that makes three for each
 // SM; fewer columns are cut to 32 channels (twice the CTAs, with twice the tokens each: forward and
 // backward of 8x2048x2048 bf16 take 56 and 96 us against 56 and 109 us with 64, but 64x512x1024,
 // which has enough columns, 56 and 104 against 53 and 91 us), and then share time in clusters until
 // there are three CTAs for each SM or no chunks left to deal.  A cluster meets at every step, so it comes last:
-// 8x2048x2048 with 64 channels and clusters of two takes 58 and 134 us.  The cut goes by sizes alone,
-// so that results do not depend on alignment.
-RecurrenceShape recurrence_shape(int64_t B, int64_t T, int64_t D, int run) {
+// 8x2048x2048 with 64 channels and clusters of two takes 58 and 134 us.  More CTAs than stay
+// resident are no use (fp32 4x2048x2048: 256 CTAs 48 and 86 us, 512 in clusters of two 57 and
+// 103 us).  The cut goes by sizes and type alone, so that results do not depend on alignment.
+RecurrenceShape recurrence_shape(int64_t B, int64_t T, int64_t D, int run, bool fp32) {
   constexpr int64_t kEnough = 3 * kSMs;
+  const int64_t resident = (fp32 ? 3 : 4) * kSMs;
   RecurrenceShape c = {};
   c.channels = B * ((D + 63) / 64) < kEnough ? 32 : 64;
   c.groups = (int32_t)((D + c.channels - 1) / c.channels);
   const int64_t columns = B * c.groups, chunk = kThreads / (c.channels / 2) * run;
   c.cluster = 1;
-  while (c.cluster < kMaxCluster && columns * c.cluster < kEnough && 2 * c.cluster * chunk <= T) c.cluster *= 2;
+  while (c.cluster < kMaxCluster && columns * c.cluster < kEnough && columns * c.cluster * 2 <= resident &&
+         2 * c.cluster * chunk <= T)
+    c.cluster *= 2;
   c.grid = (unsigned)(columns * c.cluster);
   return c;
 }
 
 cudaError_t launch_recurrence_forward(RecurrenceParams& p, int dtype, int unit, cudaStream_t s) {
-  const RecurrenceShape shape = recurrence_shape(p.B, p.T, p.D, kLen);
+  const RecurrenceShape shape = recurrence_shape(p.B, p.T, p.D, kLen, dtype == GS_F32);
   if (unit == 16) {
     const int tokens = kThreads / (shape.channels / 2) * kLen;
     if (!describe(p.maps[kMapX], p.x, p, dtype, shape.channels, tokens) ||

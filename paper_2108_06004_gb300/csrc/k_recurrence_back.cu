@@ -108,10 +108,13 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
     auto& tile = sh.in[turn & 1];
     float2 a[kLen], sr[kLen], K[kLen], U[kLen], Q[kLen];
     Run run = identity();
+    // SOME: there may be masked tokens and resets.  Runs of whole chunks without a reset, nearly all
+    // of them, do without the selections.
     auto gates = [&](auto some, auto in_series) {
+      constexpr bool SOME = decltype(some)::value;
 #pragma unroll
       for (int k = 0; k < kLen; ++k) {
-        const bool cut = RESET && (resets >> k & 1u);
+        const bool cut = RESET && SOME && (resets >> k & 1u);
         const Gate g = gate_backward<decltype(in_series)::value>(capped(tile[1].at(w, k)), capped(tile[2].at(w, k)), rate, cut);
         a[k] = g.a;
         sr[k] = g.sr;
@@ -119,15 +122,16 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
         float2 b = mul(g.K, widen(tile[0].at(w, k)));
         U[k] = mul(b, g.off);
         Q[k] = mul(b, mul(g.a, g.inv_X));
-        if (decltype(some)::value && t0 + k >= w.len) {  // past the end of the row: the state and the flow stay
+        if (SOME && t0 + k >= w.len) {  // past the end of the row: the state and the flow stay
           a[k] = two(1.f);
           K[k] = b = two(0.f);
         }
         run.a = mul(run.a, a[k]);
-        run.b = RESET ? apply(Run{a[k], b}, cut, run.b) : fma(a[k], run.b, b);
+        run.b = RESET && SOME ? apply(Run{a[k], b}, cut, run.b) : fma(a[k], run.b, b);
       }
     };
-    if (!full)
+    const bool plain = full && !(RESET && __any_sync(0xFFFFFFFFu, resets != 0));
+    if (!plain)
       gates(std::true_type(), std::false_type());
     else if (series)
       gates(std::false_type(), std::true_type());
@@ -140,10 +144,10 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
         float2 d = widen(tile[3].at(w, k));
         if (decltype(some)::value && t0 + k >= w.len) d = two(0.f);
         const float2 f = mul(a[k], add(back, d));
-        back = RESET ? choose(resets >> k & 1u, two(0.f), f) : f;
+        back = RESET && decltype(some)::value ? choose(resets >> k & 1u, two(0.f), f) : f;
       }
     };
-    if (full)
+    if (plain)
       flows(std::false_type());
     else
       flows(std::true_type());
@@ -190,15 +194,21 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
         flow = apply(back_run(k), RESET && sh.cut[k] != 0, flow);
       }
     }
+    auto states = [&](auto some) {
 #pragma unroll
-    for (int k = 0; k < kLen; ++k) {
-      Q[k] = fma(h, sr[k], make_float2(-Q[k].x, -Q[k].y));
-      const float2 b = mul(K[k], widen(tile[0].at(w, k)));
-      h = RESET ? apply(Run{a[k], b}, resets >> k & 1u, h) : fma(a[k], h, b);
-    }
+      for (int k = 0; k < kLen; ++k) {
+        Q[k] = fma(h, sr[k], make_float2(-Q[k].x, -Q[k].y));
+        const float2 b = mul(K[k], widen(tile[0].at(w, k)));
+        h = RESET && decltype(some)::value ? apply(Run{a[k], b}, resets >> k & 1u, h) : fma(a[k], h, b);
+      }
+    };
+    if (plain)
+      states(std::false_type());
+    else
+      states(std::true_type());
     float2 part = two(0.f);
-    auto token = [&](int k, float2& ox, float2& orr, float2& oi) {
-      const bool cut = RESET && (resets >> k & 1u);
+    auto token = [&](bool some, int k, float2& ox, float2& orr, float2& oi) {
+      const bool cut = RESET && some && (resets >> k & 1u);
       const float2 g = add(f, widen(tile[3].at(w, k)));
       f = choose(cut, two(0.f), mul(a[k], g));
       const float2 m = choose(cut, two(0.f), mul(f, Q[k]));
@@ -212,13 +222,13 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
 #pragma unroll
         for (int k = kLen - 1; k >= 0; --k) {
           float2 ox = two(0.f), orr = two(0.f), oi = two(0.f);
-          if (!decltype(some)::value || t0 + k < w.len) token(k, ox, orr, oi);
+          if (!decltype(some)::value || t0 + k < w.len) token(decltype(some)::value, k, ox, orr, oi);
           sh.out[0].at(w, k) = Pack2<E>::down(ox);
           sh.out[1].at(w, k) = Pack2<E>::down(orr);
           sh.out[2].at(w, k) = Pack2<E>::down(oi);
         }
       };
-      if (full)
+      if (plain)
         results(std::false_type());
       else
         results(std::true_type());
@@ -235,7 +245,7 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
 #pragma unroll
         for (int k = kLen - 1; k >= 0; --k) {
           float2 ox = two(0.f), orr = two(0.f), oi = two(0.f);
-          if (!decltype(some)::value || t0 + k < w.len) token(k, ox, orr, oi);
+          if (!decltype(some)::value || t0 + k < w.len) token(decltype(some)::value, k, ox, orr, oi);
           if (!decltype(some)::value || t0 + k < p.T) {
             store2<E, PAIR>(out_x, w.n, ox);
             store2<E, PAIR>(out_r, w.n, orr);
@@ -246,7 +256,7 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
           out_i -= p.di.token;
         }
       };
-      if (full)
+      if (plain)
         results(std::false_type());
       else
         results(std::true_type());
@@ -300,10 +310,13 @@ cudaError_t run_backward(RecurrenceParams& p, const RecurrenceShape& shape, cuda
 }  // namespace
 
 // Rows of the workspace: one for each row of the batch and CTA of a cluster.
-int64_t recurrence_partials(int64_t B, int64_t T, int64_t D) { return B * recurrence_shape(B, T, D, kLen).cluster; }
+int64_t recurrence_partials(int64_t B, int64_t T, int64_t D) {
+  const int a = recurrence_shape(B, T, D, kLen, true).cluster, b = recurrence_shape(B, T, D, kLen, false).cluster;
+  return B * (a > b ? a : b);
+}
 
 cudaError_t launch_recurrence_backward(RecurrenceParams& p, float* ddecay, int dtype, int unit, cudaStream_t s) {
-  const RecurrenceShape shape = recurrence_shape(p.B, p.T, p.D, kLen);
+  const RecurrenceShape shape = recurrence_shape(p.B, p.T, p.D, kLen, dtype == GS_F32);
   if (unit == 16 && shape.grid > 0) {
     const int tokens = kThreads / (shape.channels / 2) * kLen;
     const Seq<const void*>* in[4] = {&p.x, &p.r, &p.i, &p.dy};
