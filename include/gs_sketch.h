@@ -30,8 +30,10 @@
  *     the vectorised path (results are identical either way).
  *   - Sizes: 1 <= r <= GS_MAX_ROWS, 1 <= c <= GS_MAX_COLS, 1 <= d <= GS_MAX_DIM,
  *     1 <= k <= d, 1 <= P <= GS_MAX_WORKERS.  Vector values must be finite.
- *   - No call waits on the device for a flag; nothing spins (CTAs of a cluster meet at the
- *     hardware's cluster barrier).  Kernels launch with
+ *   - No call waits on the device for a flag in memory; nothing spins on one.  (The kernels of
+ *     gs_recurrence_forward and gs_recurrence_backward wait on mbarriers in their own shared
+ *     memory for copies and for messages within their cluster.  Each wait is bounded; one that
+ *     ran out would turn the state, and with it the results, into NaN.)  Kernels launch with
  *     programmatic stream serialization and wait in hardware for the grid before them.
  */
 #ifndef GS_SKETCH_H
@@ -428,9 +430,10 @@ gs_status gs_plan_destroy(gs_plan* plan);
  *   - A matrix of rows x cols has adjacent columns; row k starts `stride` elements after row
  *     k - 1.  A sequence tensor [B][T][D] has adjacent channels and two strides (gs_seq).
  *     Strides are in elements, any non-negative value for an input (0 repeats a row); rows of
- *     an output must not overlap.
- *   - Data is aligned to its element; 16-byte alignment of every row (base and strides) selects
- *     the vectorised path, with the same results.
+ *     an output must not overlap one another, nor an input unless a call says so.
+ *   - Data is aligned to its element.  Tensors whose rows all start at multiples of 16 bytes are
+ *     the fastest; contiguous ones of any width come next.  Alignment does not change results,
+ *     but for the order of additions in the norm's sums.
  *   - Sizes may be zero where a loop over them may be empty (rows, cols, B, T, D); such a call
  *     does what is left of its work.  Limits: rows * cols and B * T * D up to 2^40, rows and T
  *     below 2^31.
@@ -498,9 +501,9 @@ typedef struct {
  *   h_t = a_t * h_{t-1} + sqrt(1 - a_t^2) * s(i_t) * x_t,   y_t = h_t,   h_{-1} = h0.
  * h0 (fp32[B][D], NULL for zeros).  reset (uint8[B][T], nullable): where it is not zero a new
  * document begins: a_t is 0, nothing before it (not even an infinity) is seen.  lengths
- * (int32[B], nullable; taken to [0, T]): tokens from a row's length on are not read, their y is
+ * (int32[B], nullable; taken to [0, T]): tokens from a row's length on have no influence, their y is
  * zero and the state stays.  h_last (fp32[B][D], nullable): the state after the last token, h0
- * for a row of length zero; it may be h0.  states (nullable): gs_recurrence_states_size bytes,
+ * for a row of length zero; it may be h0 itself.  states (nullable): gs_recurrence_states_size bytes,
  * 256-byte aligned, filled for the backward pass (the fp32 state at fixed intervals).
  * c > 0 and finite; decay must be finite.  The gs_seq are read during the call. */
 gs_status gs_recurrence_states_size(int64_t B, int64_t T, int64_t D, size_t* bytes);
@@ -514,8 +517,8 @@ gs_status gs_recurrence_forward(const gs_seq* x, const gs_seq* r, const gs_seq* 
  *   g_t = dy_t + a_{t+1} g_{t+1} (dh_last past the last token),
  *   dlog a_t = g_t (a_t h_{t-1} - s(i_t) x_t a_t^2 / sqrt(1 - a_t^2))   (0 at a reset),
  *   dx, di, dr by the chain rule, ddecay (fp32[D], overwritten) summed over all tokens,
- *   dh0 (fp32[B][D], nullable) = a_0 g_0.
- * Masked tokens get zeros; dy is not read there.  workspace must hold
+ *   dh0 (fp32[B][D], nullable) = a_0 g_0; it may be dh_last itself.
+ * Masked tokens get zeros; dy has no influence there.  workspace must hold
  * gs_recurrence_workspace_size bytes, 256-byte aligned. */
 gs_status gs_recurrence_workspace_size(int64_t B, int64_t T, int64_t D, size_t* bytes);
 gs_status gs_recurrence_backward(const gs_seq* dy, const float* dh_last, const gs_seq* x, const gs_seq* r,

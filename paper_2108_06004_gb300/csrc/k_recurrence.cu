@@ -189,8 +189,9 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
       const int64_t t = t0 + w.slot * kLen + k;
       if (t < p.T) store2<E, PAIR>(y + t * p.y.token, w.n, two(0.f));
     }
+  // no CTA leaves while another may still write to it, and all have read h0, which h_last may be
+  if (w.cluster > 1) cg::this_cluster().sync();
   if (p.h_last && w.rank == 0 && w.slot == 0) store_f32(p.h_last + w.b * p.D + w.d, w.n, state);
-  if (w.cluster > 1) cg::this_cluster().sync();  // no CTA leaves while another may still write to it
 }
 
 template <typename E, int CH, int UNIT, int STAGES, bool RESET>

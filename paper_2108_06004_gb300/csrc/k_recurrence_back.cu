@@ -273,9 +273,10 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
         store2<E, PAIR>(di + t * p.di.token, w.n, two(0.f));
       }
     }
-  if (w.cluster > 1) cg::this_cluster().sync();  // no CTA leaves while another may still write to it
-  if (OUT && threadIdx.x == 0) store_wait();     // nor while its tiles are being read
+  // no CTA leaves while another may still write to it, and all have read dh_last, which dh0 may be
+  if (w.cluster > 1) cg::this_cluster().sync();
   if (p.dh0 && w.rank == 0 && w.slot == 0) store_f32(p.dh0 + w.b * p.D + w.d, w.n, flow);
+  if (OUT && threadIdx.x == 0) store_wait();     // nor while its tiles are being read
   // the CTA's share of the decay's gradient, its runs in order
   __syncthreads();
   sh.back[w.slot][w.pair] = sum;
