@@ -477,9 +477,8 @@ def _dtype(func: str, t) -> int:
     return code
 
 
-def _expect(func: str, name: str, t, shape, dtype, device) -> None:
-    if t.shape == shape and t.dtype == dtype and t.device == device:
-        return
+def _unlike(func: str, name: str, t, shape, dtype, device):
+    """Refuses a tensor that is not of this shape and type on this device."""
     if t.shape != shape:
         _refuse(func, f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if t.dtype != dtype:
@@ -501,7 +500,8 @@ def _dense(func: str, name: str, t, shape, dtype, device):
     """Address of a contiguous tensor, or None for an absent one."""
     if t is None:
         return None
-    _expect(func, name, t, shape, dtype, device)
+    if t.shape != shape or t.dtype is not dtype or t.device != device:
+        _unlike(func, name, t, shape, dtype, device)
     if not t.is_contiguous():
         _refuse(func, f"{name} must be contiguous")
     return t.data_ptr()
@@ -512,7 +512,8 @@ def _matrix(func: str, name: str, t, shape, dtype, device):
     walked with one stride; (None, 0) for an absent one."""
     if t is None:
         return None, 0
-    _expect(func, name, t, shape, dtype, device)
+    if t.shape != shape or t.dtype is not dtype or t.device != device:
+        _unlike(func, name, t, shape, dtype, device)
     if t.is_contiguous():
         return t.data_ptr(), shape[-1]
     stride = t.stride()
@@ -612,7 +613,8 @@ def gs_dropout_add_norm_backward(dz, dy, y, weight, rstd, dx, dresidual, dweight
 
 
 def _seq(func: str, name: str, t, shape, dtype, device):
-    _expect(func, name, t, shape, dtype, device)
+    if t.shape != shape or t.dtype is not dtype or t.device != device:
+        _unlike(func, name, t, shape, dtype, device)
     b, s, d = t.stride()
     if d != 1 and shape[2] > 1:
         _refuse(func, f"{name}: the channels must be adjacent")
