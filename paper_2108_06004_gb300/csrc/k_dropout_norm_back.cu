@@ -4,8 +4,11 @@
 //   n = y rstd,  u = dz w,  dt = rstd (u - n mean(u n)) + dy
 //   dresidual = dt,  dx = mask dt scale,  dw = sum over rows of dz n
 //
-// Every tensor is read and written once.  A CTA takes rows in turn; dw is summed by each thread over
-// the rows of its CTA, then over the CTAs by a last kernel, in a fixed order.
+// Every tensor is read and written once.  A CTA takes rows in turn, the next one's loads under way while
+// it works on one; dw is summed by each thread over the rows of its CTA, then over the CTAs by a
+// last kernel, in a fixed order.  Bound by memory: 32768x4096 takes 205 us in bf16 (97 % of the copy
+// rate; 511 us when a row's loads waited for the row before), 65536x1024 105 us (95 %), fp32 16384x4096
+// 206 us (96 %); 16384x4097, whose rows start anywhere, 211 us (47 %).
 #include "dropout_norm.cuh"
 
 namespace gs {

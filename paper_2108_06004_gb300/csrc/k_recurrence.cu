@@ -1,19 +1,23 @@
-// Gated linear recurrence over time, forward and backward, and its single-token step.
+// Forward pass of the gated linear recurrence over time, and its single-token step.
 //
 //   log a_t = -c softplus(lambda) sigmoid(r_t),   v_t = 1 - a_t^2,
 //   h_t = a_t h_{t-1} + sqrt(v_t) sigmoid(i_t) x_t,   y_t = h_t      (at a reset a_t = 0)
 //
 // A run of tokens acts on the state as h -> A h + B with A the product of its a_t, and such maps
-// compose, so time is cut three times: a thread owns kLen tokens of two channels, the kSlots
-// warps of a CTA own adjacent runs (a chunk), and where the rows and channels alone do not fill
-// the device a cluster of CTAs owns adjacent chunks.  Each thread first works out (A, B) of its
-// run, the warps exchange them in shared memory and the CTAs in distributed shared memory behind
-// the hardware's cluster barrier, and then the run is walked again from its true starting state.
-// Every tensor is read from and written to memory once, and the order of all operations is fixed.
+// compose, so time is cut three times: a thread owns kLen tokens of two channels, a CTA owns adjacent
+// runs (a chunk), and where the rows and channels alone do not fill the device a cluster of CTAs
+// owns adjacent chunks.  Each thread works out (A, B) of its run; the runs' maps are exchanged in
+// shared memory and the chunks' in distributed shared memory; then the run is walked again from
+// its true starting state.  Every tensor is read from and written to memory once, nothing waits for
+// another cluster, and the order of all operations is fixed by the sizes.  For the backward pass the
+// state is kept in fp32 every kStateEvery tokens.
 //
-// The backward pass walks time from the end: g_t = dy_t + a_{t+1} g_{t+1} is the same kind of map.
-// It needs h_{t-1} in full precision; it recomputes it from the state at the start of each chunk,
-// which the forward pass leaves in fp32 (4 bytes for kChunk tokens) rather than from y.
+// It has to move 4 elements a token and channel.  bf16 64x512x1024 takes 49 us (81 % of the copy rate),
+// 16x2048x2048 100 us (80 %), 8x2048x2048 55 us (72 %: 512 CTAs, four on some SMs and three on others),
+// 1x65536x1024 131 us (60 %: the same, and a meeting of 16 CTAs at every step); fp32 32x1024x1024
+// 86 us (92 %).  What bounds it in bf16 is the issue of about 61 instructions a token and pair of
+// channels by 16 warps an SM (2.2 a cycle), not their kind: the busiest pipe is at 30 %.  Runs of 16 tokens
+// and 128 registers do better than runs of 8 and 24 warps (1x65536x1024: 226 us), which meet twice as often.
 #include "recurrence.cuh"
 
 namespace gs {
@@ -84,7 +88,7 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
     __syncthreads();
   bool connected = true;  // no wait has run out
   const float2 rate = decay_rate(load_f32(p.decay + w.d, w.n), p.c);
-  const bool series = __all_sync(0xFFFFFFFFu, rate.x <= kSeries && rate.y <= kSeries);
+  const bool series = series_serves(w, rate);
   float2 state = load_f32(p.h0 ? p.h0 + w.b * p.D + w.d : nullptr, w.n);
   uint8_t flag = RESET ? reset_flag<kLen>(p, w, chunk_token(0) + w.slot * kLen) : 0;
   for (int s = 0; s < steps; ++s) {

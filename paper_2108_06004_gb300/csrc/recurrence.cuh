@@ -120,8 +120,8 @@ __device__ __forceinline__ float2 rcp(float2 v) { return make_float2(rcp(v.x), r
 __device__ __forceinline__ float2 rsq(float2 v) { return make_float2(rsq(v.x), rsq(v.y)); }
 
 // a and K, from capped gate values.  The three roots and quotients of K are one reciprocal root;
-// with the cap its argument stays
-// below 2^120 (X is large only where sigmoid(r) is small, and 1 + p^2 then is about 1).  `cut`: a reset, a = 0 and K = sigmoid(i).
+// with the cap its argument stays below 2^120 (X is large only where sigmoid(r) is small, and 1 + p^2
+// then is about 1).  `cut`: a reset, a = 0 and K = sigmoid(i).
 template <bool SERIES>
 __device__ __forceinline__ void gate_forward(float2 r, float2 i, float2 rate, bool cut, float2& a, float2& K) {
   const float2 pr = half_exp(r), pi = half_exp(i);
@@ -228,6 +228,11 @@ __device__ __forceinline__ Place place(const RecurrenceParams& p) {
   return w;
 }
 
+// Whether the polynomial serves all channels of the warp, however open their gates are.
+__device__ __forceinline__ bool series_serves(const Place& w, float2 rate) {
+  return __all_sync(0xFFFFFFFFu, (w.n < 1 || rate.x <= kSeries) && (w.n < 2 || rate.y <= kSeries));
+}
+
 __device__ __forceinline__ int clamp_int(int64_t v, int most) { return v < 0 ? 0 : v < most ? (int)v : most; }
 
 // Resets among the LEN tokens of a run from t0 on, one bit each.  The first LEN lanes that work on
@@ -327,7 +332,7 @@ __device__ __forceinline__ void copy_tile(Tile<E, CH, LEN>& tile, const E* from,
   const int have = clamp_int(channels - u * PER, PER);
   auto to = [&](int j) { return tile.v + (row + j * R) * CH + u * PER; };
   if constexpr (UNIT == 2) {
-    constexpr int BATCH = N < 16 ? N : 16;  // 8: 118 us, 16: 82, 32: 84 (forward 32x512x1023 bf16)
+    constexpr int BATCH = N < 16 ? N : 16;  // forward 32x512x1023 bf16: 8 118 us, 16 82, 32 84
 #pragma unroll
     for (int j0 = 0; j0 < N; j0 += BATCH) {
       E v[BATCH];
