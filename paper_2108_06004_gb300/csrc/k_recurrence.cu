@@ -46,7 +46,7 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
   constexpr int kRuns = Shared::kRuns, kChunk = kRuns * kLen;
   extern __shared__ __align__(128) unsigned char raw[];
   Shared& sh = *reinterpret_cast<Shared*>(raw);
-  grid_begin();
+  begin_cluster((int)cg::this_cluster().num_blocks());
   const Place w = place<CH>(p);
   Table<CH>& table = *reinterpret_cast<Table<CH>*>(raw + sizeof(Shared));  // there with a cluster only
   const int64_t chunks = (w.len + kChunk - 1) / kChunk;
