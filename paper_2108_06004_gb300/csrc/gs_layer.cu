@@ -507,8 +507,8 @@ gs_status gs_recurrence_step(const void* x, int64_t x_stride, const void* r, int
   p.n_slots = n_slots;
   p.c = c;
   const uintptr_t two = 2 * item(dtype);
-  const bool pair = (x_stride | r_stride | i_stride | y_stride) % 2 == 0 && aligned(x, two) && aligned(r, two) &&
-                    aligned(i, two) && aligned(y, two);
+  const bool pair = D % 2 == 0 && (x_stride | r_stride | i_stride | y_stride | state_stride) % 2 == 0 && aligned(x, two) &&
+                    aligned(r, two) && aligned(i, two) && aligned(y, two) && aligned(state, 8);
   const cudaError_t e = gs::launch_recurrence_step(p, dtype, pair, as_stream(stream));
   return e == cudaSuccess ? GS_OK : gs::record_cuda_failure(e, "recurrence_step launch");
   GS_GUARD_END

@@ -220,35 +220,58 @@ cudaError_t run_forward(RecurrenceParams& p, const RecurrenceShape& shape, cudaS
   return p.reset ? run_forward<E, CH, UNIT, 1, true>(p, shape, s) : run_forward<E, CH, UNIT, 1, false>(p, shape, s);
 }
 
-// Two adjacent channels of one token, zero where they do not exist.
+// Two adjacent channels of one token, zero where they do not exist.  PAIR: both exist or neither.
 template <typename E, bool PAIR>
 __device__ __forceinline__ float2 load2(const E* p, int n) {
-  if (PAIR && n == 2) return widen(*reinterpret_cast<const typename Pack2<E>::type*>(p));
+  if (PAIR) return n > 0 ? widen(*reinterpret_cast<const typename Pack2<E>::type*>(p)) : two(0.f);
   return make_float2(n > 0 ? to_f32(p[0]) : 0.f, n > 1 ? to_f32(p[1]) : 0.f);
 }
 
+// One token of each of p.B rows.  A thread owns two channels of `rows` rows, so that a channel's rate is
+// worked out once for them, and loads kAhead rows at a time.  In a graph 1x1024 bf16 takes 1.8 us, all of
+// it latency, and 256x4096 6.3 us (9.5 us with one row a thread; 6.8 with four at a time, 7.3 with one and
+// 4864 CTAs; 2.3 us at the copy rate: ramp and latency).
+constexpr int kStepThreads = 128, kAhead = 2;
+
 template <typename E, bool PAIR>
-__global__ void __launch_bounds__(128) k_recurrence_step(const __grid_constant__ RecurrenceStepParams p) {
+__global__ void __launch_bounds__(kStepThreads)
+k_recurrence_step(const __grid_constant__ RecurrenceStepParams p, int64_t rows) {
   grid_begin();
-  const int64_t d = 2 * ((int64_t)blockIdx.x * 128 + threadIdx.x);
+  const int64_t d = 2 * ((int64_t)blockIdx.x * kStepThreads + threadIdx.x);
   const int n = (int)(p.D - d < 0 ? 0 : p.D - d < 2 ? p.D - d : 2);
   if (n == 0) return;
-  for (int64_t b = blockIdx.y; b < p.B; b += gridDim.y) {
-    const int64_t slot = p.slots ? p.slots[b] : b;
-    float2 h = make_float2(0.f, 0.f);
-    if (slot >= 0 && slot < p.n_slots) {
-      const float2 lam = load_f32(p.decay + d, n);
-      const float2 xv = load2<E, PAIR>(static_cast<const E*>(p.x) + b * p.x_stride + d, n);
-      const float2 rv = load2<E, PAIR>(static_cast<const E*>(p.r) + b * p.r_stride + d, n);
-      const float2 iv = load2<E, PAIR>(static_cast<const E*>(p.i) + b * p.i_stride + d, n);
-      float* state = p.state + slot * p.state_stride + d;
-      h = load_f32(state, n);
-      float2 a, K;
-      gate_forward<false>(capped(rv), capped(iv), decay_rate(lam, p.c), false, a, K);
-      h = fma(a, h, mul(K, xv));
-      store_f32(state, n, h);
+  const float2 lam = load_f32(p.decay + d, n);
+  const int64_t b0 = (int64_t)blockIdx.y * rows, b1 = b0 + rows < p.B ? b0 + rows : p.B;
+  float2 rate = two(0.f);
+  for (int64_t b = b0; b < b1; b += kAhead) {
+    // loads without a branch in between: a row past the end reads the last one, an idle one its own
+    int64_t slot[kAhead];
+    float2 x[kAhead], r[kAhead], i[kAhead], h[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int64_t row = b + k < b1 ? b + k : b1 - 1;
+      slot[k] = p.slots ? p.slots[row] : row;
+      x[k] = load2<E, PAIR>(static_cast<const E*>(p.x) + row * p.x_stride + d, n);
+      r[k] = load2<E, PAIR>(static_cast<const E*>(p.r) + row * p.r_stride + d, n);
+      i[k] = load2<E, PAIR>(static_cast<const E*>(p.i) + row * p.i_stride + d, n);
     }
-    store2<E, PAIR>(static_cast<E*>(p.y) + b * p.y_stride + d, n, h);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const bool live = slot[k] >= 0 && slot[k] < p.n_slots;
+      h[k] = load2<float, PAIR>(p.state + slot[k] * p.state_stride + d, live ? n : 0);
+    }
+    if (b == b0) rate = decay_rate(lam, p.c);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (b + k >= b1) break;
+      if (slot[k] >= 0 && slot[k] < p.n_slots) {
+        float2 a, K;
+        gate_forward<false>(capped(r[k]), capped(i[k]), rate, false, a, K);
+        h[k] = fma(a, h[k], mul(K, x[k]));
+        store2<float, PAIR>(p.state + slot[k] * p.state_stride + d, n, h[k]);
+      }
+      store2<E, PAIR>(static_cast<E*>(p.y) + (b + k) * p.y_stride + d, n, h[k]);
+    }
   }
 }
 
@@ -302,11 +325,15 @@ cudaError_t launch_recurrence_forward(RecurrenceParams& p, int dtype, int unit, 
 }
 
 cudaError_t launch_recurrence_step(const RecurrenceStepParams& p, int dtype, bool pair, cudaStream_t s) {
-  const dim3 grid((unsigned)((p.D + 255) / 256), (unsigned)(p.B < 65535 ? p.B : 65535));
+  const int64_t columns = (p.D + 2 * kStepThreads - 1) / (2 * kStepThreads);
+  // as many CTAs as stay resident, and no more than a grid's second dimension has
+  int64_t rows = (p.B * columns + 24 * kSMs - 1) / (24 * kSMs);
+  if (rows < (p.B + 65534) / 65535) rows = (p.B + 65534) / 65535;
+  const dim3 grid((unsigned)columns, (unsigned)((p.B + rows - 1) / rows));
   return with_type(dtype, [&](auto e) {
     using E = decltype(e);
-    return pair ? launch(k_recurrence_step<E, true>, grid, dim3(128), s, p)
-                : launch(k_recurrence_step<E, false>, grid, dim3(128), s, p);
+    return pair ? launch(k_recurrence_step<E, true>, grid, dim3(kStepThreads), s, p, rows)
+                : launch(k_recurrence_step<E, false>, grid, dim3(kStepThreads), s, p, rows);
   });
 }
 
