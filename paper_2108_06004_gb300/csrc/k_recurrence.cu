@@ -326,7 +326,7 @@ cudaError_t launch_recurrence_forward(RecurrenceParams& p, int dtype, int unit, 
 
 cudaError_t launch_recurrence_step(const RecurrenceStepParams& p, int dtype, bool pair, cudaStream_t s) {
   const int64_t columns = (p.D + 2 * kStepThreads - 1) / (2 * kStepThreads);
-  // as many CTAs as stay resident, and no more than a grid's second dimension has
+  // about as many CTAs as stay resident, and no more than a grid has rows
   int64_t rows = (p.B * columns + 24 * kSMs - 1) / (24 * kSMs);
   if (rows < (p.B + 65534) / 65535) rows = (p.B + 65534) / 65535;
   const dim3 grid((unsigned)columns, (unsigned)((p.B + rows - 1) / rows));
