@@ -13,7 +13,7 @@ template <int TPR>
 __device__ __forceinline__ float row_sum(float v, float* scratch) {
 #pragma unroll
   for (int o = TPR < 32 ? TPR / 2 : 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
-  if (TPR > 32) {
+  if constexpr (TPR > 32) {
     const int warp = threadIdx.x >> 5;
     if ((threadIdx.x & 31) == 0) scratch[warp] = v;
     __syncthreads();

@@ -149,7 +149,8 @@ gs_status dropout_impl(const void* x, int64_t x_stride, const void* residual, in
   }
   const std::initializer_list<Matrix> all = {{x, x_stride}, {residual, residual_stride}, {out, out_stride}};
   const gs::Layout layout = layout_of(all, q.rows, q.cols, dtype, &q.lead);
-  q.spaced = spaced(all);
+  // in place, what lies beside a row is being written while it is read
+  q.spaced = spaced(all) && out != x && out != residual;
   const cudaError_t e = gs::launch_dropout(q, dtype, layout, as_stream(stream));
   return e == cudaSuccess ? GS_OK : gs::record_cuda_failure(e, "dropout launch");
 }
@@ -295,7 +296,7 @@ gs_status gs_dropout_add_norm(const void* x, int64_t x_stride, const void* resid
   q.eps = eps;
   const std::initializer_list<Matrix> all = {{x, x_stride}, {residual, residual_stride}, {y, y_stride}, {z, z_stride}};
   gs::Layout layout = layout_of(all, rows, cols, dtype, &q.lead);
-  q.spaced = spaced(all);
+  q.spaced = spaced(all) && y != x && y != residual;
   if (!aligned(weight, 16)) layout = gs::kApart;
   const cudaError_t e = gs::launch_norm_forward(q, dtype, layout, as_stream(stream));
   return e == cudaSuccess ? GS_OK : gs::record_cuda_failure(e, "dropout_add_norm launch");

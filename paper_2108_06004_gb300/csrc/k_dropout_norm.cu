@@ -3,9 +3,9 @@
 //   y = residual + dropout(x),  rstd = (mean(y^2) + eps)^(-1/2),  z = y rstd w
 //
 // A row is held in the registers of its threads, one or two groups of eight elements each, so every
-// tensor is read and written once.  Bound by memory: 32768x4096 takes 164 us in bf16 (97 % of the copy
-// rate) and 304 us in fp32; 131072x64 13 us (76 %); 4096x1024 9.3 us (53 %: one and a third waves
-// of CTAs, whose rows pass from load to store once).  16384x4097, whose rows start anywhere, 144 us (55 %).
+// tensor is read and written once.  Bound by memory: 32768x4096 takes 158 us in bf16 and 302 us in fp32 (both at
+// the copy rate), 131072x64 13 us (76 %), 4096x1024 7.9 us (63 %: one wave of CTAs, whose rows pass
+// from load to store once).  16384x4097, whose rows start anywhere, 130 us (61 %).
 #include "dropout_norm.cuh"
 
 namespace gs {
@@ -13,8 +13,10 @@ namespace {
 
 using namespace norm;
 
+// Few enough registers that 1792 threads stay resident: 4096x1024 bf16 takes 7.9 us with seven CTAs
+// of 256 threads an SM, 9.4 us with the five that the compiler's own choice leaves room for.
 template <typename E, int TPR, int V, int L>
-__global__ void __launch_bounds__(kCtaThreads<TPR>)
+__global__ void __launch_bounds__(kCtaThreads<TPR>, 1792 / kCtaThreads<TPR>)
 k_norm_forward(const __grid_constant__ NormForwardParams p) {
   grid_begin();
   __shared__ float scratch[32];
