@@ -34,7 +34,8 @@
  *     gs_recurrence_forward and gs_recurrence_backward wait on mbarriers in their own shared
  *     memory for copies and for messages within their cluster.  Each wait is bounded; one that
  *     ran out would turn the state, and with it the results, into NaN.)  Kernels launch with
- *     programmatic stream serialization and wait in hardware for the grid before them.
+ *     programmatic stream serialization and wait in hardware for the grid before them; the
+ *     recurrence's clusters launch in plain stream order.
  */
 #ifndef GS_SKETCH_H
 #define GS_SKETCH_H
