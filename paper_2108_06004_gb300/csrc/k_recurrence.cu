@@ -97,7 +97,7 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
     const uint32_t resets = RESET ? reset_bits<CH, kLen>(flag) : 0;
     if (RESET) flag = reset_flag<kLen>(p, w, chunk_token(s + 1) + w.slot * kLen);
     if constexpr (TILES) {
-      connected = connected && barrier_wait(&sh.full[s % STAGES], s / STAGES);
+      connected = connected && barrier_wait<false>(&sh.full[s % STAGES], s / STAGES);
     } else {
       if (s + 1 < steps)
         copy_wait<STAGES - 1>();
@@ -153,7 +153,7 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
         extend(total, cut, as_run(sh.run[k][w.pair]), RESET && sh.cut[k] != 0);
       }
       send<CH, kRuns>(table, s & 1, w, total, RESET && cut);
-      connected = connected && barrier_wait(&table.arrived[s & 1], s >> 1);
+      connected = connected && barrier_wait<true>(&table.arrived[s & 1], s >> 1);
       if (!connected) state = two(nanf(""));
 #pragma unroll 4
       for (int k = 0; k < w.rank; ++k) state = apply_total<RESET>(table, s & 1, k, w, state);

@@ -104,7 +104,7 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
     float2 h = kept_at < kept ? load_f32(p.states + (w.b * kept + kept_at) * p.D + w.d, w.n) : two(0.f);
     const int turn = steps - 1 - s;
     if constexpr (TILES) {
-      connected = connected && barrier_wait(&sh.full[turn & 1], turn >> 1);
+      connected = connected && barrier_wait<false>(&sh.full[turn & 1], turn >> 1);
     } else {
       copy_wait<0>();
     }
@@ -184,7 +184,7 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
         extend(total, cut, back_run(k), RESET && sh.cut[k] != 0);
       }
       send<CH, kRuns>(table, turn & 1, w, total, RESET && cut);
-      connected = connected && barrier_wait(&table.arrived[turn & 1], turn >> 1);
+      connected = connected && barrier_wait<true>(&table.arrived[turn & 1], turn >> 1);
       if (!connected) flow = two(nanf(""));
 #pragma unroll 4
       for (int k = w.cluster - 1; k > w.rank; --k) flow = apply_total<RESET>(table, turn & 1, k, w, flow);

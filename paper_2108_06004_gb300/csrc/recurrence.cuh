@@ -277,15 +277,24 @@ __device__ __forceinline__ void barrier_expect(uint64_t* bar, uint32_t bytes) {
 }
 // Whether the barrier's `phase`-th phase has come to its end.  Every wait is bounded: one that runs
 // out, which nothing that these kernels do can cause, makes the caller give up all further waits
-// and turn its state into NaN.
+// and turn its state into NaN.  CLUSTER: other CTAs of the cluster write what the phase stands for, so
+// the wait has to acquire at their scope; for the CTA's own tiles its own is enough.
+template <bool CLUSTER>
 __device__ __forceinline__ bool barrier_wait(uint64_t* bar, int phase) {
   for (int tries = 0; tries < (1 << 20); ++tries) {
     uint32_t done;
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-        : "=r"(done)
-        : "r"(shared_address(bar)), "r"(phase & 1)
-        : "memory");
+    if (CLUSTER)
+      asm volatile(
+          "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+          : "=r"(done)
+          : "r"(shared_address(bar)), "r"(phase & 1)
+          : "memory");
+    else
+      asm volatile(
+          "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+          : "=r"(done)
+          : "r"(shared_address(bar)), "r"(phase & 1)
+          : "memory");
     if (done) return true;
   }
   return false;
