@@ -532,6 +532,21 @@ def _matrix(func: str, name: str, t, shape, dtype, device):
     return t.data_ptr(), shape[-1] if row is None else row
 
 
+def _room(func: str, name: str, t, device, size=None):
+    """(address, bytes) of a workspace: a contiguous tensor, of which `size` bytes may be used, or an
+    address with its size."""
+    if not hasattr(t, "data_ptr"):
+        return _ptr(t), size or 0
+    if t.device != device:
+        _refuse(func, f"{name} is on {t.device}, expected {device}")
+    if not t.is_contiguous():
+        _refuse(func, f"{name} must be contiguous")
+    have = t.numel() * t.element_size()
+    if size is not None and size > have:
+        _refuse(func, f"{name} holds {have} bytes, not {size}")
+    return t.data_ptr(), have if size is None else size
+
+
 def _rows_cols(func: str, t):
     if t.dim() < 1:
         _refuse(func, "a tensor of at least one dimension is expected")
@@ -606,10 +621,11 @@ def gs_dropout_add_norm_backward(dz, dy, y, weight, rstd, dx, dresidual, dweight
     yp, ys = _matrix(f, "y", y, shape, dtype, dev)
     xp, xs = _matrix(f, "dx", dx, shape, dtype, dev)
     rp, rs = _matrix(f, "dresidual", dresidual, shape, dtype, dev)
+    wp, wn = _room(f, "workspace", workspace, dev, workspace_bytes)
     _check(load_library().gs_dropout_add_norm_backward(
         gp, gstride, dp, ds, yp, ys, _dense(f, "weight", weight, (cols,), f32, dev),
         _dense(f, "rstd", rstd, shape[:-1], f32, dev), xp, xs, rp, rs, _dense(f, "dweight", dweight, (cols,), f32, dev),
-        rows, cols, code, p, seed, offset, _ptr(workspace), _nbytes(workspace, workspace_bytes), stream), f)
+        rows, cols, code, p, seed, offset, wp, wn, stream), f)
 
 
 def _seq(func: str, name: str, t, shape, dtype, device):
@@ -653,7 +669,9 @@ def gs_recurrence_workspace_size(B: int, T: int, D: int) -> int:
 _states_size = functools.lru_cache(maxsize=256)(gs_recurrence_states_size)   # a function of the sizes alone
 
 
-def _states_fit(func: str, states, B: int, T: int, D: int) -> None:
+def _states_fit(func: str, states, B: int, T: int, D: int, device=None) -> None:
+    if device is not None and states.device != device:
+        _refuse(func, f"states is on {states.device}, expected {device}")
     if states.numel() * states.element_size() < _states_size(B, T, D) or not states.is_contiguous():
         _refuse(func, "states must be contiguous and hold gs_recurrence_states_size(B, T, D) bytes")
 
@@ -668,7 +686,7 @@ def gs_recurrence_forward(x, r, i, decay, y, h0=None, reset=None, lengths=None, 
     stream = _launch_stream(f, x, stream)
     dtype, dev, f32 = x.dtype, x.device, _torch().float32
     if states is not None:
-        _states_fit(f, states, B, T, D)
+        _states_fit(f, states, B, T, D, dev)
     _check(load_library().gs_recurrence_forward(
         _seq(f, "x", x, shape, dtype, dev), _seq(f, "r", r, shape, dtype, dev), _seq(f, "i", i, shape, dtype, dev),
         _dense(f, "decay", decay, (D,), f32, dev), _dense(f, "h0", h0, (B, D), f32, dev),
@@ -685,7 +703,8 @@ def gs_recurrence_backward(dy, x, r, i, decay, states, dx, dr, di, ddecay, works
     shape = B, T, D = _sequence(f, x)
     stream = _launch_stream(f, x, stream)
     dtype, dev, f32 = x.dtype, x.device, _torch().float32
-    _states_fit(f, states, B, T, D)
+    _states_fit(f, states, B, T, D, dev)
+    wp, wn = _room(f, "workspace", workspace, dev, workspace_bytes)
     _check(load_library().gs_recurrence_backward(
         _seq(f, "dy", dy, shape, dtype, dev), _dense(f, "dh_last", dh_last, (B, D), f32, dev),
         _seq(f, "x", x, shape, dtype, dev), _seq(f, "r", r, shape, dtype, dev), _seq(f, "i", i, shape, dtype, dev),
@@ -693,7 +712,7 @@ def gs_recurrence_backward(dy, x, r, i, decay, states, dx, dr, di, ddecay, works
         _whole(f, "lengths", lengths, (B,), dev), _ptr(states), _seq(f, "dx", dx, shape, dtype, dev),
         _seq(f, "dr", dr, shape, dtype, dev), _seq(f, "di", di, shape, dtype, dev),
         _dense(f, "ddecay", ddecay, (D,), f32, dev), _dense(f, "dh0", dh0, (B, D), f32, dev), B, T, D, code, c,
-        _ptr(workspace), _nbytes(workspace, workspace_bytes), stream), f)
+        wp, wn, stream), f)
 
 
 def gs_recurrence_step(x, r, i, decay, state, y, slots=None, c: float = 8.0, stream=None) -> None:
