@@ -32,8 +32,9 @@
  *     1 <= k <= d, 1 <= P <= GS_MAX_WORKERS.  Vector values must be finite.
  *   - No call waits on the device for a flag in memory; nothing spins on one.  (The kernels of
  *     gs_recurrence_forward and gs_recurrence_backward wait on mbarriers in their own shared
- *     memory for copies and for messages within their cluster.  Each wait is bounded; one that
- *     ran out would turn the state, and with it the results, into NaN.)  Kernels launch with
+ *     memory for copies and for messages within their cluster.  Each wait is bounded, to about a
+ *     second.  One that ran out, which nothing in a call can cause, would turn into NaN every
+ *     result that has to do with what did not come; the call itself has returned by then.)  Kernels launch with
  *     programmatic stream serialization and wait in hardware for the grid before them; the
  *     recurrence's clusters launch in plain stream order.
  */
@@ -528,6 +529,11 @@ gs_status gs_recurrence_backward(const gs_seq* dy, const float* dh_last, const g
                                  const gs_seq* dr, const gs_seq* di, float* ddecay, float* dh0, int64_t B,
                                  int64_t T, int64_t D, int32_t dtype, float c, void* workspace,
                                  size_t workspace_bytes, gs_stream stream);
+
+/* For tests of what a wait that runs out does: the tries, 0 ... 2^20 (the default), of the waits for
+ * tiles and for messages in later calls of gs_recurrence_forward and gs_recurrence_backward by this host
+ * thread.  A try takes a microsecond at most. */
+gs_status gs_recurrence_wait_tries(int32_t tiles, int32_t messages);
 
 /* One token of each of B streams: the recurrence's next state, in place, and y = that state.
  * x, r, i, y are [B][D] matrices.  state: fp32, n_slots rows of state_stride elements; stream b

@@ -102,6 +102,7 @@ SIGNATURES = {
     "gs_recurrence_forward": [_SEQ, _SEQ, _SEQ, _vp, _vp, _vp, _vp, _SEQ, _vp, _vp, _i64, _i64, _i64, _i32, _f32, _vp],
     "gs_recurrence_backward": [_SEQ, _vp, _SEQ, _SEQ, _SEQ, _vp, _vp, _vp, _vp, _SEQ, _SEQ, _SEQ, _vp, _vp, _i64, _i64,
                                _i64, _i32, _f32, _vp, _sz, _vp],
+    "gs_recurrence_wait_tries": [_i32, _i32],
     "gs_recurrence_step": [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64, _vp, _vp, _i64, _i64, _i64, _i32,
                            _f32, _vp],
     "gs_insert_request_ceiling_window_size": [_vp, ctypes.POINTER(_sz)],
@@ -713,6 +714,11 @@ def gs_recurrence_backward(dy, x, r, i, decay, states, dx, dr, di, ddecay, works
         _seq(f, "dr", dr, shape, dtype, dev), _seq(f, "di", di, shape, dtype, dev),
         _dense(f, "ddecay", ddecay, (D,), f32, dev), _dense(f, "dh0", dh0, (B, D), f32, dev), B, T, D, code, c,
         wp, wn, stream), f)
+
+
+def gs_recurrence_wait_tries(tiles: int = 1 << 20, messages: int = 1 << 20) -> None:
+    """Tries of the sequence kernels' waits in later calls of this thread, for tests of waits that run out."""
+    _check(load_library().gs_recurrence_wait_tries(tiles, messages), "gs_recurrence_wait_tries")
 
 
 def gs_recurrence_step(x, r, i, decay, state, y, slots=None, c: float = 8.0, stream=None) -> None:

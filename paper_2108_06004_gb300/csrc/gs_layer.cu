@@ -236,6 +236,14 @@ size_t recurrence_ws_bytes(int64_t B, int64_t T, int64_t D) {
   return round256((size_t)gs::recurrence_partials(B, T, D) * (size_t)D * sizeof(float));
 }
 
+// Tries of the recurrence's waits in calls of this thread.
+thread_local int32_t tile_tries = gs::kMostTries, message_tries = gs::kMostTries;
+
+void set_tries(gs::RecurrenceParams& p) {
+  p.tile_tries = tile_tries;
+  p.message_tries = message_tries;
+}
+
 gs_status check_c(float c) {
   if (!(c > 0.f) || std::isinf(c)) return bad("c must be positive and finite");
   return GS_OK;
@@ -412,6 +420,7 @@ gs_status gs_recurrence_forward(const gs_seq* x, const gs_seq* r, const gs_seq* 
   p.T = T;
   p.D = D;
   p.c = c;
+  set_tries(p);
   const int unit = copy_unit({x, r, i}, {y}, B, T, D, dtype);
   const cudaError_t e = gs::launch_recurrence_forward(p, dtype, unit, as_stream(stream));
   return e == cudaSuccess ? GS_OK : gs::record_cuda_failure(e, "recurrence_forward launch");
@@ -463,10 +472,19 @@ gs_status gs_recurrence_backward(const gs_seq* dy, const float* dh_last, const g
   p.T = T;
   p.D = D;
   p.c = c;
+  set_tries(p);
   const int unit = copy_unit({x, r, i, dy}, {dx, dr, di}, B, T, D, dtype);
   const cudaError_t e = gs::launch_recurrence_backward(p, ddecay, dtype, unit, as_stream(stream));
   return e == cudaSuccess ? GS_OK : gs::record_cuda_failure(e, "recurrence_backward launch");
   GS_GUARD_END
+}
+
+gs_status gs_recurrence_wait_tries(int32_t tiles, int32_t messages) {
+  if (tiles < 0 || tiles > gs::kMostTries || messages < 0 || messages > gs::kMostTries)
+    return gs::record_failure(GS_ERR_INVALID_ARG, "tries must lie in [0, 2^20]");
+  tile_tries = tiles;
+  message_tries = messages;
+  return GS_OK;
 }
 
 gs_status gs_recurrence_step(const void* x, int64_t x_stride, const void* r, int64_t r_stride, const void* i,

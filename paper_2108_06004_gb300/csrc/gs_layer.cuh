@@ -271,7 +271,9 @@ struct RecurrenceParams {
   int64_t B, T, D;
   float c;
   int32_t groups;           // channel groups of a row
+  int32_t tile_tries, message_tries;  // of a wait, before it gives up
 };
+constexpr int32_t kMostTries = 1 << 20;
 enum { kMapX, kMapR, kMapI, kMapDy, kMapY, kMapDx = kMapY, kMapDr, kMapDi };
 
 struct RecurrenceStepParams {

@@ -58,12 +58,13 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
   const E* i = static_cast<const E*>(p.i.data) + w.b * p.i.batch + w.d0;
   E* y = static_cast<E*>(p.y.data) + w.b * p.y.batch + w.d;
   auto chunk_token = [&](int s) { return ((int64_t)s * w.cluster + w.rank) * kChunk; };
+  bool here = true, linked = true;  // no wait for tiles, for messages, has run out
   auto load = [&](int s) {
     if (s >= steps) return;
     const int64_t t0 = chunk_token(s);
     auto& in = sh.in[s % STAGES];
     if constexpr (TILES) {
-      if (threadIdx.x == 0) {
+      if (threadIdx.x == 0 && here) {
         uint64_t* bar = &sh.full[s % STAGES];
         barrier_expect(bar, 3 * sizeof(in[0]));
         for (int k = 0; k < 3; ++k) tile_load(&in[k], &p.maps[kMapX + k], (int)w.d0, (int)t0, (int)w.b, bar);
@@ -86,7 +87,6 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
     open_table(table);
   else
     __syncthreads();
-  bool connected = true;  // no wait has run out
   const float2 rate = decay_rate(load_f32(p.decay + w.d, w.n), p.c);
   const bool series = series_serves(w, rate);
   float2 state = load_f32(p.h0 ? p.h0 + w.b * p.D + w.d : nullptr, w.n);
@@ -94,10 +94,10 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
   for (int s = 0; s < steps; ++s) {
     const int64_t t0 = chunk_token(s) + w.slot * kLen;
     const bool full = chunk_token(s) + kChunk <= w.len;  // the chunk has no masked token
-    const uint32_t resets = RESET ? reset_bits<CH, kLen>(flag) : 0;
+    uint32_t resets = RESET ? reset_bits<CH, kLen>(flag) : 0;
     if (RESET) flag = reset_flag<kLen>(p, w, chunk_token(s + 1) + w.slot * kLen);
     if constexpr (TILES) {
-      connected = connected && barrier_wait<false>(&sh.full[s % STAGES], s / STAGES);
+      here = here && barrier_wait<false>(&sh.full[s % STAGES], s / STAGES, p.tile_tries);
     } else {
       if (s + 1 < steps)
         copy_wait<STAGES - 1>();
@@ -135,6 +135,10 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
       gates(std::false_type(), std::true_type());
     else
       gates(std::false_type(), std::false_type());
+    if (TILES && !here) {  // the run turns whatever state into NaN
+      run = Run{two(nanf("")), two(nanf(""))};
+      resets = 0;
+    }
     sh.run[w.slot][w.pair] = as_float4(run);
     if (RESET && w.pair == 0) sh.cut[w.slot] = resets;
     __syncthreads();
@@ -152,22 +156,27 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
         }
         extend(total, cut, as_run(sh.run[k][w.pair]), RESET && sh.cut[k] != 0);
       }
-      send<CH, kRuns>(table, s & 1, w, total, RESET && cut);
-      connected = connected && barrier_wait<true>(&table.arrived[s & 1], s >> 1);
-      if (!connected) state = two(nanf(""));
+      if (linked) {
+        send<CH, kRuns>(table, s & 1, w, total, RESET && cut);
+        linked = barrier_wait<true>(&table.arrived[s & 1], s >> 1, p.message_tries);
+      }
 #pragma unroll 4
       for (int k = 0; k < w.rank; ++k) state = apply_total<RESET>(table, s & 1, k, w, state);
       h = apply(before, RESET && before_cut, state);
 #pragma unroll 4
       for (int k = w.rank; k < w.cluster; ++k) state = apply_total<RESET>(table, s & 1, k, w, state);
+      if (!linked) {
+        state = two(nanf(""));
+        h = apply(before, RESET && before_cut, state);
+      }
     } else {
-      if (!connected) state = two(nanf(""));
 #pragma unroll
       for (int k = 0; k < kRuns; ++k) {
         if (k == w.slot) h = state;
         state = apply(as_run(sh.run[k][w.pair]), RESET && sh.cut[k] != 0, state);
       }
     }
+    if (TILES && !here) h = two(nanf(""));
     if (p.states && t0 % kStateEvery == 0 && t0 / kStateEvery < kept)
       store_f32(p.states + (w.b * kept + t0 / kStateEvery) * p.D + w.d, w.n, h);
     E* out = y + t0 * p.y.token;
@@ -195,6 +204,7 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
     }
   // no CTA leaves while another may still write to it, and all have read h0, which h_last may be
   if (w.cluster > 1) cg::this_cluster().sync();
+  if (!here || !linked) pause();
   if (p.h_last && w.rank == 0 && w.slot == 0) store_f32(p.h_last + w.b * p.D + w.d, w.n, state);
 }
 

@@ -60,12 +60,13 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
   E* dr = static_cast<E*>(p.dr.data) + w.b * p.dr.batch + w.d;
   E* di = static_cast<E*>(p.di.data) + w.b * p.di.batch + w.d;
   auto chunk_token = [&](int s) { return ((int64_t)s * w.cluster + w.rank) * kChunk; };
+  bool here = true, linked = true;  // no wait for tiles, for messages, has run out
   // step s is the turn-th from the end
   auto load = [&](int turn) {
     const int64_t t0 = chunk_token(steps - 1 - turn);
     auto& in = sh.in[turn & 1];
     if constexpr (TILES) {
-      if (threadIdx.x == 0) {
+      if (threadIdx.x == 0 && here) {
         uint64_t* bar = &sh.full[turn & 1];
         barrier_expect(bar, 4 * sizeof(in[0]));
         for (int k = 0; k < 4; ++k) tile_load(&in[k], &p.maps[kMapX + k], (int)w.d0, (int)t0, (int)w.b, bar);
@@ -89,7 +90,6 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
     open_table(table);
   else
     __syncthreads();
-  bool connected = true;  // no wait has run out
   const float2 rate = decay_rate(load_f32(p.decay + w.d, w.n), p.c);
   const bool series = series_serves(w, rate);
   float2 flow = load_f32(p.dh_last ? p.dh_last + w.b * p.D + w.d : nullptr, w.n);
@@ -98,13 +98,13 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
   for (int s = steps - 1; s >= 0; --s) {
     const int64_t t0 = chunk_token(s) + w.slot * kLen;
     const bool full = chunk_token(s) + kChunk <= w.len;  // the chunk has no masked token
-    const uint32_t resets = RESET ? reset_bits<CH, kLen>(flag) : 0;
+    uint32_t resets = RESET ? reset_bits<CH, kLen>(flag) : 0;
     if (RESET && s > 0) flag = reset_flag<kLen>(p, w, chunk_token(s - 1) + w.slot * kLen);
     const int64_t kept_at = chunk_token(s) / kStateEvery;
     float2 h = kept_at < kept ? load_f32(p.states + (w.b * kept + kept_at) * p.D + w.d, w.n) : two(0.f);
     const int turn = steps - 1 - s;
     if constexpr (TILES) {
-      connected = connected && barrier_wait<false>(&sh.full[turn & 1], turn >> 1);
+      here = here && barrier_wait<false>(&sh.full[turn & 1], turn >> 1, p.tile_tries);
     } else {
       copy_wait<0>();
     }
@@ -156,6 +156,11 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
       flows(std::false_type());
     else
       flows(std::true_type());
+    if (TILES && !here) {  // the run turns whatever state and flow into NaN
+      run = Run{two(nanf("")), two(nanf(""))};
+      back = two(nanf(""));
+      resets = 0;
+    }
     sh.run[w.slot][w.pair] = as_float4(run);
     sh.back[w.slot][w.pair] = back;
     if (RESET && w.pair == 0) sh.cut[w.slot] = resets;
@@ -183,22 +188,27 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
         }
         extend(total, cut, back_run(k), RESET && sh.cut[k] != 0);
       }
-      send<CH, kRuns>(table, turn & 1, w, total, RESET && cut);
-      connected = connected && barrier_wait<true>(&table.arrived[turn & 1], turn >> 1);
-      if (!connected) flow = two(nanf(""));
+      if (linked) {
+        send<CH, kRuns>(table, turn & 1, w, total, RESET && cut);
+        linked = barrier_wait<true>(&table.arrived[turn & 1], turn >> 1, p.message_tries);
+      }
 #pragma unroll 4
       for (int k = w.cluster - 1; k > w.rank; --k) flow = apply_total<RESET>(table, turn & 1, k, w, flow);
       f = apply(after, RESET && after_cut, flow);
 #pragma unroll 4
       for (int k = w.rank; k >= 0; --k) flow = apply_total<RESET>(table, turn & 1, k, w, flow);
+      if (!linked) {
+        flow = two(nanf(""));
+        f = apply(after, RESET && after_cut, flow);
+      }
     } else {
-      if (!connected) flow = two(nanf(""));
 #pragma unroll
       for (int k = kRuns - 1; k >= 0; --k) {
         if (k == w.slot) f = flow;
         flow = apply(back_run(k), RESET && sh.cut[k] != 0, flow);
       }
     }
+    if (TILES && !here) f = two(nanf(""));
     auto states = [&](auto some) {
 #pragma unroll
       for (int k = 0; k < kLen; ++k) {
@@ -280,6 +290,7 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
     }
   // no CTA leaves while another may still write to it, and all have read dh_last, which dh0 may be
   if (w.cluster > 1) cg::this_cluster().sync();
+  if (!here || !linked) pause();
   if (p.dh0 && w.rank == 0 && w.slot == 0) store_f32(p.dh0 + w.b * p.D + w.d, w.n, flow);
   if (OUT && threadIdx.x == 0) store_wait();     // nor while its tiles are being read
   // the CTA's share of the decay's gradient, its runs in order

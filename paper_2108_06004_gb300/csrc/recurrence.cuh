@@ -275,23 +275,26 @@ __device__ __forceinline__ void barrier_init(uint64_t* bar) {
 __device__ __forceinline__ void barrier_expect(uint64_t* bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(shared_address(bar)), "r"(bytes) : "memory");
 }
-// Whether the barrier's `phase`-th phase has come to its end.  Every wait is bounded: one that runs
-// out, which nothing that these kernels do can cause, makes the caller give up all further waits
-// and turn its state into NaN.  CLUSTER: other CTAs of the cluster write what the phase stands for, so
+// Whether the barrier's `phase`-th phase has come to its end.  Every wait is bounded: a try is suspended
+// for a microsecond at most, so kMostTries take about a second.  A wait that runs out, which nothing
+// that these kernels do can cause, is the thread's last of its kind.  Without its tiles a thread
+// publishes and stores NaN, and thread 0 loads no more of them.  Without its messages its state is
+// NaN, and it sends no more, so that no half of a table is written before it has been read.  Either
+// way nothing that has not come gets into a result.  CLUSTER: other CTAs of the cluster write what the phase stands for, so
 // the wait has to acquire at their scope; for the CTA's own tiles its own is enough.
 template <bool CLUSTER>
-__device__ __forceinline__ bool barrier_wait(uint64_t* bar, int phase) {
-  for (int tries = 0; tries < (1 << 20); ++tries) {
+__device__ __forceinline__ bool barrier_wait(uint64_t* bar, int phase, int tries) {
+  for (; tries > 0; --tries) {
     uint32_t done;
     if (CLUSTER)
       asm volatile(
-          "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+          "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, 1000;\n selp.u32 %0, 1, 0, p;\n}"
           : "=r"(done)
           : "r"(shared_address(bar)), "r"(phase & 1)
           : "memory");
     else
       asm volatile(
-          "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+          "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2, 1000;\n selp.u32 %0, 1, 0, p;\n}"
           : "=r"(done)
           : "r"(shared_address(bar)), "r"(phase & 1)
           : "memory");
@@ -375,6 +378,12 @@ struct Table {
   float4 run[2][kMaxCluster][CH / 2];
   uint64_t arrived[2];
 };
+
+// What a thread that has given up does last: copies and messages still under way to its CTA land before
+// the shared memory is given back.
+__device__ __forceinline__ void pause() {
+  for (int k = 0; k < 1000; ++k) __nanosleep(1000);
+}
 
 __device__ __forceinline__ uint32_t in_cta(uint32_t address, int rank) {
   uint32_t there;
