@@ -507,7 +507,8 @@ typedef struct {
  * zero and the state stays.  h_last (fp32[B][D], nullable): the state after the last token, h0
  * for a row of length zero; it may be h0 itself.  states (nullable): gs_recurrence_states_size bytes,
  * 256-byte aligned, filled for the backward pass (the fp32 state at fixed intervals).
- * c > 0 and finite; decay must be finite.  The gs_seq are read during the call. */
+ * c > 0 and finite; decay must be finite; a product c * softplus(decay) above 2^100 counts as 2^100, one
+ * below 1e-37 as 1e-37.  The gs_seq are read during the call. */
 gs_status gs_recurrence_states_size(int64_t B, int64_t T, int64_t D, size_t* bytes);
 gs_status gs_recurrence_forward(const gs_seq* x, const gs_seq* r, const gs_seq* i, const float* decay,
                                 const float* h0, const uint8_t* reset, const int32_t* lengths,

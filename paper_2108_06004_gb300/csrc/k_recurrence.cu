@@ -88,7 +88,7 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
   else
     __syncthreads();
   const float2 rate = decay_rate(load_f32(p.decay + w.d, w.n), p.c);
-  const bool series = series_serves(w, rate);
+  const bool slow = rates_within(w, rate, kSeries), medium = rates_within(w, rate, kModerate);
   float2 state = load_f32(p.h0 ? p.h0 + w.b * p.D + w.d : nullptr, w.n);
   uint8_t flag = RESET ? reset_flag<kLen>(p, w, chunk_token(0) + w.slot * kLen) : 0;
   for (int s = 0; s < steps; ++s) {
@@ -112,13 +112,13 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
     Run run = identity();
     // SOME: there may be masked tokens and resets.  Runs of whole chunks without a reset, nearly all
     // of them, do without the selections.
-    auto gates = [&](auto some, auto in_series) {
+    auto gates = [&](auto some, auto rates) {
       constexpr bool SOME = decltype(some)::value;
 #pragma unroll
       for (int k = 0; k < kLen; ++k) {
         const bool cut = RESET && SOME && (resets >> k & 1u);
         float2 K;
-        gate_forward<decltype(in_series)::value>(capped(tile[1].at(w, k)), capped(tile[2].at(w, k)), rate, cut, a[k], K);
+        gate_forward<decltype(rates)::value>(capped(tile[1].at(w, k)), capped(tile[2].at(w, k)), rate, cut, a[k], K);
         b[k] = mul(K, widen(tile[0].at(w, k)));
         if (SOME && t0 + k >= w.len) {  // past the end of the row: the state stays
           a[k] = two(1.f);
@@ -129,12 +129,12 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
       }
     };
     const bool plain = full && !(RESET && __any_sync(0xFFFFFFFFu, resets != 0));
-    if (!plain)
-      gates(std::true_type(), std::false_type());
-    else if (series)
-      gates(std::false_type(), std::true_type());
+    if (!plain || !medium)
+      gates(std::true_type(), std::integral_constant<int, kAny>());
+    else if (slow)
+      gates(std::false_type(), std::integral_constant<int, kSlow>());
     else
-      gates(std::false_type(), std::false_type());
+      gates(std::false_type(), std::integral_constant<int, kMedium>());
     if (TILES && !here) {  // the run turns whatever state into NaN
       run = Run{two(nanf("")), two(nanf(""))};
       resets = 0;
@@ -276,7 +276,7 @@ k_recurrence_step(const __grid_constant__ RecurrenceStepParams p, int64_t rows) 
       if (b + k >= b1) break;
       if (slot[k] >= 0 && slot[k] < p.n_slots) {
         float2 a, K;
-        gate_forward<false>(capped(r[k]), capped(i[k]), rate, false, a, K);
+        gate_forward<kAny>(capped(r[k]), capped(i[k]), rate, false, a, K);
         h[k] = fma(a, h[k], mul(K, x[k]));
         store2<float, PAIR>(p.state + slot[k] * p.state_stride + d, n, h[k]);
       }

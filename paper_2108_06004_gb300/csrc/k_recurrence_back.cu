@@ -4,12 +4,15 @@
 // g_t = dy_t + F_t, F is the same kind of recurrence as h, walked from the end: F_{t-1} = a_t (F_t + dy_t).
 // Per token, with K = sqrt(1 - a^2) sigmoid(i), b = K x and 1 - a^2 = sigmoid(r) X:
 //   dx = g K,  di = g b (1 - sigmoid(i)),
-//   m = a g (h_{t-1} sigmoid(r) - b a / X),   dr = -rate (1 - sigmoid(r)) m,   ddecay = -c sigmoid(lambda) sum m.
+//   m = a g (h_{t-1} rate sigmoid(r) - b a rate / X),   dr = -(1 - sigmoid(r)) m,
+//   ddecay = -c sigmoid(lambda) / rate sum m.
+// The rate stands inside m, where it meets the small sigmoid of a gate that keeps a fast decay's state
+// alive; outside, m would be as small as that sigmoid and lose bits below the smallest numbers.
 // h_{t-1} is recomputed in fp32 from the state at the start of the chunk, which the forward pass
 // kept (4 bytes for kStateEvery tokens and channel), not read back from the rounded y.
 //
 // The cut of time over threads, warps and cluster CTAs is that of the forward pass, with runs of 8
-// tokens: a token's five factors (a, sigmoid(r), K, b (1 - sigmoid(i)), b a / X) stay in registers from the
+// tokens: a token's five factors (a, sigmoid(r), K, b (1 - sigmoid(i)), b a rate / X) stay in registers from the
 // first walk, which needs all transcendental functions, to the last, which writes.
 //
 // It has to move 7 elements a token and channel (and 4 bytes of state for 32 tokens); bf16 64x512x1024
@@ -91,7 +94,7 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
   else
     __syncthreads();
   const float2 rate = decay_rate(load_f32(p.decay + w.d, w.n), p.c);
-  const bool series = series_serves(w, rate);
+  const bool series = rates_within(w, rate, kSeries);
   float2 flow = load_f32(p.dh_last ? p.dh_last + w.b * p.D + w.d : nullptr, w.n);
   float2 sum = two(0.f);
   uint8_t flag = RESET && steps > 0 ? reset_flag<kLen>(p, w, chunk_token(steps - 1) + w.slot * kLen) : 0;
@@ -126,7 +129,7 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
         K[k] = g.K;
         float2 b = mul(g.K, widen(tile[0].at(w, k)));
         U[k] = mul(b, g.off);
-        Q[k] = mul(b, mul(g.a, g.inv_X));
+        Q[k] = mul(b, mul(g.a, g.rate_X));
         if (SOME && t0 + k >= w.len) {  // past the end of the row: the state and the flow stay
           a[k] = two(1.f);
           K[k] = b = two(0.f);
@@ -212,7 +215,7 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
     auto states = [&](auto some) {
 #pragma unroll
       for (int k = 0; k < kLen; ++k) {
-        Q[k] = fma(h, sr[k], make_float2(-Q[k].x, -Q[k].y));
+        Q[k] = fma(h, mul(rate, sr[k]), make_float2(-Q[k].x, -Q[k].y));
         const float2 b = mul(K[k], widen(tile[0].at(w, k)));
         h = RESET && decltype(some)::value ? apply(Run{a[k], b}, resets >> k & 1u, h) : fma(a[k], h, b);
       }
@@ -230,7 +233,7 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
       part = add(part, m);
       ox = mul(g, K[k]);
       oi = mul(g, U[k]);
-      orr = choose(cut, two(0.f), mul(mul(rate, fma(sr[k], two(1.f), two(-1.f))), m));
+      orr = choose(cut, two(0.f), mul(addc(sr[k], -1.f), m));
     };
     if constexpr (OUT) {
       auto results = [&](auto some) {
@@ -300,7 +303,7 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
   if (w.slot == 0) {
 #pragma unroll
     for (int k = 1; k < kRuns; ++k) sum = add(sum, sh.back[k][w.pair]);
-    store_f32(p.partial + (w.b * w.cluster + w.rank) * p.D + w.d, w.n, sum);
+    store_f32(p.partial + (w.b * w.cluster + w.rank) * p.D + w.d, w.n, make_float2(sum.x / rate.x, sum.y / rate.y));
   }
 }
 

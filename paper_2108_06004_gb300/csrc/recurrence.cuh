@@ -70,13 +70,21 @@ __device__ __forceinline__ float2 choose(bool c, float2 a, float2 b) { return ma
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSeries = 0.5f;     // the series serves -q up to here
+constexpr float kModerate = 0x1p40f;  // rates for which one root serves all of K
+
+// What is known of a warp's rates.
+enum Rates { kSlow, kMedium, kAny };  // at most kSeries, at most kModerate, at most 2^100
 
 // softplus without overflow; for very negative arguments it is exp(x) and goes to zero.
 __device__ __forceinline__ float softplus(float x) { return x > 20.f ? x : log1pf(expf(x)); }
 
-// c softplus(lambda), kept from underflowing so that rsqrt(X) below stays finite.
+// c softplus(lambda), kept from underflowing so that rsqrt(X) below stays finite, and below 2^100 so
+// that X and its products do.
+__device__ __forceinline__ float decay_rate(float lam, float c) {
+  return fminf(fmaxf(c * softplus(lam), 1e-37f), 0x1p100f);
+}
 __device__ __forceinline__ float2 decay_rate(float2 lam, float c) {
-  return make_float2(fmaxf(c * softplus(lam.x), 1e-37f), fmaxf(c * softplus(lam.y), 1e-37f));
+  return make_float2(decay_rate(lam.x, c), decay_rate(lam.y, c));
 }
 
 // What a token's gates give, with rate = c softplus(lambda) and q = log a = -rate sigmoid(r):
@@ -90,8 +98,9 @@ __device__ __forceinline__ float2 decay_rate(float2 lam, float c) {
 // would add up over the thousands of tokens that a state lives.  X is about 2 rate even where the
 // gate is shut, so nothing here is 0/0.
 
-// SERIES: rate is at most kSeries in both channels, so q always is in the polynomial's range.
-template <bool SERIES>
+// SERIES: rate is at most kSeries in both channels, so q always is in the polynomial's range.  SMALL: a
+// keeps its value below the smallest normal number too, as the square of half the exponent's power.
+template <bool SERIES, bool SMALL>
 __device__ __forceinline__ void decay_of(float2 sr, float2 rate, float2& a, float2& X) {
   const float2 q = mul(make_float2(-rate.x, -rate.y), sr);
   float2 s = addc(mulc(q, 0.006782862555491099f), 0.041013210491015605f);
@@ -100,12 +109,17 @@ __device__ __forceinline__ void decay_of(float2 sr, float2 rate, float2& a, floa
   s = fmac(q, s, 0.999999928937559f);
   a = fmac(q, s, 1.f);
   if (!SERIES) {
+    const auto power = [](float q) {
+      if (!SMALL) return ex2(kLog2e * q);
+      const float root = ex2(0.5f * kLog2e * q);
+      return root * root;
+    };
     if (q.x < -kSeries) {
-      a.x = ex2(kLog2e * q.x);
+      a.x = power(q.x);
       s.x = (1.f - a.x) * rcp(-q.x);
     }
     if (q.y < -kSeries) {
-      a.y = ex2(kLog2e * q.y);
+      a.y = power(q.y);
       s.y = (1.f - a.y) * rcp(-q.y);
     }
   }
@@ -119,26 +133,31 @@ __device__ __forceinline__ float2 half_exp(float2 v) {
 __device__ __forceinline__ float2 rcp(float2 v) { return make_float2(rcp(v.x), rcp(v.y)); }
 __device__ __forceinline__ float2 rsq(float2 v) { return make_float2(rsq(v.x), rsq(v.y)); }
 
-// a and K, from capped gate values.  The three roots and quotients of K are one reciprocal root;
-// with the cap its argument stays below 2^120 (X is large only where sigmoid(r) is small, and 1 + p^2
-// then is about 1).  `cut`: a reset, a = 0 and K = sigmoid(i).
-template <bool SERIES>
+// a and K, from capped gate values.  The three roots and quotients of K are one reciprocal root.  X is at
+// most twice the rate, and large only where sigmoid(r) is small and 1 + p^2 then about 1, so that with the
+// cap the root's argument stays below 2^120 for rates up to kModerate.  For larger ones X with 1 + p^2 has
+// a root of its own (16x2048x2048 bf16 with rates of 0.2 to 6 takes 128 us that way, 116 the other).
+// `cut`: a reset, a = 0 and K = sigmoid(i).
+template <int RATES>
 __device__ __forceinline__ void gate_forward(float2 r, float2 i, float2 rate, bool cut, float2& a, float2& K) {
   const float2 pr = half_exp(r), pi = half_exp(i);
   const float2 sqr = mul(pr, pr), sqi = mul(pi, pi);
   const float2 ur = addc(sqr, 1.f), ui = addc(sqi, 1.f);
   float2 X;
-  decay_of<SERIES>(mul(sqr, rcp(ur)), rate, a, X);
-  K = mul(mul(mul(pr, sqi), X), rsq(mul(mul(ur, ui), mul(ui, X))));
-  if (cut) {
-    a = two(0.f);
-    K = mul(sqi, rcp(ui));
+  decay_of<RATES == kSlow, false>(mul(sqr, rcp(ur)), rate, a, X);
+  if (RATES != kAny) {
+    K = mul(mul(mul(pr, sqi), X), rsq(mul(mul(ur, ui), mul(ui, X))));
+    if (cut) K = mul(sqi, rcp(ui));
+  } else {
+    const float2 si = mul(sqi, rcp(ui));
+    K = choose(cut, si, mul(mul(pr, mul(X, rsq(mul(ur, X)))), si));
   }
+  if (cut) a = two(0.f);
 }
 
-// What the backward pass needs: sigmoid(r), a, K, 1 - sigmoid(i) and 1 / X.
+// What the backward pass needs: sigmoid(r), a, K, 1 - sigmoid(i) and rate / X.
 struct Gate {
-  float2 sr, a, K, off, inv_X;
+  float2 sr, a, K, off, rate_X;
 };
 template <bool SERIES>
 __device__ __forceinline__ Gate gate_backward(float2 r, float2 i, float2 rate, bool cut) {
@@ -149,9 +168,9 @@ __device__ __forceinline__ Gate gate_backward(float2 r, float2 i, float2 rate, b
   g.off = rcp(add(sqi, one));
   g.sr = mul(z, z);
   float2 X;
-  decay_of<SERIES>(g.sr, rate, g.a, X);
+  decay_of<SERIES, true>(g.sr, rate, g.a, X);
   const float2 si = mul(sqi, g.off), rx = rsq(X);
-  g.inv_X = mul(rx, rx);
+  g.rate_X = mul(mul(rx, rx), rate);
   g.K = mul(mul(mul(z, X), rx), si);
   if (cut) {
     g.a = two(0.f);
@@ -228,9 +247,9 @@ __device__ __forceinline__ Place place(const RecurrenceParams& p) {
   return w;
 }
 
-// Whether the polynomial serves all channels of the warp, however open their gates are.
-__device__ __forceinline__ bool series_serves(const Place& w, float2 rate) {
-  return __all_sync(0xFFFFFFFFu, (w.n < 1 || rate.x <= kSeries) && (w.n < 2 || rate.y <= kSeries));
+// Whether the rates of all channels of the warp are at most `most`.
+__device__ __forceinline__ bool rates_within(const Place& w, float2 rate, float most) {
+  return __all_sync(0xFFFFFFFFu, (w.n < 1 || rate.x <= most) && (w.n < 2 || rate.y <= most));
 }
 
 __device__ __forceinline__ int clamp_int(int64_t v, int most) { return v < 0 ? 0 : v < most ? (int)v : most; }
