@@ -118,7 +118,7 @@ k_recurrence_forward(const __grid_constant__ RecurrenceParams p) {
       for (int k = 0; k < kLen; ++k) {
         const bool cut = RESET && SOME && (resets >> k & 1u);
         float2 K;
-        gate_forward<decltype(rates)::value>(capped(tile[1].at(w, k)), capped(tile[2].at(w, k)), rate, cut, a[k], K);
+        gate_forward<decltype(rates)::value>(capped<kMostForward>(tile[1].at(w, k)), capped<kMostForward>(tile[2].at(w, k)), rate, cut, a[k], K);
         b[k] = mul(K, widen(tile[0].at(w, k)));
         if (SOME && t0 + k >= w.len) {  // past the end of the row: the state stays
           a[k] = two(1.f);
@@ -276,7 +276,7 @@ k_recurrence_step(const __grid_constant__ RecurrenceStepParams p, int64_t rows) 
       if (b + k >= b1) break;
       if (slot[k] >= 0 && slot[k] < p.n_slots) {
         float2 a, K;
-        gate_forward<kAny>(capped(r[k]), capped(i[k]), rate, false, a, K);
+        gate_forward<kAny>(capped<kMostForward>(r[k]), capped<kMostForward>(i[k]), rate, false, a, K);
         h[k] = fma(a, h[k], mul(K, x[k]));
         store2<float, PAIR>(p.state + slot[k] * p.state_stride + d, n, h[k]);
       }

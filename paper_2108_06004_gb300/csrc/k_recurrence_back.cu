@@ -45,6 +45,7 @@ __global__ void __launch_bounds__(kThreads, 4)
 k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
   constexpr bool TILES = UNIT == 16, PAIR = UNIT > (int)sizeof(E);  // results as pairs
   using Shared = BackwardShared<E, CH, OUT>;
+  using Raw = typename Pack2<E>::type;
   constexpr int kRuns = Shared::kRuns, kChunk = kRuns * kLen;
   static_assert(kChunk % kStateEvery == 0, "a step starts at a kept state");
   extern __shared__ __align__(128) unsigned char raw[];
@@ -115,6 +116,31 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
     if (s > 0) load(turn + 1);
     auto& tile = sh.in[turn & 1];
     float2 a[kLen], sr[kLen], K[kLen], U[kLen], Q[kLen];
+    // 1 - sigmoid(r), for which no registers are left, stays where the thread has read its gates, in one
+    // word of each tile with a 2-byte type.  kTurned: two runs of a warp, whose rows lie in the same banks,
+    // do so in every other row the other way round (backward of 1x65536x1024 bf16 251 us, 259 without).
+    constexpr bool kTurned = sizeof(E) == 2 && CH < 64;
+    const int turned = kTurned ? w.slot % 2 * (CH / 2) : 0;
+    auto word = [&](int which, int k) -> Raw& { return *(&tile[which].at(w, k) + (k % 2 == 0 ? turned : -turned)); };
+    auto keep = [&](int k, float2 v) {
+      if constexpr (sizeof(E) == 4) {
+        tile[1].at(w, k) = v;
+      } else {
+        memcpy(&word(1, k), &v.x, sizeof(Raw));
+        memcpy(&word(2, k), &v.y, sizeof(Raw));
+      }
+    };
+    auto kept_value = [&](int k) {
+      float2 v;
+      if constexpr (sizeof(E) == 4) {
+        v = tile[1].at(w, k);
+      } else {
+        memcpy(&v.x, &word(1, k), sizeof(Raw));
+        memcpy(&v.y, &word(2, k), sizeof(Raw));
+      }
+      return v;
+    };
+    float2 last_shut = two(0.f);
     Run run = identity();
     // SOME: there may be masked tokens and resets.  Runs of whole chunks without a reset, nearly all
     // of them, do without the selections.
@@ -123,9 +149,16 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
 #pragma unroll
       for (int k = 0; k < kLen; ++k) {
         const bool cut = RESET && SOME && (resets >> k & 1u);
-        const Gate g = gate_backward<decltype(in_series)::value>(capped(tile[1].at(w, k)), capped(tile[2].at(w, k)), rate, cut);
+        const Gate g = gate_backward<decltype(in_series)::value>(capped<kMostBackward>(tile[1].at(w, k)),
+                                                                    capped<kMostBackward>(tile[2].at(w, k)), rate, cut);
         a[k] = g.a;
         sr[k] = g.sr;
+        if (!kTurned) keep(k, g.shut);
+        if (kTurned && k % 2 == 1) {
+          keep(k - 1, last_shut);
+          keep(k, g.shut);
+        }
+        last_shut = g.shut;
         K[k] = g.K;
         float2 b = mul(g.K, widen(tile[0].at(w, k)));
         U[k] = mul(b, g.off);
@@ -233,7 +266,7 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
       part = add(part, m);
       ox = mul(g, K[k]);
       oi = mul(g, U[k]);
-      orr = choose(cut, two(0.f), mul(addc(sr[k], -1.f), m));
+      orr = choose(cut, two(0.f), mul(kept_value(k), make_float2(-m.x, -m.y)));
     };
     if constexpr (OUT) {
       auto results = [&](auto some) {
@@ -278,6 +311,7 @@ k_recurrence_backward(const __grid_constant__ RecurrenceParams p) {
         results(std::false_type());
       else
         results(std::true_type());
+      if (TILES) tile_fence();  // the tiles, which the threads have written to, are loaded again
     }
     sum = add(sum, part);
   }

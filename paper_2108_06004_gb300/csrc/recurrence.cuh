@@ -46,17 +46,19 @@ __device__ __forceinline__ float2 widen(float2 v) { return v; }
 __device__ __forceinline__ float2 widen(__half2 v) { return Pack2<__half>::up(v); }
 __device__ __forceinline__ float2 widen(__nv_bfloat162 v) { return Pack2<__nv_bfloat16>::up(v); }
 
-constexpr float kMostGate = 27.f;   // sigmoid is 1 to fp32 from well below this
+// A gate's value, capped where its sigmoid has long been 1 in fp32, so that no square of an exponential
+// below overflows: 27 in the forward pass, 80 in the backward pass, which needs 1 - sigmoid too and has
+// it right up to there.  The cap is exact in every type and taken before widening, two elements at once.
+constexpr int kMostForward = 27, kMostBackward = 80;
 
-// A gate's value, capped where its sigmoid is 1 in fp32, so that no square of an exponential below
-// overflows.  The cap is exact in every type and taken before widening, two elements at once.
+template <int MOST>
 __device__ __forceinline__ float2 capped(float2 v) {
-  return make_float2(at_most(v.x, kMostGate), at_most(v.y, kMostGate));
+  return make_float2(at_most(v.x, MOST), at_most(v.y, MOST));
 }
-__device__ __forceinline__ float2 capped(__half2 v) { return widen(__hmin2_nan(v, __float2half2_rn(kMostGate))); }
-__device__ __forceinline__ float2 capped(__nv_bfloat162 v) {
-  return widen(__hmin2_nan(v, __float2bfloat162_rn(kMostGate)));
-}
+template <int MOST>
+__device__ __forceinline__ float2 capped(__half2 v) { return widen(__hmin2_nan(v, __float2half2_rn(MOST))); }
+template <int MOST>
+__device__ __forceinline__ float2 capped(__nv_bfloat162 v) { return widen(__hmin2_nan(v, __float2bfloat162_rn(MOST))); }
 
 // Two channels at a time: one instruction for both.
 __device__ __forceinline__ float2 two(float v) { return make_float2(v, v); }
@@ -155,20 +157,25 @@ __device__ __forceinline__ void gate_forward(float2 r, float2 i, float2 rate, bo
   if (cut) a = two(0.f);
 }
 
-// What the backward pass needs: sigmoid(r), a, K, 1 - sigmoid(i) and rate / X.
+// What the backward pass needs.  The differences from 1 are not taken as such, which would leave them no
+// digits from gate values of 17 on.
 struct Gate {
-  float2 sr, a, K, off, rate_X;
+  float2 sr, shut;  // sigmoid(r), 1 - sigmoid(r)
+  float2 a, K;
+  float2 off;       // 1 - sigmoid(i)
+  float2 rate_X;    // rate / X
 };
 template <bool SERIES>
 __device__ __forceinline__ Gate gate_backward(float2 r, float2 i, float2 rate, bool cut) {
   Gate g;
   const float2 one = two(1.f);
   const float2 pr = half_exp(r), pi = half_exp(i);
-  const float2 z = mul(pr, rsq(fma(pr, pr, one))), sqi = mul(pi, pi);
+  const float2 w = rsq(fma(pr, pr, one)), z = mul(pr, w), sr = mul(z, z), sqi = mul(pi, pi);
   g.off = rcp(add(sqi, one));
-  g.sr = mul(z, z);
+  g.sr = sr;
+  g.shut = mul(w, w);
   float2 X;
-  decay_of<SERIES, true>(g.sr, rate, g.a, X);
+  decay_of<SERIES, true>(sr, rate, g.a, X);
   const float2 si = mul(sqi, g.off), rx = rsq(X);
   g.rate_X = mul(mul(rx, rx), rate);
   g.K = mul(mul(mul(z, X), rx), si);
