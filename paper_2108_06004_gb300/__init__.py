@@ -469,6 +469,8 @@ def _refuse(func: str, msg: str):
 
 
 def _dtype(func: str, t) -> int:
+    if t is None:
+        _refuse(func, "the first tensor is missing")
     if not _CODES:
         torch = _torch()
         _CODES.update({torch.float32: GS_F32, torch.float16: GS_F16, torch.bfloat16: GS_BF16})
@@ -630,6 +632,8 @@ def gs_dropout_add_norm_backward(dz, dy, y, weight, rstd, dx, dresidual, dweight
 
 
 def _seq(func: str, name: str, t, shape, dtype, device):
+    if t is None:
+        return None
     if t.shape != shape or t.dtype is not dtype or t.device != device:
         _unlike(func, name, t, shape, dtype, device)
     b, s, d = t.stride()
@@ -671,6 +675,8 @@ _states_size = functools.lru_cache(maxsize=256)(gs_recurrence_states_size)   # a
 
 
 def _states_fit(func: str, states, B: int, T: int, D: int, device=None) -> None:
+    if states is None:
+        return   # the library knows whether it needs them
     if device is not None and states.device != device:
         _refuse(func, f"states is on {states.device}, expected {device}")
     if states.numel() * states.element_size() < _states_size(B, T, D) or not states.is_contiguous():
@@ -686,8 +692,7 @@ def gs_recurrence_forward(x, r, i, decay, y, h0=None, reset=None, lengths=None, 
     shape = B, T, D = _sequence(f, x)
     stream = _launch_stream(f, x, stream)
     dtype, dev, f32 = x.dtype, x.device, _torch().float32
-    if states is not None:
-        _states_fit(f, states, B, T, D, dev)
+    _states_fit(f, states, B, T, D, dev)
     _check(load_library().gs_recurrence_forward(
         _seq(f, "x", x, shape, dtype, dev), _seq(f, "r", r, shape, dtype, dev), _seq(f, "i", i, shape, dtype, dev),
         _dense(f, "decay", decay, (D,), f32, dev), _dense(f, "h0", h0, (B, D), f32, dev),
@@ -732,7 +737,7 @@ def gs_recurrence_step(x, r, i, decay, state, y, slots=None, c: float = 8.0, str
     rp, rs = _matrix(f, "r", r, shape, dtype, dev)
     ip, istride = _matrix(f, "i", i, shape, dtype, dev)
     yp, ys = _matrix(f, "y", y, shape, dtype, dev)
-    if state.dim() != 2:
+    if state is None or state.dim() != 2:
         _refuse(f, "state must have two dimensions")
     n = state.shape[0]
     sp, ss = _matrix(f, "state", state, (n, D), f32, dev)
