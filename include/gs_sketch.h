@@ -434,7 +434,10 @@ gs_status gs_plan_destroy(gs_plan* plan);
  *     Strides are in elements, any non-negative value for an input (0 repeats a row); rows of
  *     an output must not overlap one another, nor an input unless a call says so.
  *   - Data is aligned to its element.  Tensors whose rows all start at multiples of 16 bytes are
- *     the fastest; contiguous ones of any width come next.  Alignment does not change results,
+ *     the fastest; contiguous ones of any width come next.  Dropout and the norm are two to three
+ *     times slower where the rows of a call's tensors lie at different distances from 16-byte
+ *     boundaries, and the norm also where its weight does not start at one (parameters that are slices
+ *     of one vector: keep their offsets multiples of four floats).  Alignment does not change results,
  *     but for the order of additions in the norm's sums.
  *   - Sizes may be zero where a loop over them may be empty (rows, cols, B, T, D); such a call
  *     does what is left of its work.  Limits: rows * cols and B * T * D up to 2^40, rows and T

@@ -10,7 +10,9 @@
 // Bound by memory but for bf16 without a residual, where the generator's integer instructions (64 % of
 // their pipe) come close: 16384x4096 takes 42 us in bf16 (94 % of the copy rate, 98 % with p = 0), 58 us
 // with a residual and 79 us in fp32 (both at the copy rate).  Rows with strides take 51 us (a
-// division a group); odd widths 71 us, with rows that differ in alignment 121 us (single elements).
+// division a group).  Where rows are padded and their width is no multiple of eight, a group lies in two blocks
+// of the generator, and all ten rounds are run for both: 16384x4097 71 us, 121 us with rows that differ in
+// alignment too (single elements).
 #include "gs_layer.cuh"
 
 namespace gs {

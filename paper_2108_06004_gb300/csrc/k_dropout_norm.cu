@@ -4,8 +4,10 @@
 //
 // A row is held in the registers of its threads, one or two groups of eight elements each, so every
 // tensor is read and written once.  Bound by memory: 32768x4096 takes 158 us in bf16 and 302 us in fp32 (both at
-// the copy rate), 131072x64 13 us (76 %), 4096x1024 7.9 us (63 %: one wave of CTAs, whose rows pass
-// from load to store once).  16384x4097, whose rows start anywhere, 130 us (61 %).
+// the copy rate), 131072x64 13 us (76 %), 4096x1024 7.8 us (63 %: one wave of CTAs, whose rows pass
+// from load to store once).  Rows that start anywhere: 16384x4097 129 us (61 %), 32768x1001 66 us (59 %),
+// 131072x65 40 us (25 %); tensors whose rows differ in alignment, or a weight that does not start at a
+// 16-byte boundary, make all elements move one by one: 32768x1024 138 us (43 with an aligned weight).
 #include "dropout_norm.cuh"
 
 namespace gs {
@@ -13,8 +15,11 @@ namespace {
 
 using namespace norm;
 
-// Few enough registers that 1792 threads stay resident: 4096x1024 bf16 takes 7.9 us with seven CTAs
-// of 256 threads an SM, 9.4 us with the five that the compiler's own choice leaves room for.
+// Few enough registers that 1792 threads stay resident: 4096x1024 bf16 takes 7.8 us with seven CTAs
+// of 256 threads an SM, 9.4 us with the five that the compiler's own choice leaves room for.  Rows of 2-byte
+// types that start anywhere spill up to 176 bytes a thread for it (their groups take more registers), and are
+// faster all the same where they are wide (16384x4097 129 us, 183 without the cap; 16384x2047 70, 81;
+// 131072x65 40, 42) or within 7 % (65536x257 65, 61); 300x1001, a call of 3 us, is 0.5 us slower.
 template <typename E, int TPR, int V, int L>
 __global__ void __launch_bounds__(kCtaThreads<TPR>, 1792 / kCtaThreads<TPR>)
 k_norm_forward(const __grid_constant__ NormForwardParams p) {

@@ -8,7 +8,12 @@
 // it works on one; dw is summed by each thread over the rows of its CTA, then over the CTAs by a
 // last kernel, in a fixed order.  Bound by memory: 32768x4096 takes 205 us in bf16 (97 % of the copy
 // rate; 511 us when a row's loads waited for the row before), 65536x1024 105 us (95 %), fp32 16384x4096
-// 206 us (96 %); 16384x4097, whose rows start anywhere, 211 us (47 %).
+// 205 us (97 %).  What is in flight goes by threads and registers: past 4096 columns of a 2-byte type a row
+// takes 384 threads, of which one CTA fits an SM where two of 256 did, and bf16 16384x4104 takes 137 us (73 %),
+// 16384x5120 151 us (82 %), 16384x6144 170 us (88 %).  Rows that start anywhere pay for single elements at both ends
+// and weights out of step with the groups on top: 16384x4097 211 us (47 %), 32768x1001 85 us (57 %).  Above
+// 8192 columns (fp32 4096) the next row is not loaded ahead: 16384x12288 412 us (72 %), 16384x16384 572 us (69 %).
+// Single elements throughout (see the forward pass): 32768x1024 180 us, 56 with an aligned weight.
 #include "dropout_norm.cuh"
 
 namespace gs {

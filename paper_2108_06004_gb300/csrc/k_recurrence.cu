@@ -12,12 +12,15 @@
 // another cluster, and the order of all operations is fixed by the sizes.  For the backward pass the
 // state is kept in fp32 every kStateEvery tokens.
 //
-// It has to move 4 elements a token and channel.  bf16 64x512x1024 takes 49 us (81 % of the copy rate),
-// 16x2048x2048 100 us (80 %), 8x2048x2048 55 us (72 %: 512 CTAs, four on some SMs and three on others),
-// 1x65536x1024 131 us (60 %: the same, and a meeting of 16 CTAs at every step); fp32 32x1024x1024
-// 86 us (92 %).  What bounds it in bf16 is the issue of about 61 instructions a token and pair of
-// channels by 16 warps an SM (2.2 a cycle), not their kind: the busiest pipe is at 30 %.  Runs of 16 tokens
-// and 128 registers do better than runs of 8 and 24 warps (1x65536x1024: 226 us), which meet twice as often.
+// It has to move 4 elements a token and channel.  bf16 64x512x1024 takes 48 us (83 % of the copy rate),
+// 16x2048x2048 100 us (79 %), 8x2048x2048 56 us (71 %: 512 CTAs, four on some SMs and three on others),
+// 1x65536x1024 135 us (59 %: the same, and a meeting of 16 CTAs at every step); fp32 32x1024x1024
+// 85 us (93 %).  What bounds it in bf16 is latency: 11 to 14 warps of an SM are active on average, and they
+// issue 2.0 to 2.2 instructions a cycle of the 4 that it could, about 61 a token and pair of channels and 74
+// in clusters; the busiest pipe is at 32 %.  With 32 channels a CTA a warp holds two runs whose rows lie in the same 16
+// banks, so every tile access takes two turns (shared memory 34 % busy, 16 % with 64 channels).  Runs of 16
+// tokens and 128 registers do better than runs of 8 and 24 warps (1x65536x1024: 226 us), which meet twice as
+// often.  Decay rates above 1/2 leave the polynomial: 16x2048x2048 with rates of 0.2 to 6 takes 116 us.
 #include "recurrence.cuh"
 
 namespace gs {
@@ -292,8 +295,8 @@ int64_t recurrence_states(int64_t T) { return (T + kStateEvery - 1) / kStateEver
 // How a pass of `run` tokens a thread is cut: the channels of a CTA, and the CTAs of a cluster that
 // share a row's time.  An SM holds four CTAs, three with fp32.  64 channels a CTA where that makes three for each
 // SM; fewer columns are cut to 32 channels (twice the CTAs, with twice the tokens each: forward and
-// backward of 8x2048x2048 bf16 take 56 and 96 us against 56 and 109 us with 64, but 64x512x1024,
-// which has enough columns, 56 and 104 against 53 and 91 us), and then share time in clusters until
+// backward of 8x2048x2048 bf16 took 56 and 96 us against 56 and 109 us with 64, but 64x512x1024,
+// which has enough columns, 56 and 104 against 53 and 91 us, all when the cut was chosen), and then share time in clusters until
 // there are three CTAs for each SM or no chunks left to deal.  A cluster meets at every step, so it comes last:
 // 8x2048x2048 with 64 channels and clusters of two takes 58 and 134 us.  More CTAs than stay
 // resident are no use (fp32 4x2048x2048: 256 CTAs 48 and 86 us, 512 in clusters of two 57 and

@@ -16,9 +16,11 @@
 // first walk, which needs all transcendental functions, to the last, which writes.
 //
 // It has to move 7 elements a token and channel (and 4 bytes of state for 32 tokens); bf16 64x512x1024
-// takes 84 us, 83 % of the copy rate, 16x2048x2048 169 us (82 %).  What bounds it is the issue of about
-// 105 instructions a token and pair of channels by 16 warps an SM (2.3 a cycle); fp32 4x2048x2048,
-// twice the bytes for the same instructions, 87 us (80 %).
+// takes 85 us, 81 % of the copy rate, 16x2048x2048 176 us (79 %), 8x2048x2048 102 us (68 %), 1x65536x1024 251 us
+// (55 %); fp32 8x2048x1024 80 us (87 %), 32x1024x1024 175 us (79 %).  What bounds it is latency: 12 to 14
+// active warps of an SM issue 2.1 to 2.4 instructions a cycle, about 111 a token and pair of channels, 144 in
+// clusters.  With 32 channels a CTA two runs of a warp share 16 banks (see the forward pass): shared memory is
+// 55 % busy, 38 % with 64 channels.  Rates of 0.2 to 6: 16x2048x2048 191 us.
 #include "recurrence.cuh"
 
 namespace gs {
