@@ -549,6 +549,126 @@ gs_status gs_recurrence_step(const void* x, int64_t x_stride, const void* r, int
                              int64_t y_stride, int64_t B, int64_t D, int32_t dtype, float c,
                              gs_stream stream);
 
+/* ---- operators of a linear attention layer ------------------------------------------ */
+/* What a residual layer computes besides its matrix products when its state is a matrix for each
+ * head: rotary positions of queries and keys, linear attention with a decay for each head, and the
+ * norms around a block with its gate and residual scale.  Types, strides, alignment, zero sizes and
+ * limits are those of the recurrent layer's operators above; the paper has no counterpart. */
+
+/* A [B][T][H][D] tensor: element (b, t, h, d) at
+ * data + b * batch_stride + t * token_stride + h * head_stride + d. */
+typedef struct {
+  void* data;
+  int64_t batch_stride, token_stride, head_stride;
+} gs_heads;
+
+/* Rotary positions (Su et al., RoFormer).  Pair j < R / 2 of each head turns by
+ * angle = position * frequencies[j]:
+ *   (a, b) -> magnitude * (a cos - b sin, a sin + b cos),
+ * where the pair is elements 2j and 2j + 1 (interleaved) or j and j + R / 2; elements from R on are
+ * copied.  inverse: the angles are negated, which is the gradient's turn.  frequencies: fp64[R / 2]
+ * on the device (gs_rotary_frequencies), finite.  positions: int32[B][T], NULL for first + t (taken
+ * modulo 2^32, as an int32).  A position's turn is worked out in 64-bit fixed point, so far positions
+ * keep their digits.  R is even and at most D; out may be x itself (same strides).
+ * 1 <= D <= GS_ROTARY_MAX_HEAD, 0 <= R <= D; magnitude must be finite. */
+#define GS_ROTARY_MAX_HEAD 512
+gs_status gs_rotary(const gs_heads* x, const gs_heads* out, const double* frequencies, const int32_t* positions,
+                    int64_t first, int64_t B, int64_t T, int64_t H, int64_t D, int64_t R, int32_t dtype,
+                    int32_t interleaved, int32_t inverse, float magnitude, gs_stream stream);
+
+/* Frequencies on the HOST (out: fp64[R / 2]): f_j = base^(-2j / R), and for contexts `factor` times as
+ * long as the `original` ones the model has seen (factor >= 1; original = 0: all frequencies are
+ * divided by it, position interpolation) by parts as in YaRN (Peng et al.): a pair that turned
+ * r = original f_j / 2 pi times over the original length keeps the share
+ * s = clamp((r - low) / (high - low), 0, 1) of its frequency, f_j (s + (1 - s) / factor).
+ * base > 0, 0 <= low < high. */
+gs_status gs_rotary_frequencies(int64_t R, double base, double factor, double original, double low, double high,
+                                double* out);
+
+/* Linear attention with a decay for each head.  With g = log_decay[h] (fp32[H], taken to [-2^13, 0]),
+ * for each sequence and head, a state S of Dk x Dv in fp32, S_{-1} = s0 (fp32[B][H][Dk][Dv], NULL for
+ * zeros):
+ *   S_t = e^g S_{t-1} + k_t v_t',   o_t = scale S_t' q_t.
+ * q is [B][T][H][Dk]; k and v have K heads, of which H / K heads in turn share one.  s_last (nullable) is
+ * the state after the last token, s0 for a sequence without tokens; it may be s0 itself.
+ * Sequences are, by default, the rows of B x T tokens.  lengths (int32[B], nullable; taken to [0, T]):
+ * tokens from a row's length on have no influence and their o is zero.  offsets (int32[B + 1],
+ * nullable, not with lengths): tensors have one row of T tokens, and sequence b is tokens offsets[b] to
+ * offsets[b + 1] - 1 (ascending, taken to [0, T]); tokens of no sequence are left as they were.
+ * q, k and v of tokens that count must be finite: a block of tokens is one matrix product, so what is not
+ * finite may show in any output of its sequence and head.  Dk, Dv in [1, GS_ATTENTION_MAX_HEAD].
+ * workspace: gs_linear_attention_workspace_size bytes (backward, packed: 0 or 1, as the call is a backward
+ * pass and has offsets), 256-byte aligned; calls that may run at once need one each. */
+#define GS_ATTENTION_MAX_HEAD 256
+gs_status gs_linear_attention_workspace_size(int64_t B, int64_t T, int64_t H, int64_t K, int64_t Dk, int64_t Dv,
+                                             int32_t dtype, int32_t backward, int32_t packed, size_t* bytes);
+gs_status gs_linear_attention_forward(const gs_heads* q, const gs_heads* k, const gs_heads* v,
+                                      const float* log_decay, const float* s0, const int32_t* lengths,
+                                      const int32_t* offsets, const gs_heads* o, float* s_last, int64_t B, int64_t T,
+                                      int64_t H, int64_t K, int64_t Dk, int64_t Dv, int32_t dtype, float scale,
+                                      void* workspace, size_t workspace_bytes, gs_stream stream);
+
+/* Gradients of gs_linear_attention_forward from d_o and ds_last (fp32[B][H][Dk][Dv], NULL for none) and its
+ * inputs: with dS_t = e^g dS_{t+1} + scale q_t do_t' (ds_last past the last token),
+ *   dq_t = scale S_t do_t,  dk_t = dS_t v_t,  dv_t = dS_t' k_t,  ds0 = e^g dS_0 (nullable),
+ * dk and dv summed in fp32 over the heads that share them.  The decay is a constant and has no gradient.
+ * Tokens that lengths mask get zeros, tokens of no sequence are left as they were.  ds0 may not be s0 or
+ * ds_last. */
+gs_status gs_linear_attention_backward(const gs_heads* d_o, const gs_heads* q, const gs_heads* k, const gs_heads* v,
+                                       const float* log_decay, const float* s0, const float* ds_last,
+                                       const int32_t* lengths, const int32_t* offsets, const gs_heads* dq,
+                                       const gs_heads* dk, const gs_heads* dv, float* ds0, int64_t B, int64_t T,
+                                       int64_t H, int64_t K, int64_t Dk, int64_t Dv, int32_t dtype, float scale,
+                                       void* workspace, size_t workspace_bytes, gs_stream stream);
+
+/* One token of each of B streams: the state in place, and o.  q, k, v and o have T = 1 (their token
+ * strides are not used).  state: fp32, n_slots states of [H][Dk][Dv], state_stride elements apart; stream
+ * b's is slots[b] (int32[B], NULL for b).  A slot outside [0, n_slots) is idle: its o is zero and nothing
+ * else is touched.  No two streams may share a slot. */
+gs_status gs_linear_attention_step(const gs_heads* q, const gs_heads* k, const gs_heads* v, const float* log_decay,
+                                   float* state, int64_t state_stride, int64_t n_slots, const int32_t* slots,
+                                   const gs_heads* o, int64_t B, int64_t H, int64_t K, int64_t Dk, int64_t Dv,
+                                   int32_t dtype, float scale, gs_stream stream);
+
+/* The norms around a block, with its gate and residual scale, row by row.  With s() the logistic
+ * function and each row's columns in `groups` equal groups of adjacent ones:
+ *   rstd[row][group] = 1 / sqrt(mean over the group of x^2 + eps),
+ *   y = residual + scale * act(gate) * x * rstd * weight,
+ *   act(u) = u s(u) (GS_GATE_SILU) or s(u) (GS_GATE_SIGMOID); 1 without a gate (GS_GATE_NONE),
+ * and with next_weight, over whole rows (groups must be 1),
+ *   next_rstd[row] = 1 / sqrt(mean(y^2) + eps),  z = y * next_rstd * next_weight.
+ * residual may be NULL for none.  gate is given exactly if act is not GS_GATE_NONE; next_weight, z and
+ * next_rstd are given together.  y (the residual stream) and z are stored; z and next_rstd come from y before
+ * it is rounded.  weight, next_weight: fp32[cols].  groups divides cols, and a group has at most
+ * GS_NORM_MAX_COLS columns.  y may be x, gate or residual itself.  eps >= 0. */
+#define GS_GATE_NONE 0
+#define GS_GATE_SIGMOID 1
+#define GS_GATE_SILU 2
+gs_status gs_gated_norm(const void* x, int64_t x_stride, const void* gate, int64_t gate_stride, const void* residual,
+                        int64_t residual_stride, const float* weight, const float* next_weight, void* y,
+                        int64_t y_stride, void* z, int64_t z_stride, float* rstd, float* next_rstd, int64_t rows,
+                        int64_t cols, int64_t groups, int32_t dtype, int32_t act, float scale, float eps,
+                        gs_stream stream);
+
+/* Device workspace bytes gs_gated_norm_backward needs. */
+gs_status gs_gated_norm_workspace_size(int64_t rows, int64_t cols, int64_t groups, size_t* bytes);
+
+/* From dy and dz (the gradients of y and of z; with next_weight dz, y and next_rstd are given and dy may be
+ * NULL for none, without it only dy is), the inputs, the stored y, rstd and next_rstd:
+ *   m = y * next_rstd,  u = dz * next_weight,  t = next_rstd * (u - m * mean(u * m)) + dy,
+ *   dresidual = t,  n = x * rstd,  e = scale * t,  dgate = e * n * weight * act'(gate),
+ *   p = e * act(gate) * weight,  dx = rstd * (p - n * mean over the group of (p * n)),
+ *   dweight = sum over rows of e * act(gate) * n,  dnext_weight = sum over rows of dz * m.
+ * dx, dgate and dresidual may each be NULL and may not be an input; dweight and (with next_weight)
+ * dnext_weight, fp32[cols], are overwritten.  workspace must hold gs_gated_norm_workspace_size bytes, 256-byte aligned. */
+gs_status gs_gated_norm_backward(const void* dy, int64_t dy_stride, const void* dz, int64_t dz_stride, const void* x,
+                                 int64_t x_stride, const void* gate, int64_t gate_stride, const void* y,
+                                 int64_t y_stride, const float* weight, const float* next_weight, const float* rstd,
+                                 const float* next_rstd, void* dx, int64_t dx_stride, void* dgate,
+                                 int64_t dgate_stride, void* dresidual, int64_t dresidual_stride, float* dweight,
+                                 float* dnext_weight, int64_t rows, int64_t cols, int64_t groups, int32_t dtype,
+                                 int32_t act, float scale, void* workspace, size_t workspace_bytes, gs_stream stream);
+
 /* ---- measurement aid --------------------------------------------------------------- */
 /* The fused insert (gs_accumulate_insert over every group and row pass) is bound by the
  * requests its SMs send to L2: one cell reduction per (coordinate, row, group) and the

@@ -31,11 +31,17 @@ GS_F32 = 0
 GS_F16 = 1
 GS_BF16 = 2
 GS_NORM_MAX_COLS = 16384
+GS_ROTARY_MAX_HEAD = 512
+GS_ATTENTION_MAX_HEAD = 256
+GS_GATE_NONE = 0
+GS_GATE_SIGMOID = 1
+GS_GATE_SILU = 2
 
 _lib = None
 
 _vp = ctypes.c_void_p
 _i32, _i64, _u64, _f32, _sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_float, ctypes.c_size_t
+_f64 = ctypes.c_double
 _PP = ctypes.POINTER(ctypes.c_void_p)
 
 
@@ -44,7 +50,13 @@ class GsSeq(ctypes.Structure):
     _fields_ = [("data", _vp), ("batch_stride", _i64), ("token_stride", _i64)]
 
 
+class GsHeads(ctypes.Structure):
+    """A [B][T][H][D] tensor: its address, batch, token and head strides in elements."""
+    _fields_ = [("data", _vp), ("batch_stride", _i64), ("token_stride", _i64), ("head_stride", _i64)]
+
+
 _SEQ = ctypes.POINTER(GsSeq)
+_HEADS = ctypes.POINTER(GsHeads)
 
 # name -> argument types (all return gs_status / int32 unless listed in _RESTYPES)
 SIGNATURES = {
@@ -105,6 +117,20 @@ SIGNATURES = {
     "gs_recurrence_wait_tries": [_i32, _i32],
     "gs_recurrence_step": [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64, _vp, _vp, _i64, _i64, _i64, _i32,
                            _f32, _vp],
+    "gs_rotary": [_HEADS, _HEADS, _vp, _vp, _i64, _i64, _i64, _i64, _i64, _i64, _i32, _i32, _i32, _f32, _vp],
+    "gs_rotary_frequencies": [_i64, _f64, _f64, _f64, _f64, _f64, _vp],
+    "gs_linear_attention_workspace_size": [_i64, _i64, _i64, _i64, _i64, _i64, _i32, _i32, _i32, ctypes.POINTER(_sz)],
+    "gs_linear_attention_forward": [_HEADS, _HEADS, _HEADS, _vp, _vp, _vp, _vp, _HEADS, _vp, _i64, _i64, _i64, _i64, _i64,
+                                    _i64, _i32, _f32, _vp, _sz, _vp],
+    "gs_linear_attention_backward": [_HEADS, _HEADS, _HEADS, _HEADS, _vp, _vp, _vp, _vp, _vp, _HEADS, _HEADS, _HEADS, _vp,
+                                     _i64, _i64, _i64, _i64, _i64, _i64, _i32, _f32, _vp, _sz, _vp],
+    "gs_linear_attention_step": [_HEADS, _HEADS, _HEADS, _vp, _vp, _i64, _i64, _vp, _HEADS, _i64, _i64, _i64, _i64, _i64,
+                                 _i32, _f32, _vp],
+    "gs_gated_norm": [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64, _i64, _i32, _i32,
+                      _f32, _f32, _vp],
+    "gs_gated_norm_workspace_size": [_i64, _i64, _i64, ctypes.POINTER(_sz)],
+    "gs_gated_norm_backward": [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _i64,
+                               _vp, _i64, _vp, _vp, _i64, _i64, _i64, _i32, _i32, _f32, _vp, _sz, _vp],
     "gs_insert_request_ceiling_window_size": [_vp, ctypes.POINTER(_sz)],
     "gs_insert_request_ceiling": [_vp, _i64, _vp, _sz, ctypes.POINTER(_f32), _vp],
     "gs_query_request_ceiling": [_vp, _i64, _vp, _sz, ctypes.POINTER(_f32), _vp],
@@ -468,12 +494,16 @@ def _refuse(func: str, msg: str):
     raise GsError(GS_ERR_INVALID_ARG, func, msg)
 
 
+def _fill_codes():
+    torch = _torch()
+    _CODES.update({torch.float32: GS_F32, torch.float16: GS_F16, torch.bfloat16: GS_BF16})
+
+
 def _dtype(func: str, t) -> int:
     if t is None:
         _refuse(func, "the first tensor is missing")
     if not _CODES:
-        torch = _torch()
-        _CODES.update({torch.float32: GS_F32, torch.float16: GS_F16, torch.bfloat16: GS_BF16})
+        _fill_codes()
     code = _CODES.get(t.dtype)
     if code is None:
         _refuse(func, f"dtype {t.dtype} is none of float32, float16, bfloat16")
@@ -744,6 +774,196 @@ def gs_recurrence_step(x, r, i, decay, state, y, slots=None, c: float = 8.0, str
     _check(load_library().gs_recurrence_step(
         xp, xs, rp, rs, ip, istride, _dense(f, "decay", decay, (D,), f32, dev), sp, ss, n,
         _whole(f, "slots", slots, (B,), dev), yp, ys, B, D, code, c, stream), f)
+
+
+# ---- operators of a linear attention layer ------------------------------------------------
+
+_ACTS = {"none": GS_GATE_NONE, "sigmoid": GS_GATE_SIGMOID, "silu": GS_GATE_SILU}
+
+
+def _heads(func: str, name: str, t, shape, dtype, device):
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype is not dtype or t.device != device:
+        _unlike(func, name, t, shape, dtype, device)
+    b, s, h, d = t.stride()
+    if d != 1 and shape[3] > 1:
+        _refuse(func, f"{name}: the elements of a head must be adjacent")
+    return GsHeads(t.data_ptr(), b, s, h)
+
+
+def _head_sizes(func: str, name: str, t, dims: int):
+    if t is None:
+        _refuse(func, f"{name} is missing")
+    if t.dim() != dims:
+        _refuse(func, f"{name} must have {dims} dimensions, got {t.dim()}")
+    return t.shape
+
+
+def gs_rotary(x, out, frequencies, positions=None, first: int = 0, interleaved: bool = False, inverse: bool = False,
+              magnitude: float = 1.0, stream=None) -> None:
+    """Turns the pairs of each head of x [B][T][H][D] by position * frequency; out may be x."""
+    f = "gs_rotary"
+    code = _dtype(f, x)
+    shape = B, T, H, D = _head_sizes(f, "x", x, 4)
+    stream = _launch_stream(f, x, stream)
+    dtype, dev = x.dtype, x.device
+    if frequencies is None or frequencies.dim() != 1:
+        _refuse(f, "frequencies must have one dimension")
+    R = 2 * frequencies.shape[0]
+    _check(load_library().gs_rotary(
+        _heads(f, "x", x, shape, dtype, dev), _heads(f, "out", out, shape, dtype, dev),
+        _dense(f, "frequencies", frequencies, (R // 2,), _torch().float64, dev), _whole(f, "positions", positions, (B, T), dev),
+        first, B, T, H, D, R, code, int(interleaved), int(inverse), magnitude, stream), f)
+
+
+def gs_rotary_frequencies(R: int, base: float = 10000.0, factor: float = 1.0, original: float = 0.0, low: float = 1.0,
+                          high: float = 32.0):
+    """The R / 2 frequencies as an fp64 tensor on the host."""
+    out = _torch().empty(max(R, 0) // 2, dtype=_torch().float64)
+    _check(load_library().gs_rotary_frequencies(R, base, factor, original, low, high, out.data_ptr()), "gs_rotary_frequencies")
+    return out
+
+
+def gs_linear_attention_workspace_size(B: int, T: int, H: int, K: int, Dk: int, Dv: int, dtype, backward: bool = False,
+                                       packed: bool = False) -> int:
+    """Bytes of workspace for B sequences; T is the tokens of a row, or, packed, of all sequences."""
+    f, out = "gs_linear_attention_workspace_size", _sz()
+    if not _CODES:
+        _fill_codes()
+    if dtype not in _CODES:
+        _refuse(f, f"dtype {dtype} is none of float32, float16, bfloat16")
+    _check(load_library().gs_linear_attention_workspace_size(B, T, H, K, Dk, Dv, _CODES[dtype], int(backward), int(packed),
+                                                             ctypes.byref(out)), f)
+    return out.value
+
+
+def _attention_sizes(func: str, q, k, v, offsets):
+    """(sequences, rows, T, H, K, Dk, Dv)"""
+    (rows, T, H, Dk), K, Dv = _head_sizes(func, "q", q, 4), _head_sizes(func, "k", k, 4)[2], _head_sizes(func, "v", v, 4)[3]
+    if offsets is None:
+        return rows, rows, T, H, K, Dk, Dv
+    if rows != 1:
+        _refuse(func, f"with offsets, tensors have one row of tokens, got {rows}")
+    if offsets.dim() != 1 or offsets.shape[0] < 1:
+        _refuse(func, "offsets must have one dimension of at least one entry")
+    return offsets.shape[0] - 1, rows, T, H, K, Dk, Dv
+
+
+def gs_linear_attention_forward(q, k, v, log_decay, o, workspace, s0=None, lengths=None, offsets=None, s_last=None,
+                                scale: float = 1.0, workspace_bytes=None, stream=None) -> None:
+    """o [B][T][H][Dv] of linear attention with a decay for each head; q [B][T][H][Dk], k and v with K heads.
+    With offsets [sequences + 1], B is 1 and the sequences lie one after another."""
+    f = "gs_linear_attention_forward"
+    code = _dtype(f, q)
+    B, rows, T, H, K, Dk, Dv = _attention_sizes(f, q, k, v, offsets)
+    stream = _launch_stream(f, q, stream)
+    dtype, dev, f32 = q.dtype, q.device, _torch().float32
+    wp, wn = _room(f, "workspace", workspace, dev, workspace_bytes)
+    state = (B, H, Dk, Dv)
+    _check(load_library().gs_linear_attention_forward(
+        _heads(f, "q", q, (rows, T, H, Dk), dtype, dev), _heads(f, "k", k, (rows, T, K, Dk), dtype, dev),
+        _heads(f, "v", v, (rows, T, K, Dv), dtype, dev), _dense(f, "log_decay", log_decay, (H,), f32, dev),
+        _dense(f, "s0", s0, state, f32, dev), _whole(f, "lengths", lengths, (B,), dev),
+        _whole(f, "offsets", offsets, (B + 1,), dev), _heads(f, "o", o, (rows, T, H, Dv), dtype, dev),
+        _dense(f, "s_last", s_last, state, f32, dev), B, T, H, K, Dk, Dv, code, scale, wp, wn, stream), f)
+
+
+def gs_linear_attention_backward(d_o, q, k, v, log_decay, dq, dk, dv, workspace, s0=None, ds_last=None, lengths=None,
+                                 offsets=None, ds0=None, scale: float = 1.0, workspace_bytes=None, stream=None) -> None:
+    """Gradients of gs_linear_attention_forward from d_o and ds_last and its inputs."""
+    f = "gs_linear_attention_backward"
+    code = _dtype(f, q)
+    B, rows, T, H, K, Dk, Dv = _attention_sizes(f, q, k, v, offsets)
+    stream = _launch_stream(f, q, stream)
+    dtype, dev, f32 = q.dtype, q.device, _torch().float32
+    wp, wn = _room(f, "workspace", workspace, dev, workspace_bytes)
+    state, qs, ks, vs = (B, H, Dk, Dv), (rows, T, H, Dk), (rows, T, K, Dk), (rows, T, K, Dv)
+    _check(load_library().gs_linear_attention_backward(
+        _heads(f, "d_o", d_o, (rows, T, H, Dv), dtype, dev), _heads(f, "q", q, qs, dtype, dev),
+        _heads(f, "k", k, ks, dtype, dev), _heads(f, "v", v, vs, dtype, dev),
+        _dense(f, "log_decay", log_decay, (H,), f32, dev), _dense(f, "s0", s0, state, f32, dev),
+        _dense(f, "ds_last", ds_last, state, f32, dev), _whole(f, "lengths", lengths, (B,), dev),
+        _whole(f, "offsets", offsets, (B + 1,), dev), _heads(f, "dq", dq, qs, dtype, dev), _heads(f, "dk", dk, ks, dtype, dev),
+        _heads(f, "dv", dv, vs, dtype, dev), _dense(f, "ds0", ds0, state, f32, dev), B, T, H, K, Dk, Dv, code, scale, wp, wn,
+        stream), f)
+
+
+def gs_linear_attention_step(q, k, v, log_decay, state, o, slots=None, scale: float = 1.0, stream=None) -> None:
+    """One token of each of B streams, q [B][H][Dk] and k, v with K heads: states [slots][H][Dk][Dv] in place, and o."""
+    f = "gs_linear_attention_step"
+    code = _dtype(f, q)
+    (B, H, Dk), K, Dv = _head_sizes(f, "q", q, 3), _head_sizes(f, "k", k, 3)[1], _head_sizes(f, "v", v, 3)[2]
+    stream = _launch_stream(f, q, stream)
+    dtype, dev, f32 = q.dtype, q.device, _torch().float32
+    n = _head_sizes(f, "state", state, 4)[0]
+    if state.shape != (n, H, Dk, Dv) or state.dtype is not f32 or state.device != dev:
+        _unlike(f, "state", state, (n, H, Dk, Dv), f32, dev)
+    if n > 0 and not state[0].is_contiguous():
+        _refuse(f, "state: a slot's state must be contiguous")
+
+    def one(name, t, heads, d):
+        return None if t is None else _heads(f, name, t.unsqueeze(1), (B, 1, heads, d), dtype, dev)
+
+    _head_sizes(f, "o", o, 3)
+    _check(load_library().gs_linear_attention_step(
+        one("q", q, H, Dk), one("k", k, K, Dk), one("v", v, K, Dv), _dense(f, "log_decay", log_decay, (H,), f32, dev),
+        state.data_ptr(), state.stride(0) if n > 1 else H * Dk * Dv, n, _whole(f, "slots", slots, (B,), dev), one("o", o, H, Dv),
+        B, H, K, Dk, Dv, code, scale, stream), f)
+
+
+def _act(func: str, name) -> int:
+    if name not in _ACTS:
+        _refuse(func, f"activation {name!r} is none of {', '.join(_ACTS)}")
+    return _ACTS[name]
+
+
+def gs_gated_norm(x, weight, y, rstd, gate=None, residual=None, next_weight=None, z=None, next_rstd=None, groups: int = 1,
+                  activation: str = "silu", scale: float = 1.0, eps: float = 1e-6, stream=None) -> None:
+    """y = residual + scale * act(gate) * norm(x) * weight, the norm over each of `groups` parts of the last
+    dimension (rstd [..., groups]); with next_weight, z = norm(y) * next_weight.  The activation is "none" without a gate."""
+    f = "gs_gated_norm"
+    code, act = _dtype(f, x), _act(f, activation if gate is not None else "none")
+    stream = _launch_stream(f, x, stream)
+    rows, cols = _rows_cols(f, x)
+    shape, dtype, dev, f32 = x.shape, x.dtype, x.device, _torch().float32
+    xp, xs = _matrix(f, "x", x, shape, dtype, dev)
+    gp, gstride = _matrix(f, "gate", gate, shape, dtype, dev)
+    rp, rs = _matrix(f, "residual", residual, shape, dtype, dev)
+    yp, ys = _matrix(f, "y", y, shape, dtype, dev)
+    zp, zs = _matrix(f, "z", z, shape, dtype, dev)
+    _check(load_library().gs_gated_norm(
+        xp, xs, gp, gstride, rp, rs, _dense(f, "weight", weight, (cols,), f32, dev),
+        _dense(f, "next_weight", next_weight, (cols,), f32, dev), yp, ys, zp, zs,
+        _dense(f, "rstd", rstd, (*shape[:-1], groups), f32, dev), _dense(f, "next_rstd", next_rstd, shape[:-1], f32, dev), rows,
+        cols, groups, code, act, scale, eps, stream), f)
+
+
+def gs_gated_norm_workspace_size(rows: int, cols: int, groups: int = 1) -> int:
+    out = _sz()
+    _check(load_library().gs_gated_norm_workspace_size(rows, cols, groups, ctypes.byref(out)), "gs_gated_norm_workspace_size")
+    return out.value
+
+
+def gs_gated_norm_backward(dy, x, weight, rstd, dx, dweight, workspace, gate=None, dgate=None, dz=None, y=None,
+                           next_weight=None, next_rstd=None, dresidual=None, dnext_weight=None, groups: int = 1,
+                           activation: str = "silu", scale: float = 1.0, workspace_bytes=None, stream=None) -> None:
+    """Gradients of gs_gated_norm; dx, dgate and dresidual may be None, and dy too where there is dz."""
+    f = "gs_gated_norm_backward"
+    code, act = _dtype(f, x), _act(f, activation if gate is not None else "none")
+    stream = _launch_stream(f, x, stream)
+    rows, cols = _rows_cols(f, x)
+    shape, dtype, dev, f32 = x.shape, x.dtype, x.device, _torch().float32
+    ap = [v for name, t in (("dy", dy), ("dz", dz), ("x", x), ("gate", gate), ("y", y))
+          for v in _matrix(f, name, t, shape, dtype, dev)]
+    op = [v for name, t in (("dx", dx), ("dgate", dgate), ("dresidual", dresidual))
+          for v in _matrix(f, name, t, shape, dtype, dev)]
+    wp, wn = _room(f, "workspace", workspace, dev, workspace_bytes)
+    _check(load_library().gs_gated_norm_backward(
+        *ap, _dense(f, "weight", weight, (cols,), f32, dev), _dense(f, "next_weight", next_weight, (cols,), f32, dev),
+        _dense(f, "rstd", rstd, (*shape[:-1], groups), f32, dev), _dense(f, "next_rstd", next_rstd, shape[:-1], f32, dev), *op,
+        _dense(f, "dweight", dweight, (cols,), f32, dev), _dense(f, "dnext_weight", dnext_weight, (cols,), f32, dev), rows, cols,
+        groups, code, act, scale, wp, wn, stream), f)
 
 
 def gs_insert_request_ceiling_window_size(sketch: int) -> int:

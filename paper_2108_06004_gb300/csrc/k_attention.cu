@@ -1,0 +1,225 @@
+// A walk of linear attention in fp32 arithmetic, for every type, head size, stride and alignment (see
+// attention.cuh).
+//
+// In blocks of 16 tokens, with w_n = e^(g n), i and j counted from the block's first token and S the state before it:
+//   o_i = out_scale (w_{i+1} S' q_i + sum over j <= i of w_{i-j} (q_i . k_j) v_j),
+//   S  <- w_16 S + in_scale sum over j of w_{15-j} k_j v_j'.
+// (Backwards a token's decay comes after it: w_i for w_{i+1}, and w_{16-j} for w_{15-j}.)
+// A CTA holds 32 columns of one head's state in the registers of its four warps, a quarter of the rows each;
+// two multiply-adds a state element and token, fp32 FMA bound.
+//
+// Long rows are cut into pieces: the pieces' own sums, the states before them, then all outputs.
+#include "attention.cuh"
+
+namespace gs {
+namespace {
+
+constexpr int kTok = 16, kCols = 32, kWarps = 4, kThreadsA = kWarps * 32;
+
+template <typename E>
+__device__ __forceinline__ const E* row_of(const HeadsIn& t, int batch, int64_t token, int head) {
+  return static_cast<const E*>(t.data) + batch * t.batch + token * t.token + head / t.share * t.head;
+}
+
+// SUMS: only the piece's own sum, from a state of zero, into carry.
+template <typename E, typename O, int ROWS, bool SUMS>
+__global__ void __launch_bounds__(kThreadsA)
+k_attention(const __grid_constant__ AttentionParams p) {
+  grid_begin();
+  constexpr int C = kWarps * ROWS;  // contracted rows, with those that do not exist
+  __shared__ __align__(16) float q[SUMS ? 1 : kTok][C], k[kTok][C];
+  __shared__ float v[kTok][kCols], part[SUMS ? 1 : kWarps][kTok][kCols], score[kTok][kTok + 1], power[kTok + 1];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int slices = (p.D + kCols - 1) / kCols;
+  const int slice = blockIdx.x % slices, head = blockIdx.x / slices % p.H, item = blockIdx.x / slices / p.H;
+  Piece w;
+  if (!find_piece(p, item, w)) return;
+  const int c0 = slice * kCols, cols = min(p.D - c0, kCols), col = c0 + lane;
+  const bool mine = lane < cols;
+  const float g = log_decay_of(p, head);
+  if (threadIdx.x <= kTok) power[threadIdx.x] = expf(g * (float)threadIdx.x);
+  float S[ROWS];
+  const int64_t state = ((int64_t)w.sequence * p.H + head) * p.C * p.D;
+  float* carry = p.carry + ((int64_t)item * p.H + head) * p.C * p.D;
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    const int c = warp * ROWS + r;
+    S[r] = 0.f;
+    if (SUMS || c >= p.C || !mine) continue;
+    if (w.opens && w.ends)
+      S[r] = p.first ? p.first[state + c * p.state_row + col * p.state_col] : 0.f;
+    else
+      S[r] = carry[(int64_t)c * p.D + col];
+  }
+  if (SUMS && (w.ends || w.t0 >= w.length)) return;  // nothing comes after it
+  if (!SUMS && !p.offsets) {                          // tokens past the row's length
+    for (int t = max(w.t0, w.length) + warp; t < min((int64_t)w.t0 + p.segment, p.T); t += kWarps)
+      if (mine)
+        static_cast<O*>(p.o.data)[w.batch * p.o.batch + t * p.o.token + head * p.o.head + col] = from_f32<O>(0.f);
+  }
+  const int after = p.back ? 0 : 1;
+  for (int t0 = w.t0; t0 < w.t1; t0 += kTok) {
+    const int n = min(kTok, w.t1 - t0);
+    const auto token = [&](int j) { return w.start + (p.back ? w.length - 1 - (t0 + j) : t0 + j); };
+    __syncthreads();
+    for (int at = threadIdx.x; at < kTok * C; at += kThreadsA) {
+      const int j = at / C, c = at % C;
+      const bool some = j < n && c < p.C;
+      k[j][c] = some ? to_f32(row_of<E>(p.k, w.batch, token(j), head)[c]) : 0.f;
+      if constexpr (!SUMS) q[j][c] = some ? to_f32(row_of<E>(p.q, w.batch, token(j), head)[c]) : 0.f;
+    }
+    for (int j = warp; j < kTok; j += kWarps)
+      v[j][lane] = j < n && mine ? to_f32(row_of<E>(p.v, w.batch, token(j), head)[col]) : 0.f;
+    __syncthreads();
+    if constexpr (!SUMS) {
+      // each thread two scores, those above the diagonal zero
+      for (int at = threadIdx.x; at < kTok * kTok; at += kThreadsA) {
+        const int i = at / kTok, j = at % kTok;
+        float sum = 0.f;
+        if (j <= i) {
+#pragma unroll 8
+          for (int c = 0; c < C; c += 4) {
+            const float4 a = *reinterpret_cast<const float4*>(&q[i][c]), b = *reinterpret_cast<const float4*>(&k[j][c]);
+            sum = fmaf(a.x, b.x, fmaf(a.y, b.y, fmaf(a.z, b.z, fmaf(a.w, b.w, sum))));
+          }
+          sum *= power[i - j] * p.in_scale;
+        }
+        score[i][j] = sum;
+      }
+      float o[kTok];
+#pragma unroll
+      for (int i = 0; i < kTok; ++i) o[i] = 0.f;
+#pragma unroll
+      for (int r = 0; r < ROWS; r += 4)
+#pragma unroll
+        for (int i = 0; i < kTok; ++i) {
+          const float4 a = *reinterpret_cast<const float4*>(&q[i][warp * ROWS + r]);
+          o[i] = fmaf(a.x, S[r], fmaf(a.y, S[r + 1], fmaf(a.z, S[r + 2], fmaf(a.w, S[r + 3], o[i]))));
+        }
+#pragma unroll
+      for (int i = 0; i < kTok; ++i) part[warp][i][lane] = o[i];
+    }
+    const Decay d = decay_of(g * (float)n);
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) S[r] = decayed(S[r], d, 0.f);
+#pragma unroll 4
+    for (int j = 0; j < kTok; ++j) {
+      const float x = j < n ? v[j][lane] * (p.in_scale * power[n - j - after]) : 0.f;
+#pragma unroll
+      for (int r = 0; r < ROWS; r += 4) {
+        const float4 a = *reinterpret_cast<const float4*>(&k[j][warp * ROWS + r]);
+        S[r] = fmaf(a.x, x, S[r]);
+        S[r + 1] = fmaf(a.y, x, S[r + 1]);
+        S[r + 2] = fmaf(a.z, x, S[r + 2]);
+        S[r + 3] = fmaf(a.w, x, S[r + 3]);
+      }
+    }
+    if constexpr (!SUMS) {
+      __syncthreads();
+      for (int i = warp; i < n; i += kWarps) {
+        float sum = 0.f, near = 0.f;
+#pragma unroll
+        for (int q = 0; q < kWarps; ++q) sum += part[q][i][lane];
+        for (int j = 0; j <= i; ++j) near = fmaf(score[i][j], v[j][lane], near);
+        sum = fmaf(sum, power[i + after], near) * p.out_scale;
+        if (mine)
+          static_cast<O*>(p.o.data)[w.batch * p.o.batch + token(i) * p.o.token + head * p.o.head + col] = from_f32<O>(sum);
+      }
+    }
+  }
+  if (!SUMS && (!w.ends || !p.last)) return;
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    const int c = warp * ROWS + r;
+    if (c >= p.C || !mine) continue;
+    if (SUMS)
+      carry[(int64_t)c * p.D + col] = S[r];
+    else
+      p.last[state + c * p.state_row + col * p.state_col] = S[r];
+  }
+}
+
+// The states before a sequence's pieces from the pieces' own sums, in their place.
+__global__ void __launch_bounds__(256)
+k_attention_carry(const __grid_constant__ AttentionParams p) {
+  grid_begin();
+  const int64_t size = (int64_t)p.C * p.D;
+  const int blocks = (int)((size + 255) / 256), row = blockIdx.x / blocks;
+  const int sequence = row / p.H, head = row % p.H;
+  const int length = length_of(p, sequence), n = pieces_of(length, p.segment);
+  const int64_t item0 = p.offsets ? pieces_before(p, sequence) : (int64_t)sequence * p.segments;
+  const Decay d = decay_of(log_decay_of(p, head) * (float)p.segment);
+  const int64_t at = (int64_t)(blockIdx.x % blocks) * 256 + threadIdx.x;
+  if (at >= size) return;
+  const int64_t c = at / p.D, e = at % p.D;
+  float S = p.first ? p.first[((int64_t)sequence * p.H + head) * size + c * p.state_row + e * p.state_col] : 0.f;
+  for (int k = 0; k + 1 < n && item0 + k < p.items; ++k) {
+    float* x = p.carry + ((item0 + k) * p.H + head) * size + at;
+    const float u = *x;
+    *x = S;
+    S = decayed(S, d, u);
+  }
+  if (n > 1 && item0 + n - 1 < p.items) p.carry[((item0 + n - 1) * p.H + head) * size + at] = S;
+}
+
+template <typename E>
+__global__ void __launch_bounds__(256)
+k_head_sums(const __grid_constant__ HeadSumParams p) {
+  grid_begin();
+  const int64_t n = p.B * p.T * p.K * p.D;
+  for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < n; at += (int64_t)gridDim.x * 256) {
+    const int64_t row = at / p.D, d = at % p.D, token = row / p.K, t = token % p.T, b = token / p.T;
+    if (p.offsets && (t < p.offsets[0] || t >= p.offsets[p.sequences])) continue;
+    const float* x = p.part + row * p.share * p.D + d;
+    float sum = 0.f;
+    for (int k = 0; k < p.share; ++k) sum += x[(int64_t)k * p.D];
+    static_cast<E*>(p.out.data)[b * p.out.batch + t * p.out.token + row % p.K * p.out.head + d] = from_f32<E>(sum);
+  }
+}
+
+template <typename E, typename O, int ROWS>
+cudaError_t walk(AttentionParams& p, cudaStream_t s) {
+  const dim3 grid((unsigned)((int64_t)p.items * p.H * ((p.D + kCols - 1) / kCols)));
+  if (p.segments > 1) {
+    cudaError_t e = launch(k_attention<E, O, ROWS, true>, grid, dim3(kThreadsA), s, p);
+    if (e != cudaSuccess) return e;
+    const dim3 states((unsigned)(((int64_t)p.C * p.D + 255) / 256 * p.B * p.H));
+    e = launch(k_attention_carry, states, dim3(256), s, p);
+    if (e != cudaSuccess) return e;
+  }
+  return launch(k_attention<E, O, ROWS, false>, grid, dim3(kThreadsA), s, p);
+}
+
+}  // namespace
+
+AttentionShape attention_shape(int64_t B, int64_t T, int64_t H, int C, int D, int dtype, bool packed) {
+  AttentionShape shape;
+  const int64_t rows = packed ? 1 : B;
+  const int64_t ctas = rows * H * ((D + kCols - 1) / kCols);
+  // about four CTAs an SM, in pieces of 128 tokens or more
+  int64_t segment = ctas > 0 ? (T * ctas + 4 * kSMs - 1) / (4 * kSMs) : T;
+  segment = segment < 128 ? 128 : (segment + 127) / 128 * 128;
+  if (segment >= T) segment = T > 0 ? T : 1;
+  shape.segment = (int32_t)segment;
+  shape.segments = (int32_t)(T > 0 ? (T + segment - 1) / segment : 1);
+  shape.items = packed ? B + T / segment : B * shape.segments;
+  return shape;
+}
+
+cudaError_t launch_attention(AttentionParams& p, int dtype, bool wide, cudaStream_t s) {
+  const auto rows = [&](auto e, auto o) {
+    using E = decltype(e);
+    using O = decltype(o);
+    return p.C <= 32 ? walk<E, O, 8>(p, s) : p.C <= 64 ? walk<E, O, 16>(p, s) : p.C <= 128 ? walk<E, O, 32>(p, s) : walk<E, O, 64>(p, s);
+  };
+  return with_type(dtype, [&](auto e) { return wide ? rows(e, float()) : rows(e, e); });
+}
+
+cudaError_t launch_head_sums(const HeadSumParams& p, int dtype, cudaStream_t s) {
+  const int64_t n = (p.B * p.T * p.K * p.D + 255) / 256;
+  return with_type(dtype, [&](auto e) {
+    return launch(k_head_sums<decltype(e)>, dim3((unsigned)(n < kSMs * 8 ? n : kSMs * 8)), dim3(256), s, p);
+  });
+}
+
+}  // namespace gs
