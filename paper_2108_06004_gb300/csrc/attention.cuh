@@ -154,7 +154,12 @@ struct AttentionShape {
   int32_t segment, segments;
   int64_t items;
 };
+// The pieces of a walk.  Walks for the tensor cores have blocks of 128 tokens.
+inline bool for_tensor_cores(int C, int D, int dtype) { return dtype != GS_F32 && C <= 128 && C % 8 == 0 && D % 8 == 0; }
 AttentionShape attention_shape(int64_t B, int64_t T, int64_t H, int C, int D, int dtype, bool packed);
+cudaError_t launch_attention_carry(const AttentionParams& p, cudaStream_t s);
+// The walk on the tensor cores, where for_tensor_cores; not taken where a tensor's strides do not allow it.
+cudaError_t launch_attention_mma(const AttentionParams& p, int dtype, bool wide, cudaStream_t s, bool& taken);
 // One walk; o is fp32 where `wide`, for heads that are summed after.
 cudaError_t launch_attention(AttentionParams& p, int dtype, bool wide, cudaStream_t s);
 cudaError_t launch_head_sums(const HeadSumParams& p, int dtype, cudaStream_t s);

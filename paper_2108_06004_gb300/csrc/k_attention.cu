@@ -183,8 +183,7 @@ cudaError_t walk(AttentionParams& p, cudaStream_t s) {
   if (p.segments > 1) {
     cudaError_t e = launch(k_attention<E, O, ROWS, true>, grid, dim3(kThreadsA), s, p);
     if (e != cudaSuccess) return e;
-    const dim3 states((unsigned)(((int64_t)p.C * p.D + 255) / 256 * p.B * p.H));
-    e = launch(k_attention_carry, states, dim3(256), s, p);
+    e = launch_attention_carry(p, s);
     if (e != cudaSuccess) return e;
   }
   return launch(k_attention<E, O, ROWS, false>, grid, dim3(kThreadsA), s, p);
@@ -192,12 +191,21 @@ cudaError_t walk(AttentionParams& p, cudaStream_t s) {
 
 }  // namespace
 
+cudaError_t launch_attention_carry(const AttentionParams& p, cudaStream_t s) {
+  return launch(k_attention_carry, dim3((unsigned)(((int64_t)p.C * p.D + 255) / 256 * p.B * p.H)), dim3(256), s, p);
+}
+
 AttentionShape attention_shape(int64_t B, int64_t T, int64_t H, int C, int D, int dtype, bool packed) {
   AttentionShape shape;
-  const int64_t rows = packed ? 1 : B;
-  const int64_t ctas = rows * H * ((D + kCols - 1) / kCols);
-  // about four CTAs an SM, in pieces of 128 tokens or more
-  int64_t segment = ctas > 0 ? (T * ctas + 4 * kSMs - 1) / (4 * kSMs) : T;
+  const bool mma = for_tensor_cores(C, D, dtype);
+  const int columns = mma ? (D <= 64 ? 64 : 128) : kCols;
+  const int64_t heads = H * ((D + columns - 1) / columns), ctas = (packed ? 1 : B) * heads;
+  // CTAs that run at once
+  const int64_t slots = (int64_t)kSMs * (!mma ? 4 : C <= 64 && D <= 64 ? 2 : 1);
+  // Rows are cut where there are too few of them: keys and values are then read twice, which costs about
+  // six tenths of a walk.  Packed sequences are of any length: those longer than a CTA's fair share are cut.
+  int64_t segment = T;
+  if (packed || ctas * 16 < slots * 10) segment = (T * ctas + slots - 1) / slots;
   segment = segment < 128 ? 128 : (segment + 127) / 128 * 128;
   if (segment >= T) segment = T > 0 ? T : 1;
   shape.segment = (int32_t)segment;
@@ -207,6 +215,11 @@ AttentionShape attention_shape(int64_t B, int64_t T, int64_t H, int C, int D, in
 }
 
 cudaError_t launch_attention(AttentionParams& p, int dtype, bool wide, cudaStream_t s) {
+  if (for_tensor_cores(p.C, p.D, dtype)) {
+    bool taken;
+    const cudaError_t e = launch_attention_mma(p, dtype, wide, s, taken);
+    if (taken || e != cudaSuccess) return e;
+  }
   const auto rows = [&](auto e, auto o) {
     using E = decltype(e);
     using O = decltype(o);

@@ -312,3 +312,10 @@ def test_steps_continue_a_prompt(gs):
     exact = host(whole)
     close(part, exact, layer_bounds.stored(exact, tol, "bf16") + 2.0 ** -8 * np.abs(exact), "o")
     assert float((state - last).norm() / last.norm()) < 2e-6
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_every_multiprocessor_is_shared(gs, D, dtype):
+    """More heads than CTAs that run at once."""
+    Case(gs, 4, 300, 80, 80, D, D, dtype).check()
