@@ -13,8 +13,8 @@
 // size, so its parts are taken from values scaled by powers of two: block by block bounds of all of them follow from the
 // largest |q|, |k| and |v|, and the scales from the bounds.
 //
-// Eight warps do the arithmetic between the products; a thread of a ninth issues products and loads (three more are there
-// because registers can be moved from four warps to others only).  In a
+// Eight or sixteen warps do the arithmetic between the products; a thread of one more issues products and loads (three
+// others are there because registers can be moved from four warps at once only).  In a
 // block: parts of S (and S decayed) | Q S runs: A | O scaled | A V runs: weighted keys of the first 64
 // tokens | of the others | K V and the next scores run: o is stored.  A lane of tensor memory is a token for P, A and O and
 // a row of the state for S and the weighted keys.
@@ -30,26 +30,28 @@ namespace {
 
 using namespace tc;
 
-constexpr int kBlockTokens = 128, kWorkers = 256, kMmaThreads = kWorkers + 128;
+constexpr int kBlockTokens = 128;
 
 struct AttentionMmaParams {
   CUtensorMap q, k, v;
   AttentionParams a;
 };
 
-// C rows of the state (64 or 128) and D columns of it a CTA; with 64 columns, tensor memory for two CTAs.
+// C rows of the state (64 or 128) and D columns of it a CTA.  The smallest one leaves room for two CTAs an SM.
 template <int C, int D>
 struct Plan {
-  static constexpr bool kNarrow = D == 64;
-  static constexpr int kColumns = kNarrow ? 256 : 512;
-  // CTAs of an SM, and registers: all threads have the same number at first, and then the workers more and the others
-  // fewer, whose sum is at most as many.
-  static constexpr int kCtas = kNarrow && C == 64 ? 2 : 1;
-  static constexpr int kAtFirst = kCtas == 2 ? 80 : 168, kWorker = kCtas == 2 ? 96 : 224, kOther = kCtas == 2 ? 48 : 56;
-  static_assert(2 * kWorker + kOther <= 3 * kAtFirst, "more registers than the CTA has");
-  // columns: the block's own sum of keys and values, O, P (A takes its place), and the weighted keys of either half
-  // of the block.  Narrow: these take the place of O and P, when o has been read.
-  static constexpr int U = 0, O = D, P = 2 * D, W0 = kNarrow ? 64 : 384, W1 = kNarrow ? 160 : 256;
+  static constexpr bool kNarrow = C == 64 && D == 64;
+  static constexpr int kCtas = kNarrow ? 2 : 1, kColumns = 512 / kCtas;
+  // Worker warps in groups of four; a group takes 1 / kGroups of the columns.  All threads have the same number of
+  // registers at first, and then the workers more and the others fewer, whose sum is at most as many.
+  static constexpr int kGroups = D == 64 ? 2 : 4, kWorkers = 128 * kGroups, kThreads = kWorkers + 128;
+  static constexpr int kAtFirst = kNarrow ? 80 : D == 64 ? 168 : 96, kWorker = kNarrow ? 96 : D == 64 ? 224 : 112,
+                       kOther = kNarrow ? 48 : D == 64 ? 56 : 32;
+  static_assert(kGroups * kWorker + kOther <= (kGroups + 1) * kAtFirst, "more registers than the CTA has");
+  // columns: the block's own sum of keys and values, O, P (A takes its place), and the weighted keys: of either half of
+  // the block, as many of 32 as they have parts.  Narrow, they take the place of O and P when o has been read; three
+  // parts of the second half that of P.
+  static constexpr int U = 0, O = kNarrow ? 64 : 128, P = kNarrow ? 128 : 256, W0 = kNarrow ? 64 : 384;
   static constexpr int kPanel = kBlockTokens * 128;  // bytes of 64 columns of a block
   static constexpr int kQ = C / 64 * kPanel, kV = D / 64 * kPanel, kPart = C * D * 2;
   static constexpr int oQ = 0, oK = kQ, oV = oK + 2 * kQ, oS = oV + 2 * kV, oTables = oS + 2 * kPart;
@@ -59,14 +61,17 @@ struct Tables {
   float weight[256];  // in out w_d of a score at weight[128 + row - column], zero past the diagonal
   float power[129];   // w_n
   alignas(16) float key[128];  // of a row's weighted key, zero past the block's tokens
-  uint64_t q_full, kv_full[2], scores, read, done, summed, state_ready, a_ready, w_ready[2], trimmed;
+  uint64_t q_full, kv_full[2], scores, read, done, summed, state_ready, a_ready, w_ready[2];
   uint32_t tmem;
   int largest[3][3], first;  // fp16: of |q|, |k|, |v| in a block, three blocks in turn; of the first state
 };
 static_assert(sizeof(Tables) <= 3072, "tables do not fit");
 static_assert(Plan<128, 128>::kBytes <= 232448, "a CTA's shared memory");
 
-__device__ __forceinline__ void worker_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+template <int WORKERS>
+__device__ __forceinline__ void sync_workers() {
+  asm volatile("bar.sync 1, %0;" ::"n"(WORKERS) : "memory");
+}
 
 // v as a sum of N parts of the type; part n of two adjacent values.
 template <typename E>
@@ -87,14 +92,15 @@ __device__ __forceinline__ int exponent_of(float bound) {
 }
 __device__ __forceinline__ float power_of_two(int n) { return __uint_as_float((uint32_t)(min(max(n, -126), 126) + 127) << 23); }
 
-// SUMS: only the piece's own sum, from a state of zero, into carry.
-template <typename E, typename R, int C, int D, bool SUMS>
-__global__ void __launch_bounds__(kMmaThreads, Plan<C, D>::kCtas)
+// PARTS: of a weighted key.  SUMS: only the piece's own sum, from a state of zero, into carry.
+template <typename E, typename R, int C, int D, int PARTS, bool SUMS>
+__global__ void __launch_bounds__(Plan<C, D>::kThreads, Plan<C, D>::kCtas)
 k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   using L = Plan<C, D>;
   constexpr bool HALF = std::is_same<E, __half>::value;
-  constexpr int PARTS = HALF ? 2 : 3;
+  constexpr int kWorkers = L::kWorkers, COLS = D / L::kGroups;  // columns of a thread
+  constexpr int W1 = L::kNarrow || PARTS == 2 ? L::W0 + 32 * PARTS : L::P;
   extern __shared__ __align__(1024) char base[];
   Tables& tab = *reinterpret_cast<Tables*>(base + L::oTables);
   const AttentionParams& p = params.a;
@@ -118,14 +124,14 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
     barrier_init(&tab.kv_full[0], 1);
     barrier_init(&tab.kv_full[1], 1);
     for (uint64_t* b : {&tab.scores, &tab.read, &tab.done, &tab.summed}) barrier_init(b, 1);
-    for (uint64_t* b : {&tab.state_ready, &tab.a_ready, &tab.w_ready[0], &tab.w_ready[1], &tab.trimmed}) barrier_init(b, kWorkers);
+    for (uint64_t* b : {&tab.state_ready, &tab.a_ready, &tab.w_ready[0], &tab.w_ready[1]}) barrier_init(b, kWorkers);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 8) tmem_alloc<L::kColumns>(&tab.tmem);
+  if (warp == kWorkers / 32) tmem_alloc<L::kColumns>(&tab.tmem);
   if (threadIdx.x < 9) tab.largest[threadIdx.x / 3][threadIdx.x % 3] = 0;
   if (threadIdx.x == 9) tab.first = 0;
   if (threadIdx.x < 129) tab.power[threadIdx.x] = expf(g * (float)threadIdx.x);
-  if (threadIdx.x < kWorkers) {
+  if (threadIdx.x < 256) {
     const int d = p.back ? 128 - (int)threadIdx.x : (int)threadIdx.x - 128;  // tokens from a key to a query
     tab.weight[threadIdx.x] = d >= 0 ? expf(g * (float)d) * p.in_scale * p.out_scale : 0.f;
   }
@@ -136,7 +142,7 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
   const uint32_t tmem = tab.tmem;
   bool lost = false;
 
-  if (warp >= 8) {
+  if (threadIdx.x >= kWorkers) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::kOther));
     if (threadIdx.x == kWorkers && blocks > 0) {
       const auto load_kv = [&](int n) {
@@ -153,64 +159,78 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
           tile_load(base + L::oQ + j * L::kPanel, &params.q, j * 64, head / p.q.share, (int)first_token(n), w.batch, &tab.q_full);
       };
       const uint32_t q = matrix(shared_address(base + L::oQ), 0), parts = matrix(shared_address(base + L::oS), C * 128);
-      const auto score = [&](int n) {
+      const auto values = [&](int n) { return matrix(shared_address(base + L::oV + (n & 1) * L::kV), L::kPanel); };
+      // U = K' V of block n
+      const auto sum = [&](int n) {
+        const uint32_t v = values(n);
         barrier_wait(&tab.kv_full[n & 1], n >> 1, lost);
-        if (!SUMS) barrier_wait(&tab.q_full, n, lost);
-        if (tokens(n) < kBlockTokens) barrier_wait(&tab.trimmed, 0, lost);
-        if (SUMS) return;
+        each<2>([&](auto which) {
+          constexpr int h = decltype(which)::value;
+          barrier_wait(&tab.w_ready[h], n, lost);
+          after_sync();
+          each<4 * PARTS>([&](auto step) {  // the smallest parts first, while the sum is small
+            constexpr int part = PARTS - 1 - decltype(step)::value / 4, j = decltype(step)::value % 4;
+            multiply_t<(h ? W1 : L::W0) + part * 32 + j * 8, (h * 4 + j) * 2048>(tmem + L::U, tmem, v, product<E>(D, true),
+                                                                                            h > 0 || decltype(step)::value > 0);
+          });
+        });
+        commit(&tab.summed);
+      };
+      // P = Q K' of block n.  Its place is free when the products that read it are done: only products with the same
+      // sum are ordered among themselves.
+      const auto score = [&](int n) {
         const uint32_t k = matrix(shared_address(base + L::oK + (n & 1) * L::kQ), 0);
+        barrier_wait(&tab.q_full, n, lost);
         each<C / 16>([&](auto step) {
           constexpr int j = decltype(step)::value, at = j / 4 * L::kPanel + j % 4 * 32;
           multiply<at, at>(tmem + L::P, q, k, product<E>(128, false), j > 0);
         });
         commit(&tab.scores);
       };
+      constexpr bool APART = !L::kNarrow && PARTS == 2;  // the weighted keys are not in P's place
       load_kv(0);
       if (!SUMS) load_q(0);
       if (blocks > 1) load_kv(1);
-      score(0);
-      for (int n = 0; n < blocks; ++n) {
-        const uint32_t v = matrix(shared_address(base + L::oV + (n & 1) * L::kV), L::kPanel);
-        barrier_wait(&tab.state_ready, n, lost);
-        after_sync();
-        if (!SUMS) {
+      sum(0);
+      if constexpr (SUMS) {
+        for (int n = 1; n < blocks; ++n) {
+          barrier_wait(&tab.summed, n - 1, lost);
+          if (n + 1 < blocks) load_kv(n + 1);
+          sum(n);
+        }
+      } else {
+        if (!APART) barrier_wait(&tab.summed, 0, lost);
+        score(0);
+        for (int n = 0; n < blocks; ++n) {
+          barrier_wait(&tab.state_ready, n, lost);
+          after_sync();
           each<C / 8>([&](auto step) {
             constexpr int part = decltype(step)::value / (C / 16), j = decltype(step)::value % (C / 16);
             multiply<j / 4 * L::kPanel + j % 4 * 32, part * L::kPart + j * 2048>(tmem + L::O, q, parts, product<E>(D, true), part + j > 0);
           });
           commit(&tab.read);
-        }
-        // the keys and values of the block before have been used: state_ready comes after `summed`
-        if (n > 0 && n + 1 < blocks) load_kv(n + 1);
-        if (!SUMS) {
           if (n + 1 < blocks) {
             barrier_wait(&tab.read, n, lost);
             load_q(n + 1);
           }
           barrier_wait(&tab.a_ready, n, lost);
           after_sync();
+          const uint32_t v = values(n);
           each<16>([&](auto step) {
             constexpr int part = decltype(step)::value / 8, j = decltype(step)::value % 8;
             multiply_t<j / 2 * 32 + part * 16 + j % 2 * 8, j * 2048>(tmem + L::O, tmem + L::P, v, product<E>(D, true), true);
           });
           commit(&tab.done);
-        }
-        each<2>([&](auto half) {
-          constexpr int h = decltype(half)::value;
-          barrier_wait(&tab.w_ready[h], n, lost);
-          after_sync();
-          each<4 * PARTS>([&](auto step) {  // the smallest parts first, while the sum is small
-            constexpr int part = PARTS - 1 - decltype(step)::value / 4, j = decltype(step)::value % 4;
-            multiply_t<(h ? L::W1 : L::W0) + part * 32 + j * 8, (h * 4 + j) * 2048>(tmem + L::U, tmem, v, product<E>(D, true),
-                                                                                     h > 0 || decltype(step)::value > 0);
-          });
-        });
-        commit(&tab.summed);
-        if (n + 1 < blocks) {
-          // the scores' place is free when the products that read it are done: only products with the same sum are
-          // ordered among themselves
-          barrier_wait(&tab.summed, n, lost);
+          if (n + 1 >= blocks) break;
+          if (APART) {
+            sum(n + 1);
+            barrier_wait(&tab.done, n, lost);
+          } else {
+            sum(n + 1);
+            barrier_wait(&tab.summed, n + 1, lost);
+          }
           score(n + 1);
+          if (n + 2 < blocks) load_kv(n + 2);  // in the place of block n's, whose last product is done
         }
       }
     }
@@ -220,7 +240,7 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
       barrier_wait(bar, phase, lost);
       lost = __any_sync(0xFFFFFFFFu, lost);
     };
-    const int quad = warp & 3, half = warp >> 2, row = quad * 32 + lane;
+    const int quad = warp & 3, group = warp >> 2, row = quad * 32 + lane, col0 = group * COLS;
     const uint32_t mine = tmem + ((uint32_t)(quad * 32) << 16);
     const bool holds = quad * 32 < C;  // rows of the state
     const int64_t state = ((int64_t)w.sequence * p.H + head) * p.C * p.D;
@@ -228,18 +248,18 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
     const float nan = __uint_as_float(0x7FC00000u);
     if (!SUMS && !p.offsets) {  // tokens past the row's length
       const int64_t until = min((int64_t)w.t0 + p.segment, p.T);
-      for (int64_t t = max(w.t0, w.length) + warp; t < until; t += 8)
+      for (int64_t t = max(w.t0, w.length) + warp; t < until; t += kWorkers / 32)
         for (int d = lane; d < D && c0 + d < p.D; d += 32)
           static_cast<R*>(p.o.data)[w.batch * p.o.batch + t * p.o.token + head * p.o.head + c0 + d] = from_f32<R>(0.f);
     }
-    // the state: this thread's row, half of the CTA's columns
-    float S[D / 2];
+    // the state: this thread's row, the group's columns
+    float S[COLS];
     float bound = 0.f;
     if (holds) {
       float most = 0.f;
 #pragma unroll
-      for (int j = 0; j < D / 2; ++j) {
-        const int col = c0 + half * (D / 2) + j;
+      for (int j = 0; j < COLS; ++j) {
+        const int col = c0 + col0 + j;
         S[j] = 0.f;
         if (!SUMS && row < p.C && col < p.D) {
           if (!(w.opens && w.ends))
@@ -251,168 +271,189 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
       }
       if (HALF && !SUMS) atomicMax(&tab.first, __float_as_int(most));
     }
-    int u_scale = 0;  // of what the last block adds to the state
-    Decay decay = {1.f, 0.f};
-    // the state after the last block
-    const auto advance = [&] {
+    // the largest |x| of a tile's first rows
+    const auto largest = [&](const char* tile, int bytes, int rows, int* to) {
+      __half2 most = __float2half2_rn(0.f);
+      for (int at = threadIdx.x * 16; at < bytes; at += kWorkers * 16) {
+        if (at / 128 % kBlockTokens >= rows) continue;
+        const uint4 x = *reinterpret_cast<const uint4*>(tile + at);
+        const __half2* h = reinterpret_cast<const __half2*>(&x);
 #pragma unroll
-      for (int b = 0; b < D / 64; ++b) {
-        uint32_t x[32];
-        tmem_load(x, mine + L::U + half * (D / 2) + b * 32);
-        const float grow = HALF ? power_of_two(u_scale) : 1.f;
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          const float u = __uint_as_float(x[j]);
-          S[b * 32 + j] = decayed(S[b * 32 + j], decay, HALF ? u * grow : u);
-        }
+        for (int j = 0; j < 4; ++j) most = __hmax2(most, __habs2(h[j]));
       }
+      float f = fmaxf(__low2float(most), __high2float(most));
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) f = fmaxf(f, __shfl_xor_sync(0xFFFFFFFFu, f, o));
+      if (lane == 0) atomicMax(to, __float_as_int(f));
     };
     if (HALF && blocks > 0) {
-      worker_sync();
+      sync_workers<kWorkers>();
       bound = __int_as_float(tab.first);
     }
     int made = -1;  // tokens that the keys' weights are made for
-    for (int n = 0; n < blocks; ++n) {
-      const int m = tokens(n);
+    // What is known of a block before its keys are weighted, and of the one whose o is being worked out.
+    struct Block {
+      int m, scale;
+      float k, v;
+      Decay decay;
+    } next, now;
+    const auto open = [&](int n) {
+      next.m = tokens(n);
+      next.decay = decay_of(g * (float)next.m);
       char* k = base + L::oK + (n & 1) * L::kQ;
       char* v = base + L::oV + (n & 1) * L::kV;
       wait(&tab.kv_full[n & 1], n >> 1);
-      if (made != m) {
-        if (made >= 0) worker_sync();  // the weights of the block before have been used
-        if (threadIdx.x < 128) tab.key[threadIdx.x] = (int)threadIdx.x < m ? tab.power[p.back ? threadIdx.x + 1 : m - 1 - threadIdx.x] * p.in_scale : 0.f;
-        if (m < kBlockTokens) {
+      if (HALF && threadIdx.x < 3) tab.largest[(n + 1) % 3][threadIdx.x] = 0;  // last read two blocks ago
+      if (made != next.m) {
+        // all threads have met since the weights before were used
+        if (threadIdx.x < 128)
+          tab.key[threadIdx.x] = (int)threadIdx.x < next.m ? tab.power[p.back ? threadIdx.x + 1 : next.m - 1 - threadIdx.x] * p.in_scale : 0.f;
+        if (next.m < kBlockTokens) {
           // rows that are not the block's tokens: zeros, whatever they were
-          if (!SUMS) wait(&tab.q_full, n);
           const auto trim = [&](char* tile, int panels) {
-            for (int at = threadIdx.x; at < panels * (kBlockTokens - m) * 8; at += kWorkers) {
-              const int word = at % 8, r = at / 8 % (kBlockTokens - m), panel = at / 8 / (kBlockTokens - m);
-              *reinterpret_cast<uint4*>(tile + panel * L::kPanel + (m + r) * 128 + word * 16) = make_uint4(0, 0, 0, 0);
-            }
+            const int rows = kBlockTokens - next.m;
+            for (int at = threadIdx.x; at < panels * rows * 8; at += kWorkers)
+              *reinterpret_cast<uint4*>(tile + at / 8 / rows * L::kPanel + (next.m + at / 8 % rows) * 128 + at % 8 * 16) = make_uint4(0, 0, 0, 0);
           };
           trim(k, C / 64);
           trim(v, D / 64);
-          if (!SUMS) trim(base + L::oQ, C / 64);
           shared_fence();
-          barrier_arrive(&tab.trimmed);
         }
-        worker_sync();
-        made = m;
+        if (!HALF) sync_workers<kWorkers>();
       }
-      int a_scale = 0, s_scale = 0, w_scale = 0;
-      const Decay next_decay = decay_of(g * (float)m);
+      next.scale = 0;
       if constexpr (HALF) {
-        if (!SUMS) wait(&tab.q_full, n);
-        const auto largest = [&](const char* tile, int bytes, int* to) {
-          __half2 most = __float2half2_rn(0.f);
-          for (int at = threadIdx.x * 16; at < bytes; at += kWorkers * 16) {
-            const uint4 x = *reinterpret_cast<const uint4*>(tile + at);
-            const __half2* h = reinterpret_cast<const __half2*>(&x);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) most = __hmax2(most, __habs2(h[j]));
-          }
-          float f = fmaxf(__low2float(most), __high2float(most));
-#pragma unroll
-          for (int o = 16; o > 0; o >>= 1) f = fmaxf(f, __shfl_xor_sync(0xFFFFFFFFu, f, o));
-          if (lane == 0) atomicMax(to, __float_as_int(f));
-        };
-        // the next block's set was last read two blocks ago, before all threads met in the last one
-        int* const l = tab.largest[n % 3];
-        if (threadIdx.x < 3) tab.largest[(n + 1) % 3][threadIdx.x] = 0;
-        if (!SUMS) largest(base + L::oQ, L::kQ, l);
-        largest(k, L::kQ, l + 1);
-        largest(v, L::kV, l + 2);
-        worker_sync();
-        const float lq = __int_as_float(l[0]), lk = __int_as_float(l[1]), lv = __int_as_float(l[2]);
-        s_scale = exponent_of(bound);
-        a_scale = exponent_of(lq * lk * (float)C * fabsf(p.in_scale * p.out_scale));
-        w_scale = exponent_of(lk * fabsf(p.in_scale));
-        bound = bound * (next_decay.a + next_decay.b) * 1.0001f + lk * lv * (float)m * fabsf(p.in_scale);
+        if (made != next.m && next.m < kBlockTokens) sync_workers<kWorkers>();
+        largest(k, L::kQ, kBlockTokens, &tab.largest[n % 3][1]);
+        largest(v, L::kV, kBlockTokens, &tab.largest[n % 3][2]);
+        sync_workers<kWorkers>();
+        next.k = __int_as_float(tab.largest[n % 3][1]);
+        next.v = __int_as_float(tab.largest[n % 3][2]);
+        next.scale = exponent_of(next.k * fabsf(p.in_scale));
       }
-      // the state as a factor
-      if (n > 0) {
-        wait(&tab.summed, n - 1);
-        after_sync();
-        if (holds) advance();
-        if (!SUMS) worker_sync();  // the last block's o has left their place
-      }
-      if constexpr (!SUMS) {
-        if (holds) {
-          const float shrink = HALF ? power_of_two(-s_scale) : 1.f;
+      made = next.m;
+    };
+    // the group's weighted keys of either half of block n, transposed: this thread's row of the state
+    constexpr int PAIRS = 32 / L::kGroups;
+    uint32_t part[PARTS][PAIRS];
+    const auto weigh = [&](int n, int h) {
+      if (!holds) return;
+      const char* from = base + L::oK + (n & 1) * L::kQ + row / 64 * L::kPanel + row % 8 * 2;
+      const int t0 = h * 64 + group * 2 * PAIRS, word = row % 64 / 8;
+      const float shrink = HALF ? power_of_two(-next.scale) : 1.f;
 #pragma unroll
-          for (int j = 0; j < D / 16; ++j) {
-            const int col = half * (D / 2) + j * 8;
-            char* to = base + L::oS + col / 64 * (C * 128) + row * 128 + (((col % 64) / 8) ^ (row & 7)) * 16;
-            uint32_t hi[4], lo[4];
+      for (int j = 0; j < PAIRS; ++j) {
+        const int t = t0 + 2 * j;
+        const float2 weight = *reinterpret_cast<const float2*>(&tab.key[t]);
+        float2 f = make_float2(to_f32(*reinterpret_cast<const E*>(from + t * 128 + (word ^ ((2 * j) & 7)) * 16)),
+                               to_f32(*reinterpret_cast<const E*>(from + (t + 1) * 128 + (word ^ ((2 * j + 1) & 7)) * 16)));
+        f.x *= weight.x;
+        f.y *= weight.y;
+        if (HALF) f = make_float2(f.x * shrink, f.y * shrink);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float2 f = make_float2(S[j * 8 + 2 * i], S[j * 8 + 2 * i + 1]);
-              if (HALF) f = make_float2(f.x * shrink, f.y * shrink);
-              hi[i] = part_of<E>(f);
-              lo[i] = part_of<E>(f);
-            }
-            *reinterpret_cast<uint4*>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-            *reinterpret_cast<uint4*>(to + L::kPart) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-          }
-        }
+        for (int i = 0; i < PARTS; ++i) part[i][j] = part_of<E>(f);
       }
-      u_scale = w_scale;
-      decay = next_decay;
-      if (!SUMS) shared_fence();
+    };
+    const auto put = [&](int h) {
+      if (holds) {
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) tmem_store(part[i], mine + (h ? W1 : L::W0) + i * 32 + group * PAIRS);
+        wait_store();
+      }
       before_sync();
-      barrier_arrive(&tab.state_ready);
-      // weighted keys of 32 tokens of either half, transposed: this thread's row of the state
-      const auto weigh = [&](int h) {
-        if (holds) {
-          const char* from = k + row / 64 * L::kPanel + row % 8 * 2;
-          const int t0 = h * 64 + half * 32, word = row % 64 / 8;
-          const float shrink = HALF ? power_of_two(-w_scale) : 1.f;
-          uint32_t part[3][16];
+      barrier_arrive(&tab.w_ready[h]);
+    };
+    // the state after block n
+    const auto advance = [&](int n) {
+      wait(&tab.summed, n);
+      after_sync();
+      if (!holds) return;
+      uint32_t x[32];
+      tmem_load(x, mine + L::U + col0);
+      const float grow = HALF ? power_of_two(now.scale) : 1.f;
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const int t = t0 + 2 * j;
-            const float2 weight = *reinterpret_cast<const float2*>(&tab.key[t]);
-            float2 f = make_float2(to_f32(*reinterpret_cast<const E*>(from + t * 128 + (word ^ ((2 * j) & 7)) * 16)),
-                                   to_f32(*reinterpret_cast<const E*>(from + (t + 1) * 128 + (word ^ ((2 * j + 1) & 7)) * 16)));
-            f.x *= weight.x;
-            f.y *= weight.y;
-            if (HALF) f = make_float2(f.x * shrink, f.y * shrink);
-#pragma unroll
-            for (int i = 0; i < PARTS; ++i) part[i][j] = part_of<E>(f);
-          }
-#pragma unroll
-          for (int i = 0; i < PARTS; ++i) tmem_store(part[i], mine + (h ? L::W1 : L::W0) + i * 32 + half * 16);
-          wait_store();
-        }
-        before_sync();
-        barrier_arrive(&tab.w_ready[h]);
-      };
+      for (int j = 0; j < COLS; ++j) {
+        const float u = __uint_as_float(x[j]);
+        S[j] = decayed(S[j], now.decay, HALF ? u * grow : u);
+      }
+    };
+    if (blocks > 0) {
+      open(0);
+      weigh(0, 0);
+      put(0);
+      weigh(0, 1);
+      put(1);
+      now = next;
+    }
+    for (int n = 0; n < blocks; ++n) {
       if constexpr (SUMS) {
-        weigh(0);
-        weigh(1);
+        if (n + 1 < blocks) open(n + 1);
+        advance(n);
+        if (n + 1 < blocks) {
+          weigh(n + 1, 0);
+          put(0);
+          weigh(n + 1, 1);
+          put(1);
+        }
+        now = next;
         continue;
       }
+      int a_scale = 0, s_scale = 0;
+      if constexpr (HALF) {
+        wait(&tab.q_full, n);
+        largest(base + L::oQ, L::kQ, now.m, &tab.largest[n % 3][0]);
+      }
+      sync_workers<kWorkers>();  // the last block's o has left the place of the parts
+      if constexpr (HALF) {
+        s_scale = exponent_of(bound);
+        a_scale = exponent_of(__int_as_float(tab.largest[n % 3][0]) * now.k * (float)C * fabsf(p.in_scale * p.out_scale));
+        bound = bound * (now.decay.a + now.decay.b) * 1.0001f + now.k * now.v * (float)now.m * fabsf(p.in_scale);
+      }
+      // the state as a factor
+      if (holds) {
+        const float shrink = HALF ? power_of_two(-s_scale) : 1.f;
+#pragma unroll
+        for (int j = 0; j < COLS / 8; ++j) {
+          const int col = col0 + j * 8;
+          char* to = base + L::oS + col / 64 * (C * 128) + row * 128 + (((col % 64) / 8) ^ (row & 7)) * 16;
+          uint32_t hi[4], lo[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float2 f = make_float2(S[j * 8 + 2 * i], S[j * 8 + 2 * i + 1]);
+            if (HALF) f = make_float2(f.x * shrink, f.y * shrink);
+            hi[i] = part_of<E>(f);
+            lo[i] = part_of<E>(f);
+          }
+          *reinterpret_cast<uint4*>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+          *reinterpret_cast<uint4*>(to + L::kPart) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        }
+      }
+      shared_fence();
+      before_sync();
+      barrier_arrive(&tab.state_ready);
       // scores to A, in their place
       wait(&tab.scores, n);
       after_sync();
       {
         const float shrink = HALF ? power_of_two(-a_scale) : 1.f;
 #pragma unroll 1
-        for (int b = 0; b < 2; ++b) {
-          const int col = half * 64 + b * 32;
-          uint32_t x[32], to[32];
+        for (int col = group * (128 / L::kGroups); col < (group + 1) * (128 / L::kGroups); col += 32) {
+          uint32_t x[32];
           if (p.back ? col + 31 < quad * 32 : col > quad * 32 + 31) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) to[j] = 0;
-          } else {
-            tmem_load(x, mine + L::P + col);
-            const float* weight = tab.weight + 128 + row - col;
+            for (int j = 0; j < 32; ++j) x[j] = 0;
+            tmem_store(x, mine + L::P + col);
+            continue;
+          }
+          tmem_load(x, mine + L::P + col);
+          const float* weight = tab.weight + 128 + row - col;
+          uint32_t to[32];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              float2 f = make_float2(__uint_as_float(x[2 * j]) * weight[-2 * j], __uint_as_float(x[2 * j + 1]) * weight[-2 * j - 1]);
-              if (HALF) f = make_float2(f.x * shrink, f.y * shrink);
-              to[j] = part_of<E>(f);
-              to[16 + j] = part_of<E>(f);
-            }
+          for (int j = 0; j < 16; ++j) {
+            float2 f = make_float2(__uint_as_float(x[2 * j]) * weight[-2 * j], __uint_as_float(x[2 * j + 1]) * weight[-2 * j - 1]);
+            if (HALF) f = make_float2(f.x * shrink, f.y * shrink);
+            to[j] = part_of<E>(f);
+            to[16 + j] = part_of<E>(f);
           }
           tmem_store(to, mine + L::P + col);
         }
@@ -422,81 +463,90 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
       wait(&tab.read, n);
       after_sync();
       {
-        const int walked = p.back ? m - 1 - row : row + 1;
-        float f = row < m ? tab.power[walked] * p.out_scale : 0.f;
+        const int walked = p.back ? now.m - 1 - row : row + 1;
+        float f = row < now.m ? tab.power[walked] * p.out_scale : 0.f;
         if (HALF) f *= power_of_two(s_scale - a_scale);
-#pragma unroll 1
-        for (int b = 0; b < D / 64; ++b) {
-          const int col = half * (D / 2) + b * 32;
-          uint32_t x[32];
-          tmem_load(x, mine + L::O + col);
+        uint32_t x[32];
+        tmem_load(x, mine + L::O + col0);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) x[j] = __float_as_uint(__uint_as_float(x[j]) * f);
-          tmem_store(x, mine + L::O + col);
-        }
+        for (int j = 0; j < 32; ++j) x[j] = __float_as_uint(__uint_as_float(x[j]) * f);
+        tmem_store(x, mine + L::O + col0);
         wait_store();
       }
       before_sync();
       barrier_arrive(&tab.a_ready);
-      if (!L::kNarrow) weigh(0);
+      // the next block's weighted keys
+      const bool more = n + 1 < blocks;
+      if (more) open(n + 1);
+      advance(n);
+      if constexpr (!L::kNarrow) {
+        if (more) {
+          weigh(n + 1, 0);
+          put(0);
+          weigh(n + 1, 1);
+          if (PARTS == 2) put(1);
+        }
+      }
       wait(&tab.done, n);
       after_sync();
-      if (!L::kNarrow) weigh(1);
+      if constexpr (!L::kNarrow && PARTS == 3) {
+        if (more) put(1);
+      }
       {
         // By way of shared memory, where the parts of the state were: the warp's 32 tokens, 64 bytes of each at a time, so that
         // a store instruction covers whole sectors of 8 rows and not 16 bytes of 32.
-        constexpr int COLS = 64 / (int)sizeof(R);
+        constexpr int N = 64 / (int)sizeof(R), WORD = 16 / (int)sizeof(R);
         const float grow = HALF ? power_of_two(a_scale) : 1.f;
         char* stage = base + L::oS + warp * 2048;
         R* o = static_cast<R*>(p.o.data) + w.batch * p.o.batch + first_token(n) * p.o.token + head * p.o.head + c0;
-#pragma unroll 1
-        for (int b = 0; b < D / 64; ++b) {
-          uint32_t x[32];
-          tmem_load(x, mine + L::O + half * (D / 2) + b * 32);
+        uint32_t x[32];
+        tmem_load(x, mine + L::O + col0);
+        if (lost) {
 #pragma unroll
-          for (int e = 0; e < 32 / COLS; ++e) {
-            const int col = half * (D / 2) + b * 32 + e * COLS;
-            __syncwarp();
+          for (int j = 0; j < 32; ++j) x[j] = 0x7FC00000u;
+        }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              uint4 word;
-              typename Pack2<R>::type* pair = reinterpret_cast<typename Pack2<R>::type*>(&word);
+        for (int e = 0; e < 32 / N; ++e) {
+          __syncwarp();
 #pragma unroll
-              for (int i = 0; i < COLS / 8; ++i) {
-                float2 f = make_float2(__uint_as_float(x[e * COLS + j * (COLS / 4) + 2 * i]), __uint_as_float(x[e * COLS + j * (COLS / 4) + 2 * i + 1]));
-                if (HALF) f = make_float2(f.x * grow, f.y * grow);
-                pair[i] = Pack2<R>::down(lost ? make_float2(nan, nan) : f);
-              }
-              *reinterpret_cast<uint4*>(stage + lane * 64 + ((j ^ (lane >> 1)) & 3) * 16) = word;
+          for (int j = 0; j < 4; ++j) {
+            uint4 word;
+            typename Pack2<R>::type* pair = reinterpret_cast<typename Pack2<R>::type*>(&word);
+#pragma unroll
+            for (int i = 0; i < WORD / 2; ++i) {
+              float2 f = make_float2(__uint_as_float(x[e * N + j * WORD + 2 * i]), __uint_as_float(x[e * N + j * WORD + 2 * i + 1]));
+              if (HALF) f = make_float2(f.x * grow, f.y * grow);
+              pair[i] = Pack2<R>::down(f);
             }
-            __syncwarp();
+            *reinterpret_cast<uint4*>(stage + lane * 64 + ((j ^ (lane >> 1)) & 3) * 16) = word;
+          }
+          __syncwarp();
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const int r = j * 8 + lane / 4, at = col + lane % 4 * (COLS / 4);
-              const uint4 word = *reinterpret_cast<const uint4*>(stage + r * 64 + ((lane ^ (r >> 1)) & 3) * 16);
-              if (quad * 32 + r < m && c0 + at < p.D) *reinterpret_cast<uint4*>(o + (quad * 32 + r) * p.o.token + at) = word;
-            }
+          for (int j = 0; j < 4; ++j) {
+            const int r = j * 8 + lane / 4, at = col0 + e * N + lane % 4 * WORD;
+            const uint4 word = *reinterpret_cast<const uint4*>(stage + r * 64 + ((lane ^ (r >> 1)) & 3) * 16);
+            if (quad * 32 + r < now.m && c0 + at < p.D) *reinterpret_cast<uint4*>(o + (quad * 32 + r) * p.o.token + at) = word;
           }
         }
       }
-      if (L::kNarrow) {
-        worker_sync();  // the keys go where O was read
-        weigh(0);
-        weigh(1);
+      if constexpr (L::kNarrow) {
+        if (more) {
+          sync_workers<kWorkers>();  // the keys go where O was read
+          weigh(n + 1, 0);
+          put(0);
+          weigh(n + 1, 1);
+          put(1);
+        }
       }
-    }
-    if (blocks > 0) {
-      wait(&tab.summed, blocks - 1);
-      after_sync();
-      if (holds) advance();
+      now = next;
     }
     float* to = SUMS ? carry : w.ends ? p.last : nullptr;
     if (to && holds && row < p.C) {
       const int64_t down = SUMS ? p.D : p.state_row, along = SUMS ? 1 : p.state_col;
       to += (SUMS ? 0 : state) + row * down;
 #pragma unroll
-      for (int j = 0; j < D / 2; ++j) {
-        const int col = c0 + half * (D / 2) + j;
+      for (int j = 0; j < COLS; ++j) {
+        const int col = c0 + col0 + j;
         if (col < p.D) to[col * along] = lost ? nan : S[j];
       }
     }
@@ -508,7 +558,7 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
   if (lost)  // copies still under way land before the shared memory is given back
     for (int k = 0; k < 1000; ++k) __nanosleep(1000);
   __syncwarp();
-  if (warp == 8) tmem_free<L::kColumns>(tmem);
+  if (warp == kWorkers / 32) tmem_free<L::kColumns>(tmem);
 }
 
 // The encoder of tile descriptors is a function of the driver.
@@ -541,9 +591,9 @@ bool describe(CUtensorMap& map, const HeadsIn& t, const AttentionParams& p, int 
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename E, typename R, int C, int D, bool SUMS>
+template <typename E, typename R, int C, int D, int PARTS, bool SUMS>
 cudaError_t launch_mma(dim3 grid, cudaStream_t s, const AttentionMmaParams& p) {
-  const auto kernel = k_attention_mma<E, R, C, D, SUMS>;
+  const auto kernel = k_attention_mma<E, R, C, D, PARTS, SUMS>;
   constexpr int smem = Plan<C, D>::kBytes;
   // shared memory beyond the default is asked for once per kernel and device
   static std::atomic<uint64_t> done{0};
@@ -556,20 +606,29 @@ cudaError_t launch_mma(dim3 grid, cudaStream_t s, const AttentionMmaParams& p) {
     if (e != cudaSuccess) return e;
     done.fetch_or(bit, std::memory_order_release);
   }
-  return launch_cluster(kernel, grid, dim3(kMmaThreads), smem, 1, s, p);
+  return launch_cluster(kernel, grid, dim3(Plan<C, D>::kThreads), smem, 1, s, p);
 }
 
-template <typename E, typename R, int C, int D>
-cudaError_t walk(const AttentionMmaParams& q, cudaStream_t s) {
+template <typename E, typename R, int C, int D, int PARTS>
+cudaError_t walk_parts(const AttentionMmaParams& q, cudaStream_t s) {
   const AttentionParams& p = q.a;
   const dim3 grid((unsigned)((int64_t)p.items * p.H * ((p.D + D - 1) / D)));
   if (p.segments > 1) {
-    cudaError_t e = launch_mma<E, R, C, D, true>(grid, s, q);
+    cudaError_t e = launch_mma<E, R, C, D, PARTS, true>(grid, s, q);
     if (e != cudaSuccess) return e;
     e = launch_attention_carry(p, s);
     if (e != cudaSuccess) return e;
   }
-  return launch_mma<E, R, C, D, false>(grid, s, q);
+  return launch_mma<E, R, C, D, PARTS, false>(grid, s, q);
+}
+
+// Keys of bf16 in three parts where a state is given back in fp32; two, which 16-bit outputs do not tell from more,
+// where none is.
+template <typename E, typename R, int C, int D>
+cudaError_t walk(const AttentionMmaParams& q, cudaStream_t s) {
+  if constexpr (std::is_same<E, __nv_bfloat16>::value)
+    if (q.a.last) return walk_parts<E, R, C, D, 3>(q, s);
+  return walk_parts<E, R, C, D, 2>(q, s);
 }
 
 }  // namespace

@@ -55,7 +55,7 @@ __device__ __forceinline__ void tmem_free(uint32_t at) {
 __device__ __forceinline__ void wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// 32 or 16 adjacent columns of the warp's own 32 lanes, a lane for each thread.
+// Adjacent columns of the warp's own 32 lanes, a lane for each thread.
 #define GS_R8(v, n) "+r"(v[n]), "+r"(v[n + 1]), "+r"(v[n + 2]), "+r"(v[n + 3]), "+r"(v[n + 4]), "+r"(v[n + 5]), "+r"(v[n + 6]), "+r"(v[n + 7])
 #define GS_O8(v, n) "=r"(v[n]), "=r"(v[n + 1]), "=r"(v[n + 2]), "=r"(v[n + 3]), "=r"(v[n + 4]), "=r"(v[n + 5]), "=r"(v[n + 6]), "=r"(v[n + 7])
 #define GS_I8(v, n) "r"(v[n]), "r"(v[n + 1]), "r"(v[n + 2]), "r"(v[n + 3]), "r"(v[n + 4]), "r"(v[n + 5]), "r"(v[n + 6]), "r"(v[n + 7])
@@ -76,6 +76,9 @@ __device__ __forceinline__ void tmem_store(const uint32_t (&v)[32], uint32_t at)
       "%18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::GS_I8(v, 0),
       GS_I8(v, 8), GS_I8(v, 16), GS_I8(v, 24), "r"(at)
       : "memory");
+}
+__device__ __forceinline__ void tmem_store(const uint32_t (&v)[8], uint32_t at) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::GS_I8(v, 0), "r"(at) : "memory");
 }
 __device__ __forceinline__ void tmem_store(const uint32_t (&v)[16], uint32_t at) {
   asm volatile(
