@@ -33,7 +33,7 @@ using namespace tc;
 constexpr int kBlockTokens = 128;
 
 struct AttentionMmaParams {
-  CUtensorMap q, k, v;
+  CUtensorMap q, k, v, o;
   AttentionParams a;
 };
 
@@ -333,31 +333,44 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
       }
       made = next.m;
     };
-    // the group's weighted keys of either half of block n, transposed: this thread's row of the state
+    // The group's weighted keys of either half of block n, transposed to rows of the state: 32 rows, in two halves, of
+    // 16 tokens, or twice 16.
     constexpr int PAIRS = 32 / L::kGroups;
-    uint32_t part[PARTS][PAIRS];
+    uint32_t part[PARTS][2][PAIRS / 2];
     const auto weigh = [&](int n, int h) {
       if (!holds) return;
-      const char* from = base + L::oK + (n & 1) * L::kQ + row / 64 * L::kPanel + row % 8 * 2;
-      const int t0 = h * 64 + group * 2 * PAIRS, word = row % 64 / 8;
+      const uint32_t from = shared_address(base + L::oK + (n & 1) * L::kQ + quad / 2 * L::kPanel);
       const float shrink = HALF ? power_of_two(-next.scale) : 1.f;
 #pragma unroll
-      for (int j = 0; j < PAIRS; ++j) {
-        const int t = t0 + 2 * j;
-        const float2 weight = *reinterpret_cast<const float2*>(&tab.key[t]);
-        float2 f = make_float2(to_f32(*reinterpret_cast<const E*>(from + t * 128 + (word ^ ((2 * j) & 7)) * 16)),
-                               to_f32(*reinterpret_cast<const E*>(from + (t + 1) * 128 + (word ^ ((2 * j + 1) & 7)) * 16)));
-        f.x *= weight.x;
-        f.y *= weight.y;
-        if (HALF) f = make_float2(f.x * shrink, f.y * shrink);
+      for (int j = 0; j < PAIRS / 8; ++j) {
+        const int t = h * 64 + group * 2 * PAIRS + j * 16;
+        const float2 weight[2] = {*reinterpret_cast<const float2*>(&tab.key[t + lane % 4 * 2]),
+                                  *reinterpret_cast<const float2*>(&tab.key[t + 8 + lane % 4 * 2])};
 #pragma unroll
-        for (int i = 0; i < PARTS; ++i) part[i][j] = part_of<E>(f);
+        for (int r = 0; r < 2; ++r) {
+          const int word = (quad % 2) * 4 + r * 2 + (lane >> 3 & 1);
+          uint32_t x[4];
+          load_across(x, from + (t + (lane >> 4) * 8 + lane % 8) * 128 + (word ^ (lane % 8)) * 16);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float2 f = Pack2<E>::up(*reinterpret_cast<const typename Pack2<E>::type*>(&x[i]));
+            f.x *= weight[i / 2].x;
+            f.y *= weight[i / 2].y;
+            if (HALF) f = make_float2(f.x * shrink, f.y * shrink);
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) part[q][r][j * 4 + i] = part_of<E>(f);
+          }
+        }
       }
     };
     const auto put = [&](int h) {
       if (holds) {
 #pragma unroll
-        for (int i = 0; i < PARTS; ++i) tmem_store(part[i], mine + (h ? W1 : L::W0) + i * 32 + group * PAIRS);
+        for (int i = 0; i < PARTS; ++i)
+#pragma unroll
+          for (int r = 0; r < 2; ++r)
+            tmem_store_matrices(part[i][r], mine + ((uint32_t)(r * 16) << 16) + (h ? W1 : L::W0) + i * 32 + group * PAIRS,
+                                std::integral_constant<int, PAIRS / 2>());
         wait_store();
       }
       before_sync();
@@ -403,6 +416,7 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
         wait(&tab.q_full, n);
         largest(base + L::oQ, L::kQ, now.m, &tab.largest[n % 3][0]);
       }
+      if (lane == 0) stores_read();
       sync_workers<kWorkers>();  // the last block's o has left the place of the parts
       if constexpr (HALF) {
         s_scale = exponent_of(bound);
@@ -493,12 +507,12 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
         if (more) put(1);
       }
       {
-        // By way of shared memory, where the parts of the state were: the warp's 32 tokens, 64 bytes of each at a time, so that
-        // a store instruction covers whole sectors of 8 rows and not 16 bytes of 32.
+        // By way of shared memory, where the parts of the state were: the warp's 32 tokens, 64 bytes of each at a time, as
+        // a tile; in a block that is cut short, whose other rows may be another sequence's, row by row.
         constexpr int N = 64 / (int)sizeof(R), WORD = 16 / (int)sizeof(R);
         const float grow = HALF ? power_of_two(a_scale) : 1.f;
         char* stage = base + L::oS + warp * 2048;
-        R* o = static_cast<R*>(p.o.data) + w.batch * p.o.batch + first_token(n) * p.o.token + head * p.o.head + c0;
+        const int64_t token = first_token(n) + quad * 32;
         uint32_t x[32];
         tmem_load(x, mine + L::O + col0);
         if (lost) {
@@ -507,6 +521,8 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
         }
 #pragma unroll
         for (int e = 0; e < 32 / N; ++e) {
+          const int col = c0 + col0 + e * N;
+          if (e > 0 && lane == 0) stores_read();
           __syncwarp();
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
@@ -520,12 +536,19 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
             }
             *reinterpret_cast<uint4*>(stage + lane * 64 + ((j ^ (lane >> 1)) & 3) * 16) = word;
           }
-          __syncwarp();
+          if (now.m == kBlockTokens) {
+            shared_fence();
+            __syncwarp();
+            if (lane == 0 && col < p.D) tile_store(stage, &params.o, col, head, (int)token, w.batch);
+          } else {
+            __syncwarp();
+            R* o = static_cast<R*>(p.o.data) + w.batch * p.o.batch + head * p.o.head;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int r = j * 8 + lane / 4, at = col0 + e * N + lane % 4 * WORD;
-            const uint4 word = *reinterpret_cast<const uint4*>(stage + r * 64 + ((lane ^ (r >> 1)) & 3) * 16);
-            if (quad * 32 + r < now.m && c0 + at < p.D) *reinterpret_cast<uint4*>(o + (quad * 32 + r) * p.o.token + at) = word;
+            for (int j = 0; j < 4; ++j) {
+              const int r = j * 8 + lane / 4, at = col + lane % 4 * WORD;
+              const uint4 word = *reinterpret_cast<const uint4*>(stage + r * 64 + ((lane ^ (r >> 1)) & 3) * 16);
+              if (quad * 32 + r < now.m && at < p.D) *reinterpret_cast<uint4*>(o + (token + r) * p.o.token + at) = word;
+            }
           }
         }
       }
@@ -540,6 +563,7 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
       }
       now = next;
     }
+    if (!SUMS && lane == 0) stores_done();
     float* to = SUMS ? carry : w.ends ? p.last : nullptr;
     if (to && holds && row < p.C) {
       const int64_t down = SUMS ? p.D : p.state_row, along = SUMS ? 1 : p.state_col;
@@ -574,20 +598,24 @@ PFN_cuTensorMapEncodeTiled_v12000 tile_encoder() {
   return found;
 }
 
-// Describes a tensor of `size` elements a head as tiles of 64 of them x 128 tokens; false where that is not possible.
-bool describe(CUtensorMap& map, const HeadsIn& t, const AttentionParams& p, int size, bool half) {
+// Describes a tensor of `heads` heads of `size` elements as tiles of 128 (or 64) bytes of a head x `tokens`; false where that
+// is not possible.
+bool describe(CUtensorMap& map, const HeadsIn& t, const AttentionParams& p, int size, int dtype, int bytes, int tokens) {
   const int64_t heads = p.H / t.share, rows = p.offsets ? 1 : p.B;
-  const int64_t item = 2, any = 16;  // a dimension of one entry may come with any stride
+  const int64_t item = dtype == GS_F32 ? 4 : 2, any = 16;  // a dimension of one entry may come with any stride
   const cuuint64_t sizes[4] = {(cuuint64_t)size, (cuuint64_t)heads, (cuuint64_t)p.T, (cuuint64_t)rows};
   const int64_t step[3] = {heads > 1 ? t.head * item : any, p.T > 1 ? t.token * item : any, rows > 1 ? t.batch * item : any};
   if (reinterpret_cast<uintptr_t>(t.data) % 16 != 0) return false;
   for (const int64_t s : step)
     if (s <= 0 || s % 16 != 0 || s >= int64_t(1) << 40) return false;
   const cuuint64_t strides[3] = {(cuuint64_t)step[0], (cuuint64_t)step[1], (cuuint64_t)step[2]};
-  const cuuint32_t box[4] = {64, 1, kBlockTokens, 1}, unit[4] = {1, 1, 1, 1};
+  const cuuint32_t box[4] = {(cuuint32_t)(bytes / item), 1, (cuuint32_t)tokens, 1}, unit[4] = {1, 1, 1, 1};
+  const CUtensorMapDataType type = dtype == GS_F32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : dtype == GS_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                                     : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   const auto encode = tile_encoder();
-  return encode && encode(&map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(t.data), sizes,
-                          strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+  return encode && encode(&map, type, 4, const_cast<void*>(t.data), sizes, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -636,15 +664,12 @@ cudaError_t walk(const AttentionMmaParams& q, cudaStream_t s) {
 cudaError_t launch_attention_mma(const AttentionParams& p, int dtype, bool wide, cudaStream_t s, bool& taken) {
   taken = false;
   if (p.T == 0) return cudaSuccess;
-  const bool half = dtype == GS_F16;
-  const int unit = wide ? 4 : 2;
-  const int64_t rows = p.offsets ? 1 : p.B;
-  if (reinterpret_cast<uintptr_t>(p.o.data) % 16 != 0 || (p.T > 1 && p.o.token * unit % 16 != 0) || (p.H > 1 && p.o.head * unit % 16 != 0) ||
-      (rows > 1 && p.o.batch * unit % 16 != 0))
-    return cudaSuccess;
   AttentionMmaParams q;
   q.a = p;
-  if (!describe(q.q, p.q, p, p.C, half) || !describe(q.k, p.k, p, p.C, half) || !describe(q.v, p.v, p, p.D, half)) return cudaSuccess;
+  const HeadsIn o = {p.o.data, p.o.batch, p.o.token, p.o.head, 1};
+  if (!describe(q.q, p.q, p, p.C, dtype, 128, kBlockTokens) || !describe(q.k, p.k, p, p.C, dtype, 128, kBlockTokens) ||
+      !describe(q.v, p.v, p, p.D, dtype, 128, kBlockTokens) || !describe(q.o, o, p, p.D, wide ? GS_F32 : dtype, 64, 32))
+    return cudaSuccess;
   taken = true;
   const auto sizes = [&](auto e, auto r) {
     using E = decltype(e);
@@ -652,7 +677,7 @@ cudaError_t launch_attention_mma(const AttentionParams& p, int dtype, bool wide,
     if (p.C <= 64) return p.D <= 64 ? walk<E, R, 64, 64>(q, s) : walk<E, R, 64, 128>(q, s);
     return p.D <= 64 ? walk<E, R, 128, 64>(q, s) : walk<E, R, 128, 128>(q, s);
   };
-  if (half) return wide ? sizes(__half(), float()) : sizes(__half(), __half());
+  if (dtype == GS_F16) return wide ? sizes(__half(), float()) : sizes(__half(), __half());
   return wide ? sizes(__nv_bfloat16(), float()) : sizes(__nv_bfloat16(), __nv_bfloat16());
 }
 

@@ -86,6 +86,22 @@ __device__ __forceinline__ void tmem_store(const uint32_t (&v)[16], uint32_t at)
       GS_I8(v, 8), "r"(at)
       : "memory");
 }
+// 8 x 8 matrices of 16-bit elements in the layout that load_across leaves them in: of 16 lanes,
+// matrix 0 (lanes 0 ... 7) and 1 (lanes 8 ... 15) in four columns, 2 and 3 in the next four, and so on.
+__device__ __forceinline__ void tmem_store_matrices(const uint32_t* v, uint32_t at, std::integral_constant<int, 4>) {
+  asm volatile("tcgen05.st.sync.aligned.16x128b.x2.b32 [%4], {%0, %1, %2, %3};" ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(at) : "memory");
+}
+__device__ __forceinline__ void tmem_store_matrices(const uint32_t* v, uint32_t at, std::integral_constant<int, 8>) {
+  asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::GS_I8(v, 0), "r"(at) : "memory");
+}
+// Four 8 x 8 matrices of 16-bit elements, transposed: lane l gives the address of row l % 8 of matrix l / 8, and gets elements
+// (2 (l % 4), l / 4) and (2 (l % 4) + 1, l / 4) of each.
+__device__ __forceinline__ void load_across(uint32_t (&v)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+               : "r"(at)
+               : "memory");
+}
 #undef GS_R8
 #undef GS_O8
 #undef GS_I8
@@ -142,6 +158,16 @@ __device__ __forceinline__ void tile_load(void* to, const CUtensorMap* map, int 
       "l"(map), "r"(d), "r"(h), "r"(t), "r"(b), "r"(shared_address(bar))
       : "memory");
 }
+
+__device__ __forceinline__ void tile_store(const void* from, const CUtensorMap* map, int d, int h, int t, int b) {
+  asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3, %4}], [%5];" ::"l"(map), "r"(d), "r"(h), "r"(t),
+               "r"(b), "r"(shared_address(from))
+               : "memory");
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// All tiles that this thread has stored have been read; are where they belong.
+__device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 }  // namespace tc
 }  // namespace gs
