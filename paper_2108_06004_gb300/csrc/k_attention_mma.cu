@@ -58,7 +58,8 @@ struct Plan {
   static constexpr int kBytes = oTables + 3072;
 };
 struct Tables {
-  float weight[256];  // in out w_d of a score at weight[128 + row - column], zero past the diagonal
+  float weight[256];  // in w_d of a score at weight[128 + row - column], zero past the diagonal
+  alignas(16) float rise[128];  // in / w of a score's column, where the row's factor comes last
   float power[129];   // w_n
   alignas(16) float key[128];  // of a row's weighted key, zero past the block's tokens
   uint64_t q_full, kv_full[2], scores, read, done, summed, state_ready, a_ready, w_ready[2];
@@ -73,18 +74,29 @@ __device__ __forceinline__ void sync_workers() {
   asm volatile("bar.sync 1, %0;" ::"n"(WORKERS) : "memory");
 }
 
-// v as a sum of N parts of the type; part n of two adjacent values.
+// Two values as a sum of parts of the type: a part of what is left of them, and the last one.  bf16's are the upper halves of fp32
+// values, cut off; the last is rounded.
+__device__ __forceinline__ float2 mul(float2 a, float2 b) { return __fmul2_rn(a, b); }
+__device__ __forceinline__ float2 mul(float2 a, float b) { return __fmul2_rn(a, make_float2(b, b)); }
+__device__ __forceinline__ float2 less(float2 a, float2 b) { return __ffma2_rn(b, make_float2(-1.f, -1.f), a); }
 template <typename E>
-__device__ __forceinline__ uint32_t part_of(float2& v) {
+__device__ __forceinline__ uint32_t last_part(float2 v) {
   const typename Pack2<E>::type h = Pack2<E>::down(v);
-  const float2 f = Pack2<E>::up(h);
-  v.x -= f.x;
-  v.y -= f.y;
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-
 template <typename E>
-__device__ __forceinline__ const E* input(const HeadsIn& t) { return static_cast<const E*>(t.data); }
+__device__ __forceinline__ uint32_t part_of(float2& v) {
+  if constexpr (std::is_same<E, __half>::value) {
+    const uint32_t h = last_part<E>(v);
+    v = less(v, Pack2<E>::up(*reinterpret_cast<const __half2*>(&h)));
+    return h;
+  } else {
+    const uint32_t x = __float_as_uint(v.x), y = __float_as_uint(v.y);
+    v = less(v, make_float2(__uint_as_float(x & 0xFFFF0000u), __uint_as_float(y & 0xFFFF0000u)));
+    return __byte_perm(x, y, 0x7632);
+  }
+}
+__device__ __forceinline__ float2 pair_of(const uint32_t* x) { return make_float2(__uint_as_float(x[0]), __uint_as_float(x[1])); }
 
 // 2^-n for the power of two that brings a bound to [2^13, 2^14); 1 for a bound of zero.
 __device__ __forceinline__ int exponent_of(float bound) {
@@ -124,7 +136,7 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
     barrier_init(&tab.kv_full[0], 1);
     barrier_init(&tab.kv_full[1], 1);
     for (uint64_t* b : {&tab.scores, &tab.read, &tab.done, &tab.summed}) barrier_init(b, 1);
-    for (uint64_t* b : {&tab.state_ready, &tab.a_ready, &tab.w_ready[0], &tab.w_ready[1]}) barrier_init(b, kWorkers);
+    for (uint64_t* b : {&tab.state_ready, &tab.a_ready, &tab.w_ready[0], &tab.w_ready[1]}) barrier_init(b, kWorkers / 32);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kWorkers / 32) tmem_alloc<L::kColumns>(&tab.tmem);
@@ -133,7 +145,7 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
   if (threadIdx.x < 129) tab.power[threadIdx.x] = expf(g * (float)threadIdx.x);
   if (threadIdx.x < 256) {
     const int d = p.back ? 128 - (int)threadIdx.x : (int)threadIdx.x - 128;  // tokens from a key to a query
-    tab.weight[threadIdx.x] = d >= 0 ? expf(g * (float)d) * p.in_scale * p.out_scale : 0.f;
+    tab.weight[threadIdx.x] = d >= 0 ? expf(g * (float)d) * p.in_scale : 0.f;
   }
   before_sync();
   __syncthreads();
@@ -218,19 +230,21 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
           const uint32_t v = values(n);
           each<16>([&](auto step) {
             constexpr int part = decltype(step)::value / 8, j = decltype(step)::value % 8;
-            multiply_t<j / 2 * 32 + part * 16 + j % 2 * 8, j * 2048>(tmem + L::O, tmem + L::P, v, product<E>(D, true), true);
+            multiply_t<j * 16 + part * 8, j * 2048>(tmem + L::O, tmem + L::P, v, product<E>(D, true), true);
           });
           commit(&tab.done);
           if (n + 1 >= blocks) break;
+          barrier_wait(&tab.done, n, lost);
           if (APART) {
+            if (n + 2 < blocks) load_kv(n + 2);  // in the place of block n's, whose last product is done
+            score(n + 1);
             sum(n + 1);
-            barrier_wait(&tab.done, n, lost);
           } else {
             sum(n + 1);
             barrier_wait(&tab.summed, n + 1, lost);
+            if (n + 2 < blocks) load_kv(n + 2);
+            score(n + 1);
           }
-          score(n + 1);
-          if (n + 2 < blocks) load_kv(n + 2);  // in the place of block n's, whose last product is done
         }
       }
     }
@@ -240,6 +254,15 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
       barrier_wait(bar, phase, lost);
       lost = __any_sync(0xFFFFFFFFu, lost);
     };
+    // What this warp has written is there for the thread that issues products.
+    const auto arrive = [&](uint64_t* bar) {
+      before_sync();
+      __syncwarp();
+      if (lane == 0) barrier_arrive(bar);
+    };
+    // Whether the queries' decay w_{i+1} comes last, after both products, and A_ij has w_{-j-1} in place of w_{i-j}: only
+    // where that stays small enough for any inputs, and for fp16 for the numbers that a part holds.
+    const bool rises = -g * kBlockTokens <= (HALF ? 8.f : 32.f);
     const int quad = warp & 3, group = warp >> 2, row = quad * 32 + lane, col0 = group * COLS;
     const uint32_t mine = tmem + ((uint32_t)(quad * 32) << 16);
     const bool holds = quad * 32 < C;  // rows of the state
@@ -297,17 +320,22 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
       float k, v;
       Decay decay;
     } next, now;
+    next.m = 0;
     const auto open = [&](int n) {
-      next.m = tokens(n);
-      next.decay = decay_of(g * (float)next.m);
+      const int m = tokens(n);
+      if (m != next.m) next.decay = decay_of(g * (float)m);
+      next.m = m;
       char* k = base + L::oK + (n & 1) * L::kQ;
       char* v = base + L::oV + (n & 1) * L::kV;
       wait(&tab.kv_full[n & 1], n >> 1);
       if (HALF && threadIdx.x < 3) tab.largest[(n + 1) % 3][threadIdx.x] = 0;  // last read two blocks ago
       if (made != next.m) {
-        // all threads have met since the weights before were used
-        if (threadIdx.x < 128)
-          tab.key[threadIdx.x] = (int)threadIdx.x < next.m ? tab.power[p.back ? threadIdx.x + 1 : next.m - 1 - threadIdx.x] * p.in_scale : 0.f;
+        if (made >= 0) sync_workers<kWorkers>();  // the tables before have been used
+        if (threadIdx.x < 128) {
+          const int r = threadIdx.x;
+          tab.key[r] = r < next.m ? tab.power[p.back ? r + 1 : next.m - 1 - r] * p.in_scale : 0.f;
+          tab.rise[r] = expf(-g * (float)(p.back ? next.m - 1 - r : r + 1)) * p.in_scale;
+        }
         if (next.m < kBlockTokens) {
           // rows that are not the block's tokens: zeros, whatever they were
           const auto trim = [&](char* tile, int panels) {
@@ -354,11 +382,11 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             float2 f = Pack2<E>::up(*reinterpret_cast<const typename Pack2<E>::type*>(&x[i]));
-            f.x *= weight[i / 2].x;
-            f.y *= weight[i / 2].y;
-            if (HALF) f = make_float2(f.x * shrink, f.y * shrink);
+            f = mul(f, weight[i / 2]);
+            if (HALF) f = mul(f, shrink);
 #pragma unroll
-            for (int q = 0; q < PARTS; ++q) part[q][r][j * 4 + i] = part_of<E>(f);
+            for (int q = 0; q + 1 < PARTS; ++q) part[q][r][j * 4 + i] = part_of<E>(f);
+            part[PARTS - 1][r][j * 4 + i] = last_part<E>(f);
           }
         }
       }
@@ -373,8 +401,7 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
                                 std::integral_constant<int, PAIRS / 2>());
         wait_store();
       }
-      before_sync();
-      barrier_arrive(&tab.w_ready[h]);
+      arrive(&tab.w_ready[h]);
     };
     // the state after block n
     const auto advance = [&](int n) {
@@ -385,9 +412,13 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
       tmem_load(x, mine + L::U + col0);
       const float grow = HALF ? power_of_two(now.scale) : 1.f;
 #pragma unroll
-      for (int j = 0; j < COLS; ++j) {
-        const float u = __uint_as_float(x[j]);
-        S[j] = decayed(S[j], now.decay, HALF ? u * grow : u);
+      for (int j = 0; j < COLS; j += 2) {
+        float2 u = pair_of(x + j);
+        if (HALF) u = mul(u, grow);
+        float2 v = make_float2(S[j], S[j + 1]);
+        v = __ffma2_rn(v, make_float2(now.decay.a, now.decay.a), __ffma2_rn(v, make_float2(now.decay.b, now.decay.b), u));
+        S[j] = v.x;
+        S[j + 1] = v.y;
       }
     };
     if (blocks > 0) {
@@ -412,6 +443,7 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
         continue;
       }
       int a_scale = 0, s_scale = 0;
+      bool last = rises;
       if constexpr (HALF) {
         wait(&tab.q_full, n);
         largest(base + L::oQ, L::kQ, now.m, &tab.largest[n % 3][0]);
@@ -420,7 +452,13 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
       sync_workers<kWorkers>();  // the last block's o has left the place of the parts
       if constexpr (HALF) {
         s_scale = exponent_of(bound);
-        a_scale = exponent_of(__int_as_float(tab.largest[n % 3][0]) * now.k * (float)C * fabsf(p.in_scale * p.out_scale));
+        const float score = __int_as_float(tab.largest[n % 3][0]) * now.k * (float)C * fabsf(p.in_scale);
+        a_scale = exponent_of(score * expf(-g * kBlockTokens));
+        last = rises && abs(a_scale - s_scale) <= 6;  // both products have one scale then
+        if (last)
+          a_scale = s_scale = max(s_scale, a_scale);
+        else
+          a_scale = exponent_of(score);
         bound = bound * (now.decay.a + now.decay.b) * 1.0001f + now.k * now.v * (float)now.m * fabsf(p.in_scale);
       }
       // the state as a factor
@@ -434,61 +472,78 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             float2 f = make_float2(S[j * 8 + 2 * i], S[j * 8 + 2 * i + 1]);
-            if (HALF) f = make_float2(f.x * shrink, f.y * shrink);
+            if (HALF) f = mul(f, shrink);
             hi[i] = part_of<E>(f);
-            lo[i] = part_of<E>(f);
+            lo[i] = last_part<E>(f);
           }
           *reinterpret_cast<uint4*>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
           *reinterpret_cast<uint4*>(to + L::kPart) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         }
       }
       shared_fence();
-      before_sync();
-      barrier_arrive(&tab.state_ready);
+      arrive(&tab.state_ready);
       // scores to A, in their place
       wait(&tab.scores, n);
       after_sync();
       {
         const float shrink = HALF ? power_of_two(-a_scale) : 1.f;
-#pragma unroll 1
-        for (int col = group * (128 / L::kGroups); col < (group + 1) * (128 / L::kGroups); col += 32) {
-          uint32_t x[32];
-          if (p.back ? col + 31 < quad * 32 : col > quad * 32 + 31) {
+        const float undo = last ? shrink / tab.power[p.back ? max(now.m - 1 - row, 0) : row + 1] : shrink;
+#pragma unroll L::kNarrow ? 1 : 2
+        for (int col = group * (128 / L::kGroups); col < (group + 1) * (128 / L::kGroups); col += 16) {
+          uint32_t x[16], hi[8], lo[8];
+          const int tile = col & ~31;
+          if (p.back ? tile < quad * 32 : tile > quad * 32) {  // past the diagonal
 #pragma unroll
-            for (int j = 0; j < 32; ++j) x[j] = 0;
-            tmem_store(x, mine + L::P + col);
-            continue;
-          }
-          tmem_load(x, mine + L::P + col);
-          const float* weight = tab.weight + 128 + row - col;
-          uint32_t to[32];
+            for (int j = 0; j < 8; ++j) hi[j] = lo[j] = 0;
+          } else {
+            tmem_load(x, mine + L::P + col);
+            if (last && tile != quad * 32) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            float2 f = make_float2(__uint_as_float(x[2 * j]) * weight[-2 * j], __uint_as_float(x[2 * j + 1]) * weight[-2 * j - 1]);
-            if (HALF) f = make_float2(f.x * shrink, f.y * shrink);
-            to[j] = part_of<E>(f);
-            to[16 + j] = part_of<E>(f);
+              for (int j = 0; j < 8; j += 2) {
+                const float4 rise = *reinterpret_cast<const float4*>(tab.rise + col + 2 * j);
+                float2 f = mul(pair_of(x + 2 * j), make_float2(rise.x, rise.y)), e = mul(pair_of(x + 2 * j + 2), make_float2(rise.z, rise.w));
+                if (HALF) f = mul(f, shrink), e = mul(e, shrink);
+                hi[j] = part_of<E>(f);
+                lo[j] = last_part<E>(f);
+                hi[j + 1] = part_of<E>(e);
+                lo[j + 1] = last_part<E>(e);
+              }
+            } else {
+              const float* weight = tab.weight + 128 + row - col;
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                float2 f = mul(mul(pair_of(x + 2 * j), make_float2(weight[-2 * j], weight[-2 * j - 1])), undo);
+                hi[j] = part_of<E>(f);
+                lo[j] = last_part<E>(f);
+              }
+            }
           }
-          tmem_store(to, mine + L::P + col);
+          tmem_store(hi, mine + L::P + col);
+          tmem_store(lo, mine + L::P + col + 8);
         }
         wait_store();
       }
       // what has been read from the state, with the query's decay
-      wait(&tab.read, n);
-      after_sync();
-      {
-        const int walked = p.back ? now.m - 1 - row : row + 1;
-        float f = row < now.m ? tab.power[walked] * p.out_scale : 0.f;
-        if (HALF) f *= power_of_two(s_scale - a_scale);
+      const int walked = p.back ? now.m - 1 - row : row + 1;
+      float factor = row < now.m ? tab.power[walked] * (last ? p.out_scale : 1.f) : 0.f;
+      if (HALF && last) factor *= power_of_two(a_scale);
+      if (!last) {
+        wait(&tab.read, n);
+        after_sync();
+        if (HALF) factor *= power_of_two(s_scale - a_scale);
         uint32_t x[32];
         tmem_load(x, mine + L::O + col0);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) x[j] = __float_as_uint(__uint_as_float(x[j]) * f);
+        for (int j = 0; j < 32; j += 2) {
+          const float2 f = mul(pair_of(x + j), factor);
+          x[j] = __float_as_uint(f.x);
+          x[j + 1] = __float_as_uint(f.y);
+        }
         tmem_store(x, mine + L::O + col0);
         wait_store();
+        factor = p.out_scale * (HALF ? power_of_two(a_scale) : 1.f);
       }
-      before_sync();
-      barrier_arrive(&tab.a_ready);
+      arrive(&tab.a_ready);
       // the next block's weighted keys
       const bool more = n + 1 < blocks;
       if (more) open(n + 1);
@@ -510,7 +565,6 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
         // By way of shared memory, where the parts of the state were: the warp's 32 tokens, 64 bytes of each at a time, as
         // a tile; in a block that is cut short, whose other rows may be another sequence's, row by row.
         constexpr int N = 64 / (int)sizeof(R), WORD = 16 / (int)sizeof(R);
-        const float grow = HALF ? power_of_two(a_scale) : 1.f;
         char* stage = base + L::oS + warp * 2048;
         const int64_t token = first_token(n) + quad * 32;
         uint32_t x[32];
@@ -530,9 +584,7 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
             typename Pack2<R>::type* pair = reinterpret_cast<typename Pack2<R>::type*>(&word);
 #pragma unroll
             for (int i = 0; i < WORD / 2; ++i) {
-              float2 f = make_float2(__uint_as_float(x[e * N + j * WORD + 2 * i]), __uint_as_float(x[e * N + j * WORD + 2 * i + 1]));
-              if (HALF) f = make_float2(f.x * grow, f.y * grow);
-              pair[i] = Pack2<R>::down(f);
+              pair[i] = Pack2<R>::down(mul(pair_of(x + e * N + j * WORD + 2 * i), factor));
             }
             *reinterpret_cast<uint4*>(stage + lane * 64 + ((j ^ (lane >> 1)) & 3) * 16) = word;
           }

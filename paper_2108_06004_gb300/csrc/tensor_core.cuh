@@ -70,6 +70,14 @@ __device__ __forceinline__ void tmem_load(uint32_t (&v)[32], uint32_t at) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" : GS_R8(v, 0), GS_R8(v, 8), GS_R8(v, 16)::"memory");
   asm volatile("" : GS_R8(v, 24));
 }
+__device__ __forceinline__ void tmem_load(uint32_t (&v)[16], uint32_t at) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : GS_O8(v, 0), GS_O8(v, 8)
+      : "r"(at)
+      : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : GS_R8(v, 0), GS_R8(v, 8)::"memory");
+}
 __device__ __forceinline__ void tmem_store(const uint32_t (&v)[32], uint32_t at) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, "
