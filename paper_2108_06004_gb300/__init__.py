@@ -889,6 +889,18 @@ def gs_linear_attention_backward(d_o, q, k, v, log_decay, dq, dk, dv, workspace,
         stream), f)
 
 
+def _one_token(func: str, name: str, t, shape, dtype, device):
+    """[B][H][D], as a [B][1][H][D] tensor."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype is not dtype or t.device != device:
+        _unlike(func, name, t, shape, dtype, device)
+    b, h, d = t.stride()
+    if d != 1 and shape[2] > 1:
+        _refuse(func, f"{name}: the elements of a head must be adjacent")
+    return GsHeads(t.data_ptr(), b, 0, h)
+
+
 def gs_linear_attention_step(q, k, v, log_decay, state, o, slots=None, scale: float = 1.0, stream=None) -> None:
     """One token of each of B streams, q [B][H][Dk] and k, v with K heads: states [slots][H][Dk][Dv] in place, and o."""
     f = "gs_linear_attention_step"
@@ -899,17 +911,13 @@ def gs_linear_attention_step(q, k, v, log_decay, state, o, slots=None, scale: fl
     n = _head_sizes(f, "state", state, 4)[0]
     if state.shape != (n, H, Dk, Dv) or state.dtype is not f32 or state.device != dev:
         _unlike(f, "state", state, (n, H, Dk, Dv), f32, dev)
-    if n > 0 and not state[0].is_contiguous():
+    if not state.is_contiguous() and n > 0 and not state[0].is_contiguous():
         _refuse(f, "state: a slot's state must be contiguous")
-
-    def one(name, t, heads, d):
-        return None if t is None else _heads(f, name, t.unsqueeze(1), (B, 1, heads, d), dtype, dev)
-
-    _head_sizes(f, "o", o, 3)
     _check(load_library().gs_linear_attention_step(
-        one("q", q, H, Dk), one("k", k, K, Dk), one("v", v, K, Dv), _dense(f, "log_decay", log_decay, (H,), f32, dev),
-        state.data_ptr(), state.stride(0) if n > 1 else H * Dk * Dv, n, _whole(f, "slots", slots, (B,), dev), one("o", o, H, Dv),
-        B, H, K, Dk, Dv, code, scale, stream), f)
+        _one_token(f, "q", q, (B, H, Dk), dtype, dev), _one_token(f, "k", k, (B, K, Dk), dtype, dev),
+        _one_token(f, "v", v, (B, K, Dv), dtype, dev), _dense(f, "log_decay", log_decay, (H,), f32, dev),
+        state.data_ptr(), state.stride(0) if n > 1 else H * Dk * Dv, n, _whole(f, "slots", slots, (B,), dev),
+        _one_token(f, "o", o, (B, H, Dv), dtype, dev), B, H, K, Dk, Dv, code, scale, stream), f)
 
 
 def _act(func: str, name) -> int:

@@ -1,4 +1,4 @@
-// Shared pieces of the kernels for the norms around a block: rows and groups, the gate.
+// Shared pieces of the kernels for the norms around a block: rows and groups, the gate, sums.
 #pragma once
 
 #include "attention.cuh"
@@ -29,16 +29,40 @@ __device__ __forceinline__ void group_weight8(const float* weight, const Span& s
   }
 }
 
-// act(u), and its slope.
-__device__ __forceinline__ float sigmoid(float u) { return __fdividef(1.f, 1.f + __expf(-u)); }
-__device__ __forceinline__ float gate_of(int act, float u) {
-  const float s = sigmoid(u);
-  return act == GS_GATE_SILU ? u * s : s;
-}
+// act(u), and its slope: 1 - sigmoid is e^-u sigmoid, and one where e^-u is past fp32.
 __device__ __forceinline__ float gate_of(int act, float u, float& slope) {
-  const float s = sigmoid(u), rest = sigmoid(-u);  // 1 - s, to its own digits
+  const float e = __expf(-u), s = __fdividef(1.f, 1.f + e), rest = s > 0.f ? e * s : 1.f;
   slope = act == GS_GATE_SILU ? s * fmaf(u, rest, 1.f) : s * rest;
   return act == GS_GATE_SILU ? u * s : s;
+}
+__device__ __forceinline__ float gate_of(int act, float u) {
+  float slope;
+  return gate_of(act, u, slope);
+}
+
+// N sums at once over the TPR threads of a row; every thread of the CTA takes part.  Two calls in turn use two
+// scratch arrays, so one barrier each is enough.
+template <int TPR, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float (*scratch)[32]) {
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int o = TPR < 32 ? TPR / 2 : 16; o > 0; o >>= 1) v[n] += __shfl_xor_sync(0xFFFFFFFFu, v[n], o);
+  if constexpr (TPR > 32) {
+    constexpr int W = TPR / 32;
+    const int warp = threadIdx.x >> 5, first = warp / W * W;
+    if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) scratch[n][warp] = v[n];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      v[n] = 0.f;
+#pragma unroll
+      for (int k = 0; k < W; ++k) v[n] += scratch[n][first + k];
+    }
+  }
 }
 
 // Threads a row and groups of eight a thread: one as long as 1024 threads do.

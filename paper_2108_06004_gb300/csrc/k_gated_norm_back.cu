@@ -7,6 +7,7 @@
 // Every tensor is read and written once.  A CTA takes rows in turn; the weights' gradients are summed by
 // each thread over its rows, whose columns and group are the same, then over the CTAs by a last kernel, in a fixed
 // order.  Bound by memory.
+#include <atomic>
 #include <numeric>
 
 #include "gated_norm.cuh"
@@ -16,13 +17,32 @@ namespace {
 
 using namespace norm;
 
+// Rows that are whole 16-byte words are copied ahead into shared memory, each thread its own words, while the row before is
+// worked on: in registers, of which the sums take 16, they would leave room for half as many threads.
 template <typename E, int TPR, int V, int L>
-__global__ void __launch_bounds__(kCtaThreads<TPR>, kCtaThreads<TPR> <= 256 ? 2 : 1)
+constexpr bool kAhead = L == kEven && V == 1 && (sizeof(E) == 2 || TPR <= 512);
+// Threads of an SM: what registers (and for fp32 the copies) leave room for.
+constexpr int resident(int item, int tpr) { return item == 4 ? (tpr <= 512 ? 512 : 1024) : tpr <= 128 ? 768 : 1024; }
+constexpr int kInputs = 5;
+enum { kX, kGate, kDy, kDz, kY };
+
+__device__ __forceinline__ void copy_word(uint4* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+
+// A row's two means come from three sums of one pass: with q = scale act(gate) w n,
+//   mean(u m) = U,  mean(p n) = mean(q (next_rstd u + dy)) - U mean(q next_rstd m).
+template <typename E, int TPR, int V, int L>
+__global__ void __launch_bounds__(kCtaThreads<TPR>, resident(sizeof(E), TPR) / kCtaThreads<TPR>)
 k_gated_norm_back(const __grid_constant__ GatedNormBackParams p, int outer) {
   grid_begin();
-  __shared__ float scratch[2][2][32];
+  __shared__ float scratch[2][3][32];
   constexpr int RPC = kRowsPerCta<TPR>;
-  extern __shared__ float fold[];  // RPC > 1 and one group a row: [RPC][width]
+  // [2][inputs][words of a group][threads] where rows are copied ahead; at the end, where RPC > 1 and a row is one
+  // group, [RPC][width]
+  extern __shared__ __align__(16) float fold[];
+  constexpr bool AHEAD = kAhead<E, TPR, V, L>;
+  constexpr int WORDS = sizeof(E) / 2, THREADS = kCtaThreads<TPR>;
   const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   // a thread's rows, `step` apart, have the same lead and the same group
   const int64_t step = (int64_t)gridDim.x * RPC, first = (int64_t)blockIdx.x * RPC;
@@ -32,126 +52,149 @@ k_gated_norm_back(const __grid_constant__ GatedNormBackParams p, int outer) {
   for (int v = 0; v < V; ++v)
 #pragma unroll
     for (int j = 0; j < 8; ++j) dw[v][j] = dnext[v][j] = 0.f;
-  constexpr bool AHEAD = V == 1 && sizeof(E) == 2 && TPR <= 512;
-  struct Row {
-    Raw8<E> x[V], gate[V], dy[V], dz[V], y[V];
-    float rstd, next_rstd;
-  };
-  const auto fetch = [&](int64_t row, Row& r) {
-    if (row >= p.rows) return;
-    const bool inner = p.spaced && row > 0 && row + 1 < p.rows;
-    r.rstd = p.rstd[row];
-    if (p.dz) r.next_rstd = p.next_rstd[row];
+  const void* const input[kInputs] = {p.x, p.gate, p.dy, p.dz, p.y};
+  const int64_t stride[kInputs] = {p.x_stride, p.gate_stride, p.dy_stride, p.dz_stride, p.y_stride};
+  float rstd = 0.f, next_rstd = 0.f, rstd_ahead = 0.f, next_rstd_ahead = 0.f;
+  uint4* const ahead = reinterpret_cast<uint4*>(fold) + threadIdx.x;
+  const auto copy = [&](int64_t row, int turn) {
+    if constexpr (AHEAD) {
+      if (row < p.rows) {
+        const Span s = span<L>(lane, lead, p.width);
+        if (s.some()) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const Span s = span<L>(v * TPR + lane, lead, p.width);
-      if (!s.some()) continue;
-      const auto get = [&](const void* t, int64_t stride) {
-        return fetch8<E, L>(static_cast<const E*>(t) + group_start(row, outer, stride, p.width) + s.col, s, inner);
-      };
-      r.x[v] = get(p.x, p.x_stride);
-      if (p.gate) r.gate[v] = get(p.gate, p.gate_stride);
-      if (p.dy) r.dy[v] = get(p.dy, p.dy_stride);
-      if (p.dz) {
-        r.dz[v] = get(p.dz, p.dz_stride);
-        r.y[v] = get(p.y, p.y_stride);
+          for (int k = 0; k < kInputs; ++k) {
+            if (!input[k]) continue;
+            const E* from = static_cast<const E*>(input[k]) + group_start(row, outer, stride[k], p.width) + s.col;
+#pragma unroll
+            for (int q = 0; q < WORDS; ++q) copy_word(ahead + ((turn * kInputs + k) * WORDS + q) * THREADS, from + q * (16 / sizeof(E)));
+          }
+        }
+        rstd_ahead = p.rstd[row];
+        if (p.dz) next_rstd_ahead = p.next_rstd[row];
       }
+      asm volatile("cp.async.commit_group;" ::: "memory");
     }
   };
-  Row now;
-  if (AHEAD) fetch(first + sub, now);
+  copy(first + sub, 0);
   int turn = 0;
   for (int64_t row0 = first; row0 < p.rows; row0 += step, turn ^= 1) {
     const int64_t row = row0 + sub;
-    const bool live = row < p.rows;
-    Row next;
-    if (AHEAD)
-      fetch(row + step, next);
-    else
-      fetch(row, now);
+    const bool live = row < p.rows, inner = p.spaced && row > 0 && row + 1 < p.rows;
     const auto put = [&](void* t, int64_t stride, const Span& s, const float(&v)[8]) {
       store8<E, L>(static_cast<E*>(t) + group_start(row, outer, stride, p.width) + s.col, s, v);
     };
-    float sum = 0.f;
-    if (p.dz) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const Span s = span<L>(v * TPR + lane, lead, p.width);
-        if (!live || !s.some()) continue;
-        float dz[8], m[8], w[8];
-        weight8<L>(p.next_weight, s, lead, p.width, w);
-        unpack8<E, L>(now.dz[v], s, dz);
-        unpack8<E, L>(now.y[v], s, m);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float a = dz[j] * (m[j] * now.next_rstd);  // zero where there is no element
-          dnext[v][j] += a;
-          sum += a * w[j];
-        }
-      }
-      sum = row_sum<TPR>(sum, scratch[0][turn]) / (float)p.width;
-    }
-    float dn[V][8], inside = 0.f;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const Span s = span<L>(v * TPR + lane, lead, p.width);
-      if (!live || !s.some()) continue;
-      float t[8], a[8], w[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) t[j] = 0.f;
-      if (p.dy) unpack8<E, L>(now.dy[v], s, t);
-      if (p.dz) {
-        float m[8];
-        weight8<L>(p.next_weight, s, lead, p.width, w);
-        unpack8<E, L>(now.dz[v], s, a);
-        unpack8<E, L>(now.y[v], s, m);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) t[j] += now.next_rstd * (a[j] * w[j] - m[j] * now.next_rstd * sum);
-      }
-      if (p.dresidual) put(p.dresidual, p.dresidual_stride, s, t);
-      float n[8];
-      group_weight8<L>(p.weight, s, lead, p.width, p.groups, row, w);
-      unpack8<E, L>(now.x[v], s, n);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        n[j] *= now.rstd;
-        t[j] *= p.scale;
-      }
-      if (p.gate) {
-        float u[8], slope[8];
-        unpack8<E, L>(now.gate[v], s, u);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) u[j] = gate_of(p.act, u[j], slope[j]);
-        if (p.dgate) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) slope[j] *= t[j] * n[j] * w[j];
-          put(p.dgate, p.dgate_stride, s, slope);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) t[j] *= u[j];
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float a = t[j] * n[j];
-        dw[v][j] += a;
-        dn[v][j] = t[j] * w[j];
-        inside += a * w[j];
-      }
-    }
-    inside = row_sum<TPR>(inside, scratch[1][turn]) / (float)p.width;
-    if (live && p.dx) {
+    Raw8<E> raw[kInputs][AHEAD ? 1 : V];
+    if constexpr (AHEAD) {
+      rstd = rstd_ahead;
+      next_rstd = next_rstd_ahead;
+      copy(row + step, turn ^ 1);
+      asm volatile("cp.async.wait_group 1;" ::: "memory");
+    } else if (live) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const Span s = span<L>(v * TPR + lane, lead, p.width);
         if (!s.some()) continue;
-        float n[8];
-        unpack8<E, L>(now.x[v], s, n);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) n[j] = now.rstd * (dn[v][j] - n[j] * now.rstd * inside);
-        put(p.dx, p.dx_stride, s, n);
+        for (int k = 0; k < kInputs; ++k)
+          if (input[k])
+            raw[k][v] = fetch8<E, L>(static_cast<const E*>(input[k]) + group_start(row, outer, stride[k], p.width) + s.col, s, inner);
       }
+      rstd = p.rstd[row];
+      if (p.dz) next_rstd = p.next_rstd[row];
     }
-    if (AHEAD) now = next;
+    const auto get = [&](int k, int v, const Span& s, float(&to)[8]) {
+      if constexpr (AHEAD) {
+        Raw8<E> r;
+#pragma unroll
+        for (int q = 0; q < WORDS; ++q) r.q[q] = ahead[((turn * kInputs + k) * WORDS + q) * THREADS];
+        unpack8<E, L>(r, s, to);
+      } else {
+        unpack8<E, L>(raw[k][v], s, to);
+      }
+    };
+    float sums[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const Span s = span<L>(v * TPR + lane, lead, p.width);
+      if (!live || !s.some()) continue;
+      float n[8], w[8], t[8], a[8];
+      group_weight8<L>(p.weight, s, lead, p.width, p.groups, row, w);
+      get(kX, v, s, n);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) n[j] *= rstd * p.scale * w[j];
+      if (p.gate) {
+        get(kGate, v, s, a);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) n[j] *= gate_of(p.act, a[j]);
+      }
+      // n is q now
+#pragma unroll
+      for (int j = 0; j < 8; ++j) t[j] = 0.f;
+      if (p.dy) get(kDy, v, s, t);
+      if (p.dz) {
+        weight8<L>(p.next_weight, s, lead, p.width, w);
+        get(kDz, v, s, a);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[j] = fmaf(next_rstd * w[j], a[j], t[j]);
+        float m[8];
+        get(kY, v, s, m);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          m[j] *= next_rstd;
+          const float b = a[j] * m[j];  // zero where there is no element, as all sums are
+          dnext[v][j] += b;
+          sums[0] = fmaf(b, w[j], sums[0]);
+          sums[2] = fmaf(n[j], m[j], sums[2]);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sums[1] = fmaf(n[j], t[j], sums[1]);
+    }
+    row_sums<TPR>(sums, scratch[turn]);
+    const float part = 1.f / (float)p.width, U = sums[0] * part;
+    const float inside = (sums[1] - U * next_rstd * sums[2]) * part;
+    if (!live) continue;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const Span s = span<L>(v * TPR + lane, lead, p.width);
+      if (!s.some()) continue;
+      float t[8], a[8], w[8], n[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) t[j] = 0.f;
+      if (p.dy) get(kDy, v, s, t);
+      if (p.dz) {
+        weight8<L>(p.next_weight, s, lead, p.width, w);
+        get(kDz, v, s, a);
+        get(kY, v, s, n);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[j] += next_rstd * (a[j] * w[j] - n[j] * next_rstd * U);
+      }
+      if (p.dresidual) put(p.dresidual, p.dresidual_stride, s, t);
+      group_weight8<L>(p.weight, s, lead, p.width, p.groups, row, w);
+      get(kX, v, s, n);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        n[j] *= rstd;
+        t[j] *= p.scale;
+      }
+      if (p.gate) {
+        float slope[8];
+        get(kGate, v, s, a);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          a[j] = gate_of(p.act, a[j], slope[j]);
+          slope[j] *= t[j] * n[j] * w[j];
+          t[j] *= a[j];
+        }
+        if (p.dgate) put(p.dgate, p.dgate_stride, s, slope);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        dw[v][j] = fmaf(t[j], n[j], dw[v][j]);
+        n[j] = rstd * (t[j] * w[j] - n[j] * inside);
+      }
+      if (p.dx) put(p.dx, p.dx_stride, s, n);
+    }
   }
   const int64_t n = (int64_t)gridDim.x * p.width;
   for (int which = 0; which < (p.next_weight ? 2 : 1); ++which) {
@@ -159,6 +202,7 @@ k_gated_norm_back(const __grid_constant__ GatedNormBackParams p, int outer) {
     const bool apart = p.groups > 1;
     float* part = p.partial + which * n + (int64_t)blockIdx.x * (apart ? RPC : 1) * p.width;
     float* to = RPC > 1 && !apart ? fold + sub * p.width : part + (apart ? sub * p.width : 0);
+    if (RPC > 1 && !apart) __syncthreads();  // what was copied ahead has been used
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const Span s = span<L>(v * TPR + lane, lead, p.width);
@@ -181,10 +225,10 @@ k_gated_norm_back(const __grid_constant__ GatedNormBackParams p, int outer) {
 
 // CTAs: as many as stay resident, the rows dealt round robin, so that a thread's rows share their group and (rows
 // of a thread being a multiple of eight apart) their lead.
-int64_t ctas_of(int64_t rows, int groups, const Shape& shape) {
+int64_t ctas_of(int64_t rows, int groups, const Shape& shape, int item) {
   const int64_t need = (rows + shape.rows - 1) / shape.rows;
   const int64_t even = groups / std::gcd(groups, shape.rows);  // CTAs whose rows hold whole sets of groups
-  int64_t most = (int64_t)kSMs * (shape.threads <= 512 ? 512 / shape.threads : 1);
+  int64_t most = (int64_t)kSMs * (resident(item, shape.tpr) / shape.threads);
   const int64_t unit = std::lcm(even, (int64_t)8);
   most = (most + unit - 1) / unit * unit;
   return need < most ? (need + even - 1) / even * even : most;
@@ -192,13 +236,15 @@ int64_t ctas_of(int64_t rows, int groups, const Shape& shape) {
 
 }  // namespace
 
-// CTAs times the sums that each writes, for any alignment of the rows.
+// CTAs times the sums that each writes, for any type and any alignment of the rows.
 int64_t gated_norm_most_sums(int64_t rows, int groups, int wide_cols) {
   int64_t most = 0;
   for (int wide : {wide_cols, wide_cols + 7 <= kNormMaxCols ? wide_cols + 7 : wide_cols}) {
     const Shape shape = gated_shape(wide);
-    const int64_t n = ctas_of(rows, groups, shape) * (groups > 1 ? shape.rows : 1);
-    most = n > most ? n : most;
+    for (int item : {2, 4}) {
+      const int64_t n = ctas_of(rows, groups, shape, item) * (groups > 1 ? shape.rows : 1);
+      most = n > most ? n : most;
+    }
   }
   return most;
 }
@@ -207,15 +253,30 @@ cudaError_t launch_gated_norm_backward(const GatedNormBackParams& p, int outer, 
                                        int dtype, Layout layout, cudaStream_t s) {
   if (width(p.width, layout) > kNormMaxCols) layout = kApart;
   const Shape shape = gated_shape(width(p.width, layout));
-  const int64_t ctas = ctas_of(p.rows, p.groups, shape);
+  const int64_t ctas = ctas_of(p.rows, p.groups, shape, dtype == GS_F32 ? 4 : 2);
   if (ctas > 0) {
-    const size_t smem = shape.rows > 1 && p.groups == 1 ? (size_t)shape.rows * p.width * sizeof(float) : 0;
+    const size_t fold = shape.rows > 1 && p.groups == 1 ? (size_t)shape.rows * p.width * sizeof(float) : 0;
     const cudaError_t err = with_type(dtype, [&](auto e) {
       using E = decltype(e);
       return with_gated_shape(shape, [&](auto tpr, auto v) {
         return with_layout(layout, [&](auto how) {
-          return launch_cluster(k_gated_norm_back<E, decltype(tpr)::value, decltype(v)::value, decltype(how)::value>,
-                                dim3((unsigned)ctas), dim3(shape.threads), smem, 1, s, p, outer);
+          constexpr int TPR = decltype(tpr)::value, V = decltype(v)::value, L = decltype(how)::value;
+          constexpr size_t copies = kAhead<E, TPR, V, L> ? (size_t)2 * kInputs * kCtaThreads<TPR> * 8 * sizeof(E) : 0;
+          const auto kernel = k_gated_norm_back<E, TPR, V, L>;
+          if constexpr (copies > 48 * 1024) {
+            // shared memory beyond the default is asked for once per kernel and device
+            static std::atomic<uint64_t> done{0};
+            int dev = 0;
+            cudaError_t e = cudaGetDevice(&dev);
+            if (e != cudaSuccess) return e;
+            const uint64_t bit = 1ull << (dev & 63);
+            if (!(done.load(std::memory_order_acquire) & bit)) {
+              e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)copies);
+              if (e != cudaSuccess) return e;
+              done.fetch_or(bit, std::memory_order_release);
+            }
+          }
+          return launch_cluster(kernel, dim3((unsigned)ctas), dim3(shape.threads), copies > fold ? copies : fold, 1, s, p, outer);
         });
       });
     });
