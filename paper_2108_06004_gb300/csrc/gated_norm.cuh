@@ -29,16 +29,47 @@ __device__ __forceinline__ void group_weight8(const float* weight, const Span& s
   }
 }
 
-// act(u), and its slope: 1 - sigmoid is e^-u sigmoid, and one where e^-u is past fp32.
-__device__ __forceinline__ float gate_of(int act, float u, float& slope) {
-  const float e = __expf(-u), s = __fdividef(1.f, 1.f + e), rest = s > 0.f ? e * s : 1.f;
-  slope = act == GS_GATE_SILU ? s * fmaf(u, rest, 1.f) : s * rest;
-  return act == GS_GATE_SILU ? u * s : s;
+// Two adjacent elements with one instruction.
+__device__ __forceinline__ float2 two(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float2 mul(float2 a, float2 b) { return __fmul2_rn(a, b); }
+__device__ __forceinline__ float2 mul(float2 a, float b) { return __fmul2_rn(a, two(b)); }
+__device__ __forceinline__ float2 add(float2 a, float2 b) { return __fadd2_rn(a, b); }
+__device__ __forceinline__ float2 fma(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
+__device__ __forceinline__ float2 fma(float2 a, float b, float2 c) { return __ffma2_rn(a, two(b), c); }
+using Eight = float2[4];
+template <typename E, int L>
+__device__ __forceinline__ void unpack(const Raw8<E>& r, const Span& g, Eight& v) {
+  unpack8<E, L>(r, g, reinterpret_cast<float(&)[8]>(v));
 }
-__device__ __forceinline__ float gate_of(int act, float u) {
-  float slope;
-  return gate_of(act, u, slope);
+
+// s(u) = 1 / (1 + e^-u), whose exponent stops where s is zero in fp32 (and lets NaN pass).
+__device__ __forceinline__ float power(float x) {
+  float y;
+  asm("{\n .reg .f32 t;\n min.NaN.f32 t, %1, 0f42FE0000;\n ex2.approx.ftz.f32 %0, t;\n}" : "=f"(y) : "f"(x));
+  return y;
 }
+__device__ __forceinline__ float inverse(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// act(u), and its slope: with a = act(u) and 1 - s = e^-u s, a (1 - s) + s for u s and s (1 - s) for s.
+struct Gate {
+  bool silu;
+  float keep;
+  __device__ __forceinline__ explicit Gate(int act) : silu(act == GS_GATE_SILU), keep(act == GS_GATE_SILU ? 1.f : 0.f) {}
+  __device__ __forceinline__ float2 value(float2 u, float2& slope) const {
+    const float2 x = mul(u, -1.4426950408889634f), e = make_float2(power(x.x), power(x.y)), d = add(e, two(1.f));
+    const float2 s = make_float2(inverse(d.x), inverse(d.y));
+    const float2 a = mul(silu ? u : two(1.f), s);
+    slope = fma(a, mul(e, s), mul(s, keep));
+    return a;
+  }
+  __device__ __forceinline__ float2 value(float2 u) const {
+    float2 slope;
+    return value(u, slope);
+  }
+};
 
 // N sums at once over the TPR threads of a row; every thread of the CTA takes part.  Two calls in turn use two
 // scratch arrays, so one barrier each is enough.

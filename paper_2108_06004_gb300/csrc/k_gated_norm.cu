@@ -24,60 +24,59 @@ k_gated_norm(const __grid_constant__ GatedNormParams p, int outer) {
   const bool live = row < p.rows, inner = p.spaced && row > 0 && row + 1 < p.rows;
   const int lead = lead_of<L>(row, p.x_stride, p.lead);
   const auto from = [&](const void* t, int64_t stride) { return static_cast<const E*>(t) + group_start(row, outer, stride, p.width); };
-  float t[V][8];
-  Raw8<E> gate[V], residual[V];
-  float sum = 0.f;
+  const Gate gate(p.act);
+  Eight t[V];
+  Raw8<E> gates[V], residual[V];
+  float2 sum = two(0.f);
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     const Span s = span<L>(v * TPR + lane, lead, p.width);
     if (!live || !s.some()) continue;
     const Raw8<E> x = fetch8<E, L>(from(p.x, p.x_stride) + s.col, s, inner);
-    if (p.gate) gate[v] = fetch8<E, L>(from(p.gate, p.gate_stride) + s.col, s, inner);
+    if (p.gate) gates[v] = fetch8<E, L>(from(p.gate, p.gate_stride) + s.col, s, inner);
     if (p.residual) residual[v] = fetch8<E, L>(from(p.residual, p.residual_stride) + s.col, s, inner);
-    unpack8<E, L>(x, s, t[v]);
+    unpack<E, L>(x, s, t[v]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum += t[v][j] * t[v][j];
+    for (int j = 0; j < 4; ++j) sum = fma(t[v][j], t[v][j], sum);
   }
-  sum = row_sum<TPR>(sum, scratch[0]);
-  const float rstd = rsqrtf(sum / (float)p.width + p.eps), factor = rstd * p.scale;
+  const float rstd = rsqrtf(row_sum<TPR>(sum.x + sum.y, scratch[0]) / (float)p.width + p.eps);
   if (live && lane == 0) p.rstd[row] = rstd;
-  sum = 0.f;
+  sum = two(0.f);
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     const Span s = span<L>(v * TPR + lane, lead, p.width);
     if (!live || !s.some()) continue;
-    float w[8];
-    group_weight8<L>(p.weight, s, lead, p.width, p.groups, row, w);
+    Eight w;
+    group_weight8<L>(p.weight, s, lead, p.width, p.groups, row, reinterpret_cast<float(&)[8]>(w));
 #pragma unroll
-    for (int j = 0; j < 8; ++j) t[v][j] *= factor * w[j];
+    for (int j = 0; j < 4; ++j) t[v][j] = mul(t[v][j], mul(w[j], rstd * p.scale));
     if (p.gate) {
-      unpack8<E, L>(gate[v], s, w);
+      unpack<E, L>(gates[v], s, w);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) t[v][j] *= gate_of(p.act, w[j]);
+      for (int j = 0; j < 4; ++j) t[v][j] = mul(t[v][j], gate.value(w[j]));
     }
     if (p.residual) {
-      unpack8<E, L>(residual[v], s, w);
+      unpack<E, L>(residual[v], s, w);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) t[v][j] += w[j];
+      for (int j = 0; j < 4; ++j) t[v][j] = add(t[v][j], w[j]);
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum += t[v][j] * t[v][j];  // zero where there is no element
-    store8<E, L>(static_cast<E*>(p.y) + group_start(row, outer, p.y_stride, p.width) + s.col, s, t[v]);
+    for (int j = 0; j < 4; ++j) sum = fma(t[v][j], t[v][j], sum);  // zero where there is no element
+    store8<E, L>(static_cast<E*>(p.y) + group_start(row, outer, p.y_stride, p.width) + s.col, s, reinterpret_cast<float(&)[8]>(t[v]));
   }
   if (!p.next_weight) return;
-  sum = row_sum<TPR>(sum, scratch[1]);
-  const float next = rsqrtf(sum / (float)p.width + p.eps);
+  const float next = rsqrtf(row_sum<TPR>(sum.x + sum.y, scratch[1]) / (float)p.width + p.eps);
   if (!live) return;
   if (lane == 0) p.next_rstd[row] = next;
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     const Span s = span<L>(v * TPR + lane, lead, p.width);
     if (!s.some()) continue;
-    float w[8];
-    weight8<L>(p.next_weight, s, lead, p.width, w);
+    Eight w;
+    weight8<L>(p.next_weight, s, lead, p.width, reinterpret_cast<float(&)[8]>(w));
 #pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] *= t[v][j] * next;
-    store8<E, L>(static_cast<E*>(p.z) + row * p.z_stride + s.col, s, w);
+    for (int j = 0; j < 4; ++j) w[j] = mul(w[j], mul(t[v][j], next));
+    store8<E, L>(static_cast<E*>(p.z) + row * p.z_stride + s.col, s, reinterpret_cast<float(&)[8]>(w));
   }
 }
 

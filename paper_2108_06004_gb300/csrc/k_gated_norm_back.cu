@@ -31,7 +31,7 @@ __device__ __forceinline__ void copy_word(uint4* to, const void* from) {
 }
 
 // A row's two means come from three sums of one pass: with q = scale act(gate) w n,
-//   mean(u m) = U,  mean(p n) = mean(q (next_rstd u + dy)) - U mean(q next_rstd m).
+//   mean(u m),  mean(p n) = rstd (mean(q x (next_rstd u + dy)) - next_rstd^2 mean(u m) mean(q x y)).
 template <typename E, int TPR, int V, int L>
 __global__ void __launch_bounds__(kCtaThreads<TPR>, resident(sizeof(E), TPR) / kCtaThreads<TPR>)
 k_gated_norm_back(const __grid_constant__ GatedNormBackParams p, int outer) {
@@ -47,11 +47,12 @@ k_gated_norm_back(const __grid_constant__ GatedNormBackParams p, int outer) {
   // a thread's rows, `step` apart, have the same lead and the same group
   const int64_t step = (int64_t)gridDim.x * RPC, first = (int64_t)blockIdx.x * RPC;
   const int lead = lead_of<L>(first + sub, p.x_stride, p.lead);
-  float dw[V][8], dnext[V][8];
+  const Gate gate(p.act);
+  Eight dw[V], dnext[V];
 #pragma unroll
   for (int v = 0; v < V; ++v)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) dw[v][j] = dnext[v][j] = 0.f;
+    for (int j = 0; j < 4; ++j) dw[v][j] = dnext[v][j] = two(0.f);
   const void* const input[kInputs] = {p.x, p.gate, p.dy, p.dz, p.y};
   const int64_t stride[kInputs] = {p.x_stride, p.gate_stride, p.dy_stride, p.dz_stride, p.y_stride};
   float rstd = 0.f, next_rstd = 0.f, rstd_ahead = 0.f, next_rstd_ahead = 0.f;
@@ -80,9 +81,13 @@ k_gated_norm_back(const __grid_constant__ GatedNormBackParams p, int outer) {
   for (int64_t row0 = first; row0 < p.rows; row0 += step, turn ^= 1) {
     const int64_t row = row0 + sub;
     const bool live = row < p.rows, inner = p.spaced && row > 0 && row + 1 < p.rows;
-    const auto put = [&](void* t, int64_t stride, const Span& s, const float(&v)[8]) {
-      store8<E, L>(static_cast<E*>(t) + group_start(row, outer, stride, p.width) + s.col, s, v);
+    const auto put = [&](void* t, int64_t stride, const Span& s, const Eight& v) {
+      store8<E, L>(static_cast<E*>(t) + group_start(row, outer, stride, p.width) + s.col, s, reinterpret_cast<const float(&)[8]>(v));
     };
+    const auto weights = [&](const Span& s, Eight& w) {
+      group_weight8<L>(p.weight, s, lead, p.width, p.groups, row, reinterpret_cast<float(&)[8]>(w));
+    };
+    const auto next_weights = [&](const Span& s, Eight& w) { weight8<L>(p.next_weight, s, lead, p.width, reinterpret_cast<float(&)[8]>(w)); };
     Raw8<E> raw[kInputs][AHEAD ? 1 : V];
     if constexpr (AHEAD) {
       rstd = rstd_ahead;
@@ -102,96 +107,95 @@ k_gated_norm_back(const __grid_constant__ GatedNormBackParams p, int outer) {
       rstd = p.rstd[row];
       if (p.dz) next_rstd = p.next_rstd[row];
     }
-    const auto get = [&](int k, int v, const Span& s, float(&to)[8]) {
+    const auto get = [&](int k, int v, const Span& s, Eight& to) {
       if constexpr (AHEAD) {
         Raw8<E> r;
 #pragma unroll
         for (int q = 0; q < WORDS; ++q) r.q[q] = ahead[((turn * kInputs + k) * WORDS + q) * THREADS];
-        unpack8<E, L>(r, s, to);
+        unpack<E, L>(r, s, to);
       } else {
-        unpack8<E, L>(raw[k][v], s, to);
+        unpack<E, L>(raw[k][v], s, to);
       }
     };
-    float sums[3] = {0.f, 0.f, 0.f};
+    float2 sum[3] = {two(0.f), two(0.f), two(0.f)};
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const Span s = span<L>(v * TPR + lane, lead, p.width);
       if (!live || !s.some()) continue;
-      float n[8], w[8], t[8], a[8];
-      group_weight8<L>(p.weight, s, lead, p.width, p.groups, row, w);
-      get(kX, v, s, n);
+      Eight q, w, t, a;
+      weights(s, w);
+      get(kX, v, s, q);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) n[j] *= rstd * p.scale * w[j];
+      for (int j = 0; j < 4; ++j) q[j] = mul(q[j], mul(w[j], rstd * p.scale));
       if (p.gate) {
         get(kGate, v, s, a);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) n[j] *= gate_of(p.act, a[j]);
+        for (int j = 0; j < 4; ++j) q[j] = mul(q[j], gate.value(a[j]));
       }
-      // n is q now
 #pragma unroll
-      for (int j = 0; j < 8; ++j) t[j] = 0.f;
+      for (int j = 0; j < 4; ++j) t[j] = two(0.f);
       if (p.dy) get(kDy, v, s, t);
       if (p.dz) {
-        weight8<L>(p.next_weight, s, lead, p.width, w);
+        next_weights(s, w);
         get(kDz, v, s, a);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) t[j] = fmaf(next_rstd * w[j], a[j], t[j]);
-        float m[8];
+        Eight m;
         get(kY, v, s, m);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          m[j] *= next_rstd;
-          const float b = a[j] * m[j];  // zero where there is no element, as all sums are
-          dnext[v][j] += b;
-          sums[0] = fmaf(b, w[j], sums[0]);
-          sums[2] = fmaf(n[j], m[j], sums[2]);
+        for (int j = 0; j < 4; ++j) {
+          const float2 r = mul(a[j], next_rstd), b = mul(m[j], r);  // zero where there is no element, as all sums are
+          t[j] = fma(r, w[j], t[j]);
+          dnext[v][j] = add(dnext[v][j], b);
+          sum[0] = fma(b, w[j], sum[0]);
+          sum[2] = fma(q[j], m[j], sum[2]);
         }
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sums[1] = fmaf(n[j], t[j], sums[1]);
+      for (int j = 0; j < 4; ++j) sum[1] = fma(q[j], t[j], sum[1]);
     }
+    float sums[3] = {sum[0].x + sum[0].y, sum[1].x + sum[1].y, sum[2].x + sum[2].y};
     row_sums<TPR>(sums, scratch[turn]);
-    const float part = 1.f / (float)p.width, U = sums[0] * part;
-    const float inside = (sums[1] - U * next_rstd * sums[2]) * part;
+    // the same for every element: next_rstd^2 mean(u m) as a factor of y, and mean(p n)
+    const float part = 1.f / (float)p.width, from_y = sums[0] * part * next_rstd * next_rstd;
+    const float inside = (sums[1] - from_y * sums[2]) * part * -rstd;
     if (!live) continue;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const Span s = span<L>(v * TPR + lane, lead, p.width);
       if (!s.some()) continue;
-      float t[8], a[8], w[8], n[8];
+      Eight t, a, w, n;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) t[j] = 0.f;
+      for (int j = 0; j < 4; ++j) t[j] = two(0.f);
       if (p.dy) get(kDy, v, s, t);
       if (p.dz) {
-        weight8<L>(p.next_weight, s, lead, p.width, w);
+        next_weights(s, w);
         get(kDz, v, s, a);
         get(kY, v, s, n);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) t[j] += next_rstd * (a[j] * w[j] - n[j] * next_rstd * U);
+        for (int j = 0; j < 4; ++j) t[j] = fma(n[j], -from_y, fma(mul(a[j], next_rstd), w[j], t[j]));
       }
       if (p.dresidual) put(p.dresidual, p.dresidual_stride, s, t);
-      group_weight8<L>(p.weight, s, lead, p.width, p.groups, row, w);
+      weights(s, w);
       get(kX, v, s, n);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        n[j] *= rstd;
-        t[j] *= p.scale;
+      for (int j = 0; j < 4; ++j) {
+        n[j] = mul(n[j], rstd);
+        t[j] = mul(t[j], p.scale);
       }
       if (p.gate) {
-        float slope[8];
+        Eight slope;
         get(kGate, v, s, a);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          a[j] = gate_of(p.act, a[j], slope[j]);
-          slope[j] *= t[j] * n[j] * w[j];
-          t[j] *= a[j];
+        for (int j = 0; j < 4; ++j) {
+          a[j] = gate.value(a[j], slope[j]);
+          slope[j] = mul(mul(slope[j], t[j]), mul(n[j], w[j]));
+          t[j] = mul(t[j], a[j]);
         }
         if (p.dgate) put(p.dgate, p.dgate_stride, s, slope);
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        dw[v][j] = fmaf(t[j], n[j], dw[v][j]);
-        n[j] = rstd * (t[j] * w[j] - n[j] * inside);
+      for (int j = 0; j < 4; ++j) {
+        dw[v][j] = fma(t[j], n[j], dw[v][j]);
+        n[j] = fma(n[j], inside, mul(t[j], mul(w[j], rstd)));
       }
       if (p.dx) put(p.dx, p.dx_stride, s, n);
     }
@@ -208,7 +212,7 @@ k_gated_norm_back(const __grid_constant__ GatedNormBackParams p, int outer) {
       const Span s = span<L>(v * TPR + lane, lead, p.width);
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (j >= s.lo && j < s.hi) to[s.col + j] = which ? dnext[v][j] : dw[v][j];
+        if (j >= s.lo && j < s.hi) to[s.col + j] = reinterpret_cast<const float(&)[8]>(which ? dnext[v] : dw[v])[j];
     }
     if (RPC > 1 && !apart) {
       __syncthreads();
