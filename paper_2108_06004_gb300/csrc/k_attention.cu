@@ -27,7 +27,8 @@ __global__ void __launch_bounds__(kThreadsA)
 k_attention(const __grid_constant__ AttentionParams p) {
   grid_begin();
   constexpr int C = kWarps * ROWS;  // contracted rows, with those that do not exist
-  __shared__ __align__(16) float q[SUMS ? 1 : kTok][C], k[kTok][C];
+  // rows of four floats more: sixteen keys at once lie in different banks
+  __shared__ __align__(16) float q[SUMS ? 1 : kTok][C + 4], k[kTok][C + 4];
   __shared__ float v[kTok][kCols], part[SUMS ? 1 : kWarps][kTok][kCols], score[kTok][kTok + 1], power[kTok + 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int slices = (p.D + kCols - 1) / kCols;
@@ -58,18 +59,39 @@ k_attention(const __grid_constant__ AttentionParams p) {
         static_cast<O*>(p.o.data)[w.batch * p.o.batch + t * p.o.token + head * p.o.head + col] = from_f32<O>(0.f);
   }
   const int after = p.back ? 0 : 1;
+  // The next block's rows are under way while a block is worked on.
+  constexpr int PER = kTok * C / kThreadsA, VPER = kTok / kWarps;
+  E next_q[SUMS ? 1 : PER], next_k[PER], next_v[VPER];
+  const auto fetch = [&](int t0) {
+    const int n = min(kTok, w.t1 - t0);
+    const auto token = [&](int j) { return w.start + (p.back ? w.length - 1 - (t0 + j) : t0 + j); };
+#pragma unroll
+    for (int a = 0; a < PER; ++a) {
+      const int j = (a * kThreadsA + (int)threadIdx.x) / C, c = (a * kThreadsA + (int)threadIdx.x) % C;
+      const bool some = j < n && c < p.C;
+      next_k[a] = some ? row_of<E>(p.k, w.batch, token(j), head)[c] : from_f32<E>(0.f);
+      if constexpr (!SUMS) next_q[a] = some ? row_of<E>(p.q, w.batch, token(j), head)[c] : from_f32<E>(0.f);
+    }
+#pragma unroll
+    for (int a = 0; a < VPER; ++a) {
+      const int j = a * kWarps + warp;
+      next_v[a] = j < n && mine ? row_of<E>(p.v, w.batch, token(j), head)[col] : from_f32<E>(0.f);
+    }
+  };
+  if (w.t0 < w.t1) fetch(w.t0);
   for (int t0 = w.t0; t0 < w.t1; t0 += kTok) {
     const int n = min(kTok, w.t1 - t0);
     const auto token = [&](int j) { return w.start + (p.back ? w.length - 1 - (t0 + j) : t0 + j); };
     __syncthreads();
-    for (int at = threadIdx.x; at < kTok * C; at += kThreadsA) {
-      const int j = at / C, c = at % C;
-      const bool some = j < n && c < p.C;
-      k[j][c] = some ? to_f32(row_of<E>(p.k, w.batch, token(j), head)[c]) : 0.f;
-      if constexpr (!SUMS) q[j][c] = some ? to_f32(row_of<E>(p.q, w.batch, token(j), head)[c]) : 0.f;
+#pragma unroll
+    for (int a = 0; a < PER; ++a) {
+      const int j = (a * kThreadsA + (int)threadIdx.x) / C, c = (a * kThreadsA + (int)threadIdx.x) % C;
+      k[j][c] = to_f32(next_k[a]);
+      if constexpr (!SUMS) q[j][c] = to_f32(next_q[a]);
     }
-    for (int j = warp; j < kTok; j += kWarps)
-      v[j][lane] = j < n && mine ? to_f32(row_of<E>(p.v, w.batch, token(j), head)[col]) : 0.f;
+#pragma unroll
+    for (int a = 0; a < VPER; ++a) v[a * kWarps + warp][lane] = to_f32(next_v[a]);
+    if (t0 + kTok < w.t1) fetch(t0 + kTok);
     __syncthreads();
     if constexpr (!SUMS) {
       // each thread two scores, those above the diagonal zero
@@ -120,7 +142,8 @@ k_attention(const __grid_constant__ AttentionParams p) {
         float sum = 0.f, near = 0.f;
 #pragma unroll
         for (int q = 0; q < kWarps; ++q) sum += part[q][i][lane];
-        for (int j = 0; j <= i; ++j) near = fmaf(score[i][j], v[j][lane], near);
+#pragma unroll
+        for (int j = 0; j < kTok; ++j) near = fmaf(score[i][j], v[j][lane], near);
         sum = fmaf(sum, power[i + after], near) * p.out_scale;
         if (mine)
           static_cast<O*>(p.o.data)[w.batch * p.o.batch + token(i) * p.o.token + head * p.o.head + col] = from_f32<O>(sum);
@@ -146,20 +169,29 @@ k_attention_carry(const __grid_constant__ AttentionParams p) {
   const int64_t size = (int64_t)p.C * p.D;
   const int blocks = (int)((size + 255) / 256), row = blockIdx.x / blocks;
   const int sequence = row / p.H, head = row % p.H;
-  const int length = length_of(p, sequence), n = pieces_of(length, p.segment);
+  const int n = pieces_of(length_of(p, sequence), p.segment);
+  if (n == 1) return;  // nothing is read from its place
   const int64_t item0 = p.offsets ? pieces_before(p, sequence) : (int64_t)sequence * p.segments;
   const Decay d = decay_of(log_decay_of(p, head) * (float)p.segment);
   const int64_t at = (int64_t)(blockIdx.x % blocks) * 256 + threadIdx.x;
   if (at >= size) return;
   const int64_t c = at / p.D, e = at % p.D;
   float S = p.first ? p.first[((int64_t)sequence * p.H + head) * size + c * p.state_row + e * p.state_col] : 0.f;
-  for (int k = 0; k + 1 < n && item0 + k < p.items; ++k) {
-    float* x = p.carry + ((item0 + k) * p.H + head) * size + at;
-    const float u = *x;
-    *x = S;
-    S = decayed(S, d, u);
+  const int last = (int)min((int64_t)n, p.items - item0) - 1;  // the last piece's own sum is not known, nor needed
+  const int64_t step = p.H * size;
+  float* x = p.carry + (item0 * p.H + head) * size + at;
+  constexpr int AHEAD = 16;
+  for (int k0 = 0; k0 <= last; k0 += AHEAD) {
+    float u[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) u[k] = k0 + k < last ? x[(k0 + k) * step] : 0.f;
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      if (k0 + k > last) break;
+      x[(k0 + k) * step] = S;
+      S = decayed(S, d, u[k]);
+    }
   }
-  if (n > 1 && item0 + n - 1 < p.items) p.carry[((item0 + n - 1) * p.H + head) * size + at] = S;
 }
 
 template <typename E>
@@ -203,10 +235,13 @@ AttentionShape attention_shape(int64_t B, int64_t T, int64_t H, int C, int D, in
   // CTAs that run at once
   const int64_t slots = (int64_t)kSMs * (!mma ? 4 : C <= 64 && D <= 64 ? 2 : 1);
   // Rows are cut where there are too few of them: keys and values are then read twice, which costs about
-  // six tenths of a walk.  Packed sequences are of any length: those longer than a CTA's fair share are cut.
+  // six tenths of a walk.  Packed sequences are of any length: where there are enough of them, only those are cut that
+  // are longer than three CTAs' fair shares.
+  const bool enough = (packed ? B : 1) * ctas * 16 >= slots * 10;
   int64_t segment = T;
-  if (packed || ctas * 16 < slots * 10) segment = (T * ctas + slots - 1) / slots;
-  segment = segment < 128 ? 128 : (segment + 127) / 128 * 128;
+  if (packed || !enough) segment = (T * ctas + slots - 1) / slots * (enough ? 3 : 1);
+  const int64_t unit = mma ? 128 : 64;
+  segment = segment < unit ? unit : (segment + unit - 1) / unit * unit;
   if (segment >= T) segment = T > 0 ? T : 1;
   shape.segment = (int32_t)segment;
   shape.segments = (int32_t)(T > 0 ? (T + segment - 1) / segment : 1);
