@@ -99,12 +99,16 @@ k_attention(const __grid_constant__ AttentionParams p) {
         const int i = at / kTok, j = at % kTok;
         float sum = 0.f;
         if (j <= i) {
+          float four[4] = {0.f, 0.f, 0.f, 0.f};  // sums that do not wait for one another
 #pragma unroll 8
           for (int c = 0; c < C; c += 4) {
             const float4 a = *reinterpret_cast<const float4*>(&q[i][c]), b = *reinterpret_cast<const float4*>(&k[j][c]);
-            sum = fmaf(a.x, b.x, fmaf(a.y, b.y, fmaf(a.z, b.z, fmaf(a.w, b.w, sum))));
+            four[0] = fmaf(a.x, b.x, four[0]);
+            four[1] = fmaf(a.y, b.y, four[1]);
+            four[2] = fmaf(a.z, b.z, four[2]);
+            four[3] = fmaf(a.w, b.w, four[3]);
           }
-          sum *= power[i - j] * p.in_scale;
+          sum = ((four[0] + four[1]) + (four[2] + four[3])) * (power[i - j] * p.in_scale);
         }
         score[i][j] = sum;
       }

@@ -14,7 +14,8 @@ namespace {
 using namespace norm;
 
 template <typename E, int TPR, int V, int L>
-__global__ void __launch_bounds__(kCtaThreads<TPR>)
+// Registers for 1536 threads of an SM: those of 2-byte types with no more than 128 threads a row have 46 without the cap.
+__global__ void __launch_bounds__(kCtaThreads<TPR>, V == 1 && sizeof(E) == 2 && TPR <= 768 ? 1536 / kCtaThreads<TPR> : 1)
 k_gated_norm(const __grid_constant__ GatedNormParams p, int outer) {
   grid_begin();
   __shared__ float scratch[2][32];

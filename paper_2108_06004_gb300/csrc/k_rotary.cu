@@ -4,24 +4,14 @@
 // the frequency: position 2^31 is off by 4e-8 turns at most.
 //
 // Bound by memory: every element that moves is read and written once.  A CTA works out the sines and cosines of its
-// tokens once, for all heads, and then moves units of eight pairs (16-byte words) or single pairs.
+// tokens once; a thread then has one place of a head (eight pairs as two 16-byte words, or one pair, or words that are
+// copied) of one token, whose sines and cosines stay in its registers, in every so many heads.
 #include "attention.cuh"
 
 namespace gs {
 namespace {
 
 constexpr int kRotaryThreads = 256, kRotaryPairs = 1024;  // sines and cosines that a CTA holds
-
-template <typename E>
-__device__ __forceinline__ void turn(float (&a)[8], float (&b)[8], const float2* cs) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float2 t = cs[j];
-    const float x = a[j] * t.x - b[j] * t.y;
-    b[j] = a[j] * t.y + b[j] * t.x;
-    a[j] = x;
-  }
-}
 
 // VEC: all rows start at 16-byte boundaries, R is a multiple of 16 and what is copied of 8.
 template <typename E, bool INTERLEAVED, bool VEC>
@@ -30,12 +20,12 @@ k_rotary(const __grid_constant__ RotaryParams p, int tokens, int parts) {
   grid_begin();
   __shared__ __align__(16) float2 cs[kRotaryPairs];
   const int half = p.R / 2, part = blockIdx.x % parts;
-  const int64_t n0 = (int64_t)(blockIdx.x / parts) * tokens, all = p.B * p.T;
-  const int here = (int)(all - n0 < tokens ? all - n0 : tokens);
+  const uint32_t all = (uint32_t)(p.B * p.T), n0 = blockIdx.x / parts * (uint32_t)tokens;
+  const int here = (int)min(all - n0, (uint32_t)tokens);
   for (int at = threadIdx.x; at < here * half; at += kRotaryThreads) {
-    const int64_t n = n0 + at / half;
+    const uint32_t n = n0 + at / half;
     const int j = at % half;
-    const int32_t position = p.positions ? p.positions[n] : (int32_t)(p.first + n % p.T);
+    const int32_t position = p.positions ? p.positions[n] : (int32_t)(p.first + n % (uint32_t)p.T);
     const double turns = p.frequencies[j] * 0.15915494309189533577;
     // the fraction in [0, 1] as 2^64ths; 2^64 itself is no turn at all
     const double share = (turns - floor(turns)) * 18446744073709551616.0;
@@ -46,63 +36,83 @@ k_rotary(const __grid_constant__ RotaryParams p, int tokens, int parts) {
     cs[at] = make_float2(c * p.magnitude, s * p.magnitude * p.sign);
   }
   __syncthreads();
-  const int h0 = (int)((int64_t)p.H * part / parts), heads = (int)((int64_t)p.H * (part + 1) / parts) - h0;
-  if constexpr (VEC) {
-    const int rot = p.R / 16, units = rot + (p.copy ? (p.D - p.R) / 8 : 0);
-    for (int at = threadIdx.x; at < here * heads * units; at += kRotaryThreads) {
-      const int u = at % units, row = at / units, t = row / heads;
-      const int64_t n = n0 + t, batch = n / p.T, token = n % p.T, head = h0 + row % heads;
-      const E* x = static_cast<const E*>(p.x.data) + batch * p.x.batch + token * p.x.token + head * p.x.head;
-      E* out = static_cast<E*>(p.out.data) + batch * p.out.batch + token * p.out.token + head * p.out.head;
+  const int first = (int)((int64_t)p.H * part / parts), last = (int)((int64_t)p.H * (part + 1) / parts);
+  const int turned = VEC ? p.R / 16 : half, units = turned + (!p.copy ? 0 : VEC ? (p.D - p.R) / 8 : p.D - p.R);
+  // threads side by side: places of a head, tokens, heads
+  const int wide = units < kRotaryThreads ? units : kRotaryThreads, lane = threadIdx.x / wide;
+  const int t = lane % tokens, heads = kRotaryThreads / wide / tokens, h0 = first + lane / tokens;
+  if (t >= here || lane / tokens >= heads) return;
+  const uint32_t n = n0 + t, batch = n / (uint32_t)p.T, token = n - batch * (uint32_t)p.T;
+  const E* const x = static_cast<const E*>(p.x.data) + batch * p.x.batch + token * p.x.token;
+  E* const out = static_cast<E*>(p.out.data) + batch * p.out.batch + token * p.out.token;
+  for (int u = threadIdx.x % wide; u < units; u += wide) {
+    if constexpr (VEC) {
       const Span g = {0, 0, 8};
-      if (u >= rot) {
-        const int c = p.R + (u - rot) * 8;
-        const Raw8<E> raw = fetch8<E, kEven>(x + c, g);
+      constexpr int AHEAD = 4;
+      if (u >= turned) {
+        const int c = p.R + (u - turned) * 8;
+        for (int h = h0; h < last; h += AHEAD * heads) {
+          Raw8<E> raw[AHEAD];
 #pragma unroll
-        for (int k = 0; k < (int)(sizeof(E) / 2); ++k) reinterpret_cast<uint4*>(out + c)[k] = raw.q[k];
+          for (int a = 0; a < AHEAD; ++a)
+            if (h + a * heads < last) raw[a] = fetch8<E, kEven>(x + (h + a * heads) * p.x.head + c, g);
+#pragma unroll
+          for (int a = 0; a < AHEAD; ++a) {
+            if (h + a * heads >= last) continue;
+#pragma unroll
+            for (int k = 0; k < (int)(sizeof(E) / 2); ++k) reinterpret_cast<uint4*>(out + (h + a * heads) * p.out.head + c)[k] = raw[a].q[k];
+          }
+        }
         continue;
       }
       const int ca = INTERLEAVED ? u * 16 : u * 8, cb = INTERLEAVED ? ca + 8 : ca + half;
-      const Raw8<E> ra = fetch8<E, kEven>(x + ca, g), rb = fetch8<E, kEven>(x + cb, g);
-      float a[8], b[8];
-      unpack8<E, kEven>(ra, g, a);
-      unpack8<E, kEven>(rb, g, b);
-      const float2* t8 = cs + t * half + u * 8;
-      if constexpr (INTERLEAVED) {
-        float e[8], o[8];
+      float2 f[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          e[j] = a[2 * j], o[j] = a[2 * j + 1];
-          e[4 + j] = b[2 * j], o[4 + j] = b[2 * j + 1];
-        }
-        turn<E>(e, o, t8);
+      for (int j = 0; j < 8; ++j) f[j] = cs[t * half + u * 8 + j];
+      for (int h = h0; h < last; h += AHEAD / 2 * heads) {
+        Raw8<E> ra[AHEAD / 2], rb[AHEAD / 2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          a[2 * j] = e[j], a[2 * j + 1] = o[j];
-          b[2 * j] = e[4 + j], b[2 * j + 1] = o[4 + j];
+        for (int a = 0; a < AHEAD / 2; ++a) {
+          if (h + a * heads >= last) continue;
+          const E* from = x + (h + a * heads) * p.x.head;
+          ra[a] = fetch8<E, kEven>(from + ca, g);
+          rb[a] = fetch8<E, kEven>(from + cb, g);
         }
-      } else {
-        turn<E>(a, b, t8);
+#pragma unroll
+        for (int a = 0; a < AHEAD / 2; ++a) {
+          if (h + a * heads >= last) continue;
+          E* to = out + (h + a * heads) * p.out.head;
+          float v[2][8];
+          unpack8<E, kEven>(ra[a], g, v[0]);
+          unpack8<E, kEven>(rb[a], g, v[1]);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            // pair j: two adjacent elements of one of the words, or one of each
+            float &first_one = INTERLEAVED ? v[j / 4][j % 4 * 2] : v[0][j], &other = INTERLEAVED ? v[j / 4][j % 4 * 2 + 1] : v[1][j];
+            const float one = first_one, two = other;
+            first_one = one * f[j].x - two * f[j].y;
+            other = one * f[j].y + two * f[j].x;
+          }
+          store8<E, kEven>(to + ca, g, v[0]);
+          store8<E, kEven>(to + cb, g, v[1]);
+        }
       }
-      store8<E, kEven>(out + ca, g, a);
-      store8<E, kEven>(out + cb, g, b);
-    }
-  } else {
-    const int units = half + (p.copy ? p.D - p.R : 0);
-    for (int at = threadIdx.x; at < here * heads * units; at += kRotaryThreads) {
-      const int u = at % units, row = at / units, t = row / heads;
-      const int64_t n = n0 + t, batch = n / p.T, token = n % p.T, head = h0 + row % heads;
-      const E* x = static_cast<const E*>(p.x.data) + batch * p.x.batch + token * p.x.token + head * p.x.head;
-      E* out = static_cast<E*>(p.out.data) + batch * p.out.batch + token * p.out.token + head * p.out.head;
-      if (u >= half) {
-        out[p.R + u - half] = x[p.R + u - half];
-        continue;
+    } else {
+      const bool turns = u < half;
+      const int ca = !turns ? p.R + u - half : INTERLEAVED ? 2 * u : u, cb = INTERLEAVED ? ca + 1 : u + half;
+      const float2 f = turns ? cs[t * half + u] : make_float2(0.f, 0.f);
+#pragma unroll 4
+      for (int h = h0; h < last; h += heads) {
+        const E* from = x + h * p.x.head;
+        E* to = out + h * p.out.head;
+        if (!turns) {
+          to[ca] = from[ca];
+          continue;
+        }
+        const float a = to_f32(from[ca]), b = to_f32(from[cb]);
+        to[ca] = from_f32<E>(a * f.x - b * f.y);
+        to[cb] = from_f32<E>(a * f.y + b * f.x);
       }
-      const int ca = INTERLEAVED ? 2 * u : u, cb = INTERLEAVED ? ca + 1 : u + half;
-      const float a = to_f32(x[ca]), b = to_f32(x[cb]);
-      const float2 t2 = cs[t * half + u];
-      out[ca] = from_f32<E>(a * t2.x - b * t2.y);
-      out[cb] = from_f32<E>(a * t2.y + b * t2.x);
     }
   }
 }
@@ -112,10 +122,13 @@ k_rotary(const __grid_constant__ RotaryParams p, int tokens, int parts) {
 cudaError_t launch_rotary(const RotaryParams& p, int dtype, bool interleaved, bool vec, cudaStream_t s) {
   const int64_t all = p.B * p.T;
   const int half = p.R / 2;
-  // as many tokens as the table holds, up to eight, and fewer while there are fewer than four CTAs an SM;
-  // the heads of few tokens are shared out
+  const int units = (vec ? p.R / 16 : half) + (!p.copy ? 0 : vec ? (p.D - p.R) / 8 : p.D - p.R);
+  // as many tokens as the table and the threads hold, up to eight, and fewer while there are fewer than four CTAs an
+  // SM; the heads of few tokens are shared out
   int tokens = half > 0 ? kRotaryPairs / half : 8;
   tokens = tokens > 8 ? 8 : tokens;
+  const int lanes = units < kRotaryThreads ? kRotaryThreads / units : 1;
+  tokens = tokens > lanes ? lanes : tokens;
   while (tokens > 1 && (all + tokens - 1) / tokens < 4 * kSMs) tokens /= 2;
   const int64_t groups = (all + tokens - 1) / tokens;
   int parts = 1;
