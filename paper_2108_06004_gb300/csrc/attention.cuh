@@ -40,6 +40,12 @@ struct AttentionParams {
   int32_t items;        // pieces of all sequences, at most
   float in_scale, out_scale;  // of what is added to the state, and of what is read from it
   int32_t back;         // walks from each sequence's end, and takes a token's decay after it
+  int32_t wide;         // o is fp32, for heads that are summed after
+};
+// Walks that run at once: of the same C, D, wide and, where one of them gives its last state, all do.
+struct AttentionWalks {
+  AttentionParams of[3];
+  int32_t count;
 };
 
 constexpr int kAttentionMaxHead = 256;
@@ -157,11 +163,10 @@ struct AttentionShape {
 // The pieces of a walk.  Walks for the tensor cores have blocks of 128 tokens.
 inline bool for_tensor_cores(int C, int D, int dtype) { return dtype != GS_F32 && C <= 128 && C % 8 == 0 && D % 8 == 0; }
 AttentionShape attention_shape(int64_t B, int64_t T, int64_t H, int C, int D, int dtype, bool packed);
-cudaError_t launch_attention_carry(const AttentionParams& p, cudaStream_t s);
-// The walk on the tensor cores, where for_tensor_cores; not taken where a tensor's strides do not allow it.
-cudaError_t launch_attention_mma(const AttentionParams& p, int dtype, bool wide, cudaStream_t s, bool& taken);
-// One walk; o is fp32 where `wide`, for heads that are summed after.
-cudaError_t launch_attention(AttentionParams& p, int dtype, bool wide, cudaStream_t s);
+cudaError_t launch_attention_carry(const AttentionWalks& walks, cudaStream_t s);
+// The walks on the tensor cores, where for_tensor_cores; not taken where a tensor's strides do not allow it.
+cudaError_t launch_attention_mma(const AttentionWalks& walks, int dtype, cudaStream_t s, bool& taken);
+cudaError_t launch_attention(const AttentionWalks& walks, int dtype, cudaStream_t s);
 cudaError_t launch_head_sums(const HeadSumParams& p, int dtype, cudaStream_t s);
 cudaError_t launch_attention_step(const AttentionStepParams& p, int dtype, bool vec, cudaStream_t s);
 

@@ -71,8 +71,9 @@ size_t carry_bytes(const Sizes& z, int64_t C, int64_t D) {
   return shape.segments > 1 ? round256((size_t)shape.items * z.H * C * D * sizeof(float)) : 0;
 }
 
-size_t part_bytes(const Sizes& z) {
-  return z.H > z.K ? round256((size_t)(z.packed ? 1 : z.B) * z.T * z.H * std::max(z.Dk, z.Dv) * sizeof(float)) : 0;
+// For heads that are summed after, of D elements.
+size_t part_bytes(const Sizes& z, int64_t D) {
+  return z.H > z.K ? round256((size_t)(z.packed ? 1 : z.B) * z.T * z.H * D * sizeof(float)) : 0;
 }
 
 gs_status attention_bytes(const Sizes& z, bool backward, size_t* carry, size_t* bytes) {
@@ -81,7 +82,7 @@ gs_status attention_bytes(const Sizes& z, bool backward, size_t* carry, size_t* 
       return bad("B * T * H is too large for one call");
   *carry = carry_bytes(z, z.Dk, z.Dv);
   if (backward) *carry = std::max(*carry, carry_bytes(z, z.Dv, z.Dk));
-  *bytes = *carry + (backward ? part_bytes(z) : 0);
+  *bytes = backward ? 3 * *carry + part_bytes(z, z.Dk) + part_bytes(z, z.Dv) : *carry;
   if (*bytes == 0) *bytes = 256;
   return GS_OK;
 }
@@ -98,15 +99,19 @@ gs::HeadsIn in(const gs_heads* t, int64_t share) {
 }
 gs::HeadsOut out(const gs_heads* t) { return {t->data, t->batch_stride, t->token_stride, t->head_stride}; }
 
-gs_status run_walk(const Sizes& z, gs::AttentionParams& p, bool wide, gs_stream stream, const char* what) {
-  const gs::AttentionShape shape = gs::attention_shape(z.B, z.T, z.H, p.C, p.D, z.dtype, z.packed);
-  p.B = z.B;
-  p.T = z.T;
-  p.H = (int32_t)z.H;
-  p.segment = shape.segment;
-  p.segments = shape.segments;
-  p.items = (int32_t)shape.items;
-  const cudaError_t e = gs::launch_attention(p, z.dtype, wide, as_stream(stream));
+// Walks of the same C and D, at once.
+gs_status run_walks(const Sizes& z, gs::AttentionWalks& walks, gs_stream stream, const char* what) {
+  for (int k = 0; k < walks.count; ++k) {
+    gs::AttentionParams& p = walks.of[k];
+    const gs::AttentionShape shape = gs::attention_shape(z.B, z.T, z.H, p.C, p.D, z.dtype, z.packed);
+    p.B = z.B;
+    p.T = z.T;
+    p.H = (int32_t)z.H;
+    p.segment = shape.segment;
+    p.segments = shape.segments;
+    p.items = (int32_t)shape.items;
+  }
+  const cudaError_t e = gs::launch_attention(walks, z.dtype, as_stream(stream));
   return e == cudaSuccess ? GS_OK : gs::record_cuda_failure(e, what);
 }
 
@@ -152,7 +157,7 @@ gs_status gs_rotary(const gs_heads* x, const gs_heads* o, const double* frequenc
                              (H > 1 && x->head_stride != o->head_stride)))
     return bad("out may be x itself only with the same strides");
   if (R == 0 && !p.copy) return GS_OK;
-  bool vec = R % 16 == 0 && (!p.copy || (D - R) % 8 == 0);
+  bool vec = R % (interleaved ? 8 : 16) == 0 && (!p.copy || (D - R) % 8 == 0);
   for (const gs_heads* t : {x, o})
     vec = vec && aligned(t->data, 16) && ((t->batch_stride | t->token_stride | t->head_stride) * item(dtype)) % 16 == 0;
   const cudaError_t e = gs::launch_rotary(p, dtype, interleaved != 0, vec, as_stream(stream));
@@ -212,8 +217,10 @@ gs_status gs_linear_attention_forward(const gs_heads* q, const gs_heads* k, cons
   GS_TRY(attention_bytes(z, false, &carry, &need));
   GS_TRY(check_workspace(workspace, workspace_bytes, need, "gs_linear_attention_workspace_size"));
   if (!rows) return GS_OK;
-  gs::AttentionParams p;
-  std::memset(&p, 0, sizeof(p));
+  gs::AttentionWalks walks;
+  std::memset(&walks, 0, sizeof(walks));
+  walks.count = 1;
+  gs::AttentionParams& p = walks.of[0];
   p.q = in(q, 1);
   p.k = in(k, H / K);
   p.v = in(v, H / K);
@@ -230,7 +237,7 @@ gs_status gs_linear_attention_forward(const gs_heads* q, const gs_heads* k, cons
   p.D = (int32_t)Dv;
   p.in_scale = 1.f;
   p.out_scale = scale;
-  return run_walk(z, p, false, stream, "linear_attention_forward launch");
+  return run_walks(z, walks, stream, "linear_attention_forward launch");
   GS_GUARD_END
 }
 
@@ -265,33 +272,76 @@ gs_status gs_linear_attention_backward(const gs_heads* d_o, const gs_heads* q, c
   GS_TRY(check_workspace(workspace, workspace_bytes, need, "gs_linear_attention_workspace_size"));
   if (!rows) return GS_OK;
   const int64_t share = H / K;
-  gs::AttentionParams p;
-  std::memset(&p, 0, sizeof(p));
-  p.log_decay = log_decay;
-  p.lengths = lengths;
-  p.offsets = offsets;
-  p.carry = static_cast<float*>(workspace);
+  const char* what = "linear_attention_backward launch";
+  char* ws = static_cast<char*>(workspace);
+  float* const part_k = reinterpret_cast<float*>(ws + 3 * carry);
+  float* const part_v = reinterpret_cast<float*>(ws + 3 * carry + part_bytes(z, Dk));
+  gs::AttentionWalks first, second;
+  std::memset(&first, 0, sizeof(first));
+  for (int k = 0; k < 3; ++k) {
+    gs::AttentionParams& p = first.of[k];
+    p.log_decay = log_decay;
+    p.lengths = lengths;
+    p.offsets = offsets;
+    p.carry = reinterpret_cast<float*>(ws + k * carry);
+    p.in_scale = k > 0 ? scale : 1.f;
+    p.out_scale = k > 0 ? 1.f : scale;
+    p.back = k > 0;
+  }
+  const auto shared = [&](const gs_heads* to, float* part, int64_t D) {
+    return share == 1 ? out(to) : gs::HeadsOut{part, T * H * D, H * D, D};
+  };
   // dq: do reads the transposed state that v and k make up
+  gs::AttentionParams& p = first.of[0];
   p.q = in(d_o, 1);
   p.k = in(v, share);
   p.v = in(k, share);
   p.o = out(dq);
   p.first = s0;
-  p.state_row = 1;
-  p.state_col = Dv;
-  p.C = (int32_t)Dv;
-  p.D = (int32_t)Dk;
-  p.in_scale = 1.f;
-  p.out_scale = scale;
-  GS_TRY(run_walk(z, p, false, stream, "linear_attention_backward launch"));
-  p.back = 1;
-  p.in_scale = scale;
-  p.out_scale = 1.f;
-  p.first = ds_last;
+  // dk: v reads the transposed gradient of the state, which do and q make up
+  gs::AttentionParams& r = first.of[1];
+  r.q = in(v, share);
+  r.k = in(d_o, 1);
+  r.v = in(q, 1);
+  r.o = shared(dk, part_k, Dk);
+  r.wide = share > 1;
+  r.first = ds_last;
+  for (int n = 0; n < 2; ++n) {
+    first.of[n].state_row = 1;
+    first.of[n].state_col = Dv;
+    first.of[n].C = (int32_t)Dv;
+    first.of[n].D = (int32_t)Dk;
+  }
+  // dv: k reads the gradient of the state, which q and do make up
+  gs::AttentionParams& t = first.of[2];
+  t.q = in(k, share);
+  t.k = in(q, 1);
+  t.v = in(d_o, 1);
+  t.o = shared(dv, part_v, Dv);
+  t.wide = share > 1;
+  t.first = ds_last;
+  t.last = ds0;
+  t.state_row = Dv;
+  t.state_col = 1;
+  t.C = (int32_t)Dk;
+  t.D = (int32_t)Dv;
+  // all at once, where they are of one kind: the heads' sizes, the outputs' type, whether there is a last state
+  const bool alike = Dk == Dv && !ds0;
+  second = first;
+  second.of[0] = first.of[2];
+  second.count = 1;
+  first.count = alike && share == 1 ? 3 : share == 1 ? 2 : 1;
+  GS_TRY(run_walks(z, first, stream, what));
+  if (share > 1) {
+    first.of[0] = first.of[1];
+    first.of[1] = first.of[2];
+    first.count = alike ? 2 : 1;
+    GS_TRY(run_walks(z, first, stream, what));
+  }
+  if (!alike) GS_TRY(run_walks(z, second, stream, what));
+  if (share == 1 || T == 0) return GS_OK;
   gs::HeadSumParams sum;
   std::memset(&sum, 0, sizeof(sum));
-  float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + carry);
-  sum.part = part;
   sum.lengths = lengths;
   sum.offsets = offsets;
   sum.B = batch;
@@ -299,30 +349,14 @@ gs_status gs_linear_attention_backward(const gs_heads* d_o, const gs_heads* q, c
   sum.sequences = (int32_t)B;
   sum.K = (int32_t)K;
   sum.share = (int32_t)share;
-  const auto walk = [&](const gs_heads* to, int64_t D) -> gs_status {
-    p.D = (int32_t)D;
-    p.o = share == 1 ? out(to) : gs::HeadsOut{part, T * H * D, H * D, D};
-    GS_TRY(run_walk(z, p, share > 1, stream, "linear_attention_backward launch"));
-    if (share == 1 || T == 0) return GS_OK;
-    sum.out = out(to);
-    sum.D = (int32_t)D;
+  for (const bool keys : {true, false}) {
+    sum.part = keys ? part_k : part_v;
+    sum.out = out(keys ? dk : dv);
+    sum.D = (int32_t)(keys ? Dk : Dv);
     const cudaError_t e = gs::launch_head_sums(sum, dtype, as_stream(stream));
-    return e == cudaSuccess ? GS_OK : gs::record_cuda_failure(e, "linear_attention_backward launch");
-  };
-  // dk: v reads the transposed gradient of the state, which do and q make up
-  p.q = in(v, share);
-  p.k = in(d_o, 1);
-  p.v = in(q, 1);
-  GS_TRY(walk(dk, Dk));
-  // dv: k reads the gradient of the state, which q and do make up
-  p.q = in(k, share);
-  p.k = in(q, 1);
-  p.v = in(d_o, 1);
-  p.state_row = Dv;
-  p.state_col = 1;
-  p.C = (int32_t)Dk;
-  p.last = ds0;
-  return walk(dv, Dv);
+    if (e != cudaSuccess) return gs::record_cuda_failure(e, what);
+  }
+  return GS_OK;
   GS_GUARD_END
 }
 

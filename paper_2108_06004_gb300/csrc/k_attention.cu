@@ -24,15 +24,17 @@ __device__ __forceinline__ const E* row_of(const HeadsIn& t, int batch, int64_t 
 // SUMS: only the piece's own sum, from a state of zero, into carry.
 template <typename E, typename O, int ROWS, bool SUMS>
 __global__ void __launch_bounds__(kThreadsA)
-k_attention(const __grid_constant__ AttentionParams p) {
+k_attention(const __grid_constant__ AttentionWalks walks) {
   grid_begin();
+  const uint32_t each = gridDim.x / walks.count, block = blockIdx.x % each;
+  const AttentionParams& p = walks.of[blockIdx.x / each];
   constexpr int C = kWarps * ROWS;  // contracted rows, with those that do not exist
   // rows of four floats more: sixteen keys at once lie in different banks
   __shared__ __align__(16) float q[SUMS ? 1 : kTok][C + 4], k[kTok][C + 4];
   __shared__ float v[kTok][kCols], part[SUMS ? 1 : kWarps][kTok][kCols], score[kTok][kTok + 1], power[kTok + 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int slices = (p.D + kCols - 1) / kCols;
-  const int slice = blockIdx.x % slices, head = blockIdx.x / slices % p.H, item = blockIdx.x / slices / p.H;
+  const int slice = block % slices, head = block / slices % p.H, item = block / slices / p.H;
   Piece w;
   if (!find_piece(p, item, w)) return;
   const int c0 = slice * kCols, cols = min(p.D - c0, kCols), col = c0 + lane;
@@ -168,16 +170,18 @@ k_attention(const __grid_constant__ AttentionParams p) {
 
 // The states before a sequence's pieces from the pieces' own sums, in their place.
 __global__ void __launch_bounds__(256)
-k_attention_carry(const __grid_constant__ AttentionParams p) {
+k_attention_carry(const __grid_constant__ AttentionWalks walks) {
   grid_begin();
+  const uint32_t each = gridDim.x / walks.count;
+  const AttentionParams& p = walks.of[blockIdx.x / each];
   const int64_t size = (int64_t)p.C * p.D;
-  const int blocks = (int)((size + 255) / 256), row = blockIdx.x / blocks;
+  const int blocks = (int)((size + 255) / 256), row = blockIdx.x % each / blocks;
   const int sequence = row / p.H, head = row % p.H;
   const int n = pieces_of(length_of(p, sequence), p.segment);
   if (n == 1) return;  // nothing is read from its place
   const int64_t item0 = p.offsets ? pieces_before(p, sequence) : (int64_t)sequence * p.segments;
   const Decay d = decay_of(log_decay_of(p, head) * (float)p.segment);
-  const int64_t at = (int64_t)(blockIdx.x % blocks) * 256 + threadIdx.x;
+  const int64_t at = (int64_t)(blockIdx.x % each % blocks) * 256 + threadIdx.x;
   if (at >= size) return;
   const int64_t c = at / p.D, e = at % p.D;
   float S = p.first ? p.first[((int64_t)sequence * p.H + head) * size + c * p.state_row + e * p.state_col] : 0.f;
@@ -214,21 +218,23 @@ k_head_sums(const __grid_constant__ HeadSumParams p) {
 }
 
 template <typename E, typename O, int ROWS>
-cudaError_t walk(AttentionParams& p, cudaStream_t s) {
-  const dim3 grid((unsigned)((int64_t)p.items * p.H * ((p.D + kCols - 1) / kCols)));
+cudaError_t walk(const AttentionWalks& walks, cudaStream_t s) {
+  const AttentionParams& p = walks.of[0];
+  const dim3 grid((unsigned)((int64_t)walks.count * p.items * p.H * ((p.D + kCols - 1) / kCols)));
   if (p.segments > 1) {
-    cudaError_t e = launch(k_attention<E, O, ROWS, true>, grid, dim3(kThreadsA), s, p);
+    cudaError_t e = launch(k_attention<E, O, ROWS, true>, grid, dim3(kThreadsA), s, walks);
     if (e != cudaSuccess) return e;
-    e = launch_attention_carry(p, s);
+    e = launch_attention_carry(walks, s);
     if (e != cudaSuccess) return e;
   }
-  return launch(k_attention<E, O, ROWS, false>, grid, dim3(kThreadsA), s, p);
+  return launch(k_attention<E, O, ROWS, false>, grid, dim3(kThreadsA), s, walks);
 }
 
 }  // namespace
 
-cudaError_t launch_attention_carry(const AttentionParams& p, cudaStream_t s) {
-  return launch(k_attention_carry, dim3((unsigned)(((int64_t)p.C * p.D + 255) / 256 * p.B * p.H)), dim3(256), s, p);
+cudaError_t launch_attention_carry(const AttentionWalks& walks, cudaStream_t s) {
+  const AttentionParams& p = walks.of[0];
+  return launch(k_attention_carry, dim3((unsigned)(walks.count * (((int64_t)p.C * p.D + 255) / 256 * p.B * p.H))), dim3(256), s, walks);
 }
 
 AttentionShape attention_shape(int64_t B, int64_t T, int64_t H, int C, int D, int dtype, bool packed) {
@@ -253,18 +259,22 @@ AttentionShape attention_shape(int64_t B, int64_t T, int64_t H, int C, int D, in
   return shape;
 }
 
-cudaError_t launch_attention(AttentionParams& p, int dtype, bool wide, cudaStream_t s) {
+cudaError_t launch_attention(const AttentionWalks& walks, int dtype, cudaStream_t s) {
+  const AttentionParams& p = walks.of[0];
   if (for_tensor_cores(p.C, p.D, dtype)) {
     bool taken;
-    const cudaError_t e = launch_attention_mma(p, dtype, wide, s, taken);
+    const cudaError_t e = launch_attention_mma(walks, dtype, s, taken);
     if (taken || e != cudaSuccess) return e;
   }
   const auto rows = [&](auto e, auto o) {
     using E = decltype(e);
     using O = decltype(o);
-    return p.C <= 32 ? walk<E, O, 8>(p, s) : p.C <= 64 ? walk<E, O, 16>(p, s) : p.C <= 128 ? walk<E, O, 32>(p, s) : walk<E, O, 64>(p, s);
+    return p.C <= 32    ? walk<E, O, 8>(walks, s)
+           : p.C <= 64  ? walk<E, O, 16>(walks, s)
+           : p.C <= 128 ? walk<E, O, 32>(walks, s)
+                        : walk<E, O, 64>(walks, s);
   };
-  return with_type(dtype, [&](auto e) { return wide ? rows(e, float()) : rows(e, e); });
+  return with_type(dtype, [&](auto e) { return p.wide ? rows(e, float()) : rows(e, e); });
 }
 
 cudaError_t launch_head_sums(const HeadSumParams& p, int dtype, cudaStream_t s) {

@@ -33,8 +33,10 @@ using namespace tc;
 constexpr int kBlockTokens = 128;
 
 struct AttentionMmaParams {
-  CUtensorMap q, k, v, o;
-  AttentionParams a;
+  struct {
+    CUtensorMap q, k, v, o;
+  } maps[3];
+  AttentionWalks walks;
 };
 
 // C rows of the state (64 or 128) and D columns of it a CTA.  The smallest one leaves room for two CTAs an SM.
@@ -107,7 +109,7 @@ __device__ __forceinline__ float power_of_two(int n) { return __uint_as_float((u
 // PARTS: of a weighted key.  SUMS: only the piece's own sum, from a state of zero, into carry.
 template <typename E, typename R, int C, int D, int PARTS, bool SUMS>
 __global__ void __launch_bounds__(Plan<C, D>::kThreads, Plan<C, D>::kCtas)
-k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
+k_attention_mma(const __grid_constant__ AttentionMmaParams all) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   using L = Plan<C, D>;
   constexpr bool HALF = std::is_same<E, __half>::value;
@@ -115,10 +117,12 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
   constexpr int W1 = L::kNarrow || PARTS == 2 ? L::W0 + 32 * PARTS : L::P;
   extern __shared__ __align__(1024) char base[];
   Tables& tab = *reinterpret_cast<Tables*>(base + L::oTables);
-  const AttentionParams& p = params.a;
+  const uint32_t each_walk = gridDim.x / all.walks.count, cta = blockIdx.x % each_walk, which = blockIdx.x / each_walk;
+  const AttentionParams& p = all.walks.of[which];
+  const auto& params = all.maps[which];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int slices = (p.D + D - 1) / D;
-  const int slice = blockIdx.x % slices, head = blockIdx.x / slices % p.H, item = blockIdx.x / slices / p.H;
+  const int slice = cta % slices, head = cta / slices % p.H, item = cta / slices / p.H;
   Piece w;
   if (!find_piece(p, item, w)) return;
   if (SUMS && (w.ends || w.t0 >= w.length)) return;  // nothing comes after it
@@ -691,12 +695,12 @@ cudaError_t launch_mma(dim3 grid, cudaStream_t s, const AttentionMmaParams& p) {
 
 template <typename E, typename R, int C, int D, int PARTS>
 cudaError_t walk_parts(const AttentionMmaParams& q, cudaStream_t s) {
-  const AttentionParams& p = q.a;
-  const dim3 grid((unsigned)((int64_t)p.items * p.H * ((p.D + D - 1) / D)));
+  const AttentionParams& p = q.walks.of[0];
+  const dim3 grid((unsigned)((int64_t)q.walks.count * p.items * p.H * ((p.D + D - 1) / D)));
   if (p.segments > 1) {
     cudaError_t e = launch_mma<E, R, C, D, PARTS, true>(grid, s, q);
     if (e != cudaSuccess) return e;
-    e = launch_attention_carry(p, s);
+    e = launch_attention_carry(q.walks, s);
     if (e != cudaSuccess) return e;
   }
   return launch_mma<E, R, C, D, PARTS, false>(grid, s, q);
@@ -707,21 +711,25 @@ cudaError_t walk_parts(const AttentionMmaParams& q, cudaStream_t s) {
 template <typename E, typename R, int C, int D>
 cudaError_t walk(const AttentionMmaParams& q, cudaStream_t s) {
   if constexpr (std::is_same<E, __nv_bfloat16>::value)
-    if (q.a.last) return walk_parts<E, R, C, D, 3>(q, s);
+    if (q.walks.of[0].last) return walk_parts<E, R, C, D, 3>(q, s);
   return walk_parts<E, R, C, D, 2>(q, s);
 }
 
 }  // namespace
 
-cudaError_t launch_attention_mma(const AttentionParams& p, int dtype, bool wide, cudaStream_t s, bool& taken) {
+cudaError_t launch_attention_mma(const AttentionWalks& walks, int dtype, cudaStream_t s, bool& taken) {
   taken = false;
+  const AttentionParams& p = walks.of[0];
   if (p.T == 0) return cudaSuccess;
   AttentionMmaParams q;
-  q.a = p;
-  const HeadsIn o = {p.o.data, p.o.batch, p.o.token, p.o.head, 1};
-  if (!describe(q.q, p.q, p, p.C, dtype, 128, kBlockTokens) || !describe(q.k, p.k, p, p.C, dtype, 128, kBlockTokens) ||
-      !describe(q.v, p.v, p, p.D, dtype, 128, kBlockTokens) || !describe(q.o, o, p, p.D, wide ? GS_F32 : dtype, 64, 32))
-    return cudaSuccess;
+  q.walks = walks;
+  for (int k = 0; k < walks.count; ++k) {
+    const AttentionParams& a = walks.of[k];
+    const HeadsIn o = {a.o.data, a.o.batch, a.o.token, a.o.head, 1};
+    if (!describe(q.maps[k].q, a.q, a, a.C, dtype, 128, kBlockTokens) || !describe(q.maps[k].k, a.k, a, a.C, dtype, 128, kBlockTokens) ||
+        !describe(q.maps[k].v, a.v, a, a.D, dtype, 128, kBlockTokens) || !describe(q.maps[k].o, o, a, a.D, a.wide ? GS_F32 : dtype, 64, 32))
+      return cudaSuccess;
+  }
   taken = true;
   const auto sizes = [&](auto e, auto r) {
     using E = decltype(e);
@@ -729,8 +737,8 @@ cudaError_t launch_attention_mma(const AttentionParams& p, int dtype, bool wide,
     if (p.C <= 64) return p.D <= 64 ? walk<E, R, 64, 64>(q, s) : walk<E, R, 64, 128>(q, s);
     return p.D <= 64 ? walk<E, R, 128, 64>(q, s) : walk<E, R, 128, 128>(q, s);
   };
-  if (dtype == GS_F16) return wide ? sizes(__half(), float()) : sizes(__half(), __half());
-  return wide ? sizes(__nv_bfloat16(), float()) : sizes(__nv_bfloat16(), __nv_bfloat16());
+  if (dtype == GS_F16) return p.wide ? sizes(__half(), float()) : sizes(__half(), __half());
+  return p.wide ? sizes(__nv_bfloat16(), float()) : sizes(__nv_bfloat16(), __nv_bfloat16());
 }
 
 }  // namespace gs

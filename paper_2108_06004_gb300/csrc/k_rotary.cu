@@ -4,8 +4,8 @@
 // the frequency: position 2^31 is off by 4e-8 turns at most.
 //
 // Bound by memory: every element that moves is read and written once.  A CTA works out the sines and cosines of its
-// tokens once; a thread then has one place of a head (eight pairs as two 16-byte words, or one pair, or words that are
-// copied) of one token, whose sines and cosines stay in its registers, in every so many heads.
+// tokens once; a thread then has one place of a head (pairs of one 16-byte word, or of two, or one pair, or words that
+// are copied) of one token, whose sines and cosines stay in its registers, in every so many heads.
 #include "attention.cuh"
 
 namespace gs {
@@ -13,7 +13,7 @@ namespace {
 
 constexpr int kRotaryThreads = 256, kRotaryPairs = 1024;  // sines and cosines that a CTA holds
 
-// VEC: all rows start at 16-byte boundaries, R is a multiple of 16 and what is copied of 8.
+// VEC: all rows start at 16-byte boundaries, R is a multiple of 16 (interleaved: 8) and what is copied of 8.
 template <typename E, bool INTERLEAVED, bool VEC>
 __global__ void __launch_bounds__(kRotaryThreads)
 k_rotary(const __grid_constant__ RotaryParams p, int tokens, int parts) {
@@ -37,7 +37,7 @@ k_rotary(const __grid_constant__ RotaryParams p, int tokens, int parts) {
   }
   __syncthreads();
   const int first = (int)((int64_t)p.H * part / parts), last = (int)((int64_t)p.H * (part + 1) / parts);
-  const int turned = VEC ? p.R / 16 : half, units = turned + (!p.copy ? 0 : VEC ? (p.D - p.R) / 8 : p.D - p.R);
+  const int turned = !VEC ? half : INTERLEAVED ? p.R / 8 : p.R / 16, units = turned + (!p.copy ? 0 : VEC ? (p.D - p.R) / 8 : p.D - p.R);
   // threads side by side: places of a head, tokens, heads
   const int wide = units < kRotaryThreads ? units : kRotaryThreads, lane = threadIdx.x / wide;
   const int t = lane % tokens, heads = kRotaryThreads / wide / tokens, h0 = first + lane / tokens;
@@ -65,36 +65,33 @@ k_rotary(const __grid_constant__ RotaryParams p, int tokens, int parts) {
         }
         continue;
       }
-      const int ca = INTERLEAVED ? u * 16 : u * 8, cb = INTERLEAVED ? ca + 8 : ca + half;
-      float2 f[8];
+      constexpr int WORDS = INTERLEAVED ? 1 : 2, PAIRS = 4 * WORDS, N = AHEAD / WORDS;
+      const int ca = u * 8;
+      float2 f[PAIRS];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = cs[t * half + u * 8 + j];
-      for (int h = h0; h < last; h += AHEAD / 2 * heads) {
-        Raw8<E> ra[AHEAD / 2], rb[AHEAD / 2];
+      for (int j = 0; j < PAIRS; ++j) f[j] = cs[t * half + u * PAIRS + j];
+      for (int h = h0; h < last; h += N * heads) {
+        Raw8<E> raw[N][WORDS];
 #pragma unroll
-        for (int a = 0; a < AHEAD / 2; ++a) {
+        for (int a = 0; a < N; ++a)
+#pragma unroll
+          for (int k = 0; k < WORDS; ++k)
+            if (h + a * heads < last) raw[a][k] = fetch8<E, kEven>(x + (h + a * heads) * p.x.head + ca + k * half, g);
+#pragma unroll
+        for (int a = 0; a < N; ++a) {
           if (h + a * heads >= last) continue;
-          const E* from = x + (h + a * heads) * p.x.head;
-          ra[a] = fetch8<E, kEven>(from + ca, g);
-          rb[a] = fetch8<E, kEven>(from + cb, g);
-        }
+          float v[WORDS][8];
 #pragma unroll
-        for (int a = 0; a < AHEAD / 2; ++a) {
-          if (h + a * heads >= last) continue;
-          E* to = out + (h + a * heads) * p.out.head;
-          float v[2][8];
-          unpack8<E, kEven>(ra[a], g, v[0]);
-          unpack8<E, kEven>(rb[a], g, v[1]);
+          for (int k = 0; k < WORDS; ++k) unpack8<E, kEven>(raw[a][k], g, v[k]);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            // pair j: two adjacent elements of one of the words, or one of each
-            float &first_one = INTERLEAVED ? v[j / 4][j % 4 * 2] : v[0][j], &other = INTERLEAVED ? v[j / 4][j % 4 * 2 + 1] : v[1][j];
+          for (int j = 0; j < PAIRS; ++j) {
+            float &first_one = INTERLEAVED ? v[0][j * 2 % 8] : v[0][j], &other = INTERLEAVED ? v[0][(j * 2 + 1) % 8] : v[WORDS - 1][j];
             const float one = first_one, two = other;
             first_one = one * f[j].x - two * f[j].y;
             other = one * f[j].y + two * f[j].x;
           }
-          store8<E, kEven>(to + ca, g, v[0]);
-          store8<E, kEven>(to + cb, g, v[1]);
+#pragma unroll
+          for (int k = 0; k < WORDS; ++k) store8<E, kEven>(out + (h + a * heads) * p.out.head + ca + k * half, g, v[k]);
         }
       }
     } else {
@@ -122,7 +119,7 @@ k_rotary(const __grid_constant__ RotaryParams p, int tokens, int parts) {
 cudaError_t launch_rotary(const RotaryParams& p, int dtype, bool interleaved, bool vec, cudaStream_t s) {
   const int64_t all = p.B * p.T;
   const int half = p.R / 2;
-  const int units = (vec ? p.R / 16 : half) + (!p.copy ? 0 : vec ? (p.D - p.R) / 8 : p.D - p.R);
+  const int units = (!vec ? half : interleaved ? p.R / 8 : p.R / 16) + (!p.copy ? 0 : vec ? (p.D - p.R) / 8 : p.D - p.R);
   // as many tokens as the table and the threads hold, up to eight, and fewer while there are fewer than four CTAs an
   // SM; the heads of few tokens are shared out
   int tokens = half > 0 ? kRotaryPairs / half : 8;
