@@ -62,7 +62,7 @@ struct Sizes {
 
 // A walk with C contracted rows and D columns; false where its grid would be too large.
 bool shape_fits(const Sizes& z, const gs::AttentionShape& shape, int64_t C, int64_t D) {
-  const int64_t most = (int64_t(1) << 31) - 1;
+  const int64_t most = ((int64_t(1) << 31) - 1) / 3;  // three walks may run at once
   return shape.items < most && shape.items * z.H <= most / ((D + 31) / 32) && z.B * z.H <= most / ((C * D + 255) / 256);
 }
 

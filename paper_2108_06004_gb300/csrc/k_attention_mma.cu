@@ -32,11 +32,10 @@ using namespace tc;
 
 constexpr int kBlockTokens = 128;
 
+// One walk a launch: parameters at a place that a CTA has to work out cost a walk that fills the device 5 %.
 struct AttentionMmaParams {
-  struct {
-    CUtensorMap q, k, v, o;
-  } maps[3];
-  AttentionWalks walks;
+  CUtensorMap q, k, v, o;
+  AttentionParams a;
 };
 
 // C rows of the state (64 or 128) and D columns of it a CTA.  The smallest one leaves room for two CTAs an SM.
@@ -109,7 +108,7 @@ __device__ __forceinline__ float power_of_two(int n) { return __uint_as_float((u
 // PARTS: of a weighted key.  SUMS: only the piece's own sum, from a state of zero, into carry.
 template <typename E, typename R, int C, int D, int PARTS, bool SUMS>
 __global__ void __launch_bounds__(Plan<C, D>::kThreads, Plan<C, D>::kCtas)
-k_attention_mma(const __grid_constant__ AttentionMmaParams all) {
+k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   using L = Plan<C, D>;
   constexpr bool HALF = std::is_same<E, __half>::value;
@@ -117,12 +116,10 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams all) {
   constexpr int W1 = L::kNarrow || PARTS == 2 ? L::W0 + 32 * PARTS : L::P;
   extern __shared__ __align__(1024) char base[];
   Tables& tab = *reinterpret_cast<Tables*>(base + L::oTables);
-  const uint32_t each_walk = gridDim.x / all.walks.count, cta = blockIdx.x % each_walk, which = blockIdx.x / each_walk;
-  const AttentionParams& p = all.walks.of[which];
-  const auto& params = all.maps[which];
+  const AttentionParams& p = params.a;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int slices = (p.D + D - 1) / D;
-  const int slice = cta % slices, head = cta / slices % p.H, item = cta / slices / p.H;
+  const int slice = blockIdx.x % slices, head = blockIdx.x / slices % p.H, item = blockIdx.x / slices / p.H;
   Piece w;
   if (!find_piece(p, item, w)) return;
   if (SUMS && (w.ends || w.t0 >= w.length)) return;  // nothing comes after it
@@ -269,7 +266,9 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams all) {
     const bool rises = -g * kBlockTokens <= (HALF ? 8.f : 32.f);
     const int quad = warp & 3, group = warp >> 2, row = quad * 32 + lane, col0 = group * COLS;
     const uint32_t mine = tmem + ((uint32_t)(quad * 32) << 16);
-    const bool holds = quad * 32 < C;  // rows of the state
+    // Rows of the state: 64 are in the lanes of the warps that have less of A to work out, which is triangular.
+    const int above = C == 64 && p.back ? 2 : 0, state_quad = quad - above, state_row = state_quad * 32 + lane;
+    const bool holds = state_quad >= 0 && state_quad * 32 < C;
     const int64_t state = ((int64_t)w.sequence * p.H + head) * p.C * p.D;
     float* carry = p.carry + ((int64_t)item * p.H + head) * p.C * p.D;
     const float nan = __uint_as_float(0x7FC00000u);
@@ -288,11 +287,11 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams all) {
       for (int j = 0; j < COLS; ++j) {
         const int col = c0 + col0 + j;
         S[j] = 0.f;
-        if (!SUMS && row < p.C && col < p.D) {
+        if (!SUMS && state_row < p.C && col < p.D) {
           if (!(w.opens && w.ends))
-            S[j] = carry[(int64_t)row * p.D + col];
+            S[j] = carry[(int64_t)state_row * p.D + col];
           else if (p.first)
-            S[j] = p.first[state + row * p.state_row + col * p.state_col];
+            S[j] = p.first[state + state_row * p.state_row + col * p.state_col];
         }
         most = fmaxf(most, fabsf(S[j]));
       }
@@ -371,7 +370,7 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams all) {
     uint32_t part[PARTS][2][PAIRS / 2];
     const auto weigh = [&](int n, int h) {
       if (!holds) return;
-      const uint32_t from = shared_address(base + L::oK + (n & 1) * L::kQ + quad / 2 * L::kPanel);
+      const uint32_t from = shared_address(base + L::oK + (n & 1) * L::kQ + state_quad / 2 * L::kPanel);
       const float shrink = HALF ? power_of_two(-next.scale) : 1.f;
 #pragma unroll
       for (int j = 0; j < PAIRS / 8; ++j) {
@@ -380,7 +379,7 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams all) {
                                   *reinterpret_cast<const float2*>(&tab.key[t + 8 + lane % 4 * 2])};
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const int word = (quad % 2) * 4 + r * 2 + (lane >> 3 & 1);
+          const int word = (state_quad % 2) * 4 + r * 2 + (lane >> 3 & 1);
           uint32_t x[4];
           load_across(x, from + (t + (lane >> 4) * 8 + lane % 8) * 128 + (word ^ (lane % 8)) * 16);
 #pragma unroll
@@ -471,7 +470,7 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams all) {
 #pragma unroll
         for (int j = 0; j < COLS / 8; ++j) {
           const int col = col0 + j * 8;
-          char* to = base + L::oS + col / 64 * (C * 128) + row * 128 + (((col % 64) / 8) ^ (row & 7)) * 16;
+          char* to = base + L::oS + col / 64 * (C * 128) + state_row * 128 + (((col % 64) / 8) ^ (state_row & 7)) * 16;
           uint32_t hi[4], lo[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -621,9 +620,9 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams all) {
     }
     if (!SUMS && lane == 0) stores_done();
     float* to = SUMS ? carry : w.ends ? p.last : nullptr;
-    if (to && holds && row < p.C) {
+    if (to && holds && state_row < p.C) {
       const int64_t down = SUMS ? p.D : p.state_row, along = SUMS ? 1 : p.state_col;
-      to += (SUMS ? 0 : state) + row * down;
+      to += (SUMS ? 0 : state) + state_row * down;
 #pragma unroll
       for (int j = 0; j < COLS; ++j) {
         const int col = c0 + col0 + j;
@@ -695,12 +694,15 @@ cudaError_t launch_mma(dim3 grid, cudaStream_t s, const AttentionMmaParams& p) {
 
 template <typename E, typename R, int C, int D, int PARTS>
 cudaError_t walk_parts(const AttentionMmaParams& q, cudaStream_t s) {
-  const AttentionParams& p = q.walks.of[0];
-  const dim3 grid((unsigned)((int64_t)q.walks.count * p.items * p.H * ((p.D + D - 1) / D)));
+  const AttentionParams& p = q.a;
+  const dim3 grid((unsigned)((int64_t)p.items * p.H * ((p.D + D - 1) / D)));
   if (p.segments > 1) {
     cudaError_t e = launch_mma<E, R, C, D, PARTS, true>(grid, s, q);
     if (e != cudaSuccess) return e;
-    e = launch_attention_carry(q.walks, s);
+    AttentionWalks one;
+    one.of[0] = p;
+    one.count = 1;
+    e = launch_attention_carry(one, s);
     if (e != cudaSuccess) return e;
   }
   return launch_mma<E, R, C, D, PARTS, false>(grid, s, q);
@@ -711,7 +713,7 @@ cudaError_t walk_parts(const AttentionMmaParams& q, cudaStream_t s) {
 template <typename E, typename R, int C, int D>
 cudaError_t walk(const AttentionMmaParams& q, cudaStream_t s) {
   if constexpr (std::is_same<E, __nv_bfloat16>::value)
-    if (q.walks.of[0].last) return walk_parts<E, R, C, D, 3>(q, s);
+    if (q.a.last) return walk_parts<E, R, C, D, 3>(q, s);
   return walk_parts<E, R, C, D, 2>(q, s);
 }
 
@@ -721,24 +723,28 @@ cudaError_t launch_attention_mma(const AttentionWalks& walks, int dtype, cudaStr
   taken = false;
   const AttentionParams& p = walks.of[0];
   if (p.T == 0) return cudaSuccess;
-  AttentionMmaParams q;
-  q.walks = walks;
+  AttentionMmaParams q[3];
   for (int k = 0; k < walks.count; ++k) {
-    const AttentionParams& a = walks.of[k];
+    const AttentionParams& a = q[k].a = walks.of[k];
     const HeadsIn o = {a.o.data, a.o.batch, a.o.token, a.o.head, 1};
-    if (!describe(q.maps[k].q, a.q, a, a.C, dtype, 128, kBlockTokens) || !describe(q.maps[k].k, a.k, a, a.C, dtype, 128, kBlockTokens) ||
-        !describe(q.maps[k].v, a.v, a, a.D, dtype, 128, kBlockTokens) || !describe(q.maps[k].o, o, a, a.D, a.wide ? GS_F32 : dtype, 64, 32))
+    if (!describe(q[k].q, a.q, a, a.C, dtype, 128, kBlockTokens) || !describe(q[k].k, a.k, a, a.C, dtype, 128, kBlockTokens) ||
+        !describe(q[k].v, a.v, a, a.D, dtype, 128, kBlockTokens) || !describe(q[k].o, o, a, a.D, a.wide ? GS_F32 : dtype, 64, 32))
       return cudaSuccess;
   }
   taken = true;
-  const auto sizes = [&](auto e, auto r) {
+  const auto sizes = [&](auto e, auto r, const AttentionMmaParams& w) {
     using E = decltype(e);
     using R = decltype(r);
-    if (p.C <= 64) return p.D <= 64 ? walk<E, R, 64, 64>(q, s) : walk<E, R, 64, 128>(q, s);
-    return p.D <= 64 ? walk<E, R, 128, 64>(q, s) : walk<E, R, 128, 128>(q, s);
+    if (p.C <= 64) return p.D <= 64 ? walk<E, R, 64, 64>(w, s) : walk<E, R, 64, 128>(w, s);
+    return p.D <= 64 ? walk<E, R, 128, 64>(w, s) : walk<E, R, 128, 128>(w, s);
   };
-  if (dtype == GS_F16) return p.wide ? sizes(__half(), float()) : sizes(__half(), __half());
-  return p.wide ? sizes(__nv_bfloat16(), float()) : sizes(__nv_bfloat16(), __nv_bfloat16());
+  for (int k = 0; k < walks.count; ++k) {
+    const cudaError_t e = dtype == GS_F16 ? (p.wide ? sizes(__half(), float(), q[k]) : sizes(__half(), __half(), q[k]))
+                          : p.wide        ? sizes(__nv_bfloat16(), float(), q[k])
+                                          : sizes(__nv_bfloat16(), __nv_bfloat16(), q[k]);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
 }
 
 }  // namespace gs
