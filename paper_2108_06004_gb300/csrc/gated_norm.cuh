@@ -56,14 +56,18 @@ __device__ __forceinline__ float inverse(float x) {
 // act(u), and its slope: with a = act(u) and 1 - s = e^-u s, a (1 - s) + s for u s and s (1 - s) for s.
 struct Gate {
   bool silu;
-  float keep;
-  __device__ __forceinline__ explicit Gate(int act) : silu(act == GS_GATE_SILU), keep(act == GS_GATE_SILU ? 1.f : 0.f) {}
+  __device__ __forceinline__ explicit Gate(int act) : silu(act == GS_GATE_SILU) {}
   __device__ __forceinline__ float2 value(float2 u, float2& slope) const {
     const float2 x = mul(u, -1.4426950408889634f), e = make_float2(power(x.x), power(x.y)), d = add(e, two(1.f));
     const float2 s = make_float2(inverse(d.x), inverse(d.y));
-    const float2 a = mul(silu ? u : two(1.f), s);
-    slope = fma(a, mul(e, s), mul(s, keep));
-    return a;
+    const float2 rest = mul(e, s);
+    if (silu) {
+      const float2 a = mul(u, s);
+      slope = fma(a, rest, s);
+      return a;
+    }
+    slope = mul(s, rest);
+    return s;
   }
   __device__ __forceinline__ float2 value(float2 u) const {
     float2 slope;
@@ -87,11 +91,14 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*scratch)[32]) {
       for (int n = 0; n < N; ++n) scratch[n][warp] = v[n];
     }
     __syncthreads();
+    // every warp adds the warps' sums up itself, a lane each, all lanes in the same order
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      v[n] = 0.f;
+      v[n] = (threadIdx.x & 31) < W ? scratch[n][first + (threadIdx.x & 31)] : 0.f;
 #pragma unroll
-      for (int k = 0; k < W; ++k) v[n] += scratch[n][first + k];
+      for (int o = 16; o > 0; o >>= 1)
+        if (o < W) v[n] += __shfl_xor_sync(0xFFFFFFFFu, v[n], o);
+      v[n] = __shfl_sync(0xFFFFFFFFu, v[n], 0);
     }
   }
 }

@@ -17,12 +17,14 @@ namespace {
 
 using namespace norm;
 
-// Rows that are whole 16-byte words are copied ahead into shared memory, each thread its own words, while the row before is
-// worked on: in registers, of which the sums take 16, they would leave room for half as many threads.
+// Rows that are whole 16-byte words are copied ahead into shared memory, each thread its own words, while the rows before are
+// worked on.
 template <typename E, int TPR, int V, int L>
-constexpr bool kAhead = L == kEven && V == 1 && (sizeof(E) == 2 || TPR <= 512);
-// Threads of an SM: what registers (and for fp32 the copies) leave room for.
-constexpr int resident(int item, int tpr) { return item == 4 ? (tpr <= 512 ? 512 : 1024) : tpr <= 128 ? 768 : 1024; }
+constexpr bool kAhead = L == kEven && V == 1 && TPR <= 512;
+template <typename E>
+constexpr int kStages = sizeof(E) == 2 ? 3 : 2;  // rows in shared memory
+// Threads of an SM: what registers leave room for.
+constexpr int resident(int tpr) { return tpr <= 512 ? 512 : 1024; }
 constexpr int kInputs = 5;
 enum { kX, kGate, kDy, kDz, kY };
 
@@ -30,70 +32,90 @@ __device__ __forceinline__ void copy_word(uint4* to, const void* from) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
 }
 
-// A row's two means come from three sums of one pass: with q = scale act(gate) w n,
-//   mean(u m),  mean(p n) = rstd (mean(q x (next_rstd u + dy)) - next_rstd^2 mean(u m) mean(q x y)).
+__device__ __forceinline__ void copy_float(float* to, const float* from) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+
+// A row's two means come from three sums of one pass, and what the results need of it stays in registers: with
+//   A = scale rstd act(gate),  G = scale rstd x w act'(gate),  t' = next_rstd u + dy,
+// t is t' - y next_rstd^2 mean(u m), dgate = t G, dw += t A x, dx = t A w - x rstd^2 mean(p n), and
+//   mean(p n) = mean(A w x t') - next_rstd^2 mean(u m) mean(A w x y).
 template <typename E, int TPR, int V, int L>
-__global__ void __launch_bounds__(kCtaThreads<TPR>, resident(sizeof(E), TPR) / kCtaThreads<TPR>)
+__global__ void __launch_bounds__(kCtaThreads<TPR>, resident(TPR) / kCtaThreads<TPR>)
 k_gated_norm_back(const __grid_constant__ GatedNormBackParams p, int outer) {
   grid_begin();
   __shared__ float scratch[2][3][32];
   constexpr int RPC = kRowsPerCta<TPR>;
-  // [2][inputs][words of a group][threads] where rows are copied ahead; at the end, where RPC > 1 and a row is one
+  // [rows][inputs][words of a group][threads] and [rows][2][warps or, where they are more, rows] for rstd where rows are copied ahead; at the end, where RPC > 1 and a row is one
   // group, [RPC][width]
   extern __shared__ __align__(16) float fold[];
   constexpr bool AHEAD = kAhead<E, TPR, V, L>;
-  constexpr int WORDS = sizeof(E) / 2, THREADS = kCtaThreads<TPR>;
+  constexpr int WORDS = sizeof(E) / 2, THREADS = kCtaThreads<TPR>, STAGES = kStages<E>;
   const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   // a thread's rows, `step` apart, have the same lead and the same group
   const int64_t step = (int64_t)gridDim.x * RPC, first = (int64_t)blockIdx.x * RPC;
   const int lead = lead_of<L>(first + sub, p.x_stride, p.lead);
   const Gate gate(p.act);
-  Eight dw[V], dnext[V];
+  Eight dw[V], dnext[V], weight[V], follow[V];
 #pragma unroll
-  for (int v = 0; v < V; ++v)
+  for (int v = 0; v < V; ++v) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) dw[v][j] = dnext[v][j] = two(0.f);
+    for (int j = 0; j < 4; ++j) dw[v][j] = dnext[v][j] = weight[v][j] = follow[v][j] = two(0.f);
+    const Span s = span<L>(v * TPR + lane, lead, p.width);
+    if (!s.some()) continue;
+    group_weight8<L>(p.weight, s, lead, p.width, p.groups, first + sub, reinterpret_cast<float(&)[8]>(weight[v]));
+    if (p.dz) weight8<L>(p.next_weight, s, lead, p.width, reinterpret_cast<float(&)[8]>(follow[v]));
+  }
   const void* const input[kInputs] = {p.x, p.gate, p.dy, p.dz, p.y};
   const int64_t stride[kInputs] = {p.x_stride, p.gate_stride, p.dy_stride, p.dz_stride, p.y_stride};
-  float rstd = 0.f, next_rstd = 0.f, rstd_ahead = 0.f, next_rstd_ahead = 0.f;
   uint4* const ahead = reinterpret_cast<uint4*>(fold) + threadIdx.x;
-  const auto copy = [&](int64_t row, int turn) {
-    if constexpr (AHEAD) {
-      if (row < p.rows) {
-        const Span s = span<L>(lane, lead, p.width);
-        if (s.some()) {
+  constexpr int SHARERS = TPR < 32 ? TPR : 32, SLOTS = THREADS / SHARERS;  // threads that share a copy of a row's rstd
+  float* const rstds = fold + STAGES * kInputs * WORDS * THREADS * 4 + threadIdx.x / SHARERS;
+  const auto copy = [&](int64_t row, int stage) {
+    if (row < p.rows) {
+      const Span s = span<L>(lane, lead, p.width);
+      if (s.some()) {
 #pragma unroll
-          for (int k = 0; k < kInputs; ++k) {
-            if (!input[k]) continue;
-            const E* from = static_cast<const E*>(input[k]) + group_start(row, outer, stride[k], p.width) + s.col;
+        for (int k = 0; k < kInputs; ++k) {
+          if (!input[k]) continue;
+          const E* from = static_cast<const E*>(input[k]) + group_start(row, outer, stride[k], p.width) + s.col;
 #pragma unroll
-            for (int q = 0; q < WORDS; ++q) copy_word(ahead + ((turn * kInputs + k) * WORDS + q) * THREADS, from + q * (16 / sizeof(E)));
-          }
+          for (int q = 0; q < WORDS; ++q) copy_word(ahead + ((stage * kInputs + k) * WORDS + q) * THREADS, from + q * (16 / sizeof(E)));
         }
-        rstd_ahead = p.rstd[row];
-        if (p.dz) next_rstd_ahead = p.next_rstd[row];
       }
-      asm volatile("cp.async.commit_group;" ::: "memory");
+      if (threadIdx.x % SHARERS == 0) {
+        copy_float(rstds + stage * 2 * SLOTS, p.rstd + row);
+        if (p.dz) copy_float(rstds + (stage * 2 + 1) * SLOTS, p.next_rstd + row);
+      }
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  copy(first + sub, 0);
-  int turn = 0;
+  if constexpr (AHEAD) {
+#pragma unroll
+    for (int k = 0; k + 1 < STAGES; ++k) copy(first + sub + k * step, k);
+  }
+  int turn = 0, stage = 0;
   for (int64_t row0 = first; row0 < p.rows; row0 += step, turn ^= 1) {
     const int64_t row = row0 + sub;
     const bool live = row < p.rows, inner = p.spaced && row > 0 && row + 1 < p.rows;
     const auto put = [&](void* t, int64_t stride, const Span& s, const Eight& v) {
       store8<E, L>(static_cast<E*>(t) + group_start(row, outer, stride, p.width) + s.col, s, reinterpret_cast<const float(&)[8]>(v));
     };
-    const auto weights = [&](const Span& s, Eight& w) {
-      group_weight8<L>(p.weight, s, lead, p.width, p.groups, row, reinterpret_cast<float(&)[8]>(w));
-    };
-    const auto next_weights = [&](const Span& s, Eight& w) { weight8<L>(p.next_weight, s, lead, p.width, reinterpret_cast<float(&)[8]>(w)); };
-    Raw8<E> raw[kInputs][AHEAD ? 1 : V];
+    Raw8<E> raw[kInputs][V];
+    float rstd = 0.f, next_rstd = 0.f;
     if constexpr (AHEAD) {
-      rstd = rstd_ahead;
-      next_rstd = next_rstd_ahead;
-      copy(row + step, turn ^ 1);
-      asm volatile("cp.async.wait_group 1;" ::: "memory");
+      copy(row + (STAGES - 1) * step, stage == 0 ? STAGES - 1 : stage - 1);
+      asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+#pragma unroll
+      for (int k = 0; k < kInputs; ++k)
+        if (input[k]) {
+#pragma unroll
+          for (int q = 0; q < WORDS; ++q) raw[k][0].q[q] = ahead[((stage * kInputs + k) * WORDS + q) * THREADS];
+        }
+      __syncwarp();
+      rstd = rstds[stage * 2 * SLOTS];
+      next_rstd = p.dz ? rstds[(stage * 2 + 1) * SLOTS] : 0.f;
+      stage = stage + 1 == STAGES ? 0 : stage + 1;
     } else if (live) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
@@ -107,97 +129,81 @@ k_gated_norm_back(const __grid_constant__ GatedNormBackParams p, int outer) {
       rstd = p.rstd[row];
       if (p.dz) next_rstd = p.next_rstd[row];
     }
-    const auto get = [&](int k, int v, const Span& s, Eight& to) {
-      if constexpr (AHEAD) {
-        Raw8<E> r;
-#pragma unroll
-        for (int q = 0; q < WORDS; ++q) r.q[q] = ahead[((turn * kInputs + k) * WORDS + q) * THREADS];
-        unpack<E, L>(r, s, to);
-      } else {
-        unpack<E, L>(raw[k][v], s, to);
-      }
-    };
+    const float factor = p.scale * rstd;
     float2 sum[3] = {two(0.f), two(0.f), two(0.f)};
+    Eight A[V], G[V], t[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const Span s = span<L>(v * TPR + lane, lead, p.width);
       if (!live || !s.some()) continue;
-      Eight q, w, t, a;
-      weights(s, w);
-      get(kX, v, s, q);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) q[j] = mul(q[j], mul(w[j], rstd * p.scale));
+      Eight x, q, a;
+      unpack<E, L>(raw[kX][v], s, x);
       if (p.gate) {
-        get(kGate, v, s, a);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) q[j] = mul(q[j], gate.value(a[j]));
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) t[j] = two(0.f);
-      if (p.dy) get(kDy, v, s, t);
-      if (p.dz) {
-        next_weights(s, w);
-        get(kDz, v, s, a);
-        Eight m;
-        get(kY, v, s, m);
+        unpack<E, L>(raw[kGate][v], s, a);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float2 r = mul(a[j], next_rstd), b = mul(m[j], r);  // zero where there is no element, as all sums are
-          t[j] = fma(r, w[j], t[j]);
+          float2 slope;
+          A[v][j] = mul(gate.value(a[j], slope), factor);
+          G[v][j] = mul(mul(slope, factor), mul(x[j], weight[v][j]));
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) A[v][j] = two(factor);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) q[j] = mul(mul(A[v][j], weight[v][j]), x[j]);
+      if (p.dy) {
+        unpack<E, L>(raw[kDy][v], s, t[v]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) t[v][j] = two(0.f);
+      }
+      if (p.dz) {
+        Eight y;
+        unpack<E, L>(raw[kDz][v], s, a);
+        unpack<E, L>(raw[kY][v], s, y);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 r = mul(a[j], next_rstd), b = mul(y[j], r);  // zero where there is no element, as all sums are
+          t[v][j] = fma(r, follow[v][j], t[v][j]);
           dnext[v][j] = add(dnext[v][j], b);
-          sum[0] = fma(b, w[j], sum[0]);
-          sum[2] = fma(q[j], m[j], sum[2]);
+          sum[0] = fma(b, follow[v][j], sum[0]);
+          sum[2] = fma(q[j], y[j], sum[2]);
         }
       }
 #pragma unroll
-      for (int j = 0; j < 4; ++j) sum[1] = fma(q[j], t[j], sum[1]);
+      for (int j = 0; j < 4; ++j) sum[1] = fma(q[j], t[v][j], sum[1]);
     }
     float sums[3] = {sum[0].x + sum[0].y, sum[1].x + sum[1].y, sum[2].x + sum[2].y};
     row_sums<TPR>(sums, scratch[turn]);
-    // the same for every element: next_rstd^2 mean(u m) as a factor of y, and mean(p n)
+    // the same for every element: next_rstd^2 mean(u m) as a factor of y, and rstd mean(p n) as one of x
     const float part = 1.f / (float)p.width, from_y = sums[0] * part * next_rstd * next_rstd;
-    const float inside = (sums[1] - from_y * sums[2]) * part * -rstd;
+    const float from_x = (sums[1] - from_y * sums[2]) * part * rstd * -rstd;
     if (!live) continue;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const Span s = span<L>(v * TPR + lane, lead, p.width);
       if (!s.some()) continue;
-      Eight t, a, w, n;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) t[j] = two(0.f);
-      if (p.dy) get(kDy, v, s, t);
+      Eight x;
       if (p.dz) {
-        next_weights(s, w);
-        get(kDz, v, s, a);
-        get(kY, v, s, n);
+        unpack<E, L>(raw[kY][v], s, x);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) t[j] = fma(n[j], -from_y, fma(mul(a[j], next_rstd), w[j], t[j]));
+        for (int j = 0; j < 4; ++j) t[v][j] = fma(x[j], -from_y, t[v][j]);
       }
-      if (p.dresidual) put(p.dresidual, p.dresidual_stride, s, t);
-      weights(s, w);
-      get(kX, v, s, n);
+      if (p.dresidual) put(p.dresidual, p.dresidual_stride, s, t[v]);
+      if (p.dgate) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        n[j] = mul(n[j], rstd);
-        t[j] = mul(t[j], p.scale);
+        for (int j = 0; j < 4; ++j) G[v][j] = mul(G[v][j], t[v][j]);
+        put(p.dgate, p.dgate_stride, s, G[v]);
       }
-      if (p.gate) {
-        Eight slope;
-        get(kGate, v, s, a);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          a[j] = gate.value(a[j], slope[j]);
-          slope[j] = mul(mul(slope[j], t[j]), mul(n[j], w[j]));
-          t[j] = mul(t[j], a[j]);
-        }
-        if (p.dgate) put(p.dgate, p.dgate_stride, s, slope);
-      }
+      unpack<E, L>(raw[kX][v], s, x);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        dw[v][j] = fma(t[j], n[j], dw[v][j]);
-        n[j] = fma(n[j], inside, mul(t[j], mul(w[j], rstd)));
+        const float2 e = mul(t[v][j], A[v][j]);
+        dw[v][j] = fma(e, x[j], dw[v][j]);
+        x[j] = fma(x[j], from_x, mul(e, weight[v][j]));
       }
-      if (p.dx) put(p.dx, p.dx_stride, s, n);
+      if (p.dx) put(p.dx, p.dx_stride, s, x);
     }
   }
   const int64_t n = (int64_t)gridDim.x * p.width;
@@ -229,10 +235,10 @@ k_gated_norm_back(const __grid_constant__ GatedNormBackParams p, int outer) {
 
 // CTAs: as many as stay resident, the rows dealt round robin, so that a thread's rows share their group and (rows
 // of a thread being a multiple of eight apart) their lead.
-int64_t ctas_of(int64_t rows, int groups, const Shape& shape, int item) {
+int64_t ctas_of(int64_t rows, int groups, const Shape& shape) {
   const int64_t need = (rows + shape.rows - 1) / shape.rows;
   const int64_t even = groups / std::gcd(groups, shape.rows);  // CTAs whose rows hold whole sets of groups
-  int64_t most = (int64_t)kSMs * (resident(item, shape.tpr) / shape.threads);
+  int64_t most = (int64_t)kSMs * (resident(shape.tpr) / shape.threads);
   const int64_t unit = std::lcm(even, (int64_t)8);
   most = (most + unit - 1) / unit * unit;
   return need < most ? (need + even - 1) / even * even : most;
@@ -240,15 +246,13 @@ int64_t ctas_of(int64_t rows, int groups, const Shape& shape, int item) {
 
 }  // namespace
 
-// CTAs times the sums that each writes, for any type and any alignment of the rows.
+// CTAs times the sums that each writes, for any alignment of the rows.
 int64_t gated_norm_most_sums(int64_t rows, int groups, int wide_cols) {
   int64_t most = 0;
   for (int wide : {wide_cols, wide_cols + 7 <= kNormMaxCols ? wide_cols + 7 : wide_cols}) {
     const Shape shape = gated_shape(wide);
-    for (int item : {2, 4}) {
-      const int64_t n = ctas_of(rows, groups, shape, item) * (groups > 1 ? shape.rows : 1);
-      most = n > most ? n : most;
-    }
+    const int64_t n = ctas_of(rows, groups, shape) * (groups > 1 ? shape.rows : 1);
+    most = n > most ? n : most;
   }
   return most;
 }
@@ -257,7 +261,7 @@ cudaError_t launch_gated_norm_backward(const GatedNormBackParams& p, int outer, 
                                        int dtype, Layout layout, cudaStream_t s) {
   if (width(p.width, layout) > kNormMaxCols) layout = kApart;
   const Shape shape = gated_shape(width(p.width, layout));
-  const int64_t ctas = ctas_of(p.rows, p.groups, shape, dtype == GS_F32 ? 4 : 2);
+  const int64_t ctas = ctas_of(p.rows, p.groups, shape);
   if (ctas > 0) {
     const size_t fold = shape.rows > 1 && p.groups == 1 ? (size_t)shape.rows * p.width * sizeof(float) : 0;
     const cudaError_t err = with_type(dtype, [&](auto e) {
@@ -265,7 +269,7 @@ cudaError_t launch_gated_norm_backward(const GatedNormBackParams& p, int outer, 
       return with_gated_shape(shape, [&](auto tpr, auto v) {
         return with_layout(layout, [&](auto how) {
           constexpr int TPR = decltype(tpr)::value, V = decltype(v)::value, L = decltype(how)::value;
-          constexpr size_t copies = kAhead<E, TPR, V, L> ? (size_t)2 * kInputs * kCtaThreads<TPR> * 8 * sizeof(E) : 0;
+          constexpr size_t copies = kAhead<E, TPR, V, L> ? (size_t)kStages<E> * kCtaThreads<TPR> * (kInputs * 8 * sizeof(E) + 2 * sizeof(float)) : 0;
           const auto kernel = k_gated_norm_back<E, TPR, V, L>;
           if constexpr (copies > 48 * 1024) {
             // shared memory beyond the default is asked for once per kernel and device
