@@ -5,8 +5,8 @@
 //   o_i = out_scale (w_{i+1} S' q_i + sum over j <= i of w_{i-j} (q_i . k_j) v_j),
 //   S  <- w_16 S + in_scale sum over j of w_{15-j} k_j v_j'.
 // (Backwards a token's decay comes after it: w_i for w_{i+1}, and w_{16-j} for w_{15-j}.)
-// A CTA holds 32 columns of one head's state in the registers of its four warps, a quarter of the rows each;
-// two multiply-adds a state element and token, fp32 FMA bound.
+// A CTA holds 32 columns of one head's state in the registers of its eight warps (four for more than 128 rows), a share of
+// the rows each; two multiply-adds a state element and token, fp32 FMA bound.
 //
 // Long rows are cut into pieces: the pieces' own sums, the states before them, then all outputs.
 #include "attention.cuh"
@@ -14,7 +14,7 @@
 namespace gs {
 namespace {
 
-constexpr int kTok = 16, kCols = 32, kWarps = 4, kThreadsA = kWarps * 32;
+constexpr int kTok = 16, kCols = 32;
 
 template <typename E>
 __device__ __forceinline__ const E* row_of(const HeadsIn& t, int batch, int64_t token, int head) {
@@ -22,13 +22,13 @@ __device__ __forceinline__ const E* row_of(const HeadsIn& t, int batch, int64_t 
 }
 
 // SUMS: only the piece's own sum, from a state of zero, into carry.
-template <typename E, typename O, int ROWS, bool SUMS>
-__global__ void __launch_bounds__(kThreadsA)
+template <typename E, typename O, int ROWS, int kWarps, bool SUMS>
+__global__ void __launch_bounds__(kWarps * 32)
 k_attention(const __grid_constant__ AttentionWalks walks) {
   grid_begin();
   const uint32_t each = gridDim.x / walks.count, block = blockIdx.x % each;
   const AttentionParams& p = walks.of[blockIdx.x / each];
-  constexpr int C = kWarps * ROWS;  // contracted rows, with those that do not exist
+  constexpr int C = kWarps * ROWS, kThreadsA = kWarps * 32;  // contracted rows, with those that do not exist
   // rows of four floats more: sixteen keys at once lie in different banks
   __shared__ __align__(16) float q[SUMS ? 1 : kTok][C + 4], k[kTok][C + 4];
   __shared__ float v[kTok][kCols], part[SUMS ? 1 : kWarps][kTok][kCols], score[kTok][kTok + 1], power[kTok + 1];
@@ -96,7 +96,7 @@ k_attention(const __grid_constant__ AttentionWalks walks) {
     if (t0 + kTok < w.t1) fetch(t0 + kTok);
     __syncthreads();
     if constexpr (!SUMS) {
-      // each thread two scores, those above the diagonal zero
+      // a score or two each thread, those above the diagonal zero
       for (int at = threadIdx.x; at < kTok * kTok; at += kThreadsA) {
         const int i = at / kTok, j = at % kTok;
         float sum = 0.f;
@@ -217,17 +217,17 @@ k_head_sums(const __grid_constant__ HeadSumParams p) {
   }
 }
 
-template <typename E, typename O, int ROWS>
+template <typename E, typename O, int ROWS, int WARPS>
 cudaError_t walk(const AttentionWalks& walks, cudaStream_t s) {
   const AttentionParams& p = walks.of[0];
   const dim3 grid((unsigned)((int64_t)walks.count * p.items * p.H * ((p.D + kCols - 1) / kCols)));
   if (p.segments > 1) {
-    cudaError_t e = launch(k_attention<E, O, ROWS, true>, grid, dim3(kThreadsA), s, walks);
+    cudaError_t e = launch(k_attention<E, O, ROWS, WARPS, true>, grid, dim3(WARPS * 32), s, walks);
     if (e != cudaSuccess) return e;
     e = launch_attention_carry(walks, s);
     if (e != cudaSuccess) return e;
   }
-  return launch(k_attention<E, O, ROWS, false>, grid, dim3(kThreadsA), s, walks);
+  return launch(k_attention<E, O, ROWS, WARPS, false>, grid, dim3(WARPS * 32), s, walks);
 }
 
 }  // namespace
@@ -243,7 +243,7 @@ AttentionShape attention_shape(int64_t B, int64_t T, int64_t H, int C, int D, in
   const int columns = mma ? (D <= 64 ? 64 : 128) : kCols;
   const int64_t heads = H * ((D + columns - 1) / columns), ctas = (packed ? 1 : B) * heads;
   // CTAs that run at once
-  const int64_t slots = (int64_t)kSMs * (!mma ? 4 : C <= 64 && D <= 64 ? 2 : 1);
+  const int64_t slots = (int64_t)kSMs * (!mma ? 3 : C <= 64 && D <= 64 ? 2 : 1);
   // Rows are cut where there are too few of them: keys and values are then read twice, which costs about
   // six tenths of a walk.  Packed sequences are of any length: where there are enough of them, only those are cut that
   // are longer than three CTAs' fair shares.
@@ -269,10 +269,10 @@ cudaError_t launch_attention(const AttentionWalks& walks, int dtype, cudaStream_
   const auto rows = [&](auto e, auto o) {
     using E = decltype(e);
     using O = decltype(o);
-    return p.C <= 32    ? walk<E, O, 8>(walks, s)
-           : p.C <= 64  ? walk<E, O, 16>(walks, s)
-           : p.C <= 128 ? walk<E, O, 32>(walks, s)
-                        : walk<E, O, 64>(walks, s);
+    return p.C <= 32    ? walk<E, O, 4, 8>(walks, s)
+           : p.C <= 64  ? walk<E, O, 8, 8>(walks, s)
+           : p.C <= 128 ? walk<E, O, 16, 8>(walks, s)
+                        : walk<E, O, 64, 4>(walks, s);
   };
   return with_type(dtype, [&](auto e) { return p.wide ? rows(e, float()) : rows(e, e); });
 }
