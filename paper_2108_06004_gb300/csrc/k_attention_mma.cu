@@ -64,8 +64,11 @@ struct Tables {
   float power[129];   // w_n
   alignas(16) float key[128];  // of a row's weighted key, zero past the block's tokens
   uint64_t q_full, kv_full[2], scores, read, done, summed, state_ready, a_ready, w_ready[2];
+  // fp16: the largest |q|, |k| and |v| of a block as three warps have found them, two blocks in turn, and |first state|
+  uint64_t q_known, kv_known[2];
+  float largest[2][3][3];
+  int first;
   uint32_t tmem;
-  int largest[3][3], first;  // fp16: of |q|, |k|, |v| in a block, three blocks in turn; of the first state
 };
 static_assert(sizeof(Tables) <= 3072, "tables do not fit");
 static_assert(Plan<128, 128>::kBytes <= 232448, "a CTA's shared memory");
@@ -138,10 +141,10 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
     barrier_init(&tab.kv_full[1], 1);
     for (uint64_t* b : {&tab.scores, &tab.read, &tab.done, &tab.summed}) barrier_init(b, 1);
     for (uint64_t* b : {&tab.state_ready, &tab.a_ready, &tab.w_ready[0], &tab.w_ready[1]}) barrier_init(b, kWorkers / 32);
+    for (uint64_t* b : {&tab.q_known, &tab.kv_known[0], &tab.kv_known[1]}) barrier_init(b, 3);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kWorkers / 32) tmem_alloc<L::kColumns>(&tab.tmem);
-  if (threadIdx.x < 9) tab.largest[threadIdx.x / 3][threadIdx.x % 3] = 0;
   if (threadIdx.x == 9) tab.first = 0;
   if (threadIdx.x < 129) tab.power[threadIdx.x] = expf(g * (float)threadIdx.x);
   if (threadIdx.x < 256) {
@@ -157,6 +160,46 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
 
   if (threadIdx.x >= kWorkers) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::kOther));
+    if (HALF && warp > kWorkers / 32) {
+      // the three other warps: the largest values of a tile's first m rows, before anyone needs them
+      const int mine = warp - kWorkers / 32 - 1;
+      const auto largest = [&](const char* tile, int panels, int m) {
+        __half2 most = __float2half2_rn(0.f);
+        for (int panel = 0; panel < panels; ++panel)
+#pragma unroll 4
+          for (int at = mine * 32 + lane; at < m * 8; at += 96) {
+            const uint4 x = *reinterpret_cast<const uint4*>(tile + panel * L::kPanel + at * 16);
+            const __half2* h = reinterpret_cast<const __half2*>(&x);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) most = __hmax2(most, __habs2(h[j]));
+          }
+        float f = fmaxf(__low2float(most), __high2float(most));
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) f = fmaxf(f, __shfl_xor_sync(0xFFFFFFFFu, f, o));
+        return f;
+      };
+      // A block's places are free: what was in them was read before the block before last was done, and its tiles
+      // come after that.
+      for (int n = 0; n < blocks; ++n) {
+        float* const to = tab.largest[n & 1][mine];
+        barrier_wait(&tab.kv_full[n & 1], n >> 1, lost);
+        __syncwarp();
+        const float k = largest(base + L::oK + (n & 1) * L::kQ, C / 64, tokens(n)), v = largest(base + L::oV + (n & 1) * L::kV, D / 64, tokens(n));
+        if (lane == 0) {
+          to[1] = k;
+          to[2] = v;
+          barrier_arrive(&tab.kv_known[n & 1]);
+        }
+        if (SUMS) continue;
+        barrier_wait(&tab.q_full, n, lost);
+        __syncwarp();
+        const float q = largest(base + L::oQ, C / 64, tokens(n));
+        if (lane == 0) {
+          to[0] = q;
+          barrier_arrive(&tab.q_known);
+        }
+      }
+    }
     if (threadIdx.x == kWorkers && blocks > 0) {
       const auto load_kv = [&](int n) {
         const int s = n & 1, t = (int)first_token(n);
@@ -297,20 +340,9 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
       }
       if (HALF && !SUMS) atomicMax(&tab.first, __float_as_int(most));
     }
-    // the largest |x| of a tile's first rows
-    const auto largest = [&](const char* tile, int bytes, int rows, int* to) {
-      __half2 most = __float2half2_rn(0.f);
-      for (int at = threadIdx.x * 16; at < bytes; at += kWorkers * 16) {
-        if (at / 128 % kBlockTokens >= rows) continue;
-        const uint4 x = *reinterpret_cast<const uint4*>(tile + at);
-        const __half2* h = reinterpret_cast<const __half2*>(&x);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) most = __hmax2(most, __habs2(h[j]));
-      }
-      float f = fmaxf(__low2float(most), __high2float(most));
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) f = fmaxf(f, __shfl_xor_sync(0xFFFFFFFFu, f, o));
-      if (lane == 0) atomicMax(to, __float_as_int(f));
+    const auto known = [&](int n, int what) {
+      const auto& l = tab.largest[n & 1];
+      return fmaxf(l[0][what], fmaxf(l[1][what], l[2][what]));
     };
     if (HALF && blocks > 0) {
       sync_workers<kWorkers>();
@@ -331,7 +363,6 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
       char* k = base + L::oK + (n & 1) * L::kQ;
       char* v = base + L::oV + (n & 1) * L::kV;
       wait(&tab.kv_full[n & 1], n >> 1);
-      if (HALF && threadIdx.x < 3) tab.largest[(n + 1) % 3][threadIdx.x] = 0;  // last read two blocks ago
       if (made != next.m) {
         if (made >= 0) sync_workers<kWorkers>();  // the tables before have been used
         if (threadIdx.x < 128) {
@@ -350,16 +381,13 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
           trim(v, D / 64);
           shared_fence();
         }
-        if (!HALF) sync_workers<kWorkers>();
+        sync_workers<kWorkers>();
       }
       next.scale = 0;
       if constexpr (HALF) {
-        if (made != next.m && next.m < kBlockTokens) sync_workers<kWorkers>();
-        largest(k, L::kQ, kBlockTokens, &tab.largest[n % 3][1]);
-        largest(v, L::kV, kBlockTokens, &tab.largest[n % 3][2]);
-        sync_workers<kWorkers>();
-        next.k = __int_as_float(tab.largest[n % 3][1]);
-        next.v = __int_as_float(tab.largest[n % 3][2]);
+        wait(&tab.kv_known[n & 1], n >> 1);
+        next.k = known(n, 1);
+        next.v = known(n, 2);
         next.scale = exponent_of(next.k * fabsf(p.in_scale));
       }
       made = next.m;
@@ -447,15 +475,12 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
       }
       int a_scale = 0, s_scale = 0;
       bool last = rises;
-      if constexpr (HALF) {
-        wait(&tab.q_full, n);
-        largest(base + L::oQ, L::kQ, now.m, &tab.largest[n % 3][0]);
-      }
       if (lane == 0) stores_read();
       sync_workers<kWorkers>();  // the last block's o has left the place of the parts
       if constexpr (HALF) {
+        wait(&tab.q_known, n);
         s_scale = exponent_of(bound);
-        const float score = __int_as_float(tab.largest[n % 3][0]) * now.k * (float)C * fabsf(p.in_scale);
+        const float score = known(n, 0) * now.k * (float)C * fabsf(p.in_scale);
         a_scale = exponent_of(score * expf(-g * kBlockTokens));
         last = rises && abs(a_scale - s_scale) <= 6;  // both products have one scale then
         if (last)
