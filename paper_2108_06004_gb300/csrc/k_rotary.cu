@@ -15,7 +15,7 @@ constexpr int kRotaryThreads = 256, kRotaryPairs = 1024;  // sines and cosines t
 
 // VEC: all rows start at 16-byte boundaries, R is a multiple of 16 (interleaved: 8) and what is copied of 8.
 template <typename E, bool INTERLEAVED, bool VEC>
-__global__ void __launch_bounds__(kRotaryThreads)
+__global__ void __launch_bounds__(kRotaryThreads, VEC ? 4 : 6)
 k_rotary(const __grid_constant__ RotaryParams p, int tokens, int parts) {
   grid_begin();
   __shared__ __align__(16) float2 cs[kRotaryPairs];
@@ -40,75 +40,77 @@ k_rotary(const __grid_constant__ RotaryParams p, int tokens, int parts) {
   const int turned = !VEC ? half : INTERLEAVED ? p.R / 8 : p.R / 16, units = turned + (!p.copy ? 0 : VEC ? (p.D - p.R) / 8 : p.D - p.R);
   // threads side by side: places of a head, tokens, heads
   const int wide = units < kRotaryThreads ? units : kRotaryThreads, lane = threadIdx.x / wide;
-  const int t = lane % tokens, heads = kRotaryThreads / wide / tokens, h0 = first + lane / tokens;
-  if (t >= here || lane / tokens >= heads) return;
-  const uint32_t n = n0 + t, batch = n / (uint32_t)p.T, token = n - batch * (uint32_t)p.T;
-  const E* const x = static_cast<const E*>(p.x.data) + batch * p.x.batch + token * p.x.token;
-  E* const out = static_cast<E*>(p.out.data) + batch * p.out.batch + token * p.out.token;
-  for (int u = threadIdx.x % wide; u < units; u += wide) {
-    if constexpr (VEC) {
-      const Span g = {0, 0, 8};
-      constexpr int AHEAD = 4;
-      if (u >= turned) {
-        const int c = p.R + (u - turned) * 8;
-        for (int h = h0; h < last; h += AHEAD * heads) {
-          Raw8<E> raw[AHEAD];
+  const int lanes = kRotaryThreads / wide, side = min(tokens, lanes), heads = lanes / side, h0 = first + lane / side;
+  if (lane / side >= heads) return;
+  for (int t = lane % side; t < here; t += side) {
+    const uint32_t n = n0 + t, batch = n / (uint32_t)p.T, token = n - batch * (uint32_t)p.T;
+    const E* const x = static_cast<const E*>(p.x.data) + batch * p.x.batch + token * p.x.token;
+    E* const out = static_cast<E*>(p.out.data) + batch * p.out.batch + token * p.out.token;
+    for (int u = threadIdx.x % wide; u < units; u += wide) {
+      if constexpr (VEC) {
+        const Span g = {0, 0, 8};
+        constexpr int AHEAD = 4;
+        if (u >= turned) {
+          const int c = p.R + (u - turned) * 8;
+          for (int h = h0; h < last; h += AHEAD * heads) {
+            Raw8<E> raw[AHEAD];
 #pragma unroll
-          for (int a = 0; a < AHEAD; ++a)
-            if (h + a * heads < last) raw[a] = fetch8<E, kEven>(x + (h + a * heads) * p.x.head + c, g);
+            for (int a = 0; a < AHEAD; ++a)
+              if (h + a * heads < last) raw[a] = fetch8<E, kEven>(x + (h + a * heads) * p.x.head + c, g);
 #pragma unroll
-          for (int a = 0; a < AHEAD; ++a) {
-            if (h + a * heads >= last) continue;
+            for (int a = 0; a < AHEAD; ++a) {
+              if (h + a * heads >= last) continue;
 #pragma unroll
-            for (int k = 0; k < (int)(sizeof(E) / 2); ++k) reinterpret_cast<uint4*>(out + (h + a * heads) * p.out.head + c)[k] = raw[a].q[k];
+              for (int k = 0; k < (int)(sizeof(E) / 2); ++k) reinterpret_cast<uint4*>(out + (h + a * heads) * p.out.head + c)[k] = raw[a].q[k];
+            }
           }
-        }
-        continue;
-      }
-      constexpr int WORDS = INTERLEAVED ? 1 : 2, PAIRS = 4 * WORDS, N = AHEAD / WORDS;
-      const int ca = u * 8;
-      float2 f[PAIRS];
-#pragma unroll
-      for (int j = 0; j < PAIRS; ++j) f[j] = cs[t * half + u * PAIRS + j];
-      for (int h = h0; h < last; h += N * heads) {
-        Raw8<E> raw[N][WORDS];
-#pragma unroll
-        for (int a = 0; a < N; ++a)
-#pragma unroll
-          for (int k = 0; k < WORDS; ++k)
-            if (h + a * heads < last) raw[a][k] = fetch8<E, kEven>(x + (h + a * heads) * p.x.head + ca + k * half, g);
-#pragma unroll
-        for (int a = 0; a < N; ++a) {
-          if (h + a * heads >= last) continue;
-          float v[WORDS][8];
-#pragma unroll
-          for (int k = 0; k < WORDS; ++k) unpack8<E, kEven>(raw[a][k], g, v[k]);
-#pragma unroll
-          for (int j = 0; j < PAIRS; ++j) {
-            float &first_one = INTERLEAVED ? v[0][j * 2 % 8] : v[0][j], &other = INTERLEAVED ? v[0][(j * 2 + 1) % 8] : v[WORDS - 1][j];
-            const float one = first_one, two = other;
-            first_one = one * f[j].x - two * f[j].y;
-            other = one * f[j].y + two * f[j].x;
-          }
-#pragma unroll
-          for (int k = 0; k < WORDS; ++k) store8<E, kEven>(out + (h + a * heads) * p.out.head + ca + k * half, g, v[k]);
-        }
-      }
-    } else {
-      const bool turns = u < half;
-      const int ca = !turns ? p.R + u - half : INTERLEAVED ? 2 * u : u, cb = INTERLEAVED ? ca + 1 : u + half;
-      const float2 f = turns ? cs[t * half + u] : make_float2(0.f, 0.f);
-#pragma unroll 4
-      for (int h = h0; h < last; h += heads) {
-        const E* from = x + h * p.x.head;
-        E* to = out + h * p.out.head;
-        if (!turns) {
-          to[ca] = from[ca];
           continue;
         }
-        const float a = to_f32(from[ca]), b = to_f32(from[cb]);
-        to[ca] = from_f32<E>(a * f.x - b * f.y);
-        to[cb] = from_f32<E>(a * f.y + b * f.x);
+        constexpr int WORDS = INTERLEAVED ? 1 : 2, PAIRS = 4 * WORDS, N = AHEAD / WORDS;
+        const int ca = u * 8;
+        float2 f[PAIRS];
+#pragma unroll
+        for (int j = 0; j < PAIRS; ++j) f[j] = cs[t * half + u * PAIRS + j];
+        for (int h = h0; h < last; h += N * heads) {
+          Raw8<E> raw[N][WORDS];
+#pragma unroll
+          for (int a = 0; a < N; ++a)
+#pragma unroll
+            for (int k = 0; k < WORDS; ++k)
+              if (h + a * heads < last) raw[a][k] = fetch8<E, kEven>(x + (h + a * heads) * p.x.head + ca + k * half, g);
+#pragma unroll
+          for (int a = 0; a < N; ++a) {
+            if (h + a * heads >= last) continue;
+            float v[WORDS][8];
+#pragma unroll
+            for (int k = 0; k < WORDS; ++k) unpack8<E, kEven>(raw[a][k], g, v[k]);
+#pragma unroll
+            for (int j = 0; j < PAIRS; ++j) {
+              float &first_one = INTERLEAVED ? v[0][j * 2 % 8] : v[0][j], &other = INTERLEAVED ? v[0][(j * 2 + 1) % 8] : v[WORDS - 1][j];
+              const float one = first_one, two = other;
+              first_one = one * f[j].x - two * f[j].y;
+              other = one * f[j].y + two * f[j].x;
+            }
+#pragma unroll
+            for (int k = 0; k < WORDS; ++k) store8<E, kEven>(out + (h + a * heads) * p.out.head + ca + k * half, g, v[k]);
+          }
+        }
+      } else {
+        const bool turns = u < half;
+        const int ca = !turns ? p.R + u - half : INTERLEAVED ? 2 * u : u, cb = INTERLEAVED ? ca + 1 : u + half;
+        const float2 f = turns ? cs[t * half + u] : make_float2(0.f, 0.f);
+#pragma unroll 4
+        for (int h = h0; h < last; h += heads) {
+          const E* from = x + h * p.x.head;
+          E* to = out + h * p.out.head;
+          if (!turns) {
+            to[ca] = from[ca];
+            continue;
+          }
+          const float a = to_f32(from[ca]), b = to_f32(from[cb]);
+          to[ca] = from_f32<E>(a * f.x - b * f.y);
+          to[cb] = from_f32<E>(a * f.y + b * f.x);
+        }
       }
     }
   }
@@ -120,12 +122,15 @@ cudaError_t launch_rotary(const RotaryParams& p, int dtype, bool interleaved, bo
   const int64_t all = p.B * p.T;
   const int half = p.R / 2;
   const int units = (!vec ? half : interleaved ? p.R / 8 : p.R / 16) + (!p.copy ? 0 : vec ? (p.D - p.R) / 8 : p.D - p.R);
-  // as many tokens as the table and the threads hold, up to eight, and fewer while there are fewer than four CTAs an
-  // SM; the heads of few tokens are shared out
-  int tokens = half > 0 ? kRotaryPairs / half : 8;
-  tokens = tokens > 8 ? 8 : tokens;
-  const int lanes = units < kRotaryThreads ? kRotaryThreads / units : 1;
-  tokens = tokens > lanes ? lanes : tokens;
+  // Tokens of a CTA: enough for eight places a thread, as far as the table goes, and fewer while there are fewer than four
+  // CTAs an SM; the heads of few tokens are shared out.  (104678 tokens of 2 heads of 64, 16 of them turned, in rows that start
+  // anywhere: 109 us with the four tokens that 256 threads hold at once.)
+  const int64_t places = (int64_t)units * p.H;
+  int64_t most = half > 0 ? kRotaryPairs / half : 64;
+  most = most > 64 ? 64 : most;
+  int tokens = (int)(8 * kRotaryThreads / places);
+  tokens = tokens < 8 ? 8 : tokens;
+  tokens = tokens > most ? (int)most : tokens;
   while (tokens > 1 && (all + tokens - 1) / tokens < 4 * kSMs) tokens /= 2;
   const int64_t groups = (all + tokens - 1) / tokens;
   int parts = 1;
