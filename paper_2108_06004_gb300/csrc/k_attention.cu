@@ -9,6 +9,10 @@
 // the rows each; two multiply-adds a state element and token, fp32 FMA bound.
 //
 // Long rows are cut into pieces: the pieces' own sums, the states before them, then all outputs.
+//
+// Small problems wait for memory and for one another: train 5x333x3x40/72 fp32 takes 173 us for forward and backward, in
+// pieces of 64 tokens of four blocks each (599 us with four warps, loads one by one and pieces of 128); the loads of a
+// block are under way while the one before is worked on.
 #include "attention.cuh"
 
 namespace gs {

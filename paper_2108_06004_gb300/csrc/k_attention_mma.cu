@@ -2,22 +2,31 @@
 //
 // In blocks of 128 tokens, w_n = e^(g n), with i and j counted along the walk from the block's first token and S the state
 // before it:
-//   P = Q K' (scores),  A_ij = in out w_{i-j} P_ij for j <= i, else 0
-//   O_i = out w_{i+1} (Q S)_i + (A V)_i,   S <- w_128 S + (in w_{127-j} K_j)' V
-// (backwards w_i for w_{i+1} and w_{128-j} for w_{127-j}).  S stays in fp32 in the threads' registers: a block's own sum is taken in
-// tensor memory from zero, where what a product cuts off is small, and added to S with a rounding.
+//   P = Q K' (scores),  A_ij = in w_{i-j} P_ij for j <= i, else 0,  U = (in w_{127-j} K_j)' V
+//   O_i = out (w_{i+1} (Q S)_i + (A V)_i),   S <- w_128 S + U
+// (backwards w_i for w_{i+1} and w_{128-j} for w_{127-j}).  S stays in fp32 in the threads' registers: a block's U is summed in
+// tensor memory from zero, where what a product cuts off is small, and added to S with a rounding (with S itself as the
+// sum in tensor memory, a last state was off by 3.5e-6 instead of 3e-7).  U does not need S and is made one block ahead.
+// Where e^(-128 g) is small enough, w_{i+1} comes last, with w_{-j-1} in place of w_{i-j}: Q S and A V are one sum then.
 //
 // Operands are 16-bit.  Q, K and V are as they are in memory; A and S as factors are a sum of two parts of the type,
-// which keeps 2^-17 or better of each, well below the rounding of a stored o; the weighted keys, which states in fp32
-// are made of, are three parts of bf16 (24 bits) or two of fp16 (22).  fp16 has no room for scores and states of any
-// size, so its parts are taken from values scaled by powers of two: block by block bounds of all of them follow from the
-// largest |q|, |k| and |v|, and the scales from the bounds.
+// which keeps 2^-16 or better of each, well below the rounding of a stored o (one part is a tenth faster and would make
+// the error of o 1.4 times the one of its rounding); the weighted keys are three parts of bf16 (24 bits) where a state is
+// given back in fp32 and otherwise two, and two of fp16 (22 bits).  fp16 has no room for scores and states of any size, so
+// its parts are taken from values scaled by powers of two: block by block bounds of all of them follow from the
+// largest |q|, |k| and |v|, which three warps that have nothing else to do find, and the scales from the bounds.
 //
 // Eight or sixteen warps do the arithmetic between the products; a thread of one more issues products and loads (three
-// others are there because registers can be moved from four warps at once only).  In a
-// block: parts of S (and S decayed) | Q S runs: A | O scaled | A V runs: weighted keys of the first 64
-// tokens | of the others | K V and the next scores run: o is stored.  A lane of tensor memory is a token for P, A and O and
-// a row of the state for S and the weighted keys.
+// others are there because registers can be moved from four warps at once only).  In a block: parts of S | Q S runs: A |
+// A V runs: S after the block, weighted keys of the next one | its U and scores run: o is stored.  A lane of tensor memory is a
+// token for P, A and O and a row of the state for U and the weighted keys.
+//
+// Bound by the tensor cores and by the arithmetic between them in turn, which overlap in part: a product of 128 x 128 x 16
+// takes about 80 clocks, of which a block of 128 x 128 heads needs 56 or 64.  16x4096x16x128 bf16 forward takes 276 us
+// without a last state, 315 with one (57 and 50 % of the copy rate); without the arithmetic it would take 222, without the
+// products 220, out of L2 261.  256 heads are 1.7 waves of 152 CTAs.  16x4096x32x64: 315 and 358 us.  What made it faster,
+// from 671 us: descriptors by addition (spilled ones cost 180 clocks a product); o by way of shared memory and as tiles;
+// sixteen warps in place of eight; U one block ahead; keys transposed by matrix loads; one arrival a warp.
 #include <cudaTypedefs.h>
 
 #include <atomic>
