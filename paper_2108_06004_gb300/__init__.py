@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import struct
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libgs_sketch.so")
 
@@ -56,7 +57,8 @@ class GsHeads(ctypes.Structure):
 
 
 _SEQ = ctypes.POINTER(GsSeq)
-_HEADS = ctypes.POINTER(GsHeads)
+_HEADS = ctypes.c_void_p   # a GsHeads by reference, or its bytes
+_pack_heads = struct.Struct("Nqqq").pack
 
 # name -> argument types (all return gs_status / int32 unless listed in _RESTYPES)
 SIGNATURES = {
@@ -789,7 +791,7 @@ def _heads(func: str, name: str, t, shape, dtype, device):
     b, s, h, d = t.stride()
     if d != 1 and shape[3] > 1:
         _refuse(func, f"{name}: the elements of a head must be adjacent")
-    return GsHeads(t.data_ptr(), b, s, h)
+    return _pack_heads(t.data_ptr(), b, s, h)
 
 
 def _head_sizes(func: str, name: str, t, dims: int):
@@ -898,7 +900,7 @@ def _one_token(func: str, name: str, t, shape, dtype, device):
     b, h, d = t.stride()
     if d != 1 and shape[2] > 1:
         _refuse(func, f"{name}: the elements of a head must be adjacent")
-    return GsHeads(t.data_ptr(), b, 0, h)
+    return _pack_heads(t.data_ptr(), b, 0, h)
 
 
 def gs_linear_attention_step(q, k, v, log_decay, state, o, slots=None, scale: float = 1.0, stream=None) -> None:

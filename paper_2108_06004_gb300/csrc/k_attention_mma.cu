@@ -39,7 +39,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int kBlockTokens = 128;
+constexpr int kBlockTokens = 128, kTableBytes = 3 << 10;
 
 // One walk a launch: parameters at a place that a CTA has to work out cost a walk that fills the device 5 %.
 struct AttentionMmaParams {
@@ -65,7 +65,7 @@ struct Plan {
   static constexpr int kPanel = kBlockTokens * 128;  // bytes of 64 columns of a block
   static constexpr int kQ = C / 64 * kPanel, kV = D / 64 * kPanel, kPart = C * D * 2;
   static constexpr int oQ = 0, oK = kQ, oV = oK + 2 * kQ, oS = oV + 2 * kV, oTables = oS + 2 * kPart;
-  static constexpr int kBytes = oTables + 3072;
+  static constexpr int kBytes = oTables + kTableBytes;
 };
 struct Tables {
   float weight[256];  // in w_d of a score at weight[128 + row - column], zero past the diagonal
@@ -79,7 +79,7 @@ struct Tables {
   int first;
   uint32_t tmem;
 };
-static_assert(sizeof(Tables) <= 3072, "tables do not fit");
+static_assert(sizeof(Tables) <= kTableBytes, "tables do not fit");
 static_assert(Plan<128, 128>::kBytes <= 232448, "a CTA's shared memory");
 
 template <int WORKERS>
