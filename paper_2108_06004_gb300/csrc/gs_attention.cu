@@ -110,6 +110,7 @@ gs_status run_walks(const Sizes& z, gs::AttentionWalks& walks, gs_stream stream,
     p.segment = shape.segment;
     p.segments = shape.segments;
     p.items = (int32_t)shape.items;
+    p.chained = shape.segments > 1 && shape.segments <= gs::kChainedPieces && (!p.first || p.first != p.last);
   }
   const cudaError_t e = gs::launch_attention(walks, z.dtype, as_stream(stream));
   return e == cudaSuccess ? GS_OK : gs::record_cuda_failure(e, what);

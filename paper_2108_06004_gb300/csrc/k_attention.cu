@@ -53,12 +53,23 @@ k_attention(const __grid_constant__ AttentionWalks walks) {
     const int c = warp * ROWS + r;
     S[r] = 0.f;
     if (SUMS || c >= p.C || !mine) continue;
-    if (w.opens && w.ends)
+    if ((w.opens && w.ends) || p.chained)
       S[r] = p.first ? p.first[state + c * p.state_row + col * p.state_col] : 0.f;
     else
       S[r] = carry[(int64_t)c * p.D + col];
   }
   if (SUMS && (w.ends || w.t0 >= w.length)) return;  // nothing comes after it
+  if (!SUMS && p.chained && w.t0 < w.length) {
+    const Decay d = decay_of(g * (float)p.segment);
+    for (int n = w.t0 / p.segment; n > 0; --n) {
+      const float* u = carry - (int64_t)n * p.H * p.C * p.D;
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        const int c = warp * ROWS + r;
+        if (c < p.C && mine) S[r] = decayed(S[r], d, u[(int64_t)c * p.D + col]);
+      }
+    }
+  }
   if (!SUMS && !p.offsets) {                          // tokens past the row's length
     for (int t = max(w.t0, w.length) + warp; t < min((int64_t)w.t0 + p.segment, p.T); t += kWarps)
       if (mine)
@@ -228,7 +239,7 @@ cudaError_t walk(const AttentionWalks& walks, cudaStream_t s) {
   if (p.segments > 1) {
     cudaError_t e = launch(k_attention<E, O, ROWS, WARPS, true>, grid, dim3(WARPS * 32), s, walks);
     if (e != cudaSuccess) return e;
-    e = launch_attention_carry(walks, s);
+    if (!p.chained) e = launch_attention_carry(walks, s);
     if (e != cudaSuccess) return e;
   }
   return launch(k_attention<E, O, ROWS, WARPS, false>, grid, dim3(WARPS * 32), s, walks);

@@ -334,20 +334,35 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
     float S[COLS];
     float bound = 0.f;
     if (holds) {
-      float most = 0.f;
+      const bool given = (w.opens && w.ends) || p.chained, mine_too = !SUMS && state_row < p.C;
 #pragma unroll
       for (int j = 0; j < COLS; ++j) {
         const int col = c0 + col0 + j;
         S[j] = 0.f;
-        if (!SUMS && state_row < p.C && col < p.D) {
-          if (!(w.opens && w.ends))
-            S[j] = carry[(int64_t)state_row * p.D + col];
-          else if (p.first)
-            S[j] = p.first[state + state_row * p.state_row + col * p.state_col];
-        }
-        most = fmaxf(most, fabsf(S[j]));
+        if (mine_too && given && p.first && col < p.D) S[j] = p.first[state + state_row * p.state_row + col * p.state_col];
       }
-      if (HALF && !SUMS) atomicMax(&tab.first, __float_as_int(most));
+      if (mine_too && w.t0 < w.length) {
+        const Decay d = decay_of(g * (float)p.segment);
+        // the state before the piece, or the sums of the pieces before it
+        for (int n = p.chained ? w.t0 / p.segment : given ? -1 : 0; n >= (p.chained ? 1 : 0); --n) {
+          const float* u = carry + ((int64_t)state_row - (int64_t)n * p.H * p.C) * p.D + c0 + col0;
+#pragma unroll
+          for (int j = 0; j < COLS; j += 4) {
+            if (c0 + col0 + j >= p.D) continue;
+            const float4 x = *reinterpret_cast<const float4*>(u + j);
+            S[j] = decayed(S[j], d, x.x);
+            S[j + 1] = decayed(S[j + 1], d, x.y);
+            S[j + 2] = decayed(S[j + 2], d, x.z);
+            S[j + 3] = decayed(S[j + 3], d, x.w);
+          }
+        }
+      }
+      if (HALF && !SUMS) {
+        float most = 0.f;
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) most = fmaxf(most, fabsf(S[j]));
+        atomicMax(&tab.first, __float_as_int(most));
+      }
     }
     const auto known = [&](int n, int what) {
       const auto& l = tab.largest[n & 1];
@@ -736,7 +751,7 @@ cudaError_t walk_parts(const AttentionMmaParams& q, cudaStream_t s) {
     AttentionWalks one;
     one.of[0] = p;
     one.count = 1;
-    e = launch_attention_carry(one, s);
+    if (!p.chained) e = launch_attention_carry(one, s);
     if (e != cudaSuccess) return e;
   }
   return launch_mma<E, R, C, D, PARTS, false>(grid, s, q);
