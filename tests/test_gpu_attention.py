@@ -319,3 +319,20 @@ def test_steps_continue_a_prompt(gs):
 def test_every_multiprocessor_is_shared(gs, D, dtype):
     """More heads than CTAs that run at once."""
     Case(gs, 4, 300, 80, 80, D, D, dtype).check()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("B,T,H,D,lengths", [(10, 1000, 4, 64, None), (6, 900, 3, 128, [900, 0, 257, 513, 128, 1]), (2, 190, 2, 40, [190, 65])])
+def test_few_pieces(gs, B, T, H, D, lengths, dtype):
+    """Rows of so few pieces that each adds up the ones before it, and the same with s_last in the place of s0."""
+    case = Case(gs, B, T, H, H, D, D, dtype, lengths=lengths)
+    case.check()
+    s, o = case.s0.clone(), torch.empty_like(case.o)
+    ws = torch.empty(gs.gs_linear_attention_workspace_size(*case.sizes, DT[dtype]), dtype=torch.uint8, device="cuda")
+    whole = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    gs.gs_linear_attention_forward(case.q, case.k, case.v, torch.from_numpy(case.g).cuda(), o, ws, s0=s, s_last=s, lengths=whole, scale=case.scale)
+    assert torch.equal(s, case.last) and torch.equal(o, case.o)
+
+
+def test_few_pieces_packed(gs):
+    Case(gs, 3, 1500, 8, 4, 64, 64, "bf16", offsets=[0, 900, 901, 1500]).check()
