@@ -129,18 +129,23 @@ k_attention(const __grid_constant__ AttentionWalks walks) {
         }
         score[i][j] = sum;
       }
-      float o[kTok];
+      // two rows an instruction, and eight tokens at a time, whose sums fit the registers
 #pragma unroll
-      for (int i = 0; i < kTok; ++i) o[i] = 0.f;
+      for (int i0 = 0; i0 < kTok; i0 += 8) {
+        float2 o[8];
 #pragma unroll
-      for (int r = 0; r < ROWS; r += 4)
+        for (int i = 0; i < 8; ++i) o[i] = make_float2(0.f, 0.f);
 #pragma unroll
-        for (int i = 0; i < kTok; ++i) {
-          const float4 a = *reinterpret_cast<const float4*>(&q[i][warp * ROWS + r]);
-          o[i] = fmaf(a.x, S[r], fmaf(a.y, S[r + 1], fmaf(a.z, S[r + 2], fmaf(a.w, S[r + 3], o[i]))));
-        }
+        for (int r = 0; r < ROWS; r += 4)
 #pragma unroll
-      for (int i = 0; i < kTok; ++i) part[warp][i][lane] = o[i];
+          for (int i = 0; i < 8; ++i) {
+            const float4 a = *reinterpret_cast<const float4*>(&q[i0 + i][warp * ROWS + r]);
+            o[i] = __ffma2_rn(make_float2(a.x, a.y), make_float2(S[r], S[r + 1]), o[i]);
+            o[i] = __ffma2_rn(make_float2(a.z, a.w), make_float2(S[r + 2], S[r + 3]), o[i]);
+          }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) part[warp][i0 + i][lane] = o[i].x + o[i].y;
+      }
     }
     const Decay d = decay_of(g * (float)n);
 #pragma unroll
@@ -151,10 +156,12 @@ k_attention(const __grid_constant__ AttentionWalks walks) {
 #pragma unroll
       for (int r = 0; r < ROWS; r += 4) {
         const float4 a = *reinterpret_cast<const float4*>(&k[j][warp * ROWS + r]);
-        S[r] = fmaf(a.x, x, S[r]);
-        S[r + 1] = fmaf(a.y, x, S[r + 1]);
-        S[r + 2] = fmaf(a.z, x, S[r + 2]);
-        S[r + 3] = fmaf(a.w, x, S[r + 3]);
+        const float2 one = __ffma2_rn(make_float2(a.x, a.y), make_float2(x, x), make_float2(S[r], S[r + 1]));
+        const float2 two = __ffma2_rn(make_float2(a.z, a.w), make_float2(x, x), make_float2(S[r + 2], S[r + 3]));
+        S[r] = one.x;
+        S[r + 1] = one.y;
+        S[r + 2] = two.x;
+        S[r + 3] = two.y;
       }
     }
     if constexpr (!SUMS) {
