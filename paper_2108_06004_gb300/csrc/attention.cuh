@@ -136,7 +136,7 @@ __device__ __forceinline__ float decayed(float s, const Decay& d, float add) { r
 
 // Where rows have few pieces, each one adds up those before it itself, which saves a launch and grows with the square of
 // their number: 24 sequences in 32768 tokens x16x64 bf16, which seldom have more than one piece and never more than 7, take
-// 514 us for forward and backward, 555 with the launch; prompt 1x8191x16x64, with 16 pieces, 64 us, 57 with the launch.  The
+// 512 us for forward and backward, 555 with the launch; prompt 1x8191x16x64, with 16 pieces, 64 us, 56 with the launch.  The
 // first state must stay as it is meanwhile.
 constexpr int kChainedPieces = 8;
 
