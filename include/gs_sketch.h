@@ -590,7 +590,7 @@ gs_status gs_rotary_frequencies(int64_t R, double base, double factor, double or
  * zeros):
  *   S_t = e^g S_{t-1} + k_t v_t',   o_t = scale S_t' q_t.
  * q is [B][T][H][Dk]; k and v have K heads, of which H / K heads in turn share one.  s_last (nullable) is
- * the state after the last token, s0 for a sequence without tokens; it may be s0 itself.
+ * the state after the last token, s0 for a sequence without tokens; it may be s0 itself.  o may not be an input.
  * Sequences are, by default, the rows of B x T tokens.  lengths (int32[B], nullable; taken to [0, T]):
  * tokens from a row's length on have no influence and their o is zero.  offsets (int32[B + 1],
  * nullable, not with lengths): tensors have one row of T tokens, and sequence b is tokens offsets[b] to
@@ -613,7 +613,7 @@ gs_status gs_linear_attention_forward(const gs_heads* q, const gs_heads* k, cons
  *   dq_t = scale S_t do_t,  dk_t = dS_t v_t,  dv_t = dS_t' k_t,  ds0 = e^g dS_0 (nullable),
  * dk and dv summed in fp32 over the heads that share them.  The decay is a constant and has no gradient.
  * Tokens that lengths mask get zeros, tokens of no sequence are left as they were.  ds0 may not be s0 or
- * ds_last. */
+ * ds_last; dq, dk and dv may not be inputs or one another. */
 gs_status gs_linear_attention_backward(const gs_heads* d_o, const gs_heads* q, const gs_heads* k, const gs_heads* v,
                                        const float* log_decay, const float* s0, const float* ds_last,
                                        const int32_t* lengths, const int32_t* offsets, const gs_heads* dq,
@@ -624,7 +624,8 @@ gs_status gs_linear_attention_backward(const gs_heads* d_o, const gs_heads* q, c
 /* One token of each of B streams: the state in place, and o.  q, k, v and o have T = 1 (their token
  * strides are not used).  state: fp32, n_slots states of [H][Dk][Dv], state_stride elements apart; stream
  * b's is slots[b] (int32[B], NULL for b).  A slot outside [0, n_slots) is idle: its o is zero and nothing
- * else is touched.  No two streams may share a slot. */
+ * else is touched.  No two streams may share a slot.  o may not be an
+ * input. */
 gs_status gs_linear_attention_step(const gs_heads* q, const gs_heads* k, const gs_heads* v, const float* log_decay,
                                    float* state, int64_t state_stride, int64_t n_slots, const int32_t* slots,
                                    const gs_heads* o, int64_t B, int64_t H, int64_t K, int64_t Dk, int64_t Dv,
@@ -640,7 +641,8 @@ gs_status gs_linear_attention_step(const gs_heads* q, const gs_heads* k, const g
  * residual may be NULL for none.  gate is given exactly if act is not GS_GATE_NONE; next_weight, z and
  * next_rstd are given together.  y (the residual stream) and z are stored; z and next_rstd come from y before
  * it is rounded.  weight, next_weight: fp32[cols].  groups divides cols, and a group has at most
- * GS_NORM_MAX_COLS columns.  y may be x, gate or residual itself.  eps >= 0. */
+ * GS_NORM_MAX_COLS columns.  y may be x, gate or residual itself (same
+ * strides), z none of them.  eps >= 0. */
 #define GS_GATE_NONE 0
 #define GS_GATE_SIGMOID 1
 #define GS_GATE_SILU 2
@@ -659,7 +661,7 @@ gs_status gs_gated_norm_workspace_size(int64_t rows, int64_t cols, int64_t group
  *   dresidual = t,  n = x * rstd,  e = scale * t,  dgate = e * n * weight * act'(gate),
  *   p = e * act(gate) * weight,  dx = rstd * (p - n * mean over the group of (p * n)),
  *   dweight = sum over rows of e * act(gate) * n,  dnext_weight = sum over rows of dz * m.
- * dx, dgate and dresidual may each be NULL and may not be an input; dweight and (with next_weight)
+ * dx, dgate and dresidual may each be NULL and may not be an input or one another; dweight and (with next_weight)
  * dnext_weight, fp32[cols], are overwritten.  workspace must hold gs_gated_norm_workspace_size bytes, 256-byte aligned. */
 gs_status gs_gated_norm_backward(const void* dy, int64_t dy_stride, const void* dz, int64_t dz_stride, const void* x,
                                  int64_t x_stride, const void* gate, int64_t gate_stride, const void* y,

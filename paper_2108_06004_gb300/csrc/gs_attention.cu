@@ -35,6 +35,18 @@ gs_status check_heads_output(const gs_heads* t, int64_t B, int64_t T, int64_t H,
   return GS_OK;
 }
 
+// Other CTAs read inputs while one writes its output: no output may be an input or another output.
+gs_status check_apart(std::initializer_list<const void*> outputs, std::initializer_list<const void*> inputs, const char* what) {
+  for (auto o = outputs.begin(); o != outputs.end(); ++o) {
+    if (!*o) continue;
+    for (const void* i : inputs)
+      if (*o == i) return bad(std::string(what) + " may not be an input");
+    for (auto other = outputs.begin(); other != o; ++other)
+      if (*o == *other) return bad(std::string(what) + " may not be the same tensor");
+  }
+  return GS_OK;
+}
+
 gs_status check_fraction(float f, const char* name) {
   if (!std::isfinite(f)) return bad(std::string(name) + " must be finite");
   return GS_OK;
@@ -210,6 +222,7 @@ gs_status gs_linear_attention_forward(const gs_heads* q, const gs_heads* k, cons
   GS_TRY(check_heads(k, dtype, some, "k"));
   GS_TRY(check_heads(v, dtype, some, "v"));
   GS_TRY(check_heads_output(o, z.packed ? 1 : B, T, H, Dv, dtype, some, "o"));
+  if (some) GS_TRY(check_apart({o->data}, {q->data, k->data, v->data}, "o"));
   GS_TRY(check_data(log_decay, 4, rows, "log_decay"));
   GS_TRY(check_data(s0, 4, false, "s0"));
   GS_TRY(check_data(s_last, 4, false, "s_last"));
@@ -262,6 +275,7 @@ gs_status gs_linear_attention_backward(const gs_heads* d_o, const gs_heads* q, c
   GS_TRY(check_heads_output(dq, batch, T, H, Dk, dtype, some, "dq"));
   GS_TRY(check_heads_output(dk, batch, T, K, Dk, dtype, some, "dk"));
   GS_TRY(check_heads_output(dv, batch, T, K, Dv, dtype, some, "dv"));
+  if (some) GS_TRY(check_apart({dq->data, dk->data, dv->data}, {d_o->data, q->data, k->data, v->data}, "dq, dk and dv"));
   GS_TRY(check_data(log_decay, 4, rows, "log_decay"));
   GS_TRY(check_data(s0, 4, false, "s0"));
   GS_TRY(check_data(ds_last, 4, false, "ds_last"));
@@ -375,6 +389,7 @@ gs_status gs_linear_attention_step(const gs_heads* q, const gs_heads* k, const g
   GS_TRY(check_heads(k, dtype, some, "k"));
   GS_TRY(check_heads(v, dtype, some, "v"));
   GS_TRY(check_heads_output(o, B, 1, H, Dv, dtype, some, "o"));
+  if (some) GS_TRY(check_apart({o->data}, {q->data, k->data, v->data}, "o"));
   GS_TRY(check_data(log_decay, 4, some, "log_decay"));
   GS_TRY(check_output(state, state_stride, n_slots, H * Dk * Dv, GS_F32, some && n_slots > 0, "state"));
   GS_TRY(check_data(slots, 4, false, "slots"));
@@ -493,6 +508,9 @@ gs_status gs_gated_norm(const void* x, int64_t x_stride, const void* gate, int64
   GS_TRY(check_data(rstd, 4, some, "rstd"));
   GS_TRY(check_data(next_rstd, 4, some && follow, "next_rstd"));
   if (!follow && (z || next_rstd)) return bad("z and next_rstd go with next_weight");
+  if (some) GS_TRY(check_apart({z}, {x, gate, residual, y}, "z"));
+  for (const Matrix& m : {Matrix{x, x_stride}, Matrix{gate, gate_stride}, Matrix{residual, residual_stride}})
+    if (rows > 1 && m.data == y && m.stride != y_stride) return bad("y may be an input itself only with the same stride");
   if (!some) return GS_OK;
   gs::GatedNormParams q;
   std::memset(&q, 0, sizeof(q));
@@ -564,6 +582,7 @@ gs_status gs_gated_norm_backward(const void* dy, int64_t dy_stride, const void* 
   GS_TRY(check_output(dx, dx_stride, rows, cols, dtype, false, "dx"));
   GS_TRY(check_output(dgate, dgate_stride, rows, cols, dtype, false, "dgate"));
   GS_TRY(check_output(dresidual, dresidual_stride, rows, cols, dtype, false, "dresidual"));
+  GS_TRY(check_apart({dx, dgate, dresidual}, {dy, dz, x, gate, y}, "dx, dgate and dresidual"));
   GS_TRY(check_data(dweight, 4, true, "dweight"));
   GS_TRY(check_data(dnext_weight, 4, follow, "dnext_weight"));
   GS_TRY(check_workspace(workspace, workspace_bytes, gated_ws_bytes(rows, cols, groups), "gs_gated_norm_workspace_size"));
@@ -597,10 +616,6 @@ gs_status gs_gated_norm_backward(const void* dy, int64_t dy_stride, const void* 
   q.groups = (int32_t)groups;
   q.width = (int32_t)(cols / groups);
   q.lead = l.lead;
-  bool in_place = false;
-  for (const void* t : {dx, dgate, dresidual})
-    for (const void* f : {dy, dz, x, gate, y}) in_place = in_place || (t && t == f);
-  if (in_place) return bad("no gradient may be written over an input");
   q.spaced = l.spaced;
   q.act = act;
   q.scale = scale;

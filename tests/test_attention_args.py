@@ -200,3 +200,33 @@ def test_oracle_rotary_keeps_products():
         assert np.isclose((at(q, 17, inter) * at(k, 5, inter)).sum(), (at(q, 1012, inter) * at(k, 1000, inter)).sum())
     one = attention.rotary(np.array([1.0, 0.0]).reshape(1, 1, 1, 2), np.array([np.pi / 2]), np.array([[1]]), True, False, 2.0)
     assert np.allclose(one.ravel(), [0, 2])
+
+
+def test_outputs_over_inputs(gs):
+    """Attention's outputs, a second norm's and the gradients are no input and not one another: other CTAs read those meanwhile."""
+    lib, n = gs.load_library(), 1 << 16
+    at = [heads(gs, A + i * n) for i in range(8)]
+    sizes = (2, 4, 2, 2, 8, 8, gs.GS_F32, 1.0)
+    for o in range(3):
+        assert lib.gs_linear_attention_forward(*at[:3], A, None, None, None, at[o], None, *sizes, A, n, None) == gs.GS_ERR_INVALID_ARG
+        assert b"o may not be an input" in lib.gs_last_error()
+        assert lib.gs_linear_attention_step(*at[:3], A, A, 128, 2, None, at[o], 2, 2, 2, 8, 8, gs.GS_F32, 1.0, None) == gs.GS_ERR_INVALID_ARG
+        assert b"o may not be an input" in lib.gs_last_error()
+    for place in range(3):
+        for other in range(4 + place):   # the inputs, and the gradients ahead of this one
+            to = at[4:7]
+            to[place] = at[other]
+            assert lib.gs_linear_attention_backward(*at[:4], A, None, None, None, None, *to, None, *sizes, A, n, None) == gs.GS_ERR_INVALID_ARG
+            assert b"dq, dk and dv may not be" in lib.gs_last_error()
+    x, g, r, y = (A + i * n for i in range(4))
+    for z in (x, g, r, y):
+        assert lib.gs_gated_norm(x, 8, g, 8, r, 8, A, A, y, 8, z, 8, A, A, 4, 8, 1, gs.GS_F32, gs.GS_GATE_SILU, 1.0, 1e-6, None) == gs.GS_ERR_INVALID_ARG
+        assert b"z may not be an input" in lib.gs_last_error()
+    for y in (x, g, r):
+        assert lib.gs_gated_norm(x, 8, g, 8, r, 8, A, None, y, 16, None, 0, A, None, 4, 8, 1, gs.GS_F32, gs.GS_GATE_SILU, 1.0, 1e-6,
+                                 None) == gs.GS_ERR_INVALID_ARG
+        assert b"same stride" in lib.gs_last_error()
+    for dx, dgate in ((g, None), (r, r)):   # dy is x here
+        assert lib.gs_gated_norm_backward(x, 8, None, 0, x, 8, g, 8, None, 0, A, None, A, None, dx, 8, dgate, 8, None, 0, A, None, 4, 8, 1, gs.GS_F32,
+                                          gs.GS_GATE_SILU, 1.0, A, n, None) == gs.GS_ERR_INVALID_ARG
+        assert b"dx, dgate and dresidual may not be" in lib.gs_last_error()
