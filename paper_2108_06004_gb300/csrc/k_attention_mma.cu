@@ -242,9 +242,10 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
         commit(&tab.summed);
       };
       // P = Q K' of block n.  Its place is free when the products that read it are done: only products with the same
-      // sum are ordered among themselves.
+      // sum are ordered among themselves.  Keys and queries arrive apart, so both are waited for.
       const auto score = [&](int n) {
         const uint32_t k = matrix(shared_address(base + L::oK + (n & 1) * L::kQ), 0);
+        barrier_wait(&tab.kv_full[n & 1], n >> 1, lost);
         barrier_wait(&tab.q_full, n, lost);
         each<C / 16>([&](auto step) {
           constexpr int j = decltype(step)::value, at = j / 4 * L::kPanel + j % 4 * 32;
@@ -290,8 +291,12 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
           barrier_wait(&tab.done, n, lost);
           if (APART) {
             if (n + 2 < blocks) load_kv(n + 2);  // in the place of block n's, whose last product is done
-            score(n + 1);
+            // Rows of K that are not the block's tokens are zeroed by the workers, which say so with the weighted keys: a
+            // block that is cut short has its scores after its sum.
+            const bool cut = tokens(n + 1) < kBlockTokens;
+            if (!cut) score(n + 1);
             sum(n + 1);
+            if (cut) score(n + 1);
           } else {
             sum(n + 1);
             barrier_wait(&tab.summed, n + 1, lost);
