@@ -59,7 +59,8 @@ struct Piece {
   bool opens, ends;   // the sequence's first piece, its last one
 };
 
-__device__ __forceinline__ int pieces_of(int length, int segment) { return length > 0 ? (length + segment - 1) / segment : 1; }
+// (length + segment may be past 32 bits)
+__device__ __forceinline__ int pieces_of(int length, int segment) { return length > 0 ? (length - 1) / segment + 1 : 1; }
 __device__ __forceinline__ int length_of(const AttentionParams& p, int sequence) {
   if (p.offsets) {
     const int a = min(max(p.offsets[sequence], 0), (int)p.T), e = min(max(p.offsets[sequence + 1], 0), (int)p.T);

@@ -54,15 +54,18 @@ gs_status check_fraction(float f, const char* name) {
 
 // ---- linear attention ----------------------------------------------------------------------
 
+// A walk counts tokens in 32 bits, up to a block past the last one.
+constexpr int64_t kMaxTokens = (int64_t(1) << 31) - (int64_t(1) << 10);
+
 gs_status check_attention(int64_t B, int64_t T, int64_t H, int64_t K, int64_t Dk, int64_t Dv) {
   if (B < 0 || T < 0 || H < 0 || K < 0) return bad("B, T, H and K must not be negative");
   if (Dk < 1 || Dv < 1 || Dk > GS_ATTENTION_MAX_HEAD || Dv > GS_ATTENTION_MAX_HEAD)
     return bad("Dk and Dv must lie in [1, " + std::to_string(GS_ATTENTION_MAX_HEAD) + "]");
   if (H > 0 && (K < 1 || H % K != 0)) return bad("H must be a multiple of K");
   const int64_t most = Dk > Dv ? Dk : Dv;
-  if (T > kMaxRows || B > kMaxRows || H > kMaxRows || !product_fits(B, T) || !product_fits(B * T, H) || !product_fits(B * T * H, most) ||
+  if (T > kMaxTokens || B > kMaxRows || H > kMaxRows || !product_fits(B, T) || !product_fits(B * T, H) || !product_fits(B * T * H, most) ||
       !product_fits(B, H) || !product_fits(B * H, Dk * Dv))
-    return bad("T must be below 2^31, B * T * H * D and B * H * Dk * Dv at most 2^40");
+    return bad("T must be at most 2^31 - 2^10, B and H below 2^31, B * T * H * D and B * H * Dk * Dv at most 2^40");
   return GS_OK;
 }
 
