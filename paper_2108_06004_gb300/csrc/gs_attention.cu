@@ -35,16 +35,83 @@ gs_status check_heads_output(const gs_heads* t, int64_t B, int64_t T, int64_t H,
   return GS_OK;
 }
 
-// Other CTAs read inputs while one writes its output: no output may be an input or another output.
-gs_status check_apart(std::initializer_list<const void*> outputs, std::initializer_list<const void*> inputs, const char* what) {
+// Where a tensor's elements are: rows of D adjacent ones, at multiples of up to three strides from the first.
+struct Place {
+  const void* data;
+  int64_t item, D;
+  struct {
+    int64_t n, stride;
+  } way[3];
+};
+Place place(const gs_heads* t, int64_t B, int64_t T, int64_t H, int64_t D, int32_t dtype) {
+  return {t->data, item(dtype), D, {{B, t->batch_stride}, {T, t->token_stride}, {H, t->head_stride}}};
+}
+Place place(const Matrix& m, int64_t rows, int64_t cols, int32_t dtype) { return {m.data, item(dtype), cols, {{rows, m.stride}, {1, 0}, {1, 0}}}; }
+
+// Whether two tensors of one type share an element.  With d the distance of their first ones, one of a and one of b are the
+// same where d + sum of i_k stride_k - sum of j_k stride_k lies in (-D of a, D of b).  Equal strides count once, with i_k - j_k;
+// from the largest stride to the smallest only those multiples are followed from which the rest can still get there.
+bool overlap(const Place& a, const Place& b) {
+  typedef __int128 Wide;  // strides and sizes are bounded each, their products are not
+  struct Way {
+    Wide stride, least, most;
+  } way[6];
+  int ways = 0;
+  if (!a.data || !b.data) return false;
+  const auto span = [](const Place& t) {
+    Wide n = t.D;
+    for (const auto& w : t.way) n += (Wide)(w.n > 1 ? w.n - 1 : 0) * w.stride;
+    return n;
+  };
+  const int64_t d = (int64_t)(reinterpret_cast<uintptr_t>(a.data) - reinterpret_cast<uintptr_t>(b.data)) / a.item;
+  if (d >= span(b) || -d >= span(a)) return false;
+  for (const auto& w : a.way)
+    if (w.n > 1 && w.stride > 0) way[ways++] = {w.stride, 0, w.n - 1};
+  for (const auto& w : b.way) {
+    if (w.n <= 1 || w.stride <= 0) continue;
+    int k = 0;
+    while (k < ways && (way[k].stride != w.stride || way[k].least < 0)) ++k;
+    if (k < ways)
+      way[k].least = 1 - w.n;
+    else
+      way[ways++] = {w.stride, 1 - w.n, 0};
+  }
+  std::sort(way, way + ways, [](const Way& x, const Way& y) { return x.stride > y.stride; });
+  Wide low[7], high[7];  // of what the ways from k on add
+  low[ways] = high[ways] = 0;
+  for (int k = ways; k-- > 0;) {
+    low[k] = low[k + 1] + way[k].stride * way[k].least;
+    high[k] = high[k + 1] + way[k].stride * way[k].most;
+  }
+  const auto down = [](Wide x, Wide s) { return x / s - (x % s != 0 && x < 0); };
+  int tries = 1 << 12;  // strides that are not multiples of one another might need more; what is not found is the caller's to know
+  const auto find = [&](const auto& self, int k, Wide at) -> bool {
+    if (k == ways) return at > -a.D && at < b.D;
+    const Wide s = way[k].stride;
+    const Wide first = std::max(way[k].least, -down(at + high[k + 1] + a.D - 1, s)), last = std::min(way[k].most, down(b.D - 1 - low[k + 1] - at, s));
+    for (Wide v = first; v <= last && tries-- > 0; ++v)
+      if (self(self, k + 1, at + v * s)) return true;
+    return false;
+  };
+  return find(find, 0, d);
+}
+
+// Other CTAs read inputs while one writes its output: no output may share an element with an input or another output.
+gs_status check_apart(std::initializer_list<Place> outputs, std::initializer_list<Place> inputs, const char* what) {
   for (auto o = outputs.begin(); o != outputs.end(); ++o) {
-    if (!*o) continue;
-    for (const void* i : inputs)
-      if (*o == i) return bad(std::string(what) + " may not be an input");
+    for (const Place& i : inputs)
+      if (overlap(*o, i)) return bad(std::string(what) + " may not be an input, nor overlap one");
     for (auto other = outputs.begin(); other != o; ++other)
-      if (*o == *other) return bad(std::string(what) + " may not be the same tensor");
+      if (overlap(*o, *other)) return bad(std::string(what) + " may not be the same tensor, nor overlap");
   }
   return GS_OK;
+}
+
+// Of two states of `n` floats, `to` may be `from` itself (where that is said) or apart from it.
+gs_status check_states(const float* to, const float* from, int64_t n, bool itself, const char* what) {
+  if (!to || !from || (itself && to == from)) return GS_OK;
+  const uintptr_t a = reinterpret_cast<uintptr_t>(to), b = reinterpret_cast<uintptr_t>(from), bytes = (uintptr_t)n * sizeof(float);
+  return a < b + bytes && b < a + bytes ? bad(what) : GS_OK;
 }
 
 gs_status check_fraction(float f, const char* name) {
@@ -169,9 +236,10 @@ gs_status gs_rotary(const gs_heads* x, const gs_heads* o, const double* frequenc
   p.magnitude = magnitude;
   p.sign = inverse ? -1.f : 1.f;
   p.copy = x->data != o->data && R < D;
-  if (x->data == o->data && ((B > 1 && x->batch_stride != o->batch_stride) || (T > 1 && x->token_stride != o->token_stride) ||
-                             (H > 1 && x->head_stride != o->head_stride)))
-    return bad("out may be x itself only with the same strides");
+  const bool alike = (B <= 1 || x->batch_stride == o->batch_stride) && (T <= 1 || x->token_stride == o->token_stride) &&
+                     (H <= 1 || x->head_stride == o->head_stride);
+  if (x->data == o->data ? !alike : overlap(place(o, B, T, H, D, dtype), place(x, B, T, H, D, dtype)))
+    return bad("out may be x itself only with the same strides, and may not overlap it otherwise");
   if (R == 0 && !p.copy) return GS_OK;
   bool vec = R % (interleaved ? 8 : 16) == 0 && (!p.copy || (D - R) % 8 == 0);
   for (const gs_heads* t : {x, o})
@@ -225,10 +293,15 @@ gs_status gs_linear_attention_forward(const gs_heads* q, const gs_heads* k, cons
   GS_TRY(check_heads(k, dtype, some, "k"));
   GS_TRY(check_heads(v, dtype, some, "v"));
   GS_TRY(check_heads_output(o, z.packed ? 1 : B, T, H, Dv, dtype, some, "o"));
-  if (some) GS_TRY(check_apart({o->data}, {q->data, k->data, v->data}, "o"));
+  if (some) {
+    const int64_t batch = z.packed ? 1 : B;
+    GS_TRY(check_apart({place(o, batch, T, H, Dv, dtype)},
+                       {place(q, batch, T, H, Dk, dtype), place(k, batch, T, K, Dk, dtype), place(v, batch, T, K, Dv, dtype)}, "o"));
+  }
   GS_TRY(check_data(log_decay, 4, rows, "log_decay"));
   GS_TRY(check_data(s0, 4, false, "s0"));
   GS_TRY(check_data(s_last, 4, false, "s_last"));
+  GS_TRY(check_states(s_last, s0, B * H * Dk * Dv, true, "s_last may be s0 itself, but not overlap it"));
   GS_TRY(check_sequences(lengths, offsets));
   size_t carry, need;
   GS_TRY(attention_bytes(z, false, &carry, &need));
@@ -278,12 +351,15 @@ gs_status gs_linear_attention_backward(const gs_heads* d_o, const gs_heads* q, c
   GS_TRY(check_heads_output(dq, batch, T, H, Dk, dtype, some, "dq"));
   GS_TRY(check_heads_output(dk, batch, T, K, Dk, dtype, some, "dk"));
   GS_TRY(check_heads_output(dv, batch, T, K, Dv, dtype, some, "dv"));
-  if (some) GS_TRY(check_apart({dq->data, dk->data, dv->data}, {d_o->data, q->data, k->data, v->data}, "dq, dk and dv"));
+  if (some)
+    GS_TRY(check_apart({place(dq, batch, T, H, Dk, dtype), place(dk, batch, T, K, Dk, dtype), place(dv, batch, T, K, Dv, dtype)},
+                       {place(d_o, batch, T, H, Dv, dtype), place(q, batch, T, H, Dk, dtype), place(k, batch, T, K, Dk, dtype),
+                        place(v, batch, T, K, Dv, dtype)}, "dq, dk and dv"));
   GS_TRY(check_data(log_decay, 4, rows, "log_decay"));
   GS_TRY(check_data(s0, 4, false, "s0"));
   GS_TRY(check_data(ds_last, 4, false, "ds_last"));
   GS_TRY(check_data(ds0, 4, false, "ds0"));
-  if (ds0 && (ds0 == s0 || ds0 == ds_last)) return bad("ds0 may not be s0 or ds_last");
+  for (const float* other : {s0, ds_last}) GS_TRY(check_states(ds0, other, B * H * Dk * Dv, false, "ds0 may not be s0 or ds_last, nor overlap them"));
   GS_TRY(check_sequences(lengths, offsets));
   size_t carry, need;
   GS_TRY(attention_bytes(z, true, &carry, &need));
@@ -392,7 +468,9 @@ gs_status gs_linear_attention_step(const gs_heads* q, const gs_heads* k, const g
   GS_TRY(check_heads(k, dtype, some, "k"));
   GS_TRY(check_heads(v, dtype, some, "v"));
   GS_TRY(check_heads_output(o, B, 1, H, Dv, dtype, some, "o"));
-  if (some) GS_TRY(check_apart({o->data}, {q->data, k->data, v->data}, "o"));
+  if (some)
+    GS_TRY(check_apart({place(o, B, 1, H, Dv, dtype)}, {place(q, B, 1, H, Dk, dtype), place(k, B, 1, K, Dk, dtype), place(v, B, 1, K, Dv, dtype)},
+                       "o"));
   GS_TRY(check_data(log_decay, 4, some, "log_decay"));
   GS_TRY(check_output(state, state_stride, n_slots, H * Dk * Dv, GS_F32, some && n_slots > 0, "state"));
   GS_TRY(check_data(slots, 4, false, "slots"));
@@ -511,10 +589,12 @@ gs_status gs_gated_norm(const void* x, int64_t x_stride, const void* gate, int64
   GS_TRY(check_data(rstd, 4, some, "rstd"));
   GS_TRY(check_data(next_rstd, 4, some && follow, "next_rstd"));
   if (!follow && (z || next_rstd)) return bad("z and next_rstd go with next_weight");
-  if (some) GS_TRY(check_apart({z}, {x, gate, residual, y}, "z"));
-  for (const Matrix& m : {Matrix{x, x_stride}, Matrix{gate, gate_stride}, Matrix{residual, residual_stride}})
-    if (rows > 1 && m.data == y && m.stride != y_stride) return bad("y may be an input itself only with the same stride");
   if (!some) return GS_OK;
+  const auto at = [&](const void* t, int64_t stride) { return place(Matrix{t, stride}, rows, cols, dtype); };
+  GS_TRY(check_apart({at(z, z_stride)}, {at(x, x_stride), at(gate, gate_stride), at(residual, residual_stride), at(y, y_stride)}, "z"));
+  for (const Matrix& m : {Matrix{x, x_stride}, Matrix{gate, gate_stride}, Matrix{residual, residual_stride}})
+    if (m.data == y ? rows > 1 && m.stride != y_stride : overlap(at(y, y_stride), at(m.data, m.stride)))
+      return bad("y may be an input itself only with the same stride, and may not overlap it otherwise");
   gs::GatedNormParams q;
   std::memset(&q, 0, sizeof(q));
   q.x = x;
@@ -585,7 +665,12 @@ gs_status gs_gated_norm_backward(const void* dy, int64_t dy_stride, const void* 
   GS_TRY(check_output(dx, dx_stride, rows, cols, dtype, false, "dx"));
   GS_TRY(check_output(dgate, dgate_stride, rows, cols, dtype, false, "dgate"));
   GS_TRY(check_output(dresidual, dresidual_stride, rows, cols, dtype, false, "dresidual"));
-  GS_TRY(check_apart({dx, dgate, dresidual}, {dy, dz, x, gate, y}, "dx, dgate and dresidual"));
+  if (some) {
+    const auto at = [&](const void* t, int64_t stride) { return place(Matrix{t, stride}, rows, cols, dtype); };
+    GS_TRY(check_apart({at(dx, dx_stride), at(dgate, dgate_stride), at(dresidual, dresidual_stride)},
+                       {at(dy, dy_stride), at(dz, dz_stride), at(x, x_stride), at(gate, gate_stride), at(y, y_stride)},
+                       "dx, dgate and dresidual"));
+  }
   GS_TRY(check_data(dweight, 4, true, "dweight"));
   GS_TRY(check_data(dnext_weight, 4, follow, "dnext_weight"));
   GS_TRY(check_workspace(workspace, workspace_bytes, gated_ws_bytes(rows, cols, groups), "gs_gated_norm_workspace_size"));
