@@ -622,6 +622,12 @@ gs_status gs_linear_attention_backward(const gs_heads* d_o, const gs_heads* q, c
                                        int64_t H, int64_t K, int64_t Dk, int64_t Dv, int32_t dtype, float scale,
                                        void* workspace, size_t workspace_bytes, gs_stream stream);
 
+/* For tests of what a wait that runs out does: the tries, 0 ... 2^20 (the default), of the waits on the tensor cores'
+ * path in later calls of gs_linear_attention_forward and gs_linear_attention_backward by this host thread: of the threads that
+ * issue products, that find the largest values of fp16 tensors, and that do the rest.  A try takes a microsecond at most.
+ * What has to do with a wait that has run out is NaN. */
+gs_status gs_linear_attention_wait_tries(int32_t issue, int32_t find, int32_t work);
+
 /* One token of each of B streams: the state in place, and o.  q, k, v and o have T = 1 (their token
  * strides are not used).  state: fp32, n_slots states of [H][Dk][Dv], state_stride elements apart; stream
  * b's is slots[b] (int32[B], NULL for b).  A slot outside [0, n_slots) is idle: its o is zero and nothing

@@ -126,6 +126,7 @@ SIGNATURES = {
                                     _i64, _i32, _f32, _vp, _sz, _vp],
     "gs_linear_attention_backward": [_HEADS, _HEADS, _HEADS, _HEADS, _vp, _vp, _vp, _vp, _vp, _HEADS, _HEADS, _HEADS, _vp,
                                      _i64, _i64, _i64, _i64, _i64, _i64, _i32, _f32, _vp, _sz, _vp],
+    "gs_linear_attention_wait_tries": [_i32, _i32, _i32],
     "gs_linear_attention_step": [_HEADS, _HEADS, _HEADS, _vp, _vp, _i64, _i64, _vp, _HEADS, _i64, _i64, _i64, _i64, _i64,
                                  _i32, _f32, _vp],
     "gs_gated_norm": [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _i64, _i64, _i32, _i32,
@@ -889,6 +890,11 @@ def gs_linear_attention_backward(d_o, q, k, v, log_decay, dq, dk, dv, workspace,
         _whole(f, "offsets", offsets, (B + 1,), dev), _heads(f, "dq", dq, qs, dtype, dev), _heads(f, "dk", dk, ks, dtype, dev),
         _heads(f, "dv", dv, vs, dtype, dev), _dense(f, "ds0", ds0, state, f32, dev), B, T, H, K, Dk, Dv, code, scale, wp, wn,
         stream), f)
+
+
+def gs_linear_attention_wait_tries(issue: int = 1 << 20, find: int = 1 << 20, work: int = 1 << 20) -> None:
+    """Tries of the tensor core walks' waits in later calls of this thread, for tests of waits that run out."""
+    _check(load_library().gs_linear_attention_wait_tries(issue, find, work), "gs_linear_attention_wait_tries")
 
 
 def _one_token(func: str, name: str, t, shape, dtype, device):

@@ -42,6 +42,7 @@ struct AttentionParams {
   int32_t back;         // walks from each sequence's end, and takes a token's decay after it
   int32_t wide;         // o is fp32, for heads that are summed after
   int32_t chained;      // each piece adds up the sums of those before it itself
+  int32_t issue_tries, find_tries, work_tries;  // of the tensor core walk's waits, before they give up
 };
 // Walks that run at once: of the same C, D, wide and, where one of them gives its last state, all do.
 struct AttentionWalks {

@@ -181,6 +181,8 @@ gs::HeadsIn in(const gs_heads* t, int64_t share) {
 }
 gs::HeadsOut out(const gs_heads* t) { return {t->data, t->batch_stride, t->token_stride, t->head_stride}; }
 
+thread_local int32_t issue_tries = gs::kMostTries, find_tries = gs::kMostTries, work_tries = gs::kMostTries;
+
 // Walks of the same C and D, at once.
 gs_status run_walks(const Sizes& z, gs::AttentionWalks& walks, gs_stream stream, const char* what) {
   for (int k = 0; k < walks.count; ++k) {
@@ -192,6 +194,9 @@ gs_status run_walks(const Sizes& z, gs::AttentionWalks& walks, gs_stream stream,
     p.segment = shape.segment;
     p.segments = shape.segments;
     p.items = (int32_t)shape.items;
+    p.issue_tries = issue_tries;
+    p.find_tries = find_tries;
+    p.work_tries = work_tries;
     p.chained = shape.segments > 1 && shape.segments <= gs::kChainedPieces && (!p.first || p.first != p.last);
   }
   const cudaError_t e = gs::launch_attention(walks, z.dtype, as_stream(stream));
@@ -452,6 +457,15 @@ gs_status gs_linear_attention_backward(const gs_heads* d_o, const gs_heads* q, c
   }
   return GS_OK;
   GS_GUARD_END
+}
+
+gs_status gs_linear_attention_wait_tries(int32_t issue, int32_t find, int32_t work) {
+  for (const int32_t tries : {issue, find, work})
+    if (tries < 0 || tries > gs::kMostTries) return gs::record_failure(GS_ERR_INVALID_ARG, "tries must lie in [0, 2^20]");
+  issue_tries = issue;
+  find_tries = find;
+  work_tries = work;
+  return GS_OK;
 }
 
 gs_status gs_linear_attention_step(const gs_heads* q, const gs_heads* k, const gs_heads* v, const float* log_decay,

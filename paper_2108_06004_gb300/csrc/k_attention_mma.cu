@@ -159,6 +159,8 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
   after_sync();
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const uint32_t tmem = tab.tmem;
+  // Waits end after a second or so (which nothing that this kernel does can cause). A thread whose wait has run out announces nothing
+  // more, so that the waits of all that have to do with it run out too; a worker then stores NaN.
   bool lost = false;
 
   if (threadIdx.x >= kWorkers) {
@@ -185,8 +187,7 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
       // come after that.
       for (int n = 0; n < blocks; ++n) {
         float* const to = tab.largest[n & 1][mine];
-        barrier_wait(&tab.kv_full[n & 1], n >> 1, lost);
-        __syncwarp();
+        if (lost = !barrier_wait(&tab.kv_full[n & 1], n >> 1, p.find_tries); __any_sync(0xFFFFFFFFu, lost)) break;
         const float k = largest(base + L::oK + (n & 1) * L::kQ, C / 64, tokens(n)), v = largest(base + L::oV + (n & 1) * L::kV, D / 64, tokens(n));
         if (lane == 0) {
           to[1] = k;
@@ -194,8 +195,7 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
           barrier_arrive(&tab.kv_known[n & 1]);
         }
         if (SUMS) continue;
-        barrier_wait(&tab.q_full, n, lost);
-        __syncwarp();
+        if (lost = !barrier_wait(&tab.q_full, n, p.find_tries); __any_sync(0xFFFFFFFFu, lost)) break;
         const float q = largest(base + L::oQ, C / 64, tokens(n));
         if (lane == 0) {
           to[0] = q;
@@ -219,98 +219,106 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
       };
       const uint32_t q = matrix(shared_address(base + L::oQ), 0), parts = matrix(shared_address(base + L::oS), C * 128);
       const auto values = [&](int n) { return matrix(shared_address(base + L::oV + (n & 1) * L::kV), L::kPanel); };
+      const auto wait = [&](uint64_t* bar, int phase) { return barrier_wait(bar, phase, p.issue_tries); };
       // U = K' V of block n
       const auto sum = [&](int n) {
         const uint32_t v = values(n);
-        barrier_wait(&tab.kv_full[n & 1], n >> 1, lost);
-        each<2>([&](auto which) {
+        if (!wait(&tab.kv_full[n & 1], n >> 1)) return false;
+        const auto half = [&](auto which) {
           constexpr int h = decltype(which)::value;
-          barrier_wait(&tab.w_ready[h], n, lost);
+          if (!wait(&tab.w_ready[h], n)) return false;
           after_sync();
           each<4 * PARTS>([&](auto step) {  // the smallest parts first, while the sum is small
             constexpr int part = PARTS - 1 - decltype(step)::value / 4, j = decltype(step)::value % 4;
             multiply_t<(h ? W1 : L::W0) + part * 32 + j * 8, (h * 4 + j) * 2048>(tmem + L::U, tmem, v, product<E>(D, true),
                                                                                             h > 0 || decltype(step)::value > 0);
           });
-        });
+          return true;
+        };
+        if (!half(std::integral_constant<int, 0>()) || !half(std::integral_constant<int, 1>())) return false;
         commit(&tab.summed);
+        return true;
       };
       // P = Q K' of block n.  Its place is free when the products that read it are done: only products with the same
       // sum are ordered among themselves.  Keys and queries arrive apart, so both are waited for.
       const auto score = [&](int n) {
         const uint32_t k = matrix(shared_address(base + L::oK + (n & 1) * L::kQ), 0);
-        barrier_wait(&tab.kv_full[n & 1], n >> 1, lost);
-        barrier_wait(&tab.q_full, n, lost);
+        if (!wait(&tab.kv_full[n & 1], n >> 1) || !wait(&tab.q_full, n)) return false;
         each<C / 16>([&](auto step) {
           constexpr int j = decltype(step)::value, at = j / 4 * L::kPanel + j % 4 * 32;
           multiply<at, at>(tmem + L::P, q, k, product<E>(128, false), j > 0);
         });
         commit(&tab.scores);
+        return true;
       };
       constexpr bool APART = !L::kNarrow && PARTS == 2;  // the weighted keys are not in P's place
-      load_kv(0);
-      if (!SUMS) load_q(0);
-      if (blocks > 1) load_kv(1);
-      sum(0);
-      if constexpr (SUMS) {
-        for (int n = 1; n < blocks; ++n) {
-          barrier_wait(&tab.summed, n - 1, lost);
-          if (n + 1 < blocks) load_kv(n + 1);
-          sum(n);
-        }
-      } else {
-        if (!APART) barrier_wait(&tab.summed, 0, lost);
-        score(0);
-        for (int n = 0; n < blocks; ++n) {
-          barrier_wait(&tab.state_ready, n, lost);
-          after_sync();
-          each<C / 8>([&](auto step) {
-            constexpr int part = decltype(step)::value / (C / 16), j = decltype(step)::value % (C / 16);
-            multiply<j / 4 * L::kPanel + j % 4 * 32, part * L::kPart + j * 2048>(tmem + L::O, q, parts, product<E>(D, true), part + j > 0);
-          });
-          commit(&tab.read);
-          if (n + 1 < blocks) {
-            barrier_wait(&tab.read, n, lost);
-            load_q(n + 1);
+      // False where a wait has run out.
+      const auto issue = [&] {
+        load_kv(0);
+        if (!SUMS) load_q(0);
+        if (blocks > 1) load_kv(1);
+        if (!sum(0)) return false;
+        if constexpr (SUMS) {
+          for (int n = 1; n < blocks; ++n) {
+            if (!wait(&tab.summed, n - 1)) return false;
+            if (n + 1 < blocks) load_kv(n + 1);
+            if (!sum(n)) return false;
           }
-          barrier_wait(&tab.a_ready, n, lost);
-          after_sync();
-          const uint32_t v = values(n);
-          each<16>([&](auto step) {
-            constexpr int part = decltype(step)::value / 8, j = decltype(step)::value % 8;
-            multiply_t<j * 16 + part * 8, j * 2048>(tmem + L::O, tmem + L::P, v, product<E>(D, true), true);
-          });
-          commit(&tab.done);
-          if (n + 1 >= blocks) break;
-          barrier_wait(&tab.done, n, lost);
-          if (APART) {
-            if (n + 2 < blocks) load_kv(n + 2);  // in the place of block n's, whose last product is done
-            // Rows of K that are not the block's tokens are zeroed by the workers, which say so with the weighted keys: a
-            // block that is cut short has its scores after its sum.
-            const bool cut = tokens(n + 1) < kBlockTokens;
-            if (!cut) score(n + 1);
-            sum(n + 1);
-            if (cut) score(n + 1);
-          } else {
-            sum(n + 1);
-            barrier_wait(&tab.summed, n + 1, lost);
-            if (n + 2 < blocks) load_kv(n + 2);
-            score(n + 1);
+        } else {
+          if (!APART && !wait(&tab.summed, 0)) return false;
+          if (!score(0)) return false;
+          for (int n = 0; n < blocks; ++n) {
+            if (!wait(&tab.state_ready, n)) return false;
+            after_sync();
+            each<C / 8>([&](auto step) {
+              constexpr int part = decltype(step)::value / (C / 16), j = decltype(step)::value % (C / 16);
+              multiply<j / 4 * L::kPanel + j % 4 * 32, part * L::kPart + j * 2048>(tmem + L::O, q, parts, product<E>(D, true), part + j > 0);
+            });
+            commit(&tab.read);
+            if (n + 1 < blocks) {
+              if (!wait(&tab.read, n)) return false;
+              load_q(n + 1);
+            }
+            if (!wait(&tab.a_ready, n)) return false;
+            after_sync();
+            const uint32_t v = values(n);
+            each<16>([&](auto step) {
+              constexpr int part = decltype(step)::value / 8, j = decltype(step)::value % 8;
+              multiply_t<j * 16 + part * 8, j * 2048>(tmem + L::O, tmem + L::P, v, product<E>(D, true), true);
+            });
+            commit(&tab.done);
+            if (n + 1 >= blocks) break;
+            if (!wait(&tab.done, n)) return false;
+            if (APART) {
+              if (n + 2 < blocks) load_kv(n + 2);  // in the place of block n's, whose last product is done
+              // Rows of K that are not the block's tokens are zeroed by the workers, which say so with the weighted keys: a
+              // block that is cut short has its scores after its sum.
+              const bool cut = tokens(n + 1) < kBlockTokens;
+              if (!cut && !score(n + 1)) return false;
+              if (!sum(n + 1)) return false;
+              if (cut && !score(n + 1)) return false;
+            } else {
+              if (!sum(n + 1) || !wait(&tab.summed, n + 1)) return false;
+              if (n + 2 < blocks) load_kv(n + 2);
+              if (!score(n + 1)) return false;
+            }
           }
         }
-      }
+        return true;
+      };
+      lost = !issue();
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::kWorker));
     const auto wait = [&](uint64_t* bar, int phase) {
-      barrier_wait(bar, phase, lost);
+      lost = !barrier_wait(bar, phase, lost ? 1 : p.work_tries) || lost;
       lost = __any_sync(0xFFFFFFFFu, lost);
     };
     // What this warp has written is there for the thread that issues products.
     const auto arrive = [&](uint64_t* bar) {
       before_sync();
       __syncwarp();
-      if (lane == 0) barrier_arrive(bar);
+      if (lane == 0 && !lost) barrier_arrive(bar);
     };
     // Whether the queries' decay w_{i+1} comes last, after both products, and A_ij has w_{-j-1} in place of w_{i-j}: only
     // where that stays small enough for any inputs, and for fp16 for the numbers that a part holds.
@@ -680,9 +688,9 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
     __syncwarp();
     before_sync();
   }
-  __syncthreads();
+  const bool gone = __syncthreads_or(lost);
   after_sync();
-  if (lost)  // copies still under way land before the shared memory is given back
+  if (gone)  // copies and products still under way end before their memory is given back
     for (int k = 0; k < 1000; ++k) __nanosleep(1000);
   __syncwarp();
   if (warp == kWorkers / 32) tmem_free<L::kColumns>(tmem);

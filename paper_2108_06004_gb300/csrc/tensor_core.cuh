@@ -20,21 +20,19 @@ __device__ __forceinline__ void barrier_expect(uint64_t* bar, uint32_t bytes) {
 __device__ __forceinline__ void barrier_arrive(uint64_t* bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(shared_address(bar)) : "memory");
 }
-// Waits for the end of the barrier's phase of this parity, a second at most: a try is suspended for a microsecond at
-// most.  A thread whose wait has run out (which nothing that these kernels do can cause) waits no more, so that
-// the kernel comes to its end; what it stores after is NaN.
-constexpr int kTries = 1 << 20;
-__device__ __forceinline__ void barrier_wait(uint64_t* bar, int phase, bool& lost) {
-  for (int tries = lost ? 1 : kTries; tries > 0; --tries) {
+// Waits for the end of the barrier's phase of this parity; false when that has not come after a number of tries, each of which is
+// suspended for a microsecond at most.
+__device__ __forceinline__ bool barrier_wait(uint64_t* bar, int phase, int tries) {
+  for (; tries > 0; --tries) {
     uint32_t done;
     asm volatile(
         "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2, 1000;\n selp.u32 %0, 1, 0, p;\n}"
         : "=r"(done)
         : "r"(shared_address(bar)), "r"(phase & 1)
         : "memory");
-    if (done) return;
+    if (done) return true;
   }
-  lost = true;
+  return false;
 }
 // What this thread has written to shared memory is seen by the tensor cores and bulk copies.
 __device__ __forceinline__ void shared_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
