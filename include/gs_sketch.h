@@ -596,7 +596,8 @@ gs_status gs_rotary_frequencies(int64_t R, double base, double factor, double or
  * nullable, not with lengths): tensors have one row of T tokens, and sequence b is tokens offsets[b] to
  * offsets[b + 1] - 1 (ascending, taken to [0, T]); tokens of no sequence are left as they were.
  * q, k and v of tokens that count must be finite: a block of tokens is one matrix product, so what is not
- * finite may show in any output of its sequence and head.  Dk, Dv in [1, GS_ATTENTION_MAX_HEAD], T at most
+ * finite may show in any output of its sequence and head; so may products q_i . k_j, states, and sums of their
+ * products with v or q, before scale, that reach 2^116.  Dk, Dv in [1, GS_ATTENTION_MAX_HEAD], T at most
  * 2^31 - 2^10.
  * workspace: gs_linear_attention_workspace_size bytes (backward, packed: 0 or 1, as the call is a backward
  * pass and has offsets), 256-byte aligned; calls that may run at once need one each. */

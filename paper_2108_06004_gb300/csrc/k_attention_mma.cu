@@ -7,7 +7,7 @@
 // (backwards w_i for w_{i+1} and w_{128-j} for w_{127-j}).  S stays in fp32 in the threads' registers: a block's U is summed in
 // tensor memory from zero, where what a product cuts off is small, and added to S with a rounding (with S itself as the
 // sum in tensor memory, a last state was off by 3.5e-6 instead of 3e-7).  U does not need S and is made one block ahead.
-// Where e^(-128 g) is small enough, w_{i+1} comes last, with w_{-j-1} in place of w_{i-j}: Q S and A V are one sum then.
+// Where e^(-128 g) is at most e^8, w_{i+1} comes last, with w_{-j-1} in place of w_{i-j}: Q S and A V are one sum then.
 //
 // Operands are 16-bit.  Q, K and V are as they are in memory; A and S as factors are a sum of two parts of the type,
 // which keeps 2^-17 or better of each, well below the rounding of a stored o: one in 500 or so is the neighbour of what fp32
@@ -320,9 +320,10 @@ k_attention_mma(const __grid_constant__ AttentionMmaParams params) {
       __syncwarp();
       if (lane == 0 && !lost) barrier_arrive(bar);
     };
-    // Whether the queries' decay w_{i+1} comes last, after both products, and A_ij has w_{-j-1} in place of w_{i-j}: only
-    // where that stays small enough for any inputs, and for fp16 for the numbers that a part holds.
-    const bool rises = -g * kBlockTokens <= (HALF ? 8.f : 32.f);
+    // Whether the queries' decay w_{i+1} comes last, after both products, and A_ij has w_{-j-1} in place of w_{i-j}: only where
+    // that makes them no more than e^8 times as large. (With e^32 for bf16, train 16x4096x16x128 took 1111 us, 1119 with e^8, and
+    // inputs of 1e9 left fp32's range half way to outputs that are well inside.)
+    const bool rises = -g * kBlockTokens <= 8.f;
     const int quad = warp & 3, group = warp >> 2, row = quad * 32 + lane, col0 = group * COLS;
     const uint32_t mine = tmem + ((uint32_t)(quad * 32) << 16);
     // Rows of the state: 64 are in the lanes of the warps that have less of A to work out, which is triangular.
