@@ -6,12 +6,12 @@
 //   S  <- w_16 S + in_scale sum over j of w_{15-j} k_j v_j'.
 // (Backwards a token's decay comes after it: w_i for w_{i+1}, and w_{16-j} for w_{15-j}.)
 // A CTA holds 32 columns of one head's state in the registers of its eight warps (four for more than 128 rows), a share of
-// the rows each; two multiply-adds a state element and token, two rows an instruction.  Bound by their issue: 8x2048x8x128
-// fp32 takes 5.24 ms for forward and backward, 5.49 with one row an instruction.
+// the rows each; two multiply-adds a state element and token, two rows an instruction.  8x2048x8x128 fp32 takes 4.39 ms for
+// forward and backward (5.17 with every token added to the state by itself, 5.49 with one row an instruction too).
 //
 // Long rows are cut into pieces: the pieces' own sums, the states before them, then all outputs.
 //
-// Small problems wait for memory and for one another: train 5x333x3x40/72 fp32 takes 156 us for forward and backward, in
+// Small problems wait for memory and for one another: train 5x333x3x40/72 fp32 takes 129 us for forward and backward, in
 // pieces of 64 tokens of four blocks each (599 us with four warps, loads one by one and pieces of 128); the loads of a
 // block are under way while the one before is worked on.
 #include "attention.cuh"
@@ -36,7 +36,7 @@ k_attention(const __grid_constant__ AttentionWalks walks) {
   constexpr int C = kWarps * ROWS, kThreadsA = kWarps * 32;  // contracted rows, with those that do not exist
   // rows of four floats more: sixteen keys at once lie in different banks
   __shared__ __align__(16) float q[SUMS ? 1 : kTok][C + 4], k[kTok][C + 4];
-  __shared__ float v[kTok][kCols], part[SUMS ? 1 : kWarps][kTok][kCols], score[kTok][kTok + 1], power[kTok + 1];
+  __shared__ float v[kTok][kCols], weighted[kTok][kCols], part[SUMS ? 1 : kWarps][kTok][kCols], score[kTok][kTok + 1], power[kTok + 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int slices = (p.D + kCols - 1) / kCols;
   const int slice = block % slices, head = block / slices % p.H, item = block / slices / p.H;
@@ -108,7 +108,11 @@ k_attention(const __grid_constant__ AttentionWalks walks) {
       if constexpr (!SUMS) q[j][c] = to_f32(next_q[a]);
     }
 #pragma unroll
-    for (int a = 0; a < VPER; ++a) v[a * kWarps + warp][lane] = to_f32(next_v[a]);
+    for (int a = 0; a < VPER; ++a) {
+      const int j = a * kWarps + warp;
+      v[j][lane] = to_f32(next_v[a]);
+      weighted[j][lane] = j < n ? v[j][lane] * (p.in_scale * power[n - j - after]) : 0.f;
+    }
     if (t0 + kTok < w.t1) fetch(t0 + kTok);
     __syncthreads();
     if constexpr (!SUMS) {
@@ -148,22 +152,28 @@ k_attention(const __grid_constant__ AttentionWalks walks) {
         for (int i = 0; i < 8; ++i) part[warp][i0 + i][lane] = o[i].x + o[i].y;
       }
     }
+    // The block's own sum is made from zero and added to the state once: added token by token, a state that decays slowly is
+    // rounded at its own size sixteen times as often. A few rows at a time, whose sums do not wait for one another; where a
+    // thread has 64 of them, its registers are enough for sixteen and the keys of four tokens.
     const Decay d = decay_of(g * (float)n);
+    constexpr int AT_ONCE = ROWS < 8 ? ROWS : ROWS < 64 ? 8 : 16, AHEAD = ROWS < 64 ? kTok : 4;
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) S[r] = decayed(S[r], d, 0.f);
-#pragma unroll 4
-    for (int j = 0; j < kTok; ++j) {
-      const float x = j < n ? v[j][lane] * (p.in_scale * power[n - j - after]) : 0.f;
+    for (int r0 = 0; r0 < ROWS; r0 += AT_ONCE) {
+      float2 u[AT_ONCE / 2];
 #pragma unroll
-      for (int r = 0; r < ROWS; r += 4) {
-        const float4 a = *reinterpret_cast<const float4*>(&k[j][warp * ROWS + r]);
-        const float2 one = __ffma2_rn(make_float2(a.x, a.y), make_float2(x, x), make_float2(S[r], S[r + 1]));
-        const float2 two = __ffma2_rn(make_float2(a.z, a.w), make_float2(x, x), make_float2(S[r + 2], S[r + 3]));
-        S[r] = one.x;
-        S[r + 1] = one.y;
-        S[r + 2] = two.x;
-        S[r + 3] = two.y;
+      for (int r = 0; r < AT_ONCE / 2; ++r) u[r] = make_float2(0.f, 0.f);
+#pragma unroll AHEAD
+      for (int j = 0; j < kTok; ++j) {
+        const float x = weighted[j][lane];
+#pragma unroll
+        for (int r = 0; r < AT_ONCE; r += 4) {
+          const float4 a = *reinterpret_cast<const float4*>(&k[j][warp * ROWS + r0 + r]);
+          u[r / 2] = __ffma2_rn(make_float2(a.x, a.y), make_float2(x, x), u[r / 2]);
+          u[r / 2 + 1] = __ffma2_rn(make_float2(a.z, a.w), make_float2(x, x), u[r / 2 + 1]);
+        }
       }
+#pragma unroll
+      for (int r = 0; r < AT_ONCE; ++r) S[r0 + r] = decayed(S[r0 + r], d, r % 2 ? u[r / 2].y : u[r / 2].x);
     }
     if constexpr (!SUMS) {
       __syncthreads();
