@@ -1,7 +1,8 @@
 // Rotary positions.  A position's turn is exact: with u = frequency / 2 pi as a fraction of 2^64, the low 64 bits
-// of position * u are the fraction of a turn, of which the upper 32 go into the sine and cosine (a
-// quarter of 2^-32 turns is far below an fp32 rounding of either).  u itself is right to the 53 bits of
-// the frequency: position 2^31 is off by 4e-8 turns at most.
+// of position * u are the fraction of a turn, of which the upper 32 go into the sine and cosine.  What they have
+// beyond the nearest quarter of a turn, an eighth at most, is rounded to fp32, which moves the angle by 2^-28 turns at
+// most (2.3e-8; the whole turn rounded to fp32 moved it by four times that, more than a sine's own rounding).  u itself is
+// right to the 53 bits of the frequency: position 2^31 is off by 4e-8 turns at most.
 //
 // Bound by memory: every element that moves is read and written once.  A CTA works out the sines and cosines of its
 // tokens once; a thread then has one place of a head (pairs of one 16-byte word, or of two, or one pair, or words that
@@ -33,9 +34,20 @@ k_rotary(const __grid_constant__ RotaryParams p, int tokens, int parts) {
     // the fraction in [0, 1] as 2^64ths; 2^64 itself is no turn at all
     const double share = (turns - floor(turns)) * 18446744073709551616.0;
     const uint64_t u = share < 18446744073709551616.0 ? (uint64_t)share : 0;
-    const int32_t angle = (int32_t)(((uint64_t)(int64_t)position * u) >> 32);
+    const uint32_t turn = (uint32_t)(((uint64_t)(int64_t)position * u) >> 32);
+    // an eighth of a turn either way of the nearest quarter
+    const uint32_t quarters = (turn + 0x20000000u) >> 30;
     float s, c;
-    sincospif((float)angle * 0x1p-31f, &s, &c);
+    sincospif((float)(int32_t)(turn - (quarters << 30)) * 0x1p-31f, &s, &c);
+    if (quarters & 1) {
+      const float t = c;
+      c = -s;
+      s = t;
+    }
+    if (quarters & 2) {
+      c = -c;
+      s = -s;
+    }
     cs[at] = make_float2(c * p.magnitude, s * p.magnitude * p.sign);
   }
   __syncthreads();
