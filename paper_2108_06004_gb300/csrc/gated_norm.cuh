@@ -42,7 +42,11 @@ __device__ __forceinline__ void unpack(const Raw8<E>& r, const Span& g, Eight& v
   unpack8<E, L>(r, g, reinterpret_cast<float(&)[8]>(v));
 }
 
-// s(u) = 1 / (1 + e^-u), whose exponent stops where s is zero in fp32 (and lets NaN pass).
+// act(u), and its slope: with s(u) = 1 / (1 + e^-u), a = act(u) and 1 - s = e^-u s, a (1 - s) + s for u s and s (1 - s) for s.
+// For fp32 e^-u is right to a unit in the last place whatever u is. For 16-bit types it comes from the base-two
+// exponential of a rounded product, off by |u| 2^-24 of itself, which is far below a rounding of theirs as long as s is not zero (its
+// exponent stops where s is zero in fp32), and the approximate reciprocal: 32768x4096 bf16 backward takes 429 us from cold
+// with them, 552 with fp32's; fp32 16384x1024 backward 175 us, 163 with the approximate ones.
 __device__ __forceinline__ float power(float x) {
   float y;
   asm("{\n .reg .f32 t;\n min.NaN.f32 t, %1, 0f42FE0000;\n ex2.approx.ftz.f32 %0, t;\n}" : "=f"(y) : "f"(x));
@@ -53,14 +57,27 @@ __device__ __forceinline__ float inverse(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// act(u), and its slope: with a = act(u) and 1 - s = e^-u s, a (1 - s) + s for u s and s (1 - s) for s.
+template <typename E>
 struct Gate {
   bool silu;
   __device__ __forceinline__ explicit Gate(int act) : silu(act == GS_GATE_SILU) {}
+  // s and 1 - s
+  static __device__ __forceinline__ float2 open(float2 u, float2& rest) {
+    if constexpr (sizeof(E) == 4) {
+      const float2 e = make_float2(expf(-u.x), expf(-u.y));
+      const float2 s = make_float2(__frcp_rn(e.x + 1.f), __frcp_rn(e.y + 1.f));
+      rest = make_float2(isinf(e.x) ? 1.f : e.x * s.x, isinf(e.y) ? 1.f : e.y * s.y);
+      return s;
+    } else {
+      const float2 x = mul(u, -1.4426950408889634f), e = make_float2(power(x.x), power(x.y)), d = add(e, two(1.f));
+      const float2 s = make_float2(inverse(d.x), inverse(d.y));
+      rest = mul(e, s);
+      return s;
+    }
+  }
   __device__ __forceinline__ float2 value(float2 u, float2& slope) const {
-    const float2 x = mul(u, -1.4426950408889634f), e = make_float2(power(x.x), power(x.y)), d = add(e, two(1.f));
-    const float2 s = make_float2(inverse(d.x), inverse(d.y));
-    const float2 rest = mul(e, s);
+    float2 rest;
+    const float2 s = open(u, rest);
     if (silu) {
       const float2 a = mul(u, s);
       slope = fma(a, rest, s);

@@ -26,7 +26,7 @@ k_gated_norm(const __grid_constant__ GatedNormParams p, int outer) {
   const bool live = row < p.rows, inner = p.spaced && row > 0 && row + 1 < p.rows;
   const int lead = lead_of<L>(row, p.x_stride, p.lead);
   const auto from = [&](const void* t, int64_t stride) { return static_cast<const E*>(t) + group_start(row, outer, stride, p.width); };
-  const Gate gate(p.act);
+  const Gate<E> gate(p.act);
   Eight t[V];
   Raw8<E> gates[V], residual[V];
   float2 sum = two(0.f);

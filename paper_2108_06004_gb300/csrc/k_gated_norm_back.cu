@@ -57,7 +57,7 @@ k_gated_norm_back(const __grid_constant__ GatedNormBackParams p, int outer) {
   // a thread's rows, `step` apart, have the same lead and the same group
   const int64_t step = (int64_t)gridDim.x * RPC, first = (int64_t)blockIdx.x * RPC;
   const int lead = lead_of<L>(first + sub, p.x_stride, p.lead);
-  const Gate gate(p.act);
+  const Gate<E> gate(p.act);
   Eight dw[V], dnext[V], weight[V], follow[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
