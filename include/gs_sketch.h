@@ -585,9 +585,9 @@ gs_status gs_rotary(const gs_heads* x, const gs_heads* out, const double* freque
 gs_status gs_rotary_frequencies(int64_t R, double base, double factor, double original, double low, double high,
                                 double* out);
 
-/* Linear attention with a decay for each head.  With g = log_decay[h] (fp32[H], taken to [-2^13, 0]),
- * for each sequence and head, a state S of Dk x Dv in fp32, S_{-1} = s0 (fp32[B][H][Dk][Dv], NULL for
- * zeros):
+/* Linear attention with a decay for each head.  With g = log_decay[h] (fp32[H], taken to [-2^13, 0]; NaN
+ * gives NaN), for each sequence and head, a state S of Dk x Dv in fp32, S_{-1} = s0 (fp32[B][H][Dk][Dv],
+ * NULL for zeros):
  *   S_t = e^g S_{t-1} + k_t v_t',   o_t = scale S_t' q_t.
  * q is [B][T][H][Dk]; k and v have K heads, of which H / K heads in turn share one.  s_last (nullable) is
  * the state after the last token, s0 for a sequence without tokens; it may be s0 itself.  o may not be an input.

@@ -123,9 +123,11 @@ __device__ __forceinline__ bool find_piece(const AttentionParams& p, int item, P
   return true;
 }
 
-__device__ __forceinline__ float log_decay_of(const AttentionParams& p, int head) {
-  return fminf(fmaxf(p.log_decay[head], kLeastLogDecay), 0.f);
+// In [kLeastLogDecay, 0]; NaN stays what it is.
+__device__ __forceinline__ float taken(float log_decay) {
+  return isnan(log_decay) ? log_decay : fminf(fmaxf(log_decay, kLeastLogDecay), 0.f);
 }
+__device__ __forceinline__ float log_decay_of(const AttentionParams& p, int head) { return taken(p.log_decay[head]); }
 
 // e^x for x <= 0 as a sum of a factor and a small rest, so that S e^x = fma(S, a, fma(S, b, ...)) is right to
 // a rounding of S however often it is applied: a rounded e^x close to one would bias a state

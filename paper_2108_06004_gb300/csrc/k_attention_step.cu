@@ -61,7 +61,7 @@ k_attention_step(const __grid_constant__ AttentionStepParams p) {
     k[d] = at<E>(p.k, b, head, d);
   }
   __syncthreads();
-  const Decay d = decay_of(fminf(fmaxf(p.log_decay[head], kLeastLogDecay), 0.f));
+  const Decay d = decay_of(taken(p.log_decay[head]));
   for (int r0 = group; r0 < p.Dk; r0 += AHEAD * GROUPS) {
     if (r0 != group) load(r0);
 #pragma unroll
