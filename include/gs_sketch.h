@@ -590,7 +590,7 @@ gs_status gs_rotary_frequencies(int64_t R, double base, double factor, double or
  * NULL for zeros):
  *   S_t = e^g S_{t-1} + k_t v_t',   o_t = scale S_t' q_t.
  * q is [B][T][H][Dk]; k and v have K heads, of which H / K heads in turn share one.  s_last (nullable) is
- * the state after the last token, s0 for a sequence without tokens; it may be s0 itself.  o may not be an input.
+ * the state after the last token, s0 for a sequence without tokens; it may be s0 itself.  o may not overlap an input.
  * Sequences are, by default, the rows of B x T tokens.  lengths (int32[B], nullable; taken to [0, T]):
  * tokens from a row's length on have no influence and their o is zero.  offsets (int32[B + 1],
  * nullable, not with lengths): tensors have one row of T tokens, and sequence b is tokens offsets[b] to
@@ -611,11 +611,12 @@ gs_status gs_linear_attention_forward(const gs_heads* q, const gs_heads* k, cons
                                       void* workspace, size_t workspace_bytes, gs_stream stream);
 
 /* Gradients of gs_linear_attention_forward from d_o and ds_last (fp32[B][H][Dk][Dv], NULL for none) and its
- * inputs: with dS_t = e^g dS_{t+1} + scale q_t do_t' (ds_last past the last token),
- *   dq_t = scale S_t do_t,  dk_t = dS_t v_t,  dv_t = dS_t' k_t,  ds0 = e^g dS_0 (nullable),
+ * inputs.  dS, the gradient of the state after a token, is ds_last + scale q_t do_t' at the last one and
+ * dS_t = e^g dS_{t+1} + scale q_t do_t' before it:
+ *   dq_t = scale S_t do_t,  dk_t = dS_t v_t,  dv_t = dS_t' k_t,  ds0 = e^g dS_0 (nullable; ds_last without tokens),
  * dk and dv summed in fp32 over the heads that share them.  The decay is a constant and has no gradient.
  * Tokens that lengths mask get zeros, tokens of no sequence are left as they were.  ds0 may not be s0 or
- * ds_last; dq, dk and dv may not be inputs or one another. */
+ * ds_last, and dq, dk and dv may not be inputs or one another, nor overlap them. */
 gs_status gs_linear_attention_backward(const gs_heads* d_o, const gs_heads* q, const gs_heads* k, const gs_heads* v,
                                        const float* log_decay, const float* s0, const float* ds_last,
                                        const int32_t* lengths, const int32_t* offsets, const gs_heads* dq,
