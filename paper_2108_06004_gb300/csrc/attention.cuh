@@ -1,7 +1,7 @@
 // Linear attention with a decay for each head: declarations shared by its kernels.
 //
 // The three gradients are linear attentions too.  With S_t = e^g S_{t-1} + k_t v_t' and its gradient
-// R_t = e^g R_{t+1} + scale q_t do_t',
+// R_t = e^g R_{t+1} + scale q_t do_t' (at the last token, that of the last state + scale q_t do_t'),
 //   o_t = scale S_t' q_t,  dq_t = scale S_t do_t,  dv_t = R_t' k_t,  dk_t = R_t v_t,
 // so each is a walk over the tokens, forwards or backwards, in which "queries" read a state that
 // "keys" and "values" add to: (q, k, v) for o, (do, v, k) with S' for dq, (k, q, do) for dv and
@@ -160,7 +160,6 @@ struct AttentionStepParams {
 struct HeadSumParams {
   const float* part;    // [B][T][K][share][D]
   HeadsOut out;
-  const int32_t* lengths;
   const int32_t* offsets;
   int64_t B, T;
   int32_t sequences, K, share, D;

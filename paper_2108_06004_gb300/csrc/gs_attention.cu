@@ -441,7 +441,6 @@ gs_status gs_linear_attention_backward(const gs_heads* d_o, const gs_heads* q, c
   if (share == 1 || T == 0) return GS_OK;
   gs::HeadSumParams sum;
   std::memset(&sum, 0, sizeof(sum));
-  sum.lengths = lengths;
   sum.offsets = offsets;
   sum.B = batch;
   sum.T = T;
