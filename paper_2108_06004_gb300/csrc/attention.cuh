@@ -139,9 +139,9 @@ __device__ __forceinline__ Decay decay_of(float x) { return x > -0.5f ? Decay{1.
 __device__ __forceinline__ float decayed(float s, const Decay& d, float add) { return fmaf(s, d.a, fmaf(s, d.b, add)); }
 
 // Where rows have few pieces, each one adds up those before it itself, which saves a launch and grows with the square of
-// their number: 24 sequences in 32768 tokens x16x64 bf16, which seldom have more than one piece and never more than 7, take
-// 512 us for forward and backward, 555 with the launch; prompt 1x8191x16x64, with 16 pieces, 64 us, 56 with the launch.  The
-// first state must stay as it is meanwhile.
+// their number. From cold: train 24 in 32768x16x64 bf16 packed, which seldom have more than one piece and never more than 7, 551 us,
+// 611 with the launch; 3x2048x16x128 in 3 pieces 310 and 363; 4x1000x8x64 in 8 pieces 135 and 127; forward 1x8192x24x128 in 6
+// pieces 141 and 124; 1x4096x16x64 in 16 pieces 53 and 46. The first state must stay as it is meanwhile.
 constexpr int kChainedPieces = 8;
 
 struct AttentionStepParams {

@@ -275,12 +275,17 @@ AttentionShape attention_shape(int64_t B, int64_t T, int64_t H, int C, int D, in
   const bool mma = for_tensor_cores(C, D, dtype);
   const int columns = mma ? (D <= 64 ? 64 : 128) : kCols;
   const int64_t heads = H * ((D + columns - 1) / columns), ctas = (packed ? 1 : B) * heads;
-  // CTAs that run at once
-  const int64_t slots = (int64_t)kSMs * (!mma ? 3 : C <= 64 && D <= 64 ? 2 : 1);
-  // Rows are cut where there are too few of them: keys and values are then read twice, which costs about
-  // six tenths of a walk.  Packed sequences are of any length: where there are enough of them, only those are cut that
-  // are longer than three CTAs' fair shares.
-  const bool enough = (packed ? B : 1) * ctas * 16 >= slots * 10;
+  // CTAs of a walk that share the device: for the fp32 one as many as registers leave room for, and two waves of those of more
+  // than 128 rows (train 2x2048x8x32 fp32 154 us, 193 with three an SM; 4x1000x16x64 721, 817 with three and 850 with two;
+  // 1x4096x8x128 1195, 1319 with three and 1287 with four; 1x4096x8x256 bf16 forward 1392, 1535 with three and 1559 with two)
+  const int64_t slots = (int64_t)kSMs * (mma ? (C <= 64 && D <= 64 ? 2 : 1) : C > 64 && C <= 128 ? 2 : 4);
+  // Rows are cut where there are too few of them: keys and values are then read twice, which costs about six tenths of a walk.
+  // That is worth it up to three eighths of what the device holds: B x 2048 x 16 x 128 bf16 forward takes 94 us cut and 100
+  // whole with 48 heads in all on 152 SMs, 137 and 100 with 64; heads of 64, 70 and 76 with 96 heads in 304 places, 98 and 78 with 128.
+  // Packed sequences are of any length: where there are enough of them, only those are cut that are longer than three CTAs' fair
+  // shares (train 24 in 32768x16x64 bf16 550 us, 611 with two shares, 668 with one, 547 with five; 200 in as many tokens 1021,
+  // 1352, 1363 and 1012).
+  const bool enough = (packed ? B : 1) * ctas * 16 >= slots * 6;
   int64_t segment = T;
   if (packed || !enough) segment = (T * ctas + slots - 1) / slots * (enough ? 3 : 1);
   const int64_t unit = mma ? 128 : 64;
