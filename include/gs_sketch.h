@@ -595,7 +595,7 @@ gs_status gs_rotary_frequencies(int64_t R, double base, double factor, double or
  * tokens from a row's length on have no influence and their o is zero.  offsets (int32[B + 1],
  * nullable, not with lengths): tensors have one row of T tokens, and sequence b is tokens offsets[b] to
  * offsets[b + 1] - 1 (ascending, taken to [0, T]); tokens of no sequence are left as they were.
- * q, k and v of tokens that count must be finite: a block of tokens is one matrix product, so what is not
+ * q, k and v of tokens that count, and states, must be finite: a block of tokens is one matrix product, so what is not
  * finite may show in any output of its sequence and head; so may products q_i . k_j, states, and sums of their
  * products with v or q, before scale, that reach 2^116.  Dk, Dv in [1, GS_ATTENTION_MAX_HEAD], T at most
  * 2^31 - 2^10.

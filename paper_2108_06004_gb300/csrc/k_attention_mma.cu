@@ -23,9 +23,11 @@
 // token for P, A and O and a row of the state for U and the weighted keys.
 //
 // Bound by the tensor cores and by the arithmetic between them in turn, which overlap in part: a product of 128 x 128 x 16
-// takes about 80 clocks, of which a block of 128 x 128 heads needs 56 or 64.  16x4096x16x128 bf16 forward takes 276 us
-// without a last state, 315 with one (57 and 50 % of the copy rate); without the arithmetic it would take 222, without the
-// products 220, out of L2 261.  256 heads are 1.7 waves of 152 CTAs.  16x4096x32x64: 315 and 358 us.  What made it faster,
+// takes 64 clocks at the nominal rate and about 80 at that of a large library product, of which a block of 128 x 128 heads needs 56 or
+// 64.  16x4096x16x128 bf16 forward takes 225 us without a last state where all decays are slow, 231 where all are quick, 279 and
+// 299 with one (70 and 57 % of the copy rate for the slow ones); 16x4096x32x64: 299, 316, 338 and 355; in fp16 287 to 360. Copies of
+// the kernel when it took 276 took 222 without the arithmetic, 220 without the products and 261 out of L2. 256 heads are 1.7 waves of
+// 152 CTAs.  What made it faster,
 // from 671 us: descriptors by addition (spilled ones cost 180 clocks a product); o by way of shared memory and as tiles;
 // sixteen warps in place of eight; U one block ahead; keys transposed by matrix loads; one arrival a warp.
 #include <cudaTypedefs.h>

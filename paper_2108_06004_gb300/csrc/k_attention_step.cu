@@ -5,7 +5,7 @@
 // Bound by memory: the state is read and written once.  A CTA takes 32 columns of one head's state, 16 rows of
 // eight 16-byte words (or 4 rows of single elements) at a time, all loads of a thread ahead of their use; the rows'
 // shares of o are summed over the warp and then over the CTA, in a fixed order.  200x16x128 bf16 takes 61 us (91 % of the
-// copy rate); 1x16x64 5.5 us on the device, and 10.4 us with the call from Python.
+// copy rate); 1x16x64 5.5 us on the device, and 10 to 12 us with the call from Python, by the host.
 #include "attention.cuh"
 
 namespace gs {

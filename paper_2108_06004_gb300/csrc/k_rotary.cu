@@ -7,7 +7,7 @@
 // Bound by memory: every element that moves is read and written once.  A CTA works out the sines and cosines of its
 // tokens once; a thread then has one place of a head (pairs of one 16-byte word, or of two, or one pair, or words that
 // are copied) of one token, whose sines and cosines stay in its registers, in every so many heads.  8x4096x40x128 bf16 in
-// place takes 126 us (78 % of the copy rate), half of each head turned out of place 122 us (81 %; 148 us with sines and
+// place takes 126 us (78 % of the copy rate), half of each head turned out of place 121 us (81 %; 148 us with sines and
 // cosines read again for every head).  Registers for four CTAs an SM, or six where elements move one by one: 8x4096x8x128
 // in rows that start anywhere takes 57 us, 70 with four.
 #include "attention.cuh"
