@@ -10,7 +10,7 @@
 // Where e^(-128 g) is at most e^8, w_{i+1} comes last, with w_{-j-1} in place of w_{i-j}: Q S and A V are one sum then.
 //
 // Operands are 16-bit.  Q, K and V are as they are in memory; A and S as factors are a sum of two parts of the type,
-// which keeps 2^-17 or better of each, well below the rounding of a stored o: one in 500 or so is the neighbour of what fp32
+// which keeps 2^-17 or better of each, well below the rounding of a stored o: one in 300 to 500 is the neighbour of what fp32
 // factors would give (a first part that is cut off keeps 2^-16, twice as many neighbours, and is 3 % faster for 16x4096x16x128;
 // one part is a tenth faster and would make the error of o 1.4 times the one of its rounding); the weighted keys are three parts of bf16 (24 bits) where a state is
 // given back in fp32 and otherwise two, and two of fp16 (22 bits).  fp16 has no room for scores and states of any size, so
