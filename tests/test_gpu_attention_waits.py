@@ -47,13 +47,10 @@ def run(gs, x, g, s0, lengths, state):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("who", ["issue", "find"])
-@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dtype,who", [("bf16", "issue"), ("f16", "issue"), ("f16", "find")])   # only fp16 has its largest values found
 @pytest.mark.parametrize("B,T,Dk,Dv", [(4, 300, 64, 64), (4, 300, 128, 128), (4, 300, 64, 128), (1, 2600, 128, 64), (1, 2600, 64, 64)])
 @pytest.mark.parametrize("state", [False, True])
 def test_waits_that_run_out(gs, state, B, T, Dk, Dv, dtype, who):
-    if who == "find" and dtype != "f16":
-        pytest.skip("only fp16 has its largest values found")
     rng = np.random.default_rng(1)
     x = [place((B, T, 2, d), dtype, "dense", rng=rng) for d in (Dk, Dk, Dv, Dv)]
     g, s0 = torch.tensor([-0.2, -0.01], device="cuda"), torch.from_numpy(rng.standard_normal((B, 2, Dk, Dv))).to("cuda", torch.float32)
